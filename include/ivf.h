@@ -102,7 +102,7 @@ typedef enum {
     IVF_EDEVICE = 4       /* HIP runtime error (launch failure, device fault) */
 } ivf_status;
 
-typedef enum { IVF_F32 = 0, IVF_U8 = 1 } ivf_dtype;
+typedef enum { IVF_F32 = 0, IVF_U8 = 1, IVF_F16 = 2, IVF_BF16 = 3 } ivf_dtype;
 
 /* Operation codes for ivf_workspace_bytes. */
 typedef enum {
@@ -453,6 +453,158 @@ ivf_status ivf_adc_scan(ivf_ctx *ctx, const float *queries, int64_t B, int32_t D
                         const int64_t *offsets, const uint32_t *perm, int64_t N,
                         const uint8_t *codes, int32_t M, const float *codebooks, int32_t k,
                         uint32_t *out_ids, float *out_dist);
+
+/* ------------------------------------------------------------------------
+ * A paged key/value cache held in 4 bits, with the attention that reads it.
+ * Inside a model that answers over long contexts the calls below do what
+ * routing and the compact-code scan do for a vector index: blocks of the
+ * cache are the lists, the mean of a block's keys is its centroid, a cheap
+ * score selects the blocks that a query reads, and attention runs over their
+ * codes.
+ *
+ * The cache is `blocks` blocks of block_size tokens (16, 32, 64 or 128) for
+ * `heads` key/value heads of `dim` channels (64, 96, 128, 192 or 256), for
+ * queries, keys, values and outputs of one type (IVF_F16 or IVF_BF16). Its
+ * three arrays are the caller's, on the context's device, 16-byte aligned:
+ *   records [blocks][heads] of block_size * dim * 17 / 16 bytes:
+ *             key codes    [block_size][dim / 2]
+ *             value codes  [block_size][dim / 2]
+ *             key scales   [block_size][dim / 32]
+ *             value scales [dim / 32][block_size]
+ *     A code is 4 bits (the even channel of a byte in its low half): a sign
+ *     and 0, .5, 1, 1.5, 2, 3, 4 or 6. A scale byte e stands for 2^(e - 127)
+ *     and serves 32 channels of one token. With amax the largest magnitude
+ *     of the 32, the exponent is floor(log2 amax) - 2, one more where amax
+ *     is above 7 times that power (6, the largest code, would be off by more
+ *     than 1), kept within [-13, 13] for IVF_F16 and [-125, 125] for
+ *     IVF_BF16, so that every code but 0 is a normal number of the type; the
+ *     code is the quotient to nearest, ties to even, at most 6. Where the
+ *     32 channels of a key or of the value beside it hold a NaN or an
+ *     infinity, the key's scale is 255 and all else of both is 0: they read
+ *     as NaN, every query row that attends to the token is NaN, and no other
+ *     row is touched by it.
+ *   summary [blocks][heads][dim] int8 and weight [blocks][heads] fp32:
+ *     weight * summary approximates the mean of the block's keys as stored.
+ *     Written when the block's last slot is: the mean is an fp64 sum rounded
+ *     to fp32 once (channels that read NaN count 0), times 1 / block_size;
+ *     weight = amax / 127 and summary = rint(mean * (127 / amax)) in fp32, all
+ *     zero where amax, the largest magnitude, is below 2^-100 or infinite.
+ * A slot is block * block_size + place. Tokens of a request occupy the blocks
+ * that its row of a block table names, in order; table entries outside
+ * [0, blocks) hold nothing.
+ *
+ * A batch of T tokens belongs to B requests: request b has the tokens
+ * start[b] ... start[b + 1] - 1, token t belongs to request[t] and stands at
+ * position[t] of it (0 = its first). A token with a request outside [0, B) or
+ * a negative position sees nothing. Query rows are given by strides, in
+ * elements, of tokens and heads (multiples of 8; channels are contiguous), so
+ * they may lie inside a larger array. The q_heads query heads are a multiple
+ * of `heads`; query head j reads key/value head j / (q_heads / heads).
+ * These calls take no note of the D limits above and keep the other
+ * conventions, but arrays of whole numbers and out_lse need only be aligned to
+ * their elements, and table_cols * block_size is below 2^31. */
+typedef struct {
+    void *records;
+    int8_t *summary;
+    float *weight;
+    int64_t blocks;
+    int32_t block_size;
+    int32_t heads;
+    int32_t dim;
+    int32_t dtype;
+} ivf_kv_cache;
+
+/* Block tables and slots from request lengths. Request b has cached[b] tokens
+ * in the cache and brings added[b] more (negative lengths count as 0). Its
+ * ceil((cached + added) / block_size) - ceil(cached / block_size) further
+ * blocks are taken from free_blocks in order, requests in order.
+ *   cached, added [B] int32, B <= 16384
+ *   table       [B][table_cols] int32 (rows table_cols apart), updated: the
+ *               entries of blocks that were there stay, the new blocks'
+ *               follow, the rest of the row becomes -1
+ *   free_blocks [n_free] int32; where they do not suffice the entry is -1
+ *   T           tokens that the outputs hold, at least the sum of added
+ *   out_start   [B + 1] int32 first token of each request (at most T)
+ *   out_slots   [T] int64, -1 for a token without a block (none free, or
+ *               beyond the table)
+ *   out_request, out_position [T] int32; past the last token -1
+ *   out_info    [4] int64: tokens, blocks asked for, blocks taken, requests
+ *               that the table's columns do not hold; may be NULL
+ * Errors: IVF_EINVAL, IVF_EUNSUPPORTED (B, sizes), IVF_EDEVICE. */
+ivf_status ivf_kv_plan(ivf_ctx *ctx, const int32_t *cached, const int32_t *added, int64_t B,
+                       int32_t block_size, int32_t *table, int32_t table_cols,
+                       const int32_t *free_blocks, int64_t n_free, int64_t T, int32_t *out_start,
+                       int64_t *out_slots, int32_t *out_request, int32_t *out_position,
+                       int64_t *out_info);
+
+/* Writes T tokens into the cache at slots[t] (distinct; a slot outside the
+ * cache is skipped) and the summaries of the blocks whose last slot is among
+ * them.
+ *   k, v  [T][heads][dim] by strides, type of the cache
+ * Errors: IVF_EINVAL (sizes, NULL pointers, misalignment, aliasing),
+ * IVF_EUNSUPPORTED (block size, dim, type), IVF_EDEVICE. */
+ivf_status ivf_kv_append(ivf_ctx *ctx, const ivf_kv_cache *cache, const void *k,
+                         int64_t k_token_stride, int64_t k_head_stride, const void *v,
+                         int64_t v_token_stride, int64_t v_head_stride, const int64_t *slots,
+                         int64_t T);
+
+/* Reads tokens and block means back: out_k, out_v [T][heads][dim] of the
+ * cache's type at slots[t] (NaN for a slot outside the cache), out_mean
+ * [n][heads][dim] fp32 = summary * weight of blocks[i] (NaN outside). T or n
+ * may be 0, and out_k or out_v NULL. Errors: as ivf_kv_append. */
+ivf_status ivf_kv_read(ivf_ctx *ctx, const ivf_kv_cache *cache, const int64_t *slots, int64_t T,
+                       void *out_k, void *out_v, const int32_t *blocks, int64_t n,
+                       float *out_mean);
+
+/* The blocks that each token's queries read: for every token and key/value
+ * head `count` block indexes of its request (columns of the table), ascending,
+ * padded with -1.
+ * Of the n = position / block_size + 1 blocks up to the token's own (at most
+ * table_cols), the first `first` and the last `last` are kept, and of the
+ * others the best count - first - last by (score descending, index
+ * ascending). The score is <c, summary> * weight in fp32, with the integer
+ * product exact and c the int8 code rint(u * (127 / amax)) of u, the sum of
+ * the head's group of query rows (fp64, rounded to fp32 once; non-finite
+ * channels, and all where amax is below 2^-100, count 0). Blocks without a
+ * table entry are not selected.
+ *   q        [T][q_heads][dim] by strides
+ *   request, position [T] int32     table [B][table_cols] int32
+ *   first >= 0, last >= 1, first + last <= count <= 4096
+ *   table_cols <= 32768
+ *   out_blocks [T][heads][count] int32
+ * Errors: as ivf_kv_append. No workspace. */
+ivf_status ivf_kv_select(ivf_ctx *ctx, const ivf_kv_cache *cache, const void *q,
+                         int64_t q_token_stride, int64_t q_head_stride, int32_t q_heads, int64_t T,
+                         const int32_t *request, const int32_t *position, const int32_t *table,
+                         int64_t B, int32_t table_cols, int32_t first, int32_t last, int32_t count,
+                         int32_t *out_blocks);
+
+/* Attention of the batch's queries over the cache: a row at position p sees
+ * the keys of its request at positions 0 ... p (in blocks that the table
+ * names), with `blocks` only those of the blocks listed for its token and
+ * key/value head (entries outside [0, table_cols) list nothing; a block
+ * listed twice counts twice).
+ *   out = sum_j softmax_j(scale * q.k_j) v_j, sums in fp32, probabilities
+ *   rounded to the cache's type for their product with the values.
+ *   start    [B + 1] int32, request, position [T] int32 as in ivf_kv_plan;
+ *            with `blocks` the requests' ranges are not read, without it
+ *            request[] is not, and rows outside every range are not written
+ *   longest  at least the largest number of tokens of one request, 1 ... T
+ *   blocks   [T][heads][count] int32 (ivf_kv_select), or NULL (count 0)
+ *   out      [T][q_heads][dim] of the cache's type
+ *   out_lse  [T][q_heads] fp32, log of the sum of exp(scale * q.k); may be NULL
+ * A row that sees nothing is 0 with -infinity.
+ * Workspace: ivf_kv_attend_bytes(). Errors: as ivf_kv_append, IVF_ENOMEM. */
+ivf_status ivf_kv_attend(ivf_ctx *ctx, const ivf_kv_cache *cache, const void *q,
+                         int64_t q_token_stride, int64_t q_head_stride, int32_t q_heads, int64_t T,
+                         const int32_t *start, const int32_t *request, const int32_t *position,
+                         const int32_t *table, int64_t B, int32_t table_cols, const int32_t *blocks,
+                         int32_t count, float scale, int64_t longest, void *out, float *out_lse);
+
+/* Workspace of ivf_kv_attend (the rows' parts where long key ranges are split
+ * over workgroups; 0 where none are, or for arguments that it refuses). */
+size_t ivf_kv_attend_bytes(const ivf_kv_cache *cache, int32_t q_heads, int64_t T, int64_t B,
+                           int32_t table_cols, int32_t count, int64_t longest);
 
 /* Measures the fp32 MFMA pipe for reporting: enqueues a probe kernel that
  * runs only v_mfma_f32_32x32x2_f32 (register operands, two waves per SIMD on

@@ -8,13 +8,18 @@ and the benchmark:
 * ``ivf_route``         coarse search, Eq. (1) with Eq. (6): top-nprobe lists per query;
 * ``ivf_kmeans_step``   one Lloyd iteration: assignment + mean update;
 * ``ivf_assign_build``  full assignment + cluster-major inverted lists;
-* ``ivf_build_lists``   the inverted-list build alone.
+* ``ivf_build_lists``   the inverted-list build alone;
+* ``ivf_kv_plan``, ``ivf_kv_append``, ``ivf_kv_read``, ``ivf_kv_select``, ``ivf_kv_attend``
+                        a paged key/value cache held in 4 bits (``KVCache``): its tables, writing
+                        and reading it, the blocks that queries select, attention over it.
 """
 from ._binding import (  # noqa: F401
+    IVF_BF16,
     IVF_EDEVICE,
     IVF_EINVAL,
     IVF_ENOMEM,
     IVF_EUNSUPPORTED,
+    IVF_F16,
     IVF_F32,
     IVF_OK,
     IVF_OP_ADC_SCAN,
@@ -39,12 +44,19 @@ from ._binding import (  # noqa: F401
     SIGNATURES,
     Context,
     IvfError,
+    KVCache,
+    KVPlan,
     ivf_assign_build,
     ivf_adc_scan,
     ivf_assign_cells,
     ivf_assign_graph,
     ivf_build_lists,
     ivf_kmeans_step,
+    ivf_kv_append,
+    ivf_kv_attend,
+    ivf_kv_plan,
+    ivf_kv_read,
+    ivf_kv_select,
     ivf_list_major,
     ivf_pq_encode,
     ivf_pq_train_step,

@@ -7,6 +7,7 @@ not built, or no GPU is present, the calls raise.
 """
 from __future__ import annotations
 
+import collections
 import ctypes
 import os
 
@@ -14,7 +15,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libivf.so")
 
 IVF_OK, IVF_EINVAL, IVF_EUNSUPPORTED, IVF_ENOMEM, IVF_EDEVICE = range(5)
-IVF_F32, IVF_U8 = 0, 1
+IVF_F32, IVF_U8, IVF_F16, IVF_BF16 = range(4)
 IVF_OP_ROUTE, IVF_OP_KMEANS_STEP, IVF_OP_ASSIGN_BUILD, IVF_OP_BUILD_LISTS, IVF_OP_PQ_TRAIN_STEP, IVF_OP_ADC_SCAN = range(6)
 (IVF_OPT_FORCE_FALLBACK, IVF_OPT_SAMPLE_RANK, IVF_OPT_PROFILE, IVF_OPT_BUILD_BLOCKS, IVF_OPT_SCREEN_WAVES,
  IVF_OPT_FP32_SCREEN, IVF_OPT_I8_TWO_PLANE_ONLY, IVF_OPT_FORCE_RESCREEN, IVF_OPT_RESCREEN_CAP,
@@ -49,6 +50,13 @@ SIGNATURES = [
     ("ivf_assign_cells", _INT, [_P, _P, _INT, _I64, _P, _I64, _I32, _P, _I64, _P, _P, _I64, _P, _I32, _I32, _P, _P, _P]),
     ("ivf_adc_scan", _INT, [_P, _P, _I64, _I32, _P, _I64, _P, _I32, _P, _P, _I64, _P, _I32, _P, _I32, _P, _P]),
     ("ivf_pq_train_step", _INT, [_P, _P, _I64, _I32, _I32, _P, _U64, _I32, _P, _P, _P]),
+    ("ivf_kv_plan", _INT, [_P, _P, _P, _I64, _I32, _P, _I32, _P, _I64, _I64, _P, _P, _P, _P, _P]),
+    ("ivf_kv_append", _INT, [_P, _P, _P, _I64, _I64, _P, _I64, _I64, _P, _I64]),
+    ("ivf_kv_read", _INT, [_P, _P, _P, _I64, _P, _P, _P, _I64, _P]),
+    ("ivf_kv_select", _INT, [_P, _P, _P, _I64, _I64, _I32, _I64, _P, _P, _P, _I64, _I32, _I32, _I32, _I32, _P]),
+    ("ivf_kv_attend_bytes", _SZ, [_P, _I32, _I64, _I64, _I32, _I32, _I64]),
+    ("ivf_kv_attend", _INT, [_P, _P, _P, _I64, _I64, _I32, _I64, _P, _P, _P, _P, _I64, _I32, _P, _I32,
+                             ctypes.c_float, _I64, _P, _P]),
 ]
 
 _lib = None
@@ -463,3 +471,185 @@ def ivf_adc_scan(ctx: Context, queries, centroids, probes, offsets, perm, codes,
                                    _ptr(offsets), _ptr(perm), N, _ptr(codes), M, _ptr(codebooks), k,
                                    _ptr(out_ids), _ptr(out_dist)), "ivf_adc_scan")
     return out_ids, out_dist
+
+
+# ---- the paged 4-bit key/value cache ------------------------------------------
+
+class _KvCacheStruct(ctypes.Structure):
+    """ivf_kv_cache."""
+    _fields_ = [("records", _P), ("summary", _P), ("weight", _P), ("blocks", _I64), ("block_size", _I32),
+                ("heads", _I32), ("dim", _I32), ("dtype", _I32)]
+
+
+class KVCache:
+    """A paged key/value cache held in 4 bits: `records` uint8 [blocks, heads,
+    block_size * dim * 17 / 16], `summary` int8 [blocks, heads, dim] and
+    `weight` fp32 [blocks, heads] (layout: ivf_kv_cache in include/ivf.h), for
+    keys, values and queries of `dtype` (torch.float16 or torch.bfloat16)."""
+
+    def __init__(self, records, summary, weight, block_size: int, dtype):
+        import torch
+
+        for t, name, kind in ((records, "records", torch.uint8), (summary, "summary", torch.int8),
+                              (weight, "weight", torch.float32)):
+            _device_tensor(t, name)
+            if t.dtype != kind:
+                raise TypeError("%s must be %s, got %s" % (name, kind, t.dtype))
+        codes = {torch.float16: IVF_F16, torch.bfloat16: IVF_BF16}
+        if dtype not in codes:
+            raise TypeError("the cache's type must be float16 or bfloat16, got %s" % dtype)
+        blocks, heads, dim = summary.shape
+        if tuple(records.shape) != (blocks, heads, block_size * dim * 17 // 16) or tuple(weight.shape) != (blocks, heads):
+            raise ValueError("records %s, summary %s and weight %s do not belong together (block_size %d)" % (
+                tuple(records.shape), tuple(summary.shape), tuple(weight.shape), block_size))
+        self.records, self.summary, self.weight = records, summary, weight
+        self.blocks, self.heads, self.dim, self.block_size, self.dtype = blocks, heads, dim, block_size, dtype
+        self.struct = _KvCacheStruct(records.data_ptr(), summary.data_ptr(), weight.data_ptr(), blocks, block_size,
+                                     heads, dim, codes[dtype])
+        self.ref = ctypes.byref(self.struct)
+
+    @classmethod
+    def empty(cls, blocks: int, heads: int, dim: int, block_size: int = 64, dtype=None, device="cuda"):
+        """A cache of `blocks` unwritten blocks."""
+        import torch
+
+        new = lambda shape, kind: torch.zeros(shape, dtype=kind, device=device)  # noqa: E731
+        return cls(new((blocks, heads, block_size * dim * 17 // 16), torch.uint8), new((blocks, heads, dim), torch.int8),
+                   new((blocks, heads), torch.float32), block_size, dtype or torch.bfloat16)
+
+
+KVPlan = collections.namedtuple("KVPlan", "start slots request position info")
+
+
+def _rows(t, name, cache, heads=None):
+    """(pointer, token stride, head stride) of rows [tokens, heads, dim]."""
+    if not t.is_cuda or t.dtype != cache.dtype:
+        raise TypeError("%s must be a device tensor of the cache's type %s" % (name, cache.dtype))
+    if t.dim() != 3 or t.shape[2] != cache.dim or (heads is not None and t.shape[1] != heads):
+        raise ValueError("%s must be [tokens, %s, %d], got %s" % (name, heads or "heads", cache.dim, tuple(t.shape)))
+    if t.numel() == 0:
+        return None, 0, 0
+    st, sh, sd = t.stride()
+    if sd != 1:
+        raise ValueError("%s: channels must be contiguous" % name)
+    return t.data_ptr(), st if t.shape[0] > 1 else 0, sh if t.shape[1] > 1 else 0
+
+
+def _ints(t, name, shape=None, kind=None):
+    import torch
+
+    _device_tensor(t, name)
+    if t.dtype != (kind or torch.int32):
+        raise TypeError("%s must be %s, got %s" % (name, kind or torch.int32, t.dtype))
+    if shape is not None and tuple(t.shape) != shape:
+        raise ValueError("%s must be %s, got %s" % (name, shape, tuple(t.shape)))
+    return t.data_ptr()
+
+
+def ivf_kv_plan(ctx: Context, cached, added, block_size: int, table, free_blocks, tokens: int, want_info: bool = False):
+    """Block tables and slots of a batch: requests of cached[b] tokens (int32 [B])
+    bring added[b] more, `tokens` in all. Fills `table` (int32 [B, columns]) in
+    place with blocks of free_blocks (int32, taken in order) and returns
+    KVPlan(start [B + 1], slots int64 [tokens], request [tokens], position
+    [tokens], info int64 [4] or None)."""
+    import torch
+
+    B = cached.shape[0]
+    p_cached, p_added = _ints(cached, "cached", (B,)), _ints(added, "added", (B,))
+    if table.dim() != 2 or table.shape[0] != B:
+        raise ValueError("table must be [%d, columns], got %s" % (B, tuple(table.shape)))
+    p_table, p_free = _ints(table, "table"), _ints(free_blocks, "free_blocks", (free_blocks.numel(),))
+    new = lambda n, kind: torch.empty(n, dtype=kind, device=cached.device)  # noqa: E731
+    plan = KVPlan(new(B + 1, torch.int32), new(tokens, torch.int64), new(tokens, torch.int32), new(tokens, torch.int32),
+                  new(4, torch.int64) if want_info else None)
+    ctx.bind_stream()
+    ctx.check(ctx.lib.ivf_kv_plan(ctx.handle, p_cached, p_added, B, block_size, p_table, table.shape[1], p_free,
+                                  free_blocks.numel(), tokens, plan.start.data_ptr(), plan.slots.data_ptr(),
+                                  plan.request.data_ptr(), plan.position.data_ptr(), _ptr(plan.info)), "ivf_kv_plan")
+    return plan
+
+
+def ivf_kv_append(ctx: Context, cache: KVCache, k, v, slots):
+    """Writes keys and values [T, heads, dim] into the cache at slots (int64 [T])."""
+    import torch
+
+    T = slots.shape[0]
+    p_slots = _ints(slots, "slots", (T,), torch.int64)
+    kp, kt, kh = _rows(k, "k", cache, cache.heads)
+    vp, vt, vh = _rows(v, "v", cache, cache.heads)
+    if k.shape[0] != T or v.shape[0] != T:
+        raise ValueError("k and v must hold one row per slot (%d)" % T)
+    ctx.bind_stream()
+    ctx.check(ctx.lib.ivf_kv_append(ctx.handle, cache.ref, kp, kt, kh, vp, vt, vh, p_slots, T), "ivf_kv_append")
+
+
+def ivf_kv_read(ctx: Context, cache: KVCache, slots, blocks=None):
+    """The cache's values: keys and values [T, heads, dim] at slots (int64 [T])
+    and, of `blocks` (int32 [n]), the key means [n, heads, dim] fp32 (else None)."""
+    import torch
+
+    T = slots.shape[0]
+    p_slots = _ints(slots, "slots", (T,), torch.int64)
+    k = torch.empty((T, cache.heads, cache.dim), dtype=cache.dtype, device=slots.device)
+    v = torch.empty_like(k)
+    mean, n, p_blocks, p_mean = None, 0, None, None
+    if blocks is not None:
+        n = blocks.shape[0]
+        p_blocks = _ints(blocks, "blocks", (n,))
+        mean = torch.empty((n, cache.heads, cache.dim), dtype=torch.float32, device=slots.device)
+        p_mean = mean.data_ptr()
+    ctx.bind_stream()
+    ctx.check(ctx.lib.ivf_kv_read(ctx.handle, cache.ref, p_slots, T, k.data_ptr(), v.data_ptr(), p_blocks, n, p_mean),
+              "ivf_kv_read")
+    return k, v, mean
+
+
+def ivf_kv_select(ctx: Context, cache: KVCache, q, request, position, table, count: int, first: int = 1, last: int = 1):
+    """The blocks that the queries q [T, query heads, dim] read: int32 [T, heads,
+    count] columns of the request's row of `table`, ascending, -1 behind. The
+    first `first` and the last `last` blocks are always among them."""
+    import torch
+
+    T, Hq = q.shape[0], q.shape[1]
+    qp, qt, qh = _rows(q, "q", cache)
+    out = torch.empty((T, cache.heads, count), dtype=torch.int32, device=q.device)
+    ctx.bind_stream()
+    ctx.check(ctx.lib.ivf_kv_select(ctx.handle, cache.ref, qp, qt, qh, Hq, T, _ints(request, "request", (T,)),
+                                    _ints(position, "position", (T,)), _ints(table, "table"), table.shape[0],
+                                    table.shape[1], first, last, count, out.data_ptr()), "ivf_kv_select")
+    return out
+
+
+def ivf_kv_attend(ctx: Context, cache: KVCache, q, start, request, position, table, scale: float, longest: int,
+                  blocks=None, out=None, out_lse=None, want_lse: bool = True):
+    """Attention of queries q [T, query heads, dim] over their requests' tokens in
+    the cache, or over the selected `blocks` (int32 [T, heads, count]) only:
+    outputs like q and the log-sum-exps fp32 [T, query heads]. `longest` is at
+    least the largest number of tokens that one request has in the batch."""
+    import torch
+
+    T, Hq = q.shape[0], q.shape[1]
+    B, cols = table.shape
+    qp, qt, qh = _rows(q, "q", cache)
+    p_blocks, count = None, 0
+    if blocks is not None:
+        count = blocks.shape[2]
+        p_blocks = _ints(blocks, "blocks", (T, cache.heads, count))
+    if out is None:
+        out = torch.empty((T, Hq, cache.dim), dtype=cache.dtype, device=q.device)
+    elif not out.is_contiguous() or out.dtype != cache.dtype or tuple(out.shape) != (T, Hq, cache.dim):
+        raise ValueError("out must be contiguous %s %s" % ((T, Hq, cache.dim), cache.dtype))
+    if out_lse is None and want_lse:
+        out_lse = torch.empty((T, Hq), dtype=torch.float32, device=q.device)
+    elif out_lse is not None and (not out_lse.is_contiguous() or out_lse.dtype != torch.float32
+                                  or tuple(out_lse.shape) != (T, Hq)):
+        raise ValueError("out_lse must be contiguous %s fp32" % ((T, Hq),))
+    need = ctx.lib.ivf_kv_attend_bytes(cache.ref, Hq, T, B, cols, count, longest)
+    if need:
+        ctx.ensure_workspace(need)
+    ctx.bind_stream()
+    ctx.check(ctx.lib.ivf_kv_attend(ctx.handle, cache.ref, qp, qt, qh, Hq, T, _ints(start, "start", (B + 1,)),
+                                    _ints(request, "request", (T,)), _ints(position, "position", (T,)),
+                                    _ints(table, "table"), B, cols, p_blocks, count, scale, longest, out.data_ptr(),
+                                    _ptr(out_lse)), "ivf_kv_attend")
+    return out, out_lse

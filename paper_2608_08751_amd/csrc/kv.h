@@ -1,0 +1,86 @@
+// The paged 4-bit key/value cache: its layout and the launch parameters of the
+// kernels that build its tables (kv_plan.hip), write and read it
+// (kv_cache.hip), select blocks (kv_select.hip) and attend (kv_attend.hip).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace ivf {
+
+constexpr int kKvMaxRequests = 16384;  // of one plan: their prefix sums lie in LDS
+constexpr int kKvMaxSelectCols = 32768;  // block scores of a row lie in LDS
+constexpr int kKvMaxCount = 4096;
+
+struct KvCache {
+    uint8_t *rec;
+    int8_t *summary;
+    float *weight;
+    int64_t blocks;
+    int bs;        // tokens per block, 1 << shift
+    int shift;
+    int heads;
+    int dim;
+    bool bf16;     // else f16
+    __host__ __device__ size_t rec_bytes() const { return (size_t)bs * dim / 16 * 17; }
+    // offsets inside a record
+    __host__ __device__ int v_codes() const { return bs * (dim / 2); }
+    __host__ __device__ int k_scales() const { return bs * dim; }
+    __host__ __device__ int v_scales() const { return bs * dim + bs * (dim / 32); }
+};
+
+// Query rows by strides, in elements.
+struct KvRows {
+    const void *p;
+    int64_t ts, hs;
+};
+
+hipError_t launch_kv_plan(const int32_t *cached, const int32_t *added, int B, int shift, int32_t *table, int cols,
+                          const int32_t *free_blocks, int64_t n_free, int64_t T, int32_t *start, int64_t *slots,
+                          int32_t *request, int32_t *position, int64_t *info, int num_cus, hipStream_t s);
+
+hipError_t launch_kv_append(const KvCache &c, KvRows k, KvRows v, const int64_t *slots, int64_t T, hipStream_t s);
+hipError_t launch_kv_summaries(const KvCache &c, const int64_t *slots, int64_t T, hipStream_t s);
+hipError_t launch_kv_read(const KvCache &c, const int64_t *slots, int64_t T, void *k, void *v, const int32_t *blocks,
+                          int64_t n, float *mean, hipStream_t s);
+
+struct KvSelect {
+    KvCache c;
+    KvRows q;
+    int group;  // query heads per key/value head
+    int64_t T;
+    const int32_t *request, *position, *table;
+    int64_t B;
+    int cols;
+    int first, last, count;
+    int32_t *out;
+};
+hipError_t launch_kv_select(const KvSelect &a, int num_cus, hipStream_t s);
+
+struct KvAttend {
+    KvCache c;
+    KvRows q;
+    int group;
+    int64_t T;
+    const int32_t *start, *request, *position, *table;
+    int64_t B;
+    int cols;
+    const int32_t *blocks;  // selected blocks, or null
+    int count;
+    float scale;  // times log2(e)
+    void *out;
+    float *lse;
+    // long key ranges are cut into `splits` parts, whose results lie here
+    // (row = token * query heads + head): sums [row][split][dim], and
+    // (reference, sum of exponentials) [row][split]
+    int splits;
+    float *part;
+    float2 *part_ml;
+};
+// Parts that a call of these sizes is cut into.
+int kv_attend_splits(int heads, int group, int64_t T, int64_t B, int64_t keys, int64_t longest, bool sparse,
+                     int num_cus);
+hipError_t launch_kv_attend(const KvAttend &a, int64_t longest, hipStream_t s);
+hipError_t launch_kv_combine(const KvAttend &a, hipStream_t s);
+
+}  // namespace ivf
