@@ -32,7 +32,11 @@ FLAGS = [
 
 # The PQ screen takes maxima of values whose low bits are integers; quieting
 # NaNs there would cost an instruction per value (inputs are finite).
-EXTRA_FLAGS = {"pq.hip": ["-fno-honor-nans"]}
+#
+# The attention kernels rescale their accumulators with vector instructions
+# now and then; held in the accumulation registers they would be moved there
+# and back on every step (64 moves of 500 instructions at 128 channels).
+EXTRA_FLAGS = {"pq.hip": ["-fno-honor-nans"], "kv_attend.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 
 def _compile(src: str) -> str:

@@ -51,43 +51,54 @@ template <int D> struct Strip {
     u32x4 vs[Pieces<D>::n];
 };
 
+// A lane's offsets into the four parts of a strip, whose first bytes are uniform
+// over the wave (scalar base, 32-bit lane offset).
+template <int D> struct LaneOffsets {
+    uint32_t k[Pieces<D>::n], ks[Pieces<D>::n], v[Pieces<D>::n], vs[Pieces<D>::n];
+    __device__ __forceinline__ LaneOffsets(int lane, int bs)
+    {
+        typedef Pieces<D> P;
+        const int m = lane & 15, h = lane >> 4, key = 4 * (m & 3) + (m >> 2);
+#pragma unroll
+        for (int c = 0; c < P::n; ++c) {
+            const int S = P::size(c), off = P::off(c), g = off / 32;
+            k[c] = key * (D / 2) + off / 2 + S / 8 * h;
+            ks[c] = key * (D / 32) + g + (S == 128 ? h : S == 64 ? h >> 1 : 0);
+            v[c] = h * (D / 2) + off / 2 + m * S / 32;
+            vs[c] = (g + (S == 128 ? m >> 2 : S == 64 ? m >> 3 : 0)) * bs;
+        }
+    }
+};
+
 template <int D>
-__device__ __forceinline__ void load_strip(Strip<D> &s, const uint8_t *rec, int bs, int strip, int lane)
+__device__ __forceinline__ void load_strip(Strip<D> &s, const uint8_t *rec, int bs, int strip, const LaneOffsets<D> &o)
 {
     typedef Pieces<D> P;
-    const int m = lane & 15, h = lane >> 4;
-    const int key = strip * 16 + 4 * (m & 3) + (m >> 2);
-    const uint8_t *kr = rec + key * (D / 2);
-    const uint8_t *ksr = rec + bs * D + key * (D / 32);
-    const uint8_t *vr = rec + bs * (D / 2) + (strip * 16 + h) * (D / 2);
-    const uint8_t *vsr = rec + bs * D + bs * (D / 32) + strip * 16;
+    const uint8_t *kr = rec + strip * (16 * (D / 2));
+    const uint8_t *vr = kr + bs * (D / 2);
+    const uint8_t *ksr = rec + bs * D + strip * (16 * (D / 32));
+    const uint8_t *vsr = rec + bs * (D + D / 32) + strip * 16;
 #pragma unroll
     for (int c = 0; c < P::n; ++c) {
-        constexpr int S0 = P::size(0), S1 = P::n > 1 ? P::size(1) : 32;
-        const int S = c == 0 ? S0 : S1;
-        const int off = P::off(c), g = off / 32;
+        const int S = P::size(c), g = P::off(c) / 32;
+        s.ks[c] = *(ksr + o.ks[c]);
+        s.vs[c] = *(const u32x4 *)(vsr + o.vs[c]);
         if (S == 128) {
-            const u32x4 x = *(const u32x4 *)(kr + off / 2 + 16 * h);
+            const u32x4 x = *(const u32x4 *)(kr + o.k[c]);
 #pragma unroll
             for (int i = 0; i < 4; ++i) s.k[g + i] = x[i];
-            s.ks[c] = ksr[g + h];
-            s.vs[c] = *(const u32x4 *)(vsr + (g + (m >> 2)) * bs);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s.v[c][i] = *(const uint32_t *)(vr + 4 * i * (D / 2) + off / 2 + 4 * m);
+            for (int i = 0; i < 4; ++i) s.v[c][i] = *(const uint32_t *)(vr + o.v[c] + 4 * i * (D / 2));
         } else if (S == 64) {
-            const u32x2 x = *(const u32x2 *)(kr + off / 2 + 8 * h);
+            const u32x2 x = *(const u32x2 *)(kr + o.k[c]);
             s.k[g] = x[0];
             s.k[g + 1] = x[1];
-            s.ks[c] = ksr[g + (h >> 1)];
-            s.vs[c] = *(const u32x4 *)(vsr + (g + (m >> 3)) * bs);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s.v[c][i] = *(const uint16_t *)(vr + 4 * i * (D / 2) + off / 2 + 2 * m);
+            for (int i = 0; i < 4; ++i) s.v[c][i] = *(const uint16_t *)(vr + o.v[c] + 4 * i * (D / 2));
         } else {
-            s.k[g] = *(const uint32_t *)(kr + off / 2 + 4 * h);
-            s.ks[c] = ksr[g];
-            s.vs[c] = *(const u32x4 *)(vsr + g * bs);
+            s.k[g] = *(const uint32_t *)(kr + o.k[c]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s.v[c][i] = vr[4 * i * (D / 2) + off / 2 + m];
+            for (int i = 0; i < 4; ++i) s.v[c][i] = *(vr + o.v[c] + 4 * i * (D / 2));
         }
     }
 }
@@ -229,117 +240,124 @@ __global__ __launch_bounds__(kThreads) void kv_attend_kernel(KvAttend a, int per
             }
         }
     };
-    Strip<D> cur[2], nxt[2];
-    int cpage[2], cbase[2], npage[2], nbase[2];
-    auto fetch = [&](Strip<D>(&s)[2], int(&page)[2], int(&base)[2]) {
+    const LaneOffsets<D> offs(lane, a.c.bs);
+    struct Pair {
+        Strip<D> s[2];
+        int page[2], base[2];
+    };
+    auto fetch = [&](Pair &x, int at_step) {
+        if (ahead == 32) {
+            look(at_step);
+            ahead = 0;
+        }
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            page[e] = __builtin_amdgcn_readlane(pages, 2 * ahead + e);
-            base[e] = __builtin_amdgcn_readlane(bases, 2 * ahead + e);
+            x.page[e] = __builtin_amdgcn_readlane(pages, 2 * ahead + e);
+            x.base[e] = __builtin_amdgcn_readlane(bases, 2 * ahead + e);
         }
-        if (page[0] >= 0 || page[1] >= 0) {
+        ++ahead;
+        if ((x.page[0] & x.page[1]) >= 0) {
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const uint8_t *rec = a.c.rec + ((int64_t)max(page[e], 0) * a.c.heads + head) * rec_bytes;
-                load_strip<D>(s[e], rec, a.c.bs, (base[e] >> 4) & strip_mask, lane);
+                const uint8_t *rec = a.c.rec + ((int64_t)max(x.page[e], 0) * a.c.heads + head) * rec_bytes;
+                load_strip<D>(x.s[e], rec, a.c.bs, (x.base[e] >> 4) & strip_mask, offs);
+            }
+        }
+    };
+    auto work = [&](const Pair &x) {
+        if ((x.page[0] & x.page[1]) < 0) return;  // neither strip is there
+        float t[8];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            f32x4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c < P::n; ++c) {
+                const float ks = kv_scale(x.s[e].ks[c]);
+#pragma unroll
+                for (int d = 0; d < P::size(c) / 32; ++d) {
+                    const int w = P::off(c) / 32 + d;
+                    y = TT::mfma(decode8<TT>(x.s[e].k[w], ks), qf[w], y);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) t[4 * e + i] = y[i] * a.scale;
+        }
+        float vs[P::n][8];
+#pragma unroll
+        for (int c = 0; c < P::n; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) vs[c][i] = kv_scale((x.s[i / 4].vs[c][i % 4] >> (8 * h)) & 255u);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            if (x.page[e] < 0 || x.base[e] + 15 > lim_min) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int key = x.page[e] < 0 ? INT32_MAX : x.base[e] + 4 * i + h;
+                    if (key > lim) t[4 * e + i] = -INFINITY;
+#pragma unroll
+                    for (int c = 0; c < P::n; ++c)
+                        if (key > lim_max) vs[c][4 * e + i] = 1.f;
+                }
+            }
+        }
+        const float mx = fmaxf(fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])), fmaxf(fmaxf(t[4], t[5]), fmaxf(t[6], t[7])));
+        if (__ballot(mx > ref + kRaise)) {
+            const float top = fmaxf(ref, max_over_h(mx));
+            const float f = ref == top ? 1.f : exp2_fast(ref - top);
+            ref = top;
+            sub = top == -INFINITY ? 0.f : top - kCarry;
+            sum *= f;
+#pragma unroll
+            for (int i = 0; i < kTiles; ++i) acc[i] *= f;
+        }
+        u32x4 pf;
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+            const float p0 = exp2_fast(t[i] - sub), p1 = exp2_fast(t[i + 1] - sub);
+            sum += p0 + p1;
+            pf[i / 2] = TT::pack(p0, p1);
+        }
+#pragma unroll
+        for (int c = 0; c < P::n; ++c) {
+            const int S = P::size(c);
+            uint32_t pair[8][4];  // [key][channel pair]
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t w = x.s[i / 4].v[c][i % 4];
+                pair[i][0] = TT::template decode<0>(w, vs[c][i]);
+                if (S >= 64) pair[i][1] = TT::template decode<1>(w, vs[c][i]);
+                if (S >= 128) {
+                    pair[i][2] = TT::template decode<2>(w, vs[c][i]);
+                    pair[i][3] = TT::template decode<3>(w, vs[c][i]);
+                }
+            }
+#pragma unroll
+            for (int p = 0; p < S / 32; ++p) {
+                u32x4 lo, hi;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    lo[i] = low_halves(pair[2 * i][p], pair[2 * i + 1][p]);
+                    hi[i] = high_halves(pair[2 * i][p], pair[2 * i + 1][p]);
+                }
+                const int tile = P::off(c) / 16 + 2 * p;
+                acc[tile] = TT::mfma(lo, pf, acc[tile]);
+                acc[tile + 1] = TT::mfma(hi, pf, acc[tile + 1]);
             }
         }
     };
     if (step < s_end) {
         look(step);
-        fetch(cur, cpage, cbase);
-    }
-    while (step < s_end) {
-        const int next = step + kWaves;
-        ++ahead;
-        if (next < s_end) {
-            if (ahead == 32) {
-                look(next);
-                ahead = 0;
-            }
-            fetch(nxt, npage, nbase);
-        }
-        if (cpage[0] >= 0 || cpage[1] >= 0) {
-            f32x4 st[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                f32x4 x = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int c = 0; c < P::n; ++c) {
-                    const float ks = kv_scale(cur[e].ks[c]);
-#pragma unroll
-                    for (int d = 0; d < P::size(c) / 32; ++d) {
-                        const int w = P::off(c) / 32 + d;
-                        x = TT::mfma(decode8<TT>(cur[e].k[w], ks), qf[w], x);
-                    }
-                }
-                st[e] = x;
-            }
-            bool cut[2];
-            float t[8], mx = -INFINITY;
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                cut[e] = cpage[e] < 0 || cbase[e] + 15 > lim_min;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float x = st[e][i] * a.scale;
-                    if (cut[e] && (cpage[e] < 0 || cbase[e] + 4 * i + h > lim)) x = -INFINITY;
-                    t[4 * e + i] = x;
-                    mx = fmaxf(mx, x);
-                }
-            }
-            if (__any(mx > ref + kRaise)) {
-                const float top = fmaxf(ref, max_over_h(mx));
-                const float f = ref == top ? 1.f : exp2_fast(ref - top);
-                ref = top;
-                sub = top == -INFINITY ? 0.f : top - kCarry;
-                sum *= f;
-#pragma unroll
-                for (int i = 0; i < kTiles; ++i) acc[i] *= f;
-            }
-            u32x4 pf;
-#pragma unroll
-            for (int i = 0; i < 8; i += 2) {
-                const float p0 = exp2_fast(t[i] - sub), p1 = exp2_fast(t[i + 1] - sub);
-                sum += p0 + p1;
-                pf[i / 2] = TT::pack(p0, p1);
-            }
-#pragma unroll
-            for (int c = 0; c < P::n; ++c) {
-                const int S = P::size(c);
-                uint32_t pair[2][4][4];  // [strip][key][channel pair]
-#pragma unroll
-                for (int e = 0; e < 2; ++e)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        float vs = kv_scale((cur[e].vs[c][i] >> (8 * h)) & 255u);
-                        if (cut[e] && (cpage[e] < 0 || cbase[e] + 4 * i + h > lim_max)) vs = 1.f;
-                        const uint32_t w = cur[e].v[c][i];
-                        pair[e][i][0] = TT::template decode<0>(w, vs);
-                        if (S >= 64) pair[e][i][1] = TT::template decode<1>(w, vs);
-                        if (S >= 128) {
-                            pair[e][i][2] = TT::template decode<2>(w, vs);
-                            pair[e][i][3] = TT::template decode<3>(w, vs);
-                        }
-                    }
-#pragma unroll
-                for (int p = 0; p < S / 32; ++p) {
-                    const u32x4 lo = {low_halves(pair[0][0][p], pair[0][1][p]), low_halves(pair[0][2][p], pair[0][3][p]),
-                                      low_halves(pair[1][0][p], pair[1][1][p]), low_halves(pair[1][2][p], pair[1][3][p])};
-                    const u32x4 hi = {high_halves(pair[0][0][p], pair[0][1][p]), high_halves(pair[0][2][p], pair[0][3][p]),
-                                      high_halves(pair[1][0][p], pair[1][1][p]), high_halves(pair[1][2][p], pair[1][3][p])};
-                    const int tile = P::off(c) / 16 + 2 * p;
-                    acc[tile] = TT::mfma(lo, pf, acc[tile]);
-                    acc[tile + 1] = TT::mfma(hi, pf, acc[tile + 1]);
-                }
-            }
-        }
-        step = next;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            cur[e] = nxt[e];
-            cpage[e] = npage[e];
-            cbase[e] = nbase[e];
+        Pair x, y;
+        fetch(x, step);
+        while (true) {
+            step += kWaves;
+            if (step < s_end) fetch(y, step);
+            work(x);
+            if (step >= s_end) break;
+            step += kWaves;
+            if (step < s_end) fetch(x, step);
+            work(y);
+            if (step >= s_end) break;
         }
     }
 
