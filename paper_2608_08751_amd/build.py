@@ -19,7 +19,7 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libivf.so")
 
 SOURCES = ["api.cpp", "screen.hip", "screen_i8.hip", "screen_f16.hip", "select.hip", "fallback.hip", "resolve.hip", "lists.hip", "lists_radix.hip", "kmeans.hip", "layout.hip", "pq.hip", "assign_graph.hip", "adc.hip", "probe.hip",
-           "api_kv.cpp", "kv_plan.hip", "kv_cache.hip", "kv_select.hip", "kv_attend.hip"]
+           "api_kv.cpp", "kv_plan.hip", "kv_cache.hip", "kv_select.hip", "kv_attend.hip", "kv_prompt.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
@@ -36,7 +36,8 @@ FLAGS = [
 # The attention kernels rescale their accumulators with vector instructions
 # now and then; held in the accumulation registers they would be moved there
 # and back on every step (64 moves of 500 instructions at 128 channels).
-EXTRA_FLAGS = {"pq.hip": ["-fno-honor-nans"], "kv_attend.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+VGPR_MFMA = ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
+EXTRA_FLAGS = {"pq.hip": ["-fno-honor-nans"], "kv_attend.hip": VGPR_MFMA, "kv_prompt.hip": VGPR_MFMA}
 
 
 def _compile(src: str) -> str:

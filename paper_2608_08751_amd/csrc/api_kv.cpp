@@ -119,27 +119,6 @@ ivf_status no_overlap(ivf_ctx *ctx, const Span *outs, int no, const Span *ins, i
     return IVF_OK;
 }
 
-struct AttendSizes {
-    int splits;
-    size_t bytes;  // of the workspace
-    size_t ml;     // offset of part_ml
-};
-
-AttendSizes attend_sizes(const KvCache &c, int64_t q_heads, int64_t T, int64_t B, int64_t cols, int64_t count,
-                         int64_t longest, int num_cus)
-{
-    AttendSizes r;
-    const int64_t keys = (count ? count : cols) << c.shift;
-    r.splits = kv_attend_splits(c.heads, (int)(q_heads / c.heads), T, B, keys, longest, count > 0, num_cus);
-    r.bytes = r.ml = 0;
-    if (r.splits > 1) {
-        const size_t n = (size_t)T * q_heads * r.splits;
-        r.ml = (n * c.dim * 4 + kAlign - 1) / kAlign * kAlign;
-        r.bytes = r.ml + n * 8 + kAlign;
-    }
-    return r;
-}
-
 }  // namespace
 
 extern "C" {
@@ -298,7 +277,8 @@ size_t ivf_kv_attend_bytes(const ivf_kv_cache *cache, int32_t q_heads, int64_t T
         int n = 0;
         if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && n > 0) num_cus = n;
     }
-    return attend_sizes(c, q_heads, T, B, table_cols, count, std::min(longest, T), num_cus).bytes;
+    const KvAttendPlan p = kv_attend_plan(c, q_heads / c.heads, T, B, table_cols, count, std::min(longest, T), num_cus);
+    return p.token_bytes + p.prompt_bytes;
 }
 
 ivf_status ivf_kv_attend(ivf_ctx *ctx, const ivf_kv_cache *cache, const void *q, int64_t q_token_stride,
@@ -334,15 +314,17 @@ ivf_status ivf_kv_attend(ivf_ctx *ctx, const ivf_kv_cache *cache, const void *q,
         for (const Span &o : outs)
             if (overlaps_cache(a.c, o.p, o.n)) return fail(ctx, IVF_EINVAL, "outputs overlap the cache");
         longest = std::min(longest, T);
-        const AttendSizes z = attend_sizes(a.c, q_heads, T, B, table_cols, count, longest, ctx->num_cus);
-        const int64_t per = ((blocks ? (int64_t)1 : longest) * (q_heads / a.c.heads) + 15) / 16;
-        if ((blocks ? T : B) * per * z.splits * a.c.heads > INT32_MAX)
+        const int group = q_heads / a.c.heads;
+        const KvAttendPlan p = kv_attend_plan(a.c, group, T, B, table_cols, count, longest, ctx->num_cus);
+        const int64_t tiles = (T * group + kv_prompt_rows(a.c.dim) - 1) / kv_prompt_rows(a.c.dim);
+        if (p.token_units * p.token_splits * a.c.heads > INT32_MAX || tiles * p.prompt_splits * a.c.heads > INT32_MAX)
             return fail(ctx, IVF_EUNSUPPORTED, "too many rows for one call");
-        if (z.splits > 1 && (st = check_ws(ctx, z.bytes)) != IVF_OK) return st;
+        const size_t need = p.token_bytes + p.prompt_bytes;
+        if (need && (st = check_ws(ctx, need)) != IVF_OK) return st;
         DeviceGuard g(ctx->device);
         if (!g.ok) return fail(ctx, IVF_EDEVICE, "no usable device (context device %d)", ctx->device);
         a.q = {q, q_token_stride, q_head_stride};
-        a.group = q_heads / a.c.heads;
+        a.group = group;
         a.T = T;
         a.start = start;
         a.request = request;
@@ -352,14 +334,30 @@ ivf_status ivf_kv_attend(ivf_ctx *ctx, const ivf_kv_cache *cache, const void *q,
         a.cols = table_cols;
         a.blocks = blocks;
         a.count = count;
-        a.scale = scale * 1.44269504089f;
+        // a scale of 0 as the least number above it: masked scores stay -infinity
+        a.scale = std::max(fabsf(scale) * 1.44269504089f, 0x1p-149f);
+        a.q_flip = scale < 0.f ? 0x80008000u : 0u;
         a.out = out;
         a.lse = out_lse;
-        a.splits = z.splits;
-        a.part = (float *)ctx->ws;
-        a.part_ml = (float2 *)((char *)ctx->ws + z.ml);
-        TIMED("kv_attend", launch_kv_attend(a, longest, ctx->stream));
-        if (z.splits > 1) TIMED("kv_combine", launch_kv_combine(a, ctx->stream));
+        a.small_rows = p.small_rows;
+        a.unit_rows = p.unit_rows;
+        a.per_unit = p.per_unit;
+        if (p.tokens) {
+            a.splits = p.token_splits;
+            a.part = (float *)ctx->ws;
+            a.part_ml = (float2 *)((char *)ctx->ws + p.token_ml);
+            TIMED("kv_attend", launch_kv_tokens(a, p.token_units, ctx->stream));
+            if (a.splits > 1)
+                TIMED("kv_combine", launch_kv_combine(a, !blocks, blocks ? T * q_heads : p.token_units * p.unit_rows * a.c.heads,
+                                                      ctx->stream));
+        }
+        if (p.prompt) {
+            a.splits = p.prompt_splits;
+            a.part = (float *)((char *)ctx->ws + p.token_bytes);
+            a.part_ml = (float2 *)((char *)ctx->ws + p.token_bytes + p.prompt_ml);
+            TIMED("kv_prompt", launch_kv_prompt(a, ctx->stream));
+            if (a.splits > 1) TIMED("kv_combine", launch_kv_combine(a, false, T * q_heads, ctx->stream));
+        }
         ctx->last_stats = nullptr;
         return IVF_OK;
     });

@@ -67,20 +67,40 @@ struct KvAttend {
     int cols;
     const int32_t *blocks;  // selected blocks, or null
     int count;
-    float scale;  // times log2(e)
+    float scale;      // |scale| log2(e), above 0
+    uint32_t q_flip;  // flips the signs of two query channels where the scale is negative
     void *out;
     float *lse;
-    // long key ranges are cut into `splits` parts, whose results lie here
-    // (row = token * query heads + head): sums [row][split][dim], and
-    // (reference, sum of exponentials) [row][split]
+    // a request with at most small_rows rows (tokens * group) is the single-token
+    // kernel's, any other the prompt kernel's
+    int64_t small_rows;
+    // Long key ranges are cut into `splits` parts, whose results lie here: sums
+    // [row][split][dim] and (reference, sum of exponentials) [row][split]. Rows: token *
+    // query heads + head, or, of the single-token kernel's requests, (unit *
+    // unit_rows + row of the unit) * heads + head with units of 16 rows.
     int splits;
+    int unit_rows;
+    int per_unit;  // units of a request, or of a token with `blocks`
     float *part;
     float2 *part_ml;
 };
-// Parts that a call of these sizes is cut into.
-int kv_attend_splits(int heads, int group, int64_t T, int64_t B, int64_t keys, int64_t longest, bool sparse,
-                     int num_cus);
-hipError_t launch_kv_attend(const KvAttend &a, int64_t longest, hipStream_t s);
-hipError_t launch_kv_combine(const KvAttend &a, hipStream_t s);
+
+// Which kernels take a call, in how many parts, and what those need.
+struct KvAttendPlan {
+    bool tokens, prompt;
+    int64_t small_rows;
+    int per_unit, unit_rows;
+    int token_splits, prompt_splits;
+    int64_t token_units;  // workgroups of the single-token kernel per head and part
+    size_t token_bytes, token_ml, prompt_bytes, prompt_ml;  // workspace, and where part_ml begins in it
+};
+KvAttendPlan kv_attend_plan(const KvCache &c, int group, int64_t T, int64_t B, int64_t cols, int64_t count,
+                            int64_t longest, int num_cus);
+hipError_t launch_kv_tokens(const KvAttend &a, int64_t units, hipStream_t s);
+// Joins the parts of `rows` rows (heads included) of the single-token kernel's units, or of all tokens.
+hipError_t launch_kv_combine(const KvAttend &a, bool units, int64_t rows, hipStream_t s);
+
+int kv_prompt_rows(int dim);  // rows of a workgroup
+hipError_t launch_kv_prompt(const KvAttend &a, hipStream_t s);
 
 }  // namespace ivf

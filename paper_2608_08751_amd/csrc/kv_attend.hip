@@ -23,107 +23,16 @@
 // step with its own reference, sums and output, joined in LDS. What bounds single
 // tokens is the read of the cache, 17 / 16 bytes per channel of key and value.
 #include "kv.h"
-#include "kv_types.h"
+#include "kv_strip.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace ivf {
 namespace {
 
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
-constexpr float kRaise = 6.f;  // a score may pass the reference by this much
-constexpr float kCarry = 8.f;  // probabilities are times 2^kCarry
 constexpr int kMinSteps = 8;   // steps of 32 keys that a part is worth
-
-// A row of channels is taken as one or two pieces of 128, 64 or 32.
-template <int D> struct Pieces {
-    static constexpr int first = D >= 128 ? 128 : 64, second = D - first;
-    static constexpr int n = second ? 2 : 1;
-    static constexpr int size(int c) { return c == 0 ? first : second; }
-    static constexpr int off(int c) { return c == 0 ? 0 : first; }
-};
-
-// One strip of 16 keys and values of a head, as a lane holds it.
-template <int D> struct Strip {
-    uint32_t k[D / 32];
-    uint32_t ks[Pieces<D>::n];
-    uint32_t v[Pieces<D>::n][4];
-    u32x4 vs[Pieces<D>::n];
-};
-
-// A lane's offsets into the four parts of a strip, whose first bytes are uniform
-// over the wave (scalar base, 32-bit lane offset).
-template <int D> struct LaneOffsets {
-    uint32_t k[Pieces<D>::n], ks[Pieces<D>::n], v[Pieces<D>::n], vs[Pieces<D>::n];
-    __device__ __forceinline__ LaneOffsets(int lane, int bs)
-    {
-        typedef Pieces<D> P;
-        const int m = lane & 15, h = lane >> 4, key = 4 * (m & 3) + (m >> 2);
-#pragma unroll
-        for (int c = 0; c < P::n; ++c) {
-            const int S = P::size(c), off = P::off(c), g = off / 32;
-            k[c] = key * (D / 2) + off / 2 + S / 8 * h;
-            ks[c] = key * (D / 32) + g + (S == 128 ? h : S == 64 ? h >> 1 : 0);
-            v[c] = h * (D / 2) + off / 2 + m * S / 32;
-            vs[c] = (g + (S == 128 ? m >> 2 : S == 64 ? m >> 3 : 0)) * bs;
-        }
-    }
-};
-
-template <int D>
-__device__ __forceinline__ void load_strip(Strip<D> &s, const uint8_t *rec, int bs, int strip, const LaneOffsets<D> &o)
-{
-    typedef Pieces<D> P;
-    const uint8_t *kr = rec + strip * (16 * (D / 2));
-    const uint8_t *vr = kr + bs * (D / 2);
-    const uint8_t *ksr = rec + bs * D + strip * (16 * (D / 32));
-    const uint8_t *vsr = rec + bs * (D + D / 32) + strip * 16;
-#pragma unroll
-    for (int c = 0; c < P::n; ++c) {
-        const int S = P::size(c), g = P::off(c) / 32;
-        s.ks[c] = *(ksr + o.ks[c]);
-        s.vs[c] = *(const u32x4 *)(vsr + o.vs[c]);
-        if (S == 128) {
-            const u32x4 x = *(const u32x4 *)(kr + o.k[c]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s.k[g + i] = x[i];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s.v[c][i] = *(const uint32_t *)(vr + o.v[c] + 4 * i * (D / 2));
-        } else if (S == 64) {
-            const u32x2 x = *(const u32x2 *)(kr + o.k[c]);
-            s.k[g] = x[0];
-            s.k[g + 1] = x[1];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s.v[c][i] = *(const uint16_t *)(vr + o.v[c] + 4 * i * (D / 2));
-        } else {
-            s.k[g] = *(const uint32_t *)(kr + o.k[c]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s.v[c][i] = *(vr + o.v[c] + 4 * i * (D / 2));
-        }
-    }
-}
-
-template <typename TT> __device__ __forceinline__ u32x4 decode8(uint32_t w, float scale)
-{
-    return (u32x4){TT::template decode<0>(w, scale), TT::template decode<1>(w, scale), TT::template decode<2>(w, scale),
-                   TT::template decode<3>(w, scale)};
-}
-
-__device__ __forceinline__ uint32_t low_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
-__device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
-
-__device__ __forceinline__ float max_over_h(float x)
-{
-    x = fmaxf(x, __shfl_xor(x, 16));
-    return fmaxf(x, __shfl_xor(x, 32));
-}
-__device__ __forceinline__ float sum_over_h(float x)
-{
-    x += __shfl_xor(x, 16);
-    return x + __shfl_xor(x, 32);
-}
-
-__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // The rows of one workgroup: rows r0 ... r0 + n of a request's (or token's) rows,
 // row = token * group + head of the group.
@@ -134,7 +43,7 @@ struct RowSet {
 };
 
 template <typename TT, int D, bool SPARSE>
-__global__ __launch_bounds__(kThreads) void kv_attend_kernel(KvAttend a, int per_unit)
+__global__ __launch_bounds__(kThreads) void kv_attend_kernel(KvAttend a)
 {
     typedef Pieces<D> P;
     typedef typename TT::elem elem;
@@ -150,18 +59,18 @@ __global__ __launch_bounds__(kThreads) void kv_attend_kernel(KvAttend a, int per
 
     RowSet rs;
     if (SPARSE) {
-        rs.t0 = unit / per_unit;
-        rs.r0 = (int)(unit % per_unit) * 16;
+        rs.t0 = unit / a.per_unit;
+        rs.r0 = (int)(unit % a.per_unit) * 16;
         rs.n = min(16, a.group - rs.r0);
         rs.b = a.request[rs.t0];
     } else {
-        rs.b = (int)(unit / per_unit);
-        rs.r0 = (int)(unit % per_unit) * 16;
+        rs.b = (int)(unit / a.per_unit);
+        rs.r0 = (int)(unit % a.per_unit) * 16;
         const int64_t t0 = min(max((int64_t)a.start[rs.b], (int64_t)0), a.T);
         const int64_t t1 = min(max((int64_t)a.start[rs.b + 1], t0), a.T);
         rs.t0 = t0;
         const int64_t rows = (t1 - t0) * a.group;
-        if (rs.r0 >= rows) return;
+        if (rs.r0 >= rows || rows > a.small_rows) return;
         rs.n = (int)min((int64_t)16, rows - rs.r0);
     }
     const bool live = rs.b >= 0 && rs.b < a.B;
@@ -191,7 +100,7 @@ __global__ __launch_bounds__(kThreads) void kv_attend_kernel(KvAttend a, int per
             for (int d = 0; d < P::size(c) / 32; ++d) {
                 u32x4 x = {0, 0, 0, 0};
                 if (have) x = *(const u32x4 *)(q + P::off(c) + P::size(c) / 4 * h + 8 * d);
-                qf[P::off(c) / 32 + d] = x;
+                qf[P::off(c) / 32 + d] = x ^ a.q_flip;
             }
     }
 
@@ -282,11 +191,11 @@ __global__ __launch_bounds__(kThreads) void kv_attend_kernel(KvAttend a, int per
 #pragma unroll
             for (int i = 0; i < 4; ++i) t[4 * e + i] = y[i] * a.scale;
         }
-        float vs[P::n][8];
+        float vs[P::n][2][4];
 #pragma unroll
         for (int c = 0; c < P::n; ++c)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) vs[c][i] = kv_scale((x.s[i / 4].vs[c][i % 4] >> (8 * h)) & 255u);
+            for (int i = 0; i < 8; ++i) vs[c][i / 4][i % 4] = kv_scale((x.s[i / 4].vs[c][i % 4] >> (8 * h)) & 255u);
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             if (x.page[e] < 0 || x.base[e] + 15 > lim_min) {
@@ -296,11 +205,11 @@ __global__ __launch_bounds__(kThreads) void kv_attend_kernel(KvAttend a, int per
                     if (key > lim) t[4 * e + i] = -INFINITY;
 #pragma unroll
                     for (int c = 0; c < P::n; ++c)
-                        if (key > lim_max) vs[c][4 * e + i] = 1.f;
+                        if (key > lim_max) vs[c][e][i] = 1.f;
                 }
             }
         }
-        const float mx = fmaxf(fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])), fmaxf(fmaxf(t[4], t[5]), fmaxf(t[6], t[7])));
+        const float mx = max3(max3(t[0], t[1], t[2]), max3(t[3], t[4], t[5]), max3(t[6], t[7], t[7]));
         if (__ballot(mx > ref + kRaise)) {
             const float top = fmaxf(ref, max_over_h(mx));
             const float f = ref == top ? 1.f : exp2_fast(ref - top);
@@ -317,33 +226,19 @@ __global__ __launch_bounds__(kThreads) void kv_attend_kernel(KvAttend a, int per
             sum += p0 + p1;
             pf[i / 2] = TT::pack(p0, p1);
         }
+        auto piece = [&](auto piece_c) {
+            constexpr int c = decltype(piece_c)::value, S = P::size(c);
+            u32x2 v0[S / 16], v1[S / 16];
+            value_operands<TT, S>(x.s[0].v[c], vs[c][0], v0);
+            value_operands<TT, S>(x.s[1].v[c], vs[c][1], v1);
 #pragma unroll
-        for (int c = 0; c < P::n; ++c) {
-            const int S = P::size(c);
-            uint32_t pair[8][4];  // [key][channel pair]
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const uint32_t w = x.s[i / 4].v[c][i % 4];
-                pair[i][0] = TT::template decode<0>(w, vs[c][i]);
-                if (S >= 64) pair[i][1] = TT::template decode<1>(w, vs[c][i]);
-                if (S >= 128) {
-                    pair[i][2] = TT::template decode<2>(w, vs[c][i]);
-                    pair[i][3] = TT::template decode<3>(w, vs[c][i]);
-                }
+            for (int j = 0; j < S / 16; ++j) {
+                const u32x4 v = {v0[j][0], v0[j][1], v1[j][0], v1[j][1]};
+                acc[P::off(c) / 16 + j] = TT::mfma(v, pf, acc[P::off(c) / 16 + j]);
             }
-#pragma unroll
-            for (int p = 0; p < S / 32; ++p) {
-                u32x4 lo, hi;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    lo[i] = low_halves(pair[2 * i][p], pair[2 * i + 1][p]);
-                    hi[i] = high_halves(pair[2 * i][p], pair[2 * i + 1][p]);
-                }
-                const int tile = P::off(c) / 16 + 2 * p;
-                acc[tile] = TT::mfma(lo, pf, acc[tile]);
-                acc[tile + 1] = TT::mfma(hi, pf, acc[tile + 1]);
-            }
-        }
+        };
+        piece(std::integral_constant<int, 0>());
+        if constexpr (P::n > 1) piece(std::integral_constant<int, 1>());
     };
     if (step < s_end) {
         look(step);
@@ -406,130 +301,168 @@ __global__ __launch_bounds__(kThreads) void kv_attend_kernel(KvAttend a, int per
 
     const int64_t orow = tok * ((int64_t)a.c.heads * a.group) + qhead;
     if (a.splits == 1) {
-        const float inv = total == 0.f ? 0.f : 1.f / total;
-        elem *o = (elem *)a.out + orow * D;
-#pragma unroll
-        for (int c = 0; c < P::n; ++c) {
-            const int S = P::size(c), tile0 = P::off(c) / 16;
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-#pragma unroll
-                for (int j = 0; j < S / 16; j += 2)
-                    *(uint32_t *)(o + P::off(c) + S / 4 * h + S / 16 * r + j) =
-                        TT::pack(acc[tile0 + j][r] * inv, acc[tile0 + j + 1][r] * inv);
-        }
-        if (a.lse && h == 0)
-            a.lse[orow] = total == 0.f ? -INFINITY : (top - kCarry + __builtin_amdgcn_logf(total)) * 0.69314718056f;
+        write_rows<TT, D>(acc, (elem *)a.out + orow * D, total == 0.f ? 0.f : 1.f / total, h);
+        if (a.lse && h == 0) a.lse[orow] = log_of(top, total);
     } else {
-        const int64_t at = orow * a.splits + split;
+        const int64_t prow = SPARSE ? orow : (unit * a.unit_rows + col) * a.c.heads + head;
+        const int64_t at = prow * a.splits + split;
         if (h == 0) a.part_ml[at] = make_float2(top, total);
-        float *o = a.part + at * D;
-#pragma unroll
-        for (int c = 0; c < P::n; ++c) {
-            const int S = P::size(c), tile0 = P::off(c) / 16;
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-#pragma unroll
-                for (int j = 0; j < S / 16; j += 2)
-                    *(float2 *)(o + P::off(c) + S / 4 * h + S / 16 * r + j) =
-                        make_float2(acc[tile0 + j][r], acc[tile0 + j + 1][r]);
-        }
+        write_part<D>(acc, a.part + at * D, h);
     }
 }
 
-// Joins the parts of a row: a wave per row, lanes over channels.
-template <typename TT>
-__global__ __launch_bounds__(kThreads) void kv_combine_kernel(KvAttend a)
+// Joins the parts of a row: a wave per row, lanes over channels. Parts without
+// keys lie behind the others (or hold zeros), so the loop ends at the last that has some.
+template <typename TT, bool UNITS>
+__global__ __launch_bounds__(kThreads) void kv_combine_kernel(KvAttend a, int64_t rows)
 {
     typedef typename TT::elem elem;
     const int lane = threadIdx.x & 63;
-    const int64_t heads = (int64_t)a.c.heads * a.group;
-    const int64_t row = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
-    if (row >= a.T * heads) return;
-    if (!a.blocks) {
-        const int64_t t = row / heads;
-        if (t < a.start[0] || t >= a.start[a.B]) return;
+    const int64_t row = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (row >= rows) return;
+    int64_t orow = row;
+    if (UNITS) {
+        const int head = (int)(row % a.c.heads);
+        const int64_t x = row / a.c.heads, unit = x / a.unit_rows, b = unit / a.per_unit;
+        const int64_t r = unit % a.per_unit * 16 + x % a.unit_rows;
+        const int64_t t0 = min(max((int64_t)a.start[b], (int64_t)0), a.T);
+        const int64_t n = (min(max((int64_t)a.start[b + 1], t0), a.T) - t0) * a.group;
+        if (r >= n || n > a.small_rows) return;
+        orow = ((t0 + r / a.group) * a.c.heads + head) * a.group + r % a.group;
+    } else if (!a.blocks) {
+        const int64_t t = row / ((int64_t)a.c.heads * a.group);
+        int64_t b = 0, hi = a.B;
+        while (hi - b > 1) {
+            const int64_t mid = (b + hi) >> 1;
+            if (a.start[mid] <= t) b = mid;
+            else hi = mid;
+        }
+        const int64_t t0 = min(max((int64_t)a.start[b], (int64_t)0), a.T);
+        const int64_t t1 = min(max((int64_t)a.start[b + 1], t0), a.T);
+        if (t < t0 || t >= t1 || (t1 - t0) * a.group <= a.small_rows) return;
     }
     const float2 *ml = a.part_ml + row * a.splits;
-    float top = -INFINITY;
-    for (int s = lane; s < a.splits; s += 64) top = fmaxf(top, ml[s].x);
+    const float2 none = make_float2(-INFINITY, 0.f);
+    const float2 x0 = lane < a.splits ? ml[lane] : none, x1 = lane + 64 < a.splits ? ml[lane + 64] : none;
+    float top = fmaxf(x0.x, x1.x);
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
-    float total = 0.f;
-    float2 o[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-    for (int s = 0; s < a.splits; ++s) {
-        const float2 x = ml[s];
-        if (x.y == 0.f) continue;  // a part without keys
-        const float f = x.x > -INFINITY ? exp2_fast(x.x - top) : x.y;
-        total += x.y * f;
-        const float *p = a.part + (row * a.splits + s) * a.c.dim;
+    auto factor = [&](float2 x) { return x.y == 0.f ? 0.f : x.x > -INFINITY ? exp2_fast(x.x - top) : x.y; };
+    const float f0 = factor(x0), f1 = factor(x1);
+    float total = x0.y * f0 + x1.y * f1;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int d = 2 * (lane + 64 * i);
-            if (d < a.c.dim) {
-                const float2 y = *(const float2 *)(p + d);
-                o[i].x += y.x * f;
-                o[i].y += y.y * f;
-            }
-        }
+    for (int d = 1; d < 64; d <<= 1) total += __shfl_xor(total, d);
+    const uint64_t m1 = __ballot(f1 != 0.f), m0 = __ballot(f0 != 0.f);
+    const int parts = m1 ? 128 - __clzll((long long)m1) : m0 ? 64 - __clzll((long long)m0) : 0;
+    float2 o[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+    const float *p = a.part + row * a.splits * a.c.dim + 2 * lane;
+    const bool in0 = 2 * lane < a.c.dim, in1 = 128 + 2 * lane < a.c.dim;
+#pragma unroll 8
+    for (int s = 0; s < parts; ++s) {
+        const float f = __uint_as_float(s < 64 ? __builtin_amdgcn_readlane(__float_as_uint(f0), s & 63)
+                                               : __builtin_amdgcn_readlane(__float_as_uint(f1), s & 63));
+        const float2 y0 = in0 ? *(const float2 *)(p + (int64_t)s * a.c.dim) : make_float2(0.f, 0.f);
+        const float2 y1 = in1 ? *(const float2 *)(p + (int64_t)s * a.c.dim + 128) : make_float2(0.f, 0.f);
+        o[0].x += y0.x * f;
+        o[0].y += y0.y * f;
+        o[1].x += y1.x * f;
+        o[1].y += y1.y * f;
     }
     const float inv = total == 0.f ? 0.f : 1.f / total;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int d = 2 * (lane + 64 * i);
-        if (d < a.c.dim) *(uint32_t *)((elem *)a.out + row * a.c.dim + d) = TT::pack(o[i].x * inv, o[i].y * inv);
-    }
-    if (a.lse && lane == 0)
-        a.lse[row] = total == 0.f ? -INFINITY : (top - kCarry + __builtin_amdgcn_logf(total)) * 0.69314718056f;
+    elem *out = (elem *)a.out + orow * a.c.dim + 2 * lane;
+    if (in0) *(uint32_t *)out = TT::pack(o[0].x * inv, o[0].y * inv);
+    if (in1) *(uint32_t *)(out + 128) = TT::pack(o[1].x * inv, o[1].y * inv);
+    if (a.lse && lane == 0) a.lse[orow] = log_of(top, total);
 }
 
-template <typename TT, int D> hipError_t launch_attend(const KvAttend &a, int64_t longest, hipStream_t s)
+template <typename TT, int D> hipError_t launch_tokens(const KvAttend &a, int64_t units, hipStream_t s)
 {
-    const int per = (int)(a.blocks ? (a.group + 15) / 16 : (longest * a.group + 15) / 16);
-    const int64_t units = (a.blocks ? a.T : a.B) * per;
     const unsigned grid = (unsigned)(units * a.splits * a.c.heads);
     if (a.blocks)
-        hipLaunchKernelGGL((kv_attend_kernel<TT, D, true>), dim3(grid), dim3(kThreads), 0, s, a, per);
+        hipLaunchKernelGGL((kv_attend_kernel<TT, D, true>), dim3(grid), dim3(kThreads), 0, s, a);
     else
-        hipLaunchKernelGGL((kv_attend_kernel<TT, D, false>), dim3(grid), dim3(kThreads), 0, s, a, per);
+        hipLaunchKernelGGL((kv_attend_kernel<TT, D, false>), dim3(grid), dim3(kThreads), 0, s, a);
     return hipGetLastError();
 }
 
-template <typename TT> hipError_t launch_attend_dim(const KvAttend &a, int64_t longest, hipStream_t s)
+template <typename TT> hipError_t launch_tokens_dim(const KvAttend &a, int64_t units, hipStream_t s)
 {
     switch (a.c.dim) {
-    case 64: return launch_attend<TT, 64>(a, longest, s);
-    case 96: return launch_attend<TT, 96>(a, longest, s);
-    case 128: return launch_attend<TT, 128>(a, longest, s);
-    case 192: return launch_attend<TT, 192>(a, longest, s);
-    default: return launch_attend<TT, 256>(a, longest, s);
+    case 64: return launch_tokens<TT, 64>(a, units, s);
+    case 96: return launch_tokens<TT, 96>(a, units, s);
+    case 128: return launch_tokens<TT, 128>(a, units, s);
+    case 192: return launch_tokens<TT, 192>(a, units, s);
+    default: return launch_tokens<TT, 256>(a, units, s);
     }
 }
 
+// Requests with at most this many rows go through the single-token kernel,
+// 16 rows a workgroup, where others take the prompt kernel.
+constexpr int64_t kSmallRows = 64;
+
 }  // namespace
 
-int kv_attend_splits(int heads, int group, int64_t T, int64_t B, int64_t keys, int64_t longest, bool sparse,
-                     int num_cus)
+KvAttendPlan kv_attend_plan(const KvCache &c, int group, int64_t T, int64_t B, int64_t cols, int64_t count,
+                            int64_t longest, int num_cus)
 {
-    const int64_t units = (sparse ? T * ((group + 15) / 16) : B * ((longest * group + 15) / 16)) * heads;
+    KvAttendPlan p = {};
+    const int64_t keys = (count ? count : cols) << c.shift;
     const int64_t most = std::max<int64_t>(1, keys / (32 * kMinSteps));
-    const int64_t want = ((int64_t)num_cus * 8 + units - 1) / units;
-    return (int)std::max<int64_t>(1, std::min<int64_t>(std::min(want, most), 128));
+    auto align = [](size_t n) { return (n + 255) / 256 * 256; };
+    int64_t rows;  // of one unit at most, of one request or token
+    if (count) {
+        p.tokens = true;
+        rows = group;
+        p.small_rows = INT64_MAX;
+    } else {
+        rows = longest * group;
+        p.tokens = rows <= kSmallRows || B > 1;
+        p.prompt = rows > kSmallRows;
+        p.small_rows = !p.prompt ? INT64_MAX : p.tokens ? kSmallRows : 0;
+        rows = std::min(rows, kSmallRows);
+    }
+    p.token_splits = p.prompt_splits = 1;
+    if (p.tokens) {
+        p.per_unit = (int)((rows + 15) / 16);
+        p.unit_rows = (int)std::min<int64_t>(rows, 16);
+        p.token_units = (count ? T : B) * p.per_unit;
+        // beside a prompt most of a request's units are empty
+        const int64_t busy = (p.prompt ? B * ((group + 15) / 16) : p.token_units) * c.heads;
+        const int64_t want = ((int64_t)num_cus * 8 + busy - 1) / busy;
+        p.token_splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(want, most), 128));
+        if (p.token_splits > 1) {
+            const size_t n = (size_t)(count ? T * group : p.token_units * p.unit_rows) * c.heads * p.token_splits;
+            p.token_ml = align(n * c.dim * 4);
+            p.token_bytes = p.token_ml + align(n * 8);
+        }
+    }
+    if (p.prompt) {
+        const int64_t units = (T * group + kv_prompt_rows(c.dim) - 1) / kv_prompt_rows(c.dim) * c.heads;
+        if (units < num_cus) {
+            const int64_t want = (2 * (int64_t)num_cus + units - 1) / units;
+            p.prompt_splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(want, most), 32));
+        }
+        if (p.prompt_splits > 1) {
+            const size_t n = (size_t)T * group * c.heads * p.prompt_splits;
+            p.prompt_ml = align(n * c.dim * 4);
+            p.prompt_bytes = p.prompt_ml + align(n * 8);
+        }
+    }
+    return p;
 }
 
-hipError_t launch_kv_attend(const KvAttend &a, int64_t longest, hipStream_t s)
+hipError_t launch_kv_tokens(const KvAttend &a, int64_t units, hipStream_t s)
 {
-    return a.c.bf16 ? launch_attend_dim<KvBf16>(a, longest, s) : launch_attend_dim<KvF16>(a, longest, s);
+    return a.c.bf16 ? launch_tokens_dim<KvBf16>(a, units, s) : launch_tokens_dim<KvF16>(a, units, s);
 }
 
-hipError_t launch_kv_combine(const KvAttend &a, hipStream_t s)
+hipError_t launch_kv_combine(const KvAttend &a, bool units, int64_t rows, hipStream_t s)
 {
-    const int64_t rows = a.T * a.c.heads * a.group;
-    const unsigned grid = (unsigned)((rows + kWaves - 1) / kWaves);
-    if (a.c.bf16)
-        hipLaunchKernelGGL((kv_combine_kernel<KvBf16>), dim3(grid), dim3(kThreads), 0, s, a);
-    else
-        hipLaunchKernelGGL((kv_combine_kernel<KvF16>), dim3(grid), dim3(kThreads), 0, s, a);
+    const dim3 grid((unsigned)((rows + kWaves - 1) / kWaves)), block(kThreads);
+    if (a.c.bf16 && units) hipLaunchKernelGGL((kv_combine_kernel<KvBf16, true>), grid, block, 0, s, a, rows);
+    else if (a.c.bf16) hipLaunchKernelGGL((kv_combine_kernel<KvBf16, false>), grid, block, 0, s, a, rows);
+    else if (units) hipLaunchKernelGGL((kv_combine_kernel<KvF16, true>), grid, block, 0, s, a, rows);
+    else hipLaunchKernelGGL((kv_combine_kernel<KvF16, false>), grid, block, 0, s, a, rows);
     return hipGetLastError();
 }
 
