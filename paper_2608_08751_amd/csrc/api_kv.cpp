@@ -317,7 +317,8 @@ ivf_status ivf_kv_attend(ivf_ctx *ctx, const ivf_kv_cache *cache, const void *q,
         const int group = q_heads / a.c.heads;
         const KvAttendPlan p = kv_attend_plan(a.c, group, T, B, table_cols, count, longest, ctx->num_cus);
         const int64_t tiles = (T * group + kv_prompt_rows(a.c.dim) - 1) / kv_prompt_rows(a.c.dim);
-        if (p.token_units * p.token_splits * a.c.heads > INT32_MAX || tiles * p.prompt_splits * a.c.heads > INT32_MAX)
+        if (p.token_groups * a.c.heads > INT32_MAX || p.units * 16 * a.c.heads > INT32_MAX ||
+            tiles * p.prompt_splits * a.c.heads > INT32_MAX || T * q_heads > INT32_MAX)
             return fail(ctx, IVF_EUNSUPPORTED, "too many rows for one call");
         const size_t need = p.token_bytes + p.prompt_bytes;
         if (need && (st = check_ws(ctx, need)) != IVF_OK) return st;
@@ -342,21 +343,24 @@ ivf_status ivf_kv_attend(ivf_ctx *ctx, const ivf_kv_cache *cache, const void *q,
         a.small_rows = p.small_rows;
         a.unit_rows = p.unit_rows;
         a.per_unit = p.per_unit;
+        a.units = (int)p.units;
+        a.slots = (int)p.slots;
         if (p.tokens) {
+            char *ws = (char *)ctx->ws;
             a.splits = p.token_splits;
-            a.part = (float *)ctx->ws;
-            a.part_ml = (float2 *)((char *)ctx->ws + p.token_ml);
-            TIMED("kv_attend", launch_kv_tokens(a, p.token_units, ctx->stream));
-            if (a.splits > 1)
-                TIMED("kv_combine", launch_kv_combine(a, !blocks, blocks ? T * q_heads : p.token_units * p.unit_rows * a.c.heads,
-                                                      ctx->stream));
+            a.part = (float *)ws;
+            a.part_ml = (float2 *)(ws + p.token_ml);
+            a.unit_parts = (int2 *)(ws + p.token_parts);
+            TIMED("kv_attend", launch_kv_tokens(a, p.token_groups, ctx->stream));
+            if (a.splits > 1) TIMED("kv_combine", launch_kv_combine(a, false, ctx->stream));
         }
         if (p.prompt) {
+            char *ws = (char *)ctx->ws + p.token_bytes;
             a.splits = p.prompt_splits;
-            a.part = (float *)((char *)ctx->ws + p.token_bytes);
-            a.part_ml = (float2 *)((char *)ctx->ws + p.token_bytes + p.prompt_ml);
+            a.part = (float *)ws;
+            a.part_ml = (float2 *)(ws + p.prompt_ml);
             TIMED("kv_prompt", launch_kv_prompt(a, ctx->stream));
-            if (a.splits > 1) TIMED("kv_combine", launch_kv_combine(a, false, T * q_heads, ctx->stream));
+            if (a.splits > 1) TIMED("kv_combine", launch_kv_combine(a, true, ctx->stream));
         }
         ctx->last_stats = nullptr;
         return IVF_OK;

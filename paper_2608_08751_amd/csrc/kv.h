@@ -11,6 +11,7 @@ namespace ivf {
 constexpr int kKvMaxRequests = 16384;  // of one plan: their prefix sums lie in LDS
 constexpr int kKvMaxSelectCols = 32768;  // block scores of a row lie in LDS
 constexpr int kKvMaxCount = 4096;
+constexpr int kKvMaxUnits = 1024;  // whose key ranges are shared out evenly (prefix sums in LDS)
 
 struct KvCache {
     uint8_t *rec;
@@ -74,15 +75,20 @@ struct KvAttend {
     // a request with at most small_rows rows (tokens * group) is the single-token
     // kernel's, any other the prompt kernel's
     int64_t small_rows;
-    // Long key ranges are cut into `splits` parts, whose results lie here: sums
-    // [row][split][dim] and (reference, sum of exponentials) [row][split]. Rows: token *
-    // query heads + head, or, of the single-token kernel's requests, (unit *
-    // unit_rows + row of the unit) * heads + head with units of 16 rows.
+    // Long key ranges are cut into parts, whose results lie here: sums
+    // [row][dim] and (reference, sum of exponentials) [row]. With blocks, and of the
+    // prompt kernel, every row has `splits` parts, [token][query head][split]. Of the
+    // single-token kernel without blocks `splits` workgroups a head share all units'
+    // keys; rows are [head][slot][unit_rows], and unit_parts holds each unit's first
+    // slot and number of parts (1: written to `out` at once). splits 1: no parts.
     int splits;
-    int unit_rows;
-    int per_unit;  // units of a request, or of a token with `blocks`
+    int unit_rows;  // rows that a unit has room for
+    int per_unit;   // units of a request, or of a token with `blocks`
+    int units;
+    int slots;
     float *part;
     float2 *part_ml;
+    int2 *unit_parts;
 };
 
 // Which kernels take a call, in how many parts, and what those need.
@@ -90,15 +96,16 @@ struct KvAttendPlan {
     bool tokens, prompt;
     int64_t small_rows;
     int per_unit, unit_rows;
+    int64_t units, slots;
     int token_splits, prompt_splits;
-    int64_t token_units;  // workgroups of the single-token kernel per head and part
-    size_t token_bytes, token_ml, prompt_bytes, prompt_ml;  // workspace, and where part_ml begins in it
+    int64_t token_groups;  // workgroups of the single-token kernel per head
+    // workspace, and where part_ml and unit_parts begin in it
+    size_t token_bytes, token_ml, token_parts, prompt_bytes, prompt_ml;
 };
 KvAttendPlan kv_attend_plan(const KvCache &c, int group, int64_t T, int64_t B, int64_t cols, int64_t count,
                             int64_t longest, int num_cus);
-hipError_t launch_kv_tokens(const KvAttend &a, int64_t units, hipStream_t s);
-// Joins the parts of `rows` rows (heads included) of the single-token kernel's units, or of all tokens.
-hipError_t launch_kv_combine(const KvAttend &a, bool units, int64_t rows, hipStream_t s);
+hipError_t launch_kv_tokens(const KvAttend &a, int64_t groups, hipStream_t s);
+hipError_t launch_kv_combine(const KvAttend &a, bool prompt, hipStream_t s);
 
 int kv_prompt_rows(int dim);  // rows of a workgroup
 hipError_t launch_kv_prompt(const KvAttend &a, hipStream_t s);

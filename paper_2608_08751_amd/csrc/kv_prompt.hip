@@ -38,9 +38,10 @@ __global__ __launch_bounds__(kThreads, 2) void kv_prompt_kernel(KvAttend a, int 
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, h = lane >> 4;
-    const int head = blockIdx.x % a.c.heads;
-    const int split = (blockIdx.x / a.c.heads) % a.splits;
-    const int64_t tile = tiles - 1 - blockIdx.x / a.c.heads / a.splits;  // the last rows see most keys: first
+    const uint32_t heads = a.c.heads, bid = blockIdx.x, part = bid / heads;
+    const int head = (int)(bid - part * heads);
+    const int split = (int)(part % (uint32_t)a.splits);
+    const int64_t tile = tiles - 1 - (int)(part / (uint32_t)a.splits);  // the last rows see most keys: first
 
     const int64_t all_rows = a.T * a.group, g0 = tile * kRows;
     const int64_t t_first = g0 / a.group, t_last = (min(g0 + kRows, all_rows) - 1) / a.group;
