@@ -259,7 +259,7 @@ ivf_status ivf_kv_select(ivf_ctx *ctx, const ivf_kv_cache *cache, const void *q,
         a.last = last;
         a.count = count;
         a.out = out_blocks;
-        TIMED("kv_select", launch_kv_select(a, ctx->num_cus, ctx->stream));
+        TIMED("kv_select", launch_kv_select(a, ctx->stream));
         ctx->last_stats = nullptr;
         return IVF_OK;
     });

@@ -56,7 +56,7 @@ struct KvSelect {
     int first, last, count;
     int32_t *out;
 };
-hipError_t launch_kv_select(const KvSelect &a, int num_cus, hipStream_t s);
+hipError_t launch_kv_select(const KvSelect &a, hipStream_t s);
 
 struct KvAttend {
     KvCache c;

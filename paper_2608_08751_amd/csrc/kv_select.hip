@@ -17,8 +17,6 @@
 #include "kv.h"
 #include "kv_types.h"
 
-#include <algorithm>
-
 namespace ivf {
 namespace {
 
@@ -61,76 +59,132 @@ __device__ __forceinline__ float wave_max(float m)
     return m;
 }
 
-// Keeps of keys[0, n) those of `forced` places and the best `want` of the others
-// (key descending, index ascending) and writes their indexes, ascending, to
-// out[0, count), -1 behind. forced(j): j < first or j >= tail; a key of 0 is never
-// kept. One wave. keys stay as they are.
-__device__ void wave_select(const uint32_t *keys, int n, int first, int tail, int want, int count, int32_t *out)
+__device__ __forceinline__ uint32_t wave_min_u32(uint32_t x)
 {
-    const int lane = threadIdx.x & 63;
-    // extent of the candidates' keys
-    uint32_t lo = UINT32_MAX, hi = 0;
-    for (int j = first + lane; j < tail; j += 64) {
-        const uint32_t k = keys[j];
-        if (k) lo = min(lo, k);
-        hi = max(hi, k);
-    }
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        lo = min(lo, (uint32_t)__shfl_xor((int)lo, d));
-        hi = max(hi, (uint32_t)__shfl_xor((int)hi, d));
+    for (int d = 1; d < 64; d <<= 1) x = min(x, (uint32_t)__shfl_xor((int)x, d));
+    return x;
+}
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t x)
+{
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) x = max(x, (uint32_t)__shfl_xor((int)x, d));
+    return x;
+}
+
+// What WAVES waves exchange: two counters in turn, so that one barrier an exchange is enough.
+template <int WAVES> struct Exchange {
+    uint32_t v[2][WAVES];
+};
+// The waves' values x (uniform in each), in all of them.
+template <int WAVES>
+__device__ __forceinline__ void exchange(Exchange<WAVES> &e, int &turn, int wave, uint32_t x, uint32_t (&all)[WAVES])
+{
+    if (WAVES == 1) {
+        all[0] = x;
+        return;
     }
+    if ((threadIdx.x & 63) == 0) e.v[turn][wave] = x;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) all[w] = e.v[turn][w];
+    turn ^= 1;
+}
+
+// Keeps of keys 0 ... n - 1 those of forced places (j < first or j >= tail) and the
+// best `want` of the others (key descending, index ascending), and writes their
+// indexes, ascending, to out[0, count), -1 behind; a key of 0 is never kept. WAVES
+// waves (all threads of the workgroup, or one wave by itself): lane l of wave w holds keys
+// (w KPT + i) 64 + l in k[i], zero from n on.
+template <int WAVES, int KPT>
+__device__ __forceinline__ void select_best(const uint32_t (&k)[KPT], int wave, int n, int first, int tail, int want,
+                                            int count, int32_t *out, Exchange<WAVES> &ex)
+{
+    const int lane = threadIdx.x & 63, j0 = wave * KPT * 64 + lane;
+    int turn = 0;
+    uint32_t all[WAVES];
+    uint32_t c[KPT];  // candidates: keys that are not forced
+    uint32_t lo = UINT32_MAX, hi = 0;
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) {
+        const int j = j0 + 64 * i;
+        c[i] = j >= first && j < tail ? k[i] : 0u;
+        lo = min(lo, c[i] - 1u);  // 0 becomes the largest
+        hi = max(hi, c[i]);
+    }
+    lo = wave_min_u32(lo);
+    hi = wave_max_u32(hi);
+    exchange<WAVES>(ex, turn, wave, lo, all);
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) lo = min(lo, all[w]);
+    exchange<WAVES>(ex, turn, wave, hi, all);
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) hi = max(hi, all[w]);
     auto at_least = [&](uint32_t v) {
-        int c = 0;
-        for (int j0 = first; j0 < tail; j0 += 64) {
-            const int j = j0 + lane;
-            c += __popcll(__ballot(j < tail && keys[j] >= v));
-        }
-        return c;
+        uint32_t x = 0;
+#pragma unroll
+        for (int i = 0; i < KPT; ++i) x += (uint32_t)__popcll(__ballot(c[i] >= v));
+        exchange<WAVES>(ex, turn, wave, x, all);
+        x = 0;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) x += all[w];
+        return (int)x;
     };
-    // tau: the want-th largest key; more = 0 where there are no more than `want` keys (tau = 1: all)
+    // keys above tau are kept, and the first `ties` equal to it
     uint32_t tau = 1;
-    int ties = 0;  // how many keys equal to tau are kept
+    int ties = INT32_MAX;
     if (want <= 0) {
         tau = UINT32_MAX;
         ties = 0;
-    } else if (hi == 0 || at_least(lo) <= want) {
-        tau = 1;
-        ties = 1 << 30;
-    } else {
-        // at_least(a) > want >= at_least(b)
-        uint32_t a = lo, b = hi + 1;  // hi < UINT32_MAX: no key of a number is that high
+    } else if (hi != 0 && at_least(lo + 1) > want) {
+        uint32_t a = lo + 1, b = hi + 1;  // at_least(a) > want >= at_least(b); no number's key is UINT32_MAX
         int cb = 0;
         while (b - a > 1 && cb != want) {
             const uint32_t mid = a + (b - a) / 2;
-            const int c = at_least(mid);
-            if (c > want) a = mid;
-            else b = mid, cb = c;
+            const int x = at_least(mid);
+            if (x > want) a = mid;
+            else b = mid, cb = x;
         }
-        if (cb == want) {
-            tau = b;
-            ties = 1 << 30;
-        } else {
-            tau = a;  // b = a + 1: cb keys are above it
-            ties = want - cb;
-        }
+        tau = cb == want ? b : a;
+        if (cb != want) ties = want - cb;  // b = a + 1: cb keys are above a
     }
-    int kept = 0, used = 0;
-    for (int j0 = 0; j0 < n; j0 += 64) {
-        const int j = j0 + lane;
-        const uint32_t k = j < n ? keys[j] : 0u;
-        const bool forced = j < first || j >= tail;
-        const bool eq = !forced && k == tau && want > 0;
-        const uint64_t me = __ballot(eq);
-        const uint64_t below = ((uint64_t)1 << lane) - 1;
-        const bool take = k != 0 && (forced || (want > 0 && k > tau) || (eq && used + __popcll(me & below) < ties));
+    uint32_t eq = 0;
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) eq += (uint32_t)__popcll(__ballot(c[i] == tau));
+    exchange<WAVES>(ex, turn, wave, eq, all);
+    int used = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w)
+        if (w < wave) used += (int)all[w];
+    const uint64_t below = ((uint64_t)1 << lane) - 1;
+    uint32_t take = 0, kept = 0;
+    static_assert(KPT <= 32, "a bit a key");
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) {
+        const int j = j0 + 64 * i;
+        const bool same = c[i] == tau;
+        const uint64_t me = __ballot(same);
+        const bool t = ((j < first || j >= tail) && k[i] != 0) || c[i] > tau || (same && used + __popcll(me & below) < ties);
         used += __popcll(me);
-        const uint64_t mt = __ballot(take);
-        const int at = kept + __popcll(mt & below);
-        if (take && at < count) out[at] = j;
-        kept += __popcll(mt);
+        take |= (uint32_t)t << i;
+        kept += (uint32_t)__popcll(__ballot(t));
     }
-    for (int i = kept + lane; i < count; i += 64) out[i] = -1;
+    exchange<WAVES>(ex, turn, wave, kept, all);
+    int at = 0, total = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        if (w < wave) at += (int)all[w];
+        total += (int)all[w];
+    }
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) {
+        const bool t = take >> i & 1;
+        const uint64_t mt = __ballot(t);
+        const int to = at + __popcll(mt & below);
+        if (t && to < count) out[to] = j0 + 64 * i;
+        at += __popcll(mt);
+    }
+    for (int i = total + wave * 64 + lane; i < count; i += WAVES * 64) out[i] = -1;
 }
 
 // How many blocks token t ranks, and which of them are kept anyway.
@@ -149,104 +203,127 @@ __device__ __forceinline__ Extent extent_of(const KvSelect &a, int64_t t)
     return e;
 }
 
-constexpr int kOneThreads = 512;
+constexpr int kOneThreads = 1024, kOneWaves = kOneThreads / 64;
 
-template <typename TT>
+// KPT keys a thread: tables of up to 1024 KPT columns. Dynamic LDS: [cols] block ids, then keys.
+template <typename TT, int KPT>
 __global__ __launch_bounds__(kOneThreads) void kv_select_one_kernel(KvSelect a)
 {
-    extern __shared__ uint32_t lds[];  // keys [cols]
+    extern __shared__ uint32_t lds[];
     __shared__ __align__(16) int8_t code[256];
-    __shared__ float top[kOneThreads / 64];
-    const int tid = threadIdx.x;
-    const int h = blockIdx.x % a.c.heads;
-    const int64_t t = blockIdx.x / a.c.heads;
+    __shared__ float top[2];
+    __shared__ Exchange<kOneWaves> ex;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int h = blockIdx.x % (uint32_t)a.c.heads;
+    const int64_t t = blockIdx.x / (uint32_t)a.c.heads;
     const Extent e = extent_of(a, t);
     int32_t *out = a.out + (t * a.c.heads + h) * a.count;
-    if (e.n <= a.count) {  // all of them, but for holes in the table
-        for (int j = tid; j < e.n; j += kOneThreads) {
-            const int32_t id = a.table[(int64_t)e.b * a.cols + j];
-            lds[j] = id >= 0 && id < a.c.blocks;
-        }
-    } else {
+    const bool ranked = e.n > a.count;
+    for (int j = tid; j < e.n; j += kOneThreads) {
+        int32_t id = a.table[(int64_t)e.b * a.cols + j];
+        if (id >= a.c.blocks) id = -1;
+        lds[j] = ranked ? (uint32_t)id : (uint32_t)(id >= 0);  // all are kept, but for holes in the table
+    }
+    if (ranked) {
         float2 u = make_float2(0.f, 0.f);
         if (2 * tid < a.c.dim) u = group_sum<TT>(a, t, h, 2 * tid);
-        const float m = wave_max(fmaxf(fabsf(u.x), fabsf(u.y)));
-        if ((tid & 63) == 0) top[tid >> 6] = m;
-        if (tid < 128) *(uint16_t *)&code[2 * tid] = 0;
+        if (tid < 128) {  // at most 256 channels: two waves hold them
+            const float m = wave_max(fmaxf(fabsf(u.x), fabsf(u.y)));
+            if (lane == 0) top[wave] = m;
+        }
         __syncthreads();
-        const float amax = fmaxf(top[0], top[1]);  // at most 256 channels: two waves hold them
-        if (2 * tid < a.c.dim) {
-            code[2 * tid] = (int8_t)code_of(u.x, amax);
-            code[2 * tid + 1] = (int8_t)code_of(u.y, amax);
+        if (tid < 128) {
+            const float amax = fmaxf(top[0], top[1]);
+            const int c0 = code_of(u.x, amax), c1 = code_of(u.y, amax);
+            *(uint16_t *)&code[2 * tid] = (uint16_t)((c0 & 255) | (c1 & 255) << 8);
         }
         __syncthreads();
         const int part = tid & 7;  // 16 bytes of a summary, and 16 more 128 further on
         const i32x4 q0 = *(const i32x4 *)&code[16 * part], q1 = *(const i32x4 *)&code[128 + 16 * part];
         const bool has0 = 16 * part < a.c.dim, has1 = 128 + 16 * part < a.c.dim;
-        for (int j0 = 0; j0 < e.n; j0 += kOneThreads / 8) {
-            const int j = j0 + (tid >> 3);
-            int32_t id = -1;
-            if (j < e.n) id = a.table[(int64_t)e.b * a.cols + j];
-            const bool ok = id >= 0 && id < a.c.blocks;
-            int s = 0;
-            if (ok) {
-                const int8_t *p = a.c.summary + ((int64_t)id * a.c.heads + h) * a.c.dim + 16 * part;
-                if (has0) {
-                    const i32x4 x = *(const i32x4 *)p;
+        constexpr int kAhead = 4, kStep = kOneThreads / 8;
+        for (int j0 = tid >> 3; j0 < e.n; j0 += kStep * kAhead) {
+            i32x4 x0[kAhead], x1[kAhead];
+            float w[kAhead];
+            int32_t id[kAhead];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) s = __builtin_amdgcn_sdot4(x[i], q0[i], s, false);
-                }
-                if (has1) {
-                    const i32x4 x = *(const i32x4 *)(p + 128);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) s = __builtin_amdgcn_sdot4(x[i], q1[i], s, false);
+            for (int i = 0; i < kAhead; ++i) {
+                const int j = j0 + kStep * i;
+                id[i] = j < e.n ? (int32_t)lds[j] : -1;
+                x0[i] = x1[i] = (i32x4){0, 0, 0, 0};
+                w[i] = 0.f;
+                if (id[i] >= 0) {
+                    const int64_t at = (int64_t)id[i] * a.c.heads + h;
+                    const int8_t *p = a.c.summary + at * a.c.dim + 16 * part;
+                    if (has0) x0[i] = *(const i32x4 *)p;
+                    if (has1) x1[i] = *(const i32x4 *)(p + 128);
+                    if (part == 0) w[i] = a.c.weight[at];
                 }
             }
-            s += __shfl_xor(s, 1);
-            s += __shfl_xor(s, 2);
-            s += __shfl_xor(s, 4);
-            if (part == 0 && j < e.n)
-                lds[j] = ok ? key_of((float)s * a.c.weight[(int64_t)id * a.c.heads + h]) : 0u;
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                int s = 0;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    s = __builtin_amdgcn_sdot4(x0[i][r], q0[r], s, false);
+                    s = __builtin_amdgcn_sdot4(x1[i][r], q1[r], s, false);
+                }
+                s += __shfl_xor(s, 1);
+                s += __shfl_xor(s, 2);
+                s += __shfl_xor(s, 4);
+                const int j = j0 + kStep * i;
+                if (part == 0 && j < e.n) lds[j] = id[i] >= 0 ? key_of((float)s * w[i]) : 0u;
+            }
         }
     }
     __syncthreads();
-    if (tid < 64) wave_select(lds, e.n, e.first, e.tail, e.want, a.count, out);
+    uint32_t k[KPT];
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) {
+        const int j = (wave * KPT + i) * 64 + lane;
+        k[i] = j < e.n ? lds[j] : 0u;
+    }
+    select_best<kOneWaves, KPT>(k, wave, e.n, e.first, e.tail, e.want, a.count, out, ex);
 }
 
 constexpr int kTileTokens = 16, kTileThreads = 512;
 
-// Dynamic LDS: keys [16][ld], ld >= cols.
-template <typename TT>
+// KPT keys a lane: tables of up to 64 KPT columns. Dynamic LDS: keys [16][ld], ld >= cols.
+template <typename TT, int KPT>
 __global__ __launch_bounds__(kTileThreads) void kv_select_tile_kernel(KvSelect a, int ld)
 {
     extern __shared__ uint32_t lds[];
     __shared__ __align__(16) int8_t code[kTileTokens][256];
     __shared__ Extent ext[kTileTokens];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int h = blockIdx.x % a.c.heads;
-    const int64_t t0 = (int64_t)(blockIdx.x / a.c.heads) * kTileTokens;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int h = blockIdx.x % (uint32_t)a.c.heads;
+    const int64_t t0 = (int64_t)(blockIdx.x / (uint32_t)a.c.heads) * kTileTokens;
     const int tokens = (int)min((int64_t)kTileTokens, a.T - t0);
     if (tid < kTileTokens) {
         Extent e = {-1, 0, 0, 0, 0};
         if (tid < tokens) e = extent_of(a, t0 + tid);
         ext[tid] = e;
     }
-    for (int i = tid; i < kTileTokens * 64; i += kTileThreads) ((uint32_t *)code)[i] = 0;
-    __syncthreads();
-    for (int i = wave; i < tokens; i += kTileThreads / 64) {
-        float2 u[2];
-        float m = 0.f;
+    // codes of two tokens a wave (missing ones are zero)
+    {
+        float2 u[2][2];
+        float m[2] = {0.f, 0.f};
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const int d = 2 * (lane + 64 * s);
-            u[s] = d < a.c.dim ? group_sum<TT>(a, t0 + i, h, d) : make_float2(0.f, 0.f);
-            m = fmaxf(m, fmaxf(fabsf(u[s].x), fabsf(u[s].y)));
-        }
-        m = wave_max(m);
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            code[i][2 * (lane + 64 * s)] = (int8_t)code_of(u[s].x, m);
-            code[i][2 * (lane + 64 * s) + 1] = (int8_t)code_of(u[s].y, m);
+            for (int s = 0; s < 2; ++s) {
+                const int d = 2 * (lane + 64 * s), x = wave + 8 * i;
+                u[i][s] = d < a.c.dim && x < tokens ? group_sum<TT>(a, t0 + x, h, d) : make_float2(0.f, 0.f);
+                m[i] = fmaxf(m[i], fmaxf(fabsf(u[i][s].x), fabsf(u[i][s].y)));
+            }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const float amax = wave_max(m[i]);
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const int c0 = code_of(u[i][s].x, amax), c1 = code_of(u[i][s].y, amax);
+                *(uint16_t *)&code[wave + 8 * i][2 * (lane + 64 * s)] = (uint16_t)((c0 & 255) | (c1 & 255) << 8);
+            }
         }
     }
     __syncthreads();
@@ -260,74 +337,100 @@ __global__ __launch_bounds__(kTileThreads) void kv_select_tile_kernel(KvSelect a
         int i1 = i0, n = 0;
         for (; i1 < tokens && ext[i1].b == b; ++i1) n = max(n, ext[i1].n);
         const bool mine = col >= i0 && col < i1;
-        for (int j0 = 16 * wave; j0 < n; j0 += 16 * (kTileThreads / 64)) {
-            const int jr = j0 + col;  // the block that this lane loads
-            int32_t id = jr < n ? a.table[(int64_t)b * a.cols + jr] : -1;
-            if (id >= a.c.blocks) id = -1;
-            const int8_t *p = a.c.summary + ((int64_t)max(id, 0) * a.c.heads + h) * a.c.dim + 16 * hi;
-            i32x4 acc = {0, 0, 0, 0};
+        constexpr int kAhead = 4, kStep = 16 * (kTileThreads / 64);
+        for (int j0 = 16 * wave; j0 < n; j0 += kStep * kAhead) {
+            int32_t id[kAhead];
 #pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                if (s < steps) {
-                    i32x4 x = {0, 0, 0, 0};
-                    if (64 * s + 16 * hi < a.c.dim) x = *(const i32x4 *)(p + 64 * s);
-                    acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(x, qf[s], acc, 0, 0, 0);
+            for (int x = 0; x < kAhead; ++x) {
+                const int jr = j0 + kStep * x + col;  // the block that this lane loads
+                id[x] = jr < n ? a.table[(int64_t)b * a.cols + jr] : -1;
+                if (id[x] >= a.c.blocks) id[x] = -1;
+            }
+            i32x4 acc[kAhead];
+            float w[kAhead];
+#pragma unroll
+            for (int x = 0; x < kAhead; ++x) {
+                const int64_t at = (int64_t)max(id[x], 0) * a.c.heads + h;
+                const int8_t *p = a.c.summary + at * a.c.dim + 16 * hi;
+                w[x] = a.c.weight[at];
+                acc[x] = (i32x4){0, 0, 0, 0};
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                    if (s < steps) {
+                        i32x4 y = {0, 0, 0, 0};
+                        if (64 * s + 16 * hi < a.c.dim) y = *(const i32x4 *)(p + 64 * s);
+                        acc[x] = __builtin_amdgcn_mfma_i32_16x16x64_i8(y, qf[s], acc[x], 0, 0, 0);
+                    }
                 }
             }
-            const float w = id >= 0 ? a.c.weight[(int64_t)id * a.c.heads + h] : 0.f;
-            uint32_t k[4];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int src = 4 * hi + r;  // the block of row src was loaded by lane src
-                const float wr = __shfl(w, src);
-                const int idr = __shfl(id, src);
-                k[r] = idr >= 0 ? key_of((float)acc[r] * wr) : 0u;
-            }
-            if (mine) {
+            for (int x = 0; x < kAhead; ++x) {
+                if (j0 + kStep * x >= n) break;
+                uint32_t k[4];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) lds[col * ld + j0 + 4 * hi + r] = k[r];
+                for (int r = 0; r < 4; ++r) {
+                    const int src = 4 * hi + r;  // the block of row src was loaded by lane src
+                    const float wr = __shfl(w[x], src);
+                    const int idr = __shfl(id[x], src);
+                    k[r] = idr >= 0 ? key_of((float)acc[x][r] * wr) : 0u;
+                }
+                if (mine) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) lds[col * ld + j0 + kStep * x + 4 * hi + r] = k[r];
+                }
             }
         }
         i0 = i1;
     }
     __syncthreads();
-    for (int i = wave; i < tokens; i += kTileThreads / 64)
-        wave_select(lds + i * ld, ext[i].n, ext[i].first, ext[i].tail, ext[i].want, a.count,
-                    a.out + ((t0 + i) * a.c.heads + h) * a.count);
+    Exchange<1> ex;
+    for (int i = wave; i < tokens; i += kTileThreads / 64) {
+        const Extent e = ext[i];
+        uint32_t k[KPT];
+#pragma unroll
+        for (int x = 0; x < KPT; ++x) {
+            const int j = 64 * x + lane;
+            k[x] = j < e.n ? lds[i * ld + j] : 0u;
+        }
+        select_best<1, KPT>(k, 0, e.n, e.first, e.tail, e.want, a.count,
+                            a.out + ((t0 + i) * a.c.heads + h) * a.count, ex);
+    }
+}
+
+template <typename F, typename... A>
+hipError_t launch_lds(F *f, unsigned grid, int threads, size_t lds, hipStream_t s, A... args)
+{
+    if (lds > 48 * 1024) {
+        const hipError_t e = hipFuncSetAttribute((const void *)f, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(f, dim3(grid), dim3(threads), lds, s, args...);
+    return hipGetLastError();
+}
+
+template <typename TT> hipError_t launch_select(const KvSelect &a, hipStream_t s)
+{
+    // 16 tokens of a tile share the summaries where a batch brings more tokens than requests
+    if (a.T > 2 * a.B && a.cols <= 2048) {
+        const int ld = (a.cols + 15) / 16 * 16 + 4;
+        const size_t lds = (size_t)kTileTokens * ld * 4;
+        const unsigned grid = (unsigned)((a.T + kTileTokens - 1) / kTileTokens * a.c.heads);
+        return a.cols <= 512    ? launch_lds(kv_select_tile_kernel<TT, 8>, grid, kTileThreads, lds, s, a, ld)
+               : a.cols <= 1024 ? launch_lds(kv_select_tile_kernel<TT, 16>, grid, kTileThreads, lds, s, a, ld)
+                                : launch_lds(kv_select_tile_kernel<TT, 32>, grid, kTileThreads, lds, s, a, ld);
+    }
+    const size_t lds = (size_t)a.cols * 4;
+    const unsigned grid = (unsigned)(a.T * a.c.heads);
+    return a.cols <= 2048   ? launch_lds(kv_select_one_kernel<TT, 2>, grid, kOneThreads, lds, s, a)
+           : a.cols <= 8192 ? launch_lds(kv_select_one_kernel<TT, 8>, grid, kOneThreads, lds, s, a)
+                            : launch_lds(kv_select_one_kernel<TT, 32>, grid, kOneThreads, lds, s, a);
 }
 
 }  // namespace
 
-hipError_t launch_kv_select(const KvSelect &a, int num_cus, hipStream_t s)
+hipError_t launch_kv_select(const KvSelect &a, hipStream_t s)
 {
-    const int ld = (a.cols + 15) / 16 * 16 + 4;
-    const size_t tile_lds = (size_t)kTileTokens * ld * 4;
-    // 16 tokens of a tile share the summaries where a batch brings more tokens than requests
-    if (a.T > 2 * a.B && tile_lds <= 128 * 1024) {
-        const unsigned grid = (unsigned)((a.T + kTileTokens - 1) / kTileTokens * a.c.heads);
-        const void *f = a.c.bf16 ? (const void *)kv_select_tile_kernel<KvBf16> : (const void *)kv_select_tile_kernel<KvF16>;
-        if (tile_lds > 48 * 1024) {
-            const hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, (int)tile_lds);
-            if (e != hipSuccess) return e;
-        }
-        if (a.c.bf16)
-            hipLaunchKernelGGL((kv_select_tile_kernel<KvBf16>), dim3(grid), dim3(kTileThreads), tile_lds, s, a, ld);
-        else
-            hipLaunchKernelGGL((kv_select_tile_kernel<KvF16>), dim3(grid), dim3(kTileThreads), tile_lds, s, a, ld);
-        return hipGetLastError();
-    }
-    const size_t one_lds = (size_t)a.cols * 4;
-    const unsigned grid = (unsigned)(a.T * a.c.heads);
-    if (one_lds > 48 * 1024) {
-        const void *f = a.c.bf16 ? (const void *)kv_select_one_kernel<KvBf16> : (const void *)kv_select_one_kernel<KvF16>;
-        const hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, (int)one_lds);
-        if (e != hipSuccess) return e;
-    }
-    if (a.c.bf16)
-        hipLaunchKernelGGL((kv_select_one_kernel<KvBf16>), dim3(grid), dim3(kOneThreads), one_lds, s, a);
-    else
-        hipLaunchKernelGGL((kv_select_one_kernel<KvF16>), dim3(grid), dim3(kOneThreads), one_lds, s, a);
-    return hipGetLastError();
+    return a.c.bf16 ? launch_select<KvBf16>(a, s) : launch_select<KvF16>(a, s);
 }
 
 }  // namespace ivf
