@@ -91,10 +91,14 @@ def _ptr(t):
     return ctypes.c_void_p(t.data_ptr()) if t is not None else None
 
 
-def _stream_handle():
+def _stream_handle(device=None):
     import torch
 
-    return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    # torch.cuda.current_stream() builds a Stream object (3 us); the raw query is 0.1 us
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    if raw is not None:
+        return raw(torch.cuda.current_device() if device is None else device)
+    return torch.cuda.current_stream(device).cuda_stream
 
 
 class Context:
@@ -149,6 +153,13 @@ class Context:
 
     def bind_stream(self):
         self.check(self.lib.ivf_set_stream(self.handle, _stream_handle()), "ivf_set_stream")
+
+    def bind(self):
+        """Binds torch's current stream of the device; the library and the context's handle."""
+        st = self.lib.ivf_set_stream(self.handle, _stream_handle(self.device))
+        if st:
+            self.check(st, "ivf_set_stream")
+        return self.lib, self.handle
 
     def sync(self):
         self.check(self.lib.ivf_sync(self.handle), "ivf_sync")
@@ -474,6 +485,9 @@ def ivf_adc_scan(ctx: Context, queries, centroids, probes, offsets, perm, codes,
 
 
 # ---- the paged 4-bit key/value cache ------------------------------------------
+# The calls of a decoding step are small, so that the checks and allocations here
+# weigh as much as the kernels: few attribute reads, and outputs of one call carved
+# from one allocation.
 
 class _KvCacheStruct(ctypes.Structure):
     """ivf_kv_cache."""
@@ -498,6 +512,8 @@ class KVCache:
         codes = {torch.float16: IVF_F16, torch.bfloat16: IVF_BF16}
         if dtype not in codes:
             raise TypeError("the cache's type must be float16 or bfloat16, got %s" % dtype)
+        if summary.dim() != 3:
+            raise ValueError("summary must be [blocks, heads, dim], got %s" % (tuple(summary.shape),))
         blocks, heads, dim = summary.shape
         if tuple(records.shape) != (blocks, heads, block_size * dim * 17 // 16) or tuple(weight.shape) != (blocks, heads):
             raise ValueError("records %s, summary %s and weight %s do not belong together (block_size %d)" % (
@@ -507,6 +523,7 @@ class KVCache:
         self.struct = _KvCacheStruct(records.data_ptr(), summary.data_ptr(), weight.data_ptr(), blocks, block_size,
                                      heads, dim, codes[dtype])
         self.ref = ctypes.byref(self.struct)
+        self._workspace = {}  # bytes that an attention call of given sizes asks for
 
     @classmethod
     def empty(cls, blocks: int, heads: int, dim: int, block_size: int = 64, dtype=None, device="cuda"):
@@ -517,6 +534,15 @@ class KVCache:
         return cls(new((blocks, heads, block_size * dim * 17 // 16), torch.uint8), new((blocks, heads, dim), torch.int8),
                    new((blocks, heads), torch.float32), block_size, dtype or torch.bfloat16)
 
+    def attend_bytes(self, ctx, *sizes):
+        """ivf_kv_attend_bytes for these (query heads, T, B, columns, count, longest)."""
+        need = self._workspace.get(sizes)
+        if need is None:
+            if len(self._workspace) >= 1024:
+                self._workspace.clear()
+            need = self._workspace[sizes] = ctx.lib.ivf_kv_attend_bytes(self.ref, *sizes)
+        return need
+
 
 KVPlan = collections.namedtuple("KVPlan", "start slots request position info")
 
@@ -525,24 +551,25 @@ def _rows(t, name, cache, heads=None):
     """(pointer, token stride, head stride) of rows [tokens, heads, dim]."""
     if not t.is_cuda or t.dtype != cache.dtype:
         raise TypeError("%s must be a device tensor of the cache's type %s" % (name, cache.dtype))
-    if t.dim() != 3 or t.shape[2] != cache.dim or (heads is not None and t.shape[1] != heads):
-        raise ValueError("%s must be [tokens, %s, %d], got %s" % (name, heads or "heads", cache.dim, tuple(t.shape)))
-    if t.numel() == 0:
+    shape = t.shape
+    if len(shape) != 3 or shape[2] != cache.dim or (heads is not None and shape[1] != heads):
+        raise ValueError("%s must be [tokens, %s, %d], got %s" % (name, heads or "heads", cache.dim, tuple(shape)))
+    if shape[0] == 0 or shape[1] == 0:
         return None, 0, 0
     st, sh, sd = t.stride()
     if sd != 1:
         raise ValueError("%s: channels must be contiguous" % name)
-    return t.data_ptr(), st if t.shape[0] > 1 else 0, sh if t.shape[1] > 1 else 0
+    return t.data_ptr(), st if shape[0] > 1 else 0, sh if shape[1] > 1 else 0
 
 
-def _ints(t, name, shape=None, kind=None):
-    import torch
-
-    _device_tensor(t, name)
-    if t.dtype != (kind or torch.int32):
-        raise TypeError("%s must be %s, got %s" % (name, kind or torch.int32, t.dtype))
-    if shape is not None and tuple(t.shape) != shape:
-        raise ValueError("%s must be %s, got %s" % (name, shape, tuple(t.shape)))
+def _ints(t, name, shape, kind):
+    """The pointer of a contiguous device tensor of whole numbers of this shape."""
+    if t.dtype != kind or not t.is_cuda:
+        raise TypeError("%s must be a device tensor of %s, got %s on %s" % (name, kind, t.dtype, t.device))
+    if t.shape != shape:
+        raise ValueError("%s must be %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    if not t.is_contiguous():
+        raise ValueError("%s must be contiguous" % name)
     return t.data_ptr()
 
 
@@ -554,19 +581,27 @@ def ivf_kv_plan(ctx: Context, cached, added, block_size: int, table, free_blocks
     [tokens], info int64 [4] or None)."""
     import torch
 
+    i32 = torch.int32
     B = cached.shape[0]
-    p_cached, p_added = _ints(cached, "cached", (B,)), _ints(added, "added", (B,))
-    if table.dim() != 2 or table.shape[0] != B:
-        raise ValueError("table must be [%d, columns], got %s" % (B, tuple(table.shape)))
-    p_table, p_free = _ints(table, "table"), _ints(free_blocks, "free_blocks", (free_blocks.numel(),))
-    new = lambda n, kind: torch.empty(n, dtype=kind, device=cached.device)  # noqa: E731
-    plan = KVPlan(new(B + 1, torch.int32), new(tokens, torch.int64), new(tokens, torch.int32), new(tokens, torch.int32),
-                  new(4, torch.int64) if want_info else None)
-    ctx.bind_stream()
-    ctx.check(ctx.lib.ivf_kv_plan(ctx.handle, p_cached, p_added, B, block_size, p_table, table.shape[1], p_free,
-                                  free_blocks.numel(), tokens, plan.start.data_ptr(), plan.slots.data_ptr(),
-                                  plan.request.data_ptr(), plan.position.data_ptr(), _ptr(plan.info)), "ivf_kv_plan")
-    return plan
+    shape = table.shape
+    if len(shape) != 2 or shape[0] != B:
+        raise ValueError("table must be [%d, columns], got %s" % (B, tuple(shape)))
+    if tokens < 0:
+        raise ValueError("tokens must be >= 0, got %d" % tokens)
+    n_free = free_blocks.numel()
+    # slots (two words each) come first: 8-byte aligned
+    whole = torch.empty(4 * tokens + B + 1, dtype=i32, device=cached.device)
+    slots, request, position, start = whole.split((2 * tokens, tokens, tokens, B + 1))
+    info = torch.empty(4, dtype=torch.int64, device=cached.device) if want_info else None
+    at = whole.data_ptr()
+    lib, handle = ctx.bind()
+    st = lib.ivf_kv_plan(handle, _ints(cached, "cached", (B,), i32), _ints(added, "added", (B,), i32), B, block_size,
+                         _ints(table, "table", shape, i32), shape[1], _ints(free_blocks, "free_blocks", (n_free,), i32),
+                         n_free, tokens, at + 16 * tokens, at, at + 8 * tokens, at + 12 * tokens,
+                         info.data_ptr() if want_info else None)
+    if st:
+        ctx.check(st, "ivf_kv_plan")
+    return KVPlan(start, slots.view(torch.int64), request, position, info)
 
 
 def ivf_kv_append(ctx: Context, cache: KVCache, k, v, slots):
@@ -574,13 +609,14 @@ def ivf_kv_append(ctx: Context, cache: KVCache, k, v, slots):
     import torch
 
     T = slots.shape[0]
-    p_slots = _ints(slots, "slots", (T,), torch.int64)
     kp, kt, kh = _rows(k, "k", cache, cache.heads)
     vp, vt, vh = _rows(v, "v", cache, cache.heads)
     if k.shape[0] != T or v.shape[0] != T:
         raise ValueError("k and v must hold one row per slot (%d)" % T)
-    ctx.bind_stream()
-    ctx.check(ctx.lib.ivf_kv_append(ctx.handle, cache.ref, kp, kt, kh, vp, vt, vh, p_slots, T), "ivf_kv_append")
+    lib, handle = ctx.bind()
+    st = lib.ivf_kv_append(handle, cache.ref, kp, kt, kh, vp, vt, vh, _ints(slots, "slots", (T,), torch.int64), T)
+    if st:
+        ctx.check(st, "ivf_kv_append")
 
 
 def ivf_kv_read(ctx: Context, cache: KVCache, slots, blocks=None):
@@ -589,18 +625,19 @@ def ivf_kv_read(ctx: Context, cache: KVCache, slots, blocks=None):
     import torch
 
     T = slots.shape[0]
-    p_slots = _ints(slots, "slots", (T,), torch.int64)
     k = torch.empty((T, cache.heads, cache.dim), dtype=cache.dtype, device=slots.device)
     v = torch.empty_like(k)
     mean, n, p_blocks, p_mean = None, 0, None, None
     if blocks is not None:
         n = blocks.shape[0]
-        p_blocks = _ints(blocks, "blocks", (n,))
+        p_blocks = _ints(blocks, "blocks", (n,), torch.int32)
         mean = torch.empty((n, cache.heads, cache.dim), dtype=torch.float32, device=slots.device)
         p_mean = mean.data_ptr()
-    ctx.bind_stream()
-    ctx.check(ctx.lib.ivf_kv_read(ctx.handle, cache.ref, p_slots, T, k.data_ptr(), v.data_ptr(), p_blocks, n, p_mean),
-              "ivf_kv_read")
+    lib, handle = ctx.bind()
+    st = lib.ivf_kv_read(handle, cache.ref, _ints(slots, "slots", (T,), torch.int64), T, k.data_ptr(), v.data_ptr(),
+                         p_blocks, n, p_mean)
+    if st:
+        ctx.check(st, "ivf_kv_read")
     return k, v, mean
 
 
@@ -610,13 +647,17 @@ def ivf_kv_select(ctx: Context, cache: KVCache, q, request, position, table, cou
     first `first` and the last `last` blocks are always among them."""
     import torch
 
-    T, Hq = q.shape[0], q.shape[1]
+    i32 = torch.int32
     qp, qt, qh = _rows(q, "q", cache)
-    out = torch.empty((T, cache.heads, count), dtype=torch.int32, device=q.device)
-    ctx.bind_stream()
-    ctx.check(ctx.lib.ivf_kv_select(ctx.handle, cache.ref, qp, qt, qh, Hq, T, _ints(request, "request", (T,)),
-                                    _ints(position, "position", (T,)), _ints(table, "table"), table.shape[0],
-                                    table.shape[1], first, last, count, out.data_ptr()), "ivf_kv_select")
+    T, Hq, _ = q.shape
+    B, cols = table.shape
+    out = torch.empty((T, cache.heads, max(count, 0)), dtype=i32, device=q.device)
+    lib, handle = ctx.bind()
+    st = lib.ivf_kv_select(handle, cache.ref, qp, qt, qh, Hq, T, _ints(request, "request", (T,), i32),
+                           _ints(position, "position", (T,), i32), _ints(table, "table", (B, cols), i32), B, cols, first,
+                           last, count, out.data_ptr())
+    if st:
+        ctx.check(st, "ivf_kv_select")
     return out
 
 
@@ -628,28 +669,32 @@ def ivf_kv_attend(ctx: Context, cache: KVCache, q, start, request, position, tab
     least the largest number of tokens that one request has in the batch."""
     import torch
 
-    T, Hq = q.shape[0], q.shape[1]
-    B, cols = table.shape
+    i32 = torch.int32
     qp, qt, qh = _rows(q, "q", cache)
+    T, Hq, dim = q.shape
+    B, cols = table.shape
     p_blocks, count = None, 0
     if blocks is not None:
-        count = blocks.shape[2]
-        p_blocks = _ints(blocks, "blocks", (T, cache.heads, count))
+        count = blocks.shape[-1]
+        p_blocks = _ints(blocks, "blocks", (T, cache.heads, count), i32)
     if out is None:
-        out = torch.empty((T, Hq, cache.dim), dtype=cache.dtype, device=q.device)
-    elif not out.is_contiguous() or out.dtype != cache.dtype or tuple(out.shape) != (T, Hq, cache.dim):
-        raise ValueError("out must be contiguous %s %s" % ((T, Hq, cache.dim), cache.dtype))
-    if out_lse is None and want_lse:
-        out_lse = torch.empty((T, Hq), dtype=torch.float32, device=q.device)
-    elif out_lse is not None and (not out_lse.is_contiguous() or out_lse.dtype != torch.float32
-                                  or tuple(out_lse.shape) != (T, Hq)):
-        raise ValueError("out_lse must be contiguous %s fp32" % ((T, Hq),))
-    need = ctx.lib.ivf_kv_attend_bytes(cache.ref, Hq, T, B, cols, count, longest)
+        out = torch.empty((T, Hq, dim), dtype=cache.dtype, device=q.device)
+    elif not out.is_cuda or not out.is_contiguous() or out.dtype != cache.dtype or out.shape != (T, Hq, dim):
+        raise ValueError("out must be contiguous %s %s on the device" % ((T, Hq, dim), cache.dtype))
+    if out_lse is None:
+        if want_lse:
+            out_lse = torch.empty((T, Hq), dtype=torch.float32, device=q.device)
+    elif (not out_lse.is_cuda or not out_lse.is_contiguous() or out_lse.dtype != torch.float32
+          or out_lse.shape != (T, Hq)):
+        raise ValueError("out_lse must be contiguous %s fp32 on the device" % ((T, Hq),))
+    need = cache.attend_bytes(ctx, Hq, T, B, cols, count, longest)
     if need:
         ctx.ensure_workspace(need)
-    ctx.bind_stream()
-    ctx.check(ctx.lib.ivf_kv_attend(ctx.handle, cache.ref, qp, qt, qh, Hq, T, _ints(start, "start", (B + 1,)),
-                                    _ints(request, "request", (T,)), _ints(position, "position", (T,)),
-                                    _ints(table, "table"), B, cols, p_blocks, count, scale, longest, out.data_ptr(),
-                                    _ptr(out_lse)), "ivf_kv_attend")
+    lib, handle = ctx.bind()
+    st = lib.ivf_kv_attend(handle, cache.ref, qp, qt, qh, Hq, T, _ints(start, "start", (B + 1,), i32),
+                           _ints(request, "request", (T,), i32), _ints(position, "position", (T,), i32),
+                           _ints(table, "table", (B, cols), i32), B, cols, p_blocks, count, scale, longest,
+                           out.data_ptr(), None if out_lse is None else out_lse.data_ptr())
+    if st:
+        ctx.check(st, "ivf_kv_attend")
     return out, out_lse

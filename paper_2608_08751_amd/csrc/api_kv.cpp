@@ -94,7 +94,7 @@ ivf_status check_rows(ivf_ctx *ctx, const char *name, const void *p, int64_t ts,
 ivf_status check_tokens(ivf_ctx *ctx, const KvCache &c, int64_t T, int64_t heads)
 {
     if (T < 0) return fail(ctx, IVF_EINVAL, "T must be >= 0");
-    if (T > INT32_MAX || T * heads * (c.dim / 8) > ((int64_t)1 << 38))
+    if (T > INT32_MAX || T * heads > INT32_MAX)
         return fail(ctx, IVF_EUNSUPPORTED, "too many tokens for one call");
     return IVF_OK;
 }
@@ -234,7 +234,6 @@ ivf_status ivf_kv_select(ivf_ctx *ctx, const ivf_kv_cache *cache, const void *q,
         if ((st = check_table(ctx, B, table_cols, a.c.shift)) != IVF_OK) return st;
         if (table_cols > kKvMaxSelectCols)
             return fail(ctx, IVF_EUNSUPPORTED, "at most %d blocks of a request", kKvMaxSelectCols);
-        if (T * a.c.heads > INT32_MAX) return fail(ctx, IVF_EUNSUPPORTED, "too many tokens for one call");
         size_t qb;
         if ((st = check_rows(ctx, "q", q, q_token_stride, q_head_stride, T, q_heads, a.c.dim, &qb)) != IVF_OK) return st;
         const void *i32[] = {request, position, table, out_blocks};
@@ -318,7 +317,7 @@ ivf_status ivf_kv_attend(ivf_ctx *ctx, const ivf_kv_cache *cache, const void *q,
         const KvAttendPlan p = kv_attend_plan(a.c, group, T, B, table_cols, count, longest, ctx->num_cus);
         const int64_t tiles = (T * group + kv_prompt_rows(a.c.dim) - 1) / kv_prompt_rows(a.c.dim);
         if (p.token_groups * a.c.heads > INT32_MAX || p.units * 16 * a.c.heads > INT32_MAX ||
-            tiles * p.prompt_splits * a.c.heads > INT32_MAX || T * q_heads > INT32_MAX)
+            tiles * p.prompt_splits * a.c.heads > INT32_MAX)
             return fail(ctx, IVF_EUNSUPPORTED, "too many rows for one call");
         const size_t need = p.token_bytes + p.prompt_bytes;
         if (need && (st = check_ws(ctx, need)) != IVF_OK) return st;

@@ -65,44 +65,56 @@ __device__ __forceinline__ uint32_t encode(const Eight &v, float scale)
     return w;
 }
 
-// Item = (token, head, 8 channels); dim / 8 is a multiple of 4, so the lanes of
-// a scale group are neighbours of one wave.
-template <typename TT>
+// A workgroup takes U times 256 / (D / 8) consecutive tokens of one head, so that the
+// bytes it writes, tokens of a block side by side, meet in one L2 (single scale
+// bytes and 64-byte rows from workgroups on several would each be a write of their own).
+template <int D> constexpr int tokens_at_once() { return kThreads / (D / 8); }
+
+template <typename TT, int D, int U>
 __global__ __launch_bounds__(kThreads) void kv_append_kernel(KvCache c, KvRows k, KvRows v,
                                                              const int64_t *__restrict__ slots, int64_t T)
 {
-    const uint32_t per = (uint32_t)c.dim / 8, row = per * (uint32_t)c.heads;
-    const int64_t item = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    const int64_t t = item / row;
-    const bool in = t < T;
-    const uint32_t r = (uint32_t)(item - t * row), h = r / per, g8 = r - h * per;
-    u32x4 kw = {0, 0, 0, 0}, vw = {0, 0, 0, 0};
-    int64_t slot = -1;
-    if (in) {
-        slot = slots[t];
-        kw = *(const u32x4 *)((const typename TT::elem *)k.p + t * k.ts + h * k.hs + 8 * g8);
-        vw = *(const u32x4 *)((const typename TT::elem *)v.p + t * v.ts + h * v.hs + 8 * g8);
+    constexpr int kPer = D / 8, kTok = tokens_at_once<D>();
+    const int h = blockIdx.x % (uint32_t)c.heads;
+    const int64_t t0 = (int64_t)(blockIdx.x / (uint32_t)c.heads) * (kTok * U);
+    const int row = threadIdx.x / kPer, g8 = threadIdx.x % kPer;
+    u32x4 kw[U], vw[U];
+    int64_t slot[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+        const int64_t t = t0 + i * kTok + row;
+        const bool in = row < kTok && t < T;
+        slot[i] = -1;
+        kw[i] = vw[i] = (u32x4){0, 0, 0, 0};
+        if (in) {
+            slot[i] = slots[t];
+            kw[i] = *(const u32x4 *)((const typename TT::elem *)k.p + t * k.ts + h * k.hs + 8 * g8);
+            vw[i] = *(const u32x4 *)((const typename TT::elem *)v.p + t * v.ts + h * v.hs + 8 * g8);
+        }
     }
-    const Eight kx = widen<TT>(kw), vx = widen<TT>(vw);
-    bool bad = false;
-    const float ka = max4(top_of(kx, bad)), va = max4(top_of(vx, bad));
-    uint32_t b = bad;
-    b |= __shfl_xor(b, 1);
-    b |= __shfl_xor(b, 2);
-    uint32_t ke = scale_byte<TT>(ka), ve = scale_byte<TT>(va);
-    uint32_t kc = encode(kx, kv_scale(ke)), vc = encode(vx, kv_scale(ve));
-    if (b) {
-        ke = 255;
-        ve = kc = vc = 0;
-    }
-    if (slot < 0 || (slot >> c.shift) >= c.blocks) return;
-    const int place = (int)(slot & (c.bs - 1));
-    uint8_t *rec = c.rec + ((slot >> c.shift) * c.heads + h) * c.rec_bytes();
-    *(uint32_t *)(rec + place * (c.dim / 2) + 4 * g8) = kc;
-    *(uint32_t *)(rec + c.v_codes() + place * (c.dim / 2) + 4 * g8) = vc;
-    if ((g8 & 3) == 0) {
-        rec[c.k_scales() + place * (c.dim / 32) + g8 / 4] = (uint8_t)ke;
-        rec[c.v_scales() + (int)(g8 / 4) * c.bs + place] = (uint8_t)ve;
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+        const Eight kx = widen<TT>(kw[i]), vx = widen<TT>(vw[i]);
+        bool bad = false;
+        const float ka = max4(top_of(kx, bad)), va = max4(top_of(vx, bad));
+        uint32_t b = bad;
+        b |= __shfl_xor(b, 1);
+        b |= __shfl_xor(b, 2);
+        uint32_t ke = scale_byte<TT>(ka), ve = scale_byte<TT>(va);
+        uint32_t kc = encode(kx, kv_scale(ke)), vc = encode(vx, kv_scale(ve));
+        if (b) {
+            ke = 255;
+            ve = kc = vc = 0;
+        }
+        if (slot[i] < 0 || (slot[i] >> c.shift) >= c.blocks) continue;
+        const int place = (int)(slot[i] & (c.bs - 1));
+        uint8_t *rec = c.rec + ((slot[i] >> c.shift) * c.heads + h) * c.rec_bytes();
+        *(uint32_t *)(rec + place * (D / 2) + 4 * g8) = kc;
+        *(uint32_t *)(rec + c.v_codes() + place * (D / 2) + 4 * g8) = vc;
+        if ((g8 & 3) == 0) {
+            rec[c.k_scales() + place * (D / 32) + g8 / 4] = (uint8_t)ke;
+            rec[c.v_scales() + g8 / 4 * c.bs + place] = (uint8_t)ve;
+        }
     }
 }
 
@@ -120,42 +132,53 @@ template <typename TT> __device__ __forceinline__ u32x4 stored(uint32_t w, uint3
 // head: the workgroup sums such a block's keys, thread (token row, 8 channels),
 // in fp64 (exact for all but keys of far more than 2^40 different magnitudes,
 // so the order does not show).
-template <typename TT>
+template <typename TT, int D>
 __global__ __launch_bounds__(kThreads) void kv_summary_kernel(KvCache c, const int64_t *__restrict__ slots, int64_t T)
 {
-    __shared__ double sums[kThreads * 8];
+    constexpr int kPer = D / 8, kTok = tokens_at_once<D>(), kAhead = 4;
+    __shared__ double sums[kTok * D];
     __shared__ float top[kThreads / 64];
-    const int tid = threadIdx.x, h = blockIdx.y;
-    const int64_t t = (int64_t)blockIdx.x * 64 + (tid & 63);
+    const int tid = threadIdx.x, h = blockIdx.x % (uint32_t)c.heads;
+    const int64_t t = (int64_t)(blockIdx.x / (uint32_t)c.heads) * 64 + (tid & 63);
     const int64_t mine = t < T ? slots[t] : -1;
     uint64_t full = __ballot(mine >= 0 && (mine & (c.bs - 1)) == c.bs - 1 && (mine >> c.shift) < c.blocks);
-    const int per = c.dim / 8, rows = kThreads / per;
-    const int row = tid / per, g8 = tid - row * per;
+    const int row = tid / kPer, g8 = tid % kPer;
     while (full) {
         const int l = __ffsll((unsigned long long)full) - 1;
         full &= full - 1;
         const int64_t block = __shfl(mine, l) >> c.shift;
         const int64_t at = block * c.heads + h;
         const uint8_t *rec = c.rec + at * c.rec_bytes();
-        double s[8] = {};
-        if (row < rows) {
-            for (int p = row; p < c.bs; p += rows) {
-                const uint32_t w = *(const uint32_t *)(rec + p * (c.dim / 2) + 4 * g8);
-                const uint32_t e = rec[c.k_scales() + p * (c.dim / 32) + g8 / 4];
-                if (e != 255) {
-                    const Eight x = widen<TT>(stored<TT>(w, e, e));
+        if (row < kTok) {
+            double s[8] = {};
+            for (int p0 = row; p0 < c.bs; p0 += kTok * kAhead) {
+                uint32_t w[kAhead], e[kAhead];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) s[i] += (double)x.x[i];
+                for (int i = 0; i < kAhead; ++i) {
+                    const int p = p0 + i * kTok;
+                    w[i] = 0;
+                    e[i] = 127;
+                    if (p < c.bs) {
+                        w[i] = *(const uint32_t *)(rec + p * (D / 2) + 4 * g8);
+                        e[i] = rec[c.k_scales() + p * (D / 32) + g8 / 4];
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) {
+                    const Eight x = widen<TT>(stored<TT>(w[i], e[i] == 255 ? 0 : e[i], 0));  // NaN counts 0 (its codes are)
+#pragma unroll
+                    for (int d = 0; d < 8; ++d) s[d] += (double)x.x[d];
                 }
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sums[(row * per + g8) * 8 + i] = s[i];
+            for (int d = 0; d < 8; ++d) sums[(row * kPer + g8) * 8 + d] = s[d];
         }
         __syncthreads();
         float mean = 0.f;
-        if (tid < c.dim) {
+        if (tid < D) {
             double a = 0.;
-            for (int q = 0; q < rows; ++q) a += sums[q * c.dim + tid];
+#pragma unroll
+            for (int q = 0; q < kTok; ++q) a += sums[q * D + tid];
             mean = (float)a * (1.f / (float)c.bs);
         }
         float m = fabsf(mean);
@@ -167,97 +190,144 @@ __global__ __launch_bounds__(kThreads) void kv_summary_kernel(KvCache c, const i
 #pragma unroll
         for (int w = 1; w < kThreads / 64; ++w) amax = fmaxf(amax, top[w]);
         const bool live = amax >= 0x1p-100f && amax <= 3.402823466e38f;
-        if (tid < c.dim) {
+        if (tid < D) {
             const float inv = 127.f / amax;
-            c.summary[at * c.dim + tid] = live ? (int8_t)(int)rintf(mean * inv) : (int8_t)0;
+            c.summary[at * D + tid] = live ? (int8_t)(int)rintf(mean * inv) : (int8_t)0;
         }
         if (tid == 0) c.weight[at] = live ? amax / 127.f : 0.f;
         __syncthreads();
     }
 }
 
-template <typename TT>
+// The first `token_groups` workgroups a head read tokens, the others means.
+template <typename TT, int D, int U>
 __global__ __launch_bounds__(kThreads) void kv_read_kernel(KvCache c, const int64_t *__restrict__ slots, int64_t T,
                                                            typename TT::elem *k, typename TT::elem *v,
                                                            const int32_t *__restrict__ blocks, int64_t n,
-                                                           float *__restrict__ mean)
+                                                           float *__restrict__ mean, uint32_t token_groups)
 {
-    const uint32_t per = (uint32_t)c.dim / 8, row = per * (uint32_t)c.heads;
-    const int64_t item = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    int64_t t = item / row;
-    const uint32_t r = (uint32_t)(item - t * row), h = r / per, g8 = r - h * per;
-    const int64_t tokens = k || v ? T : 0;
-    if (t < tokens) {
-        const int64_t slot = slots[t];
-        u32x4 kw = {0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu}, vw = kw;
-        if (slot >= 0 && (slot >> c.shift) < c.blocks) {
-            const int place = (int)(slot & (c.bs - 1));
-            const uint8_t *rec = c.rec + ((slot >> c.shift) * c.heads + h) * c.rec_bytes();
-            const uint32_t ke = rec[c.k_scales() + place * (c.dim / 32) + g8 / 4];
-            const uint32_t ve = rec[c.v_scales() + (int)(g8 / 4) * c.bs + place];
-            kw = stored<TT>(*(const uint32_t *)(rec + place * (c.dim / 2) + 4 * g8), ke, ke);
-            vw = stored<TT>(*(const uint32_t *)(rec + c.v_codes() + place * (c.dim / 2) + 4 * g8), ve, ke);
+    constexpr int kPer = D / 8, kTok = tokens_at_once<D>();
+    const int h = blockIdx.x % (uint32_t)c.heads;
+    const uint32_t group = blockIdx.x / (uint32_t)c.heads;
+    const int row = threadIdx.x / kPer, g8 = threadIdx.x % kPer;
+    if (row >= kTok) return;
+    if (group < token_groups) {
+        const int64_t t0 = (int64_t)group * (kTok * U) + row;
+        uint32_t kc[U], vc[U], ke[U], ve[U];
+        bool there[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const int64_t t = t0 + i * kTok, slot = t < T ? slots[t] : -1;
+            there[i] = slot >= 0 && (slot >> c.shift) < c.blocks;
+            kc[i] = vc[i] = ke[i] = ve[i] = 0;
+            if (there[i]) {
+                const int place = (int)(slot & (c.bs - 1));
+                const uint8_t *rec = c.rec + ((slot >> c.shift) * c.heads + h) * c.rec_bytes();
+                ke[i] = rec[c.k_scales() + place * (D / 32) + g8 / 4];
+                ve[i] = rec[c.v_scales() + g8 / 4 * c.bs + place];
+                kc[i] = *(const uint32_t *)(rec + place * (D / 2) + 4 * g8);
+                vc[i] = *(const uint32_t *)(rec + c.v_codes() + place * (D / 2) + 4 * g8);
+            }
         }
-        const int64_t at = (t * c.heads + h) * c.dim + 8 * g8;
-        if (k) *(u32x4 *)(k + at) = kw;
-        if (v) *(u32x4 *)(v + at) = vw;
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const int64_t t = t0 + i * kTok;
+            if (t >= T) continue;
+            const uint32_t nan = there[i] ? ke[i] : 255u;
+            const int64_t at = (t * c.heads + h) * D + 8 * g8;
+            if (k) *(u32x4 *)(k + at) = stored<TT>(kc[i], ke[i], nan);
+            if (v) *(u32x4 *)(v + at) = stored<TT>(vc[i], ve[i], nan);
+        }
         return;
     }
-    t -= tokens;
-    if (t >= n) return;
-    const int64_t block = blocks[t], at = (t * c.heads + h) * c.dim + 8 * g8;
-    f32x4 lo, hi;
-    lo = hi = (f32x4){__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
-    if (block >= 0 && block < c.blocks) {
-        const int64_t b = block * c.heads + h;
-        const float w = c.weight[b];
-        const int8_t *q = c.summary + b * c.dim + 8 * g8;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            lo[i] = (float)q[i] * w;
-            hi[i] = (float)q[4 + i] * w;
+    for (int i = 0; i < U; ++i) {
+        const int64_t b = (int64_t)(group - token_groups) * (kTok * U) + i * kTok + row;
+        if (b >= n) return;
+        const int64_t block = blocks[b], at = (b * c.heads + h) * D + 8 * g8;
+        f32x4 lo, hi;
+        lo = hi = (f32x4){__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
+        if (block >= 0 && block < c.blocks) {
+            const int64_t s = block * c.heads + h;
+            const float w = c.weight[s];
+            const int8_t *q = c.summary + s * D + 8 * g8;
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+                lo[d] = (float)q[d] * w;
+                hi[d] = (float)q[4 + d] * w;
+            }
         }
+        *(f32x4 *)(mean + at) = lo;
+        *(f32x4 *)(mean + at + 4) = hi;
     }
-    *(f32x4 *)(mean + at) = lo;
-    *(f32x4 *)(mean + at + 4) = hi;
+}
+
+// Tokens a thread: 4, for more loads in flight, where that leaves workgroups for every CU.
+constexpr int64_t kManyTokens = 2048;
+
+template <typename TT, int D> struct Launch {
+    static unsigned groups(int64_t n, int u) { return (unsigned)((n + tokens_at_once<D>() * u - 1) / (tokens_at_once<D>() * u)); }
+    static hipError_t append(const KvCache &c, KvRows k, KvRows v, const int64_t *slots, int64_t T, hipStream_t s)
+    {
+        if (T >= kManyTokens)
+            hipLaunchKernelGGL((kv_append_kernel<TT, D, 4>), dim3(groups(T, 4) * c.heads), dim3(kThreads), 0, s, c, k, v, slots, T);
+        else
+            hipLaunchKernelGGL((kv_append_kernel<TT, D, 1>), dim3(groups(T, 1) * c.heads), dim3(kThreads), 0, s, c, k, v, slots, T);
+        return hipGetLastError();
+    }
+    static hipError_t summaries(const KvCache &c, const int64_t *slots, int64_t T, hipStream_t s)
+    {
+        hipLaunchKernelGGL((kv_summary_kernel<TT, D>), dim3((unsigned)((T + 63) / 64) * c.heads), dim3(kThreads), 0, s, c, slots, T);
+        return hipGetLastError();
+    }
+    static hipError_t read(const KvCache &c, const int64_t *slots, int64_t T, void *k, void *v, const int32_t *blocks,
+                           int64_t n, float *mean, hipStream_t s)
+    {
+        typedef typename TT::elem elem;
+        if (T >= kManyTokens)
+            hipLaunchKernelGGL((kv_read_kernel<TT, D, 4>), dim3((groups(T, 4) + groups(n, 4)) * c.heads), dim3(kThreads), 0, s,
+                               c, slots, T, (elem *)k, (elem *)v, blocks, n, mean, groups(T, 4));
+        else
+            hipLaunchKernelGGL((kv_read_kernel<TT, D, 1>), dim3((groups(T, 1) + groups(n, 1)) * c.heads), dim3(kThreads), 0, s,
+                               c, slots, T, (elem *)k, (elem *)v, blocks, n, mean, groups(T, 1));
+        return hipGetLastError();
+    }
+};
+
+// f(Launch<type, dim>()) for the cache's type and dim.
+template <typename TT, typename F> hipError_t by_dim(const KvCache &c, F f)
+{
+    switch (c.dim) {
+    case 64: return f(Launch<TT, 64>());
+    case 96: return f(Launch<TT, 96>());
+    case 128: return f(Launch<TT, 128>());
+    case 192: return f(Launch<TT, 192>());
+    default: return f(Launch<TT, 256>());
+    }
+}
+template <typename F> hipError_t by_cache(const KvCache &c, F f)
+{
+    return c.bf16 ? by_dim<KvBf16>(c, f) : by_dim<KvF16>(c, f);
 }
 
 }  // namespace
 
 hipError_t launch_kv_append(const KvCache &c, KvRows k, KvRows v, const int64_t *slots, int64_t T, hipStream_t s)
 {
-    const int64_t items = T * c.heads * (c.dim / 8);
-    const unsigned grid = (unsigned)((items + kThreads - 1) / kThreads);
-    if (c.bf16)
-        hipLaunchKernelGGL((kv_append_kernel<KvBf16>), dim3(grid), dim3(kThreads), 0, s, c, k, v, slots, T);
-    else
-        hipLaunchKernelGGL((kv_append_kernel<KvF16>), dim3(grid), dim3(kThreads), 0, s, c, k, v, slots, T);
-    return hipGetLastError();
+    return by_cache(c, [&](auto l) { return decltype(l)::append(c, k, v, slots, T, s); });
 }
 
 hipError_t launch_kv_summaries(const KvCache &c, const int64_t *slots, int64_t T, hipStream_t s)
 {
-    const dim3 grid((unsigned)((T + 63) / 64), (unsigned)c.heads);
-    if (c.bf16)
-        hipLaunchKernelGGL((kv_summary_kernel<KvBf16>), grid, dim3(kThreads), 0, s, c, slots, T);
-    else
-        hipLaunchKernelGGL((kv_summary_kernel<KvF16>), grid, dim3(kThreads), 0, s, c, slots, T);
-    return hipGetLastError();
+    return by_cache(c, [&](auto l) { return decltype(l)::summaries(c, slots, T, s); });
 }
 
 hipError_t launch_kv_read(const KvCache &c, const int64_t *slots, int64_t T, void *k, void *v, const int32_t *blocks,
                           int64_t n, float *mean, hipStream_t s)
 {
-    const int64_t items = ((k || v ? T : 0) + n) * c.heads * (c.dim / 8);
-    if (items == 0) return hipSuccess;
-    const unsigned grid = (unsigned)((items + kThreads - 1) / kThreads);
-    if (c.bf16)
-        hipLaunchKernelGGL((kv_read_kernel<KvBf16>), dim3(grid), dim3(kThreads), 0, s, c, slots, T, (__bf16 *)k,
-                           (__bf16 *)v, blocks, n, mean);
-    else
-        hipLaunchKernelGGL((kv_read_kernel<KvF16>), dim3(grid), dim3(kThreads), 0, s, c, slots, T, (_Float16 *)k,
-                           (_Float16 *)v, blocks, n, mean);
-    return hipGetLastError();
+    if (!k && !v) T = 0;
+    if (T + n == 0) return hipSuccess;
+    return by_cache(c, [&](auto l) { return decltype(l)::read(c, slots, T, k, v, blocks, n, mean, s); });
 }
 
 }  // namespace ivf
