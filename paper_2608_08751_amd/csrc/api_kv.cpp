@@ -340,6 +340,8 @@ ivf_status ivf_kv_attend(ivf_ctx *ctx, const ivf_kv_cache *cache, const void *q,
         a.out = out;
         a.lse = out_lse;
         a.small_rows = p.small_rows;
+        a.unit_size = p.unit_size;
+        a.team = p.team;
         a.unit_rows = p.unit_rows;
         a.per_unit = p.per_unit;
         a.units = (int)p.units;

@@ -82,7 +82,9 @@ struct KvAttend {
     // keys; rows are [head][slot][unit_rows], and unit_parts holds each unit's first
     // slot and number of parts (1: written to `out` at once). splits 1: no parts.
     int splits;
-    int unit_rows;  // rows that a unit has room for
+    int unit_size;  // rows of a unit: 8 or 16
+    int team;       // waves that share a unit: 4, or 1
+    int unit_rows;  // rows that a unit has room for in part[]
     int per_unit;   // units of a request, or of a token with `blocks`
     int units;
     int slots;
@@ -95,7 +97,7 @@ struct KvAttend {
 struct KvAttendPlan {
     bool tokens, prompt;
     int64_t small_rows;
-    int per_unit, unit_rows;
+    int per_unit, unit_size, unit_rows, team;
     int64_t units, slots;
     int token_splits, prompt_splits;
     int64_t token_groups;  // workgroups of the single-token kernel per head

@@ -2,17 +2,22 @@
 // and the joining of split key ranges.
 //
 // A row's output is sum_j p_j v_j / sum_j p_j with p_j = exp2(t_j - r), t_j = scale
-// log2(e) q.k_j and a reference r that follows the running maximum of t. Keys and
-// values go from 4 bits straight to MFMA operands in registers:
-//   * scores: S^T = K Q^T, v_mfma_f32_16x16x32 with 16 keys (a strip) as A. Lane (r =
-//     lane % 16, h = lane / 16) holds key 4 (r % 4) + r / 4 of the strip, so that its
-//     four results are keys 4 i + h of query row r; the channels of a key are taken in
-//     the order in which its row of codes lies in memory (any order serves, the query's
-//     fragments use the same), 16 bytes a lane and strip at 128 channels.
-//   * values: O^T = V^T P^T. The results above are the B operand as they are: lane h's
-//     eight probabilities of two strips are keys 4 i + h. A lane reads the codes of
-//     neighbouring channels of those keys (four loads of 256 consecutive bytes a wave),
-//     v_cvt_scalef32 makes pairs of channels with the key's scale, v_perm_b32 pairs of keys.
+// log2(e) q.k_j and a reference r that follows the running maximum of t.
+//   * scores: S^T = K Q^T with 16 keys (a strip) as rows, on
+//     v_mfma_scale_f32_16x16x128_f8f6f4: 32 channels of 4-bit codes with a power of two
+//     are its A operand as they lie in memory, 16 bytes of codes and a scale byte a lane.
+//     The query is the sum of two (f16: three) fp8 numbers a channel with a power of two per
+//     32 channels, each the rounding (4 significant bits) of what the ones before
+//     leave: exact for channels down to 2^-13 of the largest of their 32, below that
+//     off by 2^-21 of it at most. Lane (r = lane % 16, h = lane / 16) holds key 4 (r % 4) + r / 4 of the
+//     strip, so that its four results are keys 4 i + h of query row r.
+//   * values: O^T = V^T P^T on v_mfma_f32_16x16x32. The results above are the B operand as
+//     they are: lane h's eight probabilities of two strips are keys 4 i + h. A lane reads the
+//     codes of neighbouring channels of those keys (four loads of 256 consecutive bytes a
+//     wave), v_cvt_scalef32 makes pairs of channels with the key's scale, v_perm_b32 pairs of keys.
+//   * up to 8 rows (PACK) leave half of the 16 columns free: column r + 8 is row r
+//     again, columns below 8 take the exponentials of the first strip of a step and the others
+//     those of the second, each with a reference, sum and output of its own, joined at the end.
 //   * the reference is raised only when a score passes it by 2^6, for all rows of the
 //     wave at once, so the common step has no exchange between lanes. Probabilities
 //     carry 2^8, which keeps small ones normal in f16 (at most 2^14).
@@ -21,7 +26,10 @@
 //
 // A workgroup of four waves takes a range of steps of 32 keys, each wave every fourth
 // step with its own reference, sums and output, joined in LDS. What bounds single
-// tokens is the read of the cache, 17 / 16 bytes per channel of key and value.
+// tokens is the read of the cache, 17 / 16 bytes per channel of key and value;
+// of many tokens with blocks of their own the decoding of values, a vector
+// instruction a value with its share of scales, 1/16 of which serve a query row where
+// a group is one row.
 #include "kv.h"
 #include "kv_strip.h"
 
@@ -44,44 +52,53 @@ constexpr int kMinSteps = 8;   // steps of 32 keys that a part is worth
 
 // Steps of 32 keys that unit u's rows see; 0 for a unit without rows, else at
 // least 1, so that somebody writes its rows.
-__device__ int64_t unit_steps(const KvAttend &a, uint32_t u, int last_key)
+__device__ int64_t unit_steps(const KvAttend &a, uint32_t u, int unit, int last_key)
 {
     const uint32_t b = u / (uint32_t)a.per_unit;
-    const int64_t r0 = (int64_t)(u - b * (uint32_t)a.per_unit) * 16;
+    const int64_t r0 = (int64_t)(u - b * (uint32_t)a.per_unit) * unit;
     const int64_t t0 = min(max((int64_t)a.start[b], (int64_t)0), a.T);
     const int64_t rows = (min(max((int64_t)a.start[b + 1], t0), a.T) - t0) * a.group;
     if (r0 >= rows || rows > a.small_rows) return 0;
-    const int64_t r1 = min(r0 + 16, rows) - 1;
+    const int64_t r1 = min(r0 + unit, rows) - 1;
     int lim = -1;
     for (int64_t t = t0 + (uint32_t)r0 / (uint32_t)a.group; t <= t0 + (uint32_t)r1 / (uint32_t)a.group; ++t)
         lim = max(lim, min(a.position[t], last_key));
     return max(1, (lim + 32) >> 5);
 }
 
-template <typename TT, int D, bool SPARSE>
+template <typename TT, int D, bool SPARSE, bool PACK, int TEAM>
 __global__ __launch_bounds__(kThreads, D == 64 || (SPARSE && D <= 128) ? 3 : D <= 128 ? 2 : 1) void kv_attend_kernel(KvAttend a)
 {
     typedef Pieces<D> P;
     typedef typename TT::elem elem;
-    constexpr int kTiles = D / 16;
-    __shared__ float merge[2][kTiles * 4 * 64];
-    __shared__ float2 ml[kWaves][16];
+    constexpr int kTiles = D / 16, kUnit = PACK ? 8 : 16;
+    constexpr int kQueryBytes = CodedQuery<TT, D>::bytes(kUnit), kMergeBytes = 2 * kTiles * 4 * 64 * 4;
+    // TEAM waves share a unit: four join their results in LDS, one needs it for its query only
+    __shared__ __align__(16) uint8_t room[TEAM == 1 ? kWaves * kQueryBytes : kQueryBytes > kMergeBytes ? kQueryBytes : kMergeBytes];
+    __shared__ float2 ml[TEAM][16];
     __shared__ int64_t before[SPARSE ? 1 : kKvMaxUnits + 1];  // steps of the units before
     __shared__ int64_t wave_steps[kWaves];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, h = lane >> 4;
+    const int place = PACK ? col & 7 : col;  // the lane's row of the unit
+    const bool second = PACK && col >= 8;    // and the strip of a step whose scores it takes
     const uint32_t heads = a.c.heads, bid = blockIdx.x, part = bid / heads;
     const int head = (int)(bid - part * heads);
     const int last_key = (int)min((int64_t)a.cols << a.c.shift, (int64_t)INT32_MAX) - 1;
     const int strip_shift = a.c.shift - 4, strip_mask = (1 << strip_shift) - 1;
     const size_t rec_bytes = a.c.rec_bytes();
-    const LaneOffsets<D> offs(lane, a.c.bs);
+    const typename CodedKeys<D>::Offsets k_offs(lane);
+    const typename Values<D>::Offsets v_offs(lane, a.c.bs);
+    const uint32_t sel = scale_selector(h);
 
     uint32_t unit = part;
     int split = 0;
     int64_t from = 0, to = INT64_MAX, chunk = 0;  // this workgroup's steps, counted over all units
-    if (SPARSE) {
+    if (SPARSE && TEAM == 1) {
+        unit = part * kWaves + wave;
+        if (unit >= (uint32_t)a.units) return;
+    } else if (SPARSE) {
         unit = part / (uint32_t)a.splits;
         split = (int)(part - unit * (uint32_t)a.splits);
     } else if (a.splits > 1) {
@@ -91,7 +108,7 @@ __global__ __launch_bounds__(kThreads, D == 64 || (SPARSE && D <= 128) ? 3 : D <
         for (int i = 0; i < kPer; ++i) {
             const uint32_t u = tid * kPer + i;
             mine[i] = all;
-            if (u < (uint32_t)a.units) all += unit_steps(a, u, last_key);
+            if (u < (uint32_t)a.units) all += unit_steps(a, u, kUnit, last_key);
         }
         int64_t up = all;
 #pragma unroll
@@ -124,279 +141,314 @@ __global__ __launch_bounds__(kThreads, D == 64 || (SPARSE && D <= 128) ? 3 : D <
     }
 
     for (;; ++unit) {
-    // the unit's rows
-    int64_t t0;
-    int r0, rows_here, b;
-    if (SPARSE) {
-        t0 = unit / (uint32_t)a.per_unit;
-        r0 = (int)(unit % (uint32_t)a.per_unit) * 16;
-        rows_here = min(16, a.group - r0);
-        b = a.request[t0];
-    } else {
-        b = (int)(unit / (uint32_t)a.per_unit);
-        r0 = (int)(unit % (uint32_t)a.per_unit) * 16;
-        t0 = min(max((int64_t)a.start[b], (int64_t)0), a.T);
-        const int64_t rows = (min(max((int64_t)a.start[b + 1], t0), a.T) - t0) * a.group;
-        if (r0 >= rows || rows > a.small_rows) {
-            if (a.splits == 1 || (int)unit + 1 >= a.units || before[unit + 1] >= to) return;
-            continue;
-        }
-        rows_here = (int)min((int64_t)16, rows - r0);
-    }
-    const bool live = b >= 0 && b < a.B;
-
-    // this lane's row
-    const bool have = col < rows_here;
-    const uint32_t row = r0 + (have ? col : 0), row_tok = row / (uint32_t)a.group;
-    const int64_t tok = t0 + row_tok;
-    const int qhead = head * a.group + (int)(row - row_tok * (uint32_t)a.group);
-    const int lim = live ? min(a.position[tok], last_key) : -1;
-    int lim_max = have ? lim : -1, lim_min = have ? lim : INT32_MAX;
-#pragma unroll
-    for (int d = 1; d < 16; d <<= 1) {
-        lim_max = max(lim_max, __shfl_xor(lim_max, d));
-        lim_min = min(lim_min, __shfl_xor(lim_min, d));
-    }
-    lim_max = __builtin_amdgcn_readfirstlane(lim_max);
-    lim_min = __builtin_amdgcn_readfirstlane(lim_min);
-
-    u32x4 qf[D / 32];
-    {
-        const elem *q = (const elem *)a.q.p + tok * a.q.ts + (int64_t)qhead * a.q.hs;
-#pragma unroll
-        for (int c = 0; c < P::n; ++c)
-#pragma unroll
-            for (int d = 0; d < P::size(c) / 32; ++d) {
-                u32x4 x = {0, 0, 0, 0};
-                if (have) x = *(const u32x4 *)(q + P::off(c) + P::size(c) / 4 * h + 8 * d);
-                qf[P::off(c) / 32 + d] = x ^ a.q_flip;
+        // the unit's rows
+        int64_t t0;
+        int r0, rows_here, b;
+        if (SPARSE) {
+            t0 = unit / (uint32_t)a.per_unit;
+            r0 = (int)(unit % (uint32_t)a.per_unit) * kUnit;
+            rows_here = min(kUnit, a.group - r0);
+            b = a.request[t0];
+        } else {
+            b = (int)(unit / (uint32_t)a.per_unit);
+            r0 = (int)(unit % (uint32_t)a.per_unit) * kUnit;
+            t0 = min(max((int64_t)a.start[b], (int64_t)0), a.T);
+            const int64_t rows = (min(max((int64_t)a.start[b + 1], t0), a.T) - t0) * a.group;
+            if (r0 >= rows || rows > a.small_rows) {
+                if (a.splits == 1 || (int)unit + 1 >= a.units || before[unit + 1] >= to) return;
+                continue;
             }
-    }
-
-    // the steps of 32 keys of this part, wave by wave
-    int strips, s_end, step;
-    bool whole;  // all of the unit's steps
-    int slot = 0;
-    if (SPARSE) {
-        strips = lim_max < 0 ? 0 : a.count << strip_shift;
-        const int steps = (strips + 1) >> 1, per = (steps + a.splits - 1) / a.splits;
-        step = min((int64_t)steps, (int64_t)split * per);
-        s_end = min((int64_t)steps, (int64_t)step + per);
-        whole = a.splits == 1;
-    } else {
-        strips = (lim_max + 16) >> 4;
-        const int steps = (strips + 1) >> 1;
-        step = 0;
-        s_end = steps;
-        whole = true;
-        if (a.splits > 1) {
-            const int64_t u0 = before[unit], u1 = before[unit + 1];
-            const int first = (int)(u0 / chunk), last = (int)((u1 - 1) / chunk);
-            step = (int)(max(from, u0) - u0);
-            s_end = (int)min((int64_t)steps, to - u0);
-            whole = first == last;
-            slot = (int)part + (int)unit;
-            if (head == 0 && tid == 0 && (int)part == first)
-                a.unit_parts[unit] = make_int2(first + (int)unit, last - first + 1);
+            rows_here = (int)min((int64_t)kUnit, rows - r0);
         }
-    }
-    step += wave;
+        const bool live = b >= 0 && b < a.B;
 
-    const int32_t *table = a.table + (int64_t)(live ? b : 0) * a.cols;
-    const int32_t *list = SPARSE ? a.blocks + (t0 * heads + head) * a.count : nullptr;
+        typename CodedQuery<TT, D>::template Stage<64 * TEAM, kUnit> stage;
+        const int team_tid = TEAM == 1 ? lane : tid;
+        stage.load(team_tid, rows_here, [&](int r) {
+            const uint32_t x = r0 + r, t = x / (uint32_t)a.group;
+            return (const elem *)a.q.p + (t0 + t) * a.q.ts + (int64_t)(head * a.group + (int)(x - t * (uint32_t)a.group)) * a.q.hs;
+        });
 
-    f32x4 acc[kTiles];
+        // this lane's row
+        const bool have = place < rows_here;
+        const uint32_t row = r0 + (have ? place : 0), row_tok = row / (uint32_t)a.group;
+        const int lim = live ? min(a.position[t0 + row_tok], last_key) : -1;
+        int lim_max = have ? lim : -1, lim_min = have ? lim : INT32_MAX;
 #pragma unroll
-    for (int i = 0; i < kTiles; ++i) acc[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
-    float ref = -INFINITY, sub = 0.f, sum = 0.f;
+        for (int d = 1; d < 16; d <<= 1) {
+            lim_max = max(lim_max, __shfl_xor(lim_max, d));
+            lim_min = min(lim_min, __shfl_xor(lim_min, d));
+        }
+        lim_max = __builtin_amdgcn_readfirstlane(lim_max);
+        lim_min = __builtin_amdgcn_readfirstlane(lim_min);
 
-    // lane 2 i + s keeps the block and the first key of strip s of the wave's i-th next step
-    int pages = -1, bases = 0, ahead = 0;
-    auto look = [&](int first_step) {
-        const int64_t st = (int64_t)first_step + (lane >> 1) * kWaves;
-        const int64_t v = 2 * st + (lane & 1);
-        pages = -1;
-        bases = 0;
-        if (st < s_end && v < strips) {
-            int64_t j;
-            int base;
-            if (SPARSE) {
-                j = list[v >> strip_shift];
-                base = (int)(j << a.c.shift) + ((int)v & strip_mask) * 16;
-            } else {
-                base = (int)v * 16;
-                j = base >> a.c.shift;
+        // the steps of 32 keys of this part, wave by wave
+        int strips, s_end, step;
+        bool whole;  // all of the unit's steps
+        int slot = 0;
+        if (SPARSE) {
+            strips = lim_max < 0 ? 0 : a.count << strip_shift;
+            const int steps = (strips + 1) >> 1, per = (steps + a.splits - 1) / a.splits;
+            step = min((int64_t)steps, (int64_t)split * per);
+            s_end = min((int64_t)steps, (int64_t)step + per);
+            whole = a.splits == 1;
+        } else {
+            strips = (lim_max + 16) >> 4;
+            const int steps = (strips + 1) >> 1;
+            step = 0;
+            s_end = steps;
+            whole = true;
+            if (a.splits > 1) {
+                const int64_t u0 = before[unit], u1 = before[unit + 1];
+                const int first = (int)(u0 / chunk), last = (int)((u1 - 1) / chunk);
+                step = (int)(max(from, u0) - u0);
+                s_end = (int)min((int64_t)steps, to - u0);
+                whole = first == last;
+                slot = (int)part + (int)unit;
+                if (head == 0 && tid == 0 && (int)part == first)
+                    a.unit_parts[unit] = make_int2(first + (int)unit, last - first + 1);
             }
-            if (j >= 0 && j < a.cols && base <= lim_max) {
-                const int id = table[j];
-                if (id >= 0 && id < a.c.blocks) {
-                    pages = id;
-                    bases = base;
+        }
+        if (TEAM > 1) step += wave;
+
+        const int32_t *table = a.table + (int64_t)(live ? b : 0) * a.cols;
+        const int32_t *list = SPARSE ? a.blocks + (t0 * heads + head) * a.count : nullptr;
+
+        // lane 2 i + s keeps, of strip s of the wave's i-th next step, the record (bytes
+        // from the first) and the first key, or -1 where there is none
+        uint32_t rec_lo = 0, rec_hi = 0;
+        int keys = -1, ahead = 0;
+        auto look = [&](int first_step) {
+            const int64_t st = (int64_t)first_step + (lane >> 1) * TEAM;
+            const int64_t v = 2 * st + (lane & 1);
+            rec_lo = rec_hi = 0;
+            keys = -1;
+            if (st < s_end && v < strips) {
+                int64_t j;
+                int base;
+                if (SPARSE) {
+                    j = list[v >> strip_shift];
+                    base = (int)(j << a.c.shift) + ((int)v & strip_mask) * 16;
+                } else {
+                    base = (int)v * 16;
+                    j = base >> a.c.shift;
                 }
-            }
-        }
-    };
-    struct Pair {
-        Strip<D> s[2];
-        int page[2], base[2];
-    };
-    auto fetch = [&](Pair &x, int at_step) {
-        if (ahead == 32) {
-            look(at_step);
-            ahead = 0;
-        }
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            x.page[e] = __builtin_amdgcn_readlane(pages, 2 * ahead + e);
-            x.base[e] = __builtin_amdgcn_readlane(bases, 2 * ahead + e);
-        }
-        ++ahead;
-        if ((x.page[0] & x.page[1]) >= 0) {
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const uint8_t *rec = a.c.rec + ((int64_t)max(x.page[e], 0) * a.c.heads + head) * rec_bytes;
-                load_strip<D>(x.s[e], rec, a.c.bs, (x.base[e] >> 4) & strip_mask, offs);
-            }
-        }
-    };
-    auto work = [&](const Pair &x) {
-        if ((x.page[0] & x.page[1]) < 0) return;  // neither strip is there
-        float t[8];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            f32x4 y = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int c = 0; c < P::n; ++c) {
-                const float ks = kv_scale(x.s[e].ks[c]);
-#pragma unroll
-                for (int d = 0; d < P::size(c) / 32; ++d) {
-                    const int w = P::off(c) / 32 + d;
-                    y = TT::mfma(decode8<TT>(x.s[e].k[w], ks), qf[w], y);
+                if (j >= 0 && j < a.cols && base <= lim_max) {
+                    const int id = table[j];
+                    if (id >= 0 && id < a.c.blocks) {
+                        const uint64_t off = ((uint64_t)(uint32_t)id * heads + (uint32_t)head) * rec_bytes;
+                        rec_lo = (uint32_t)off;
+                        rec_hi = (uint32_t)(off >> 32);
+                        keys = base;
+                    }
                 }
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) t[4 * e + i] = y[i] * a.scale;
-        }
-        float vs[P::n][2][4];
-#pragma unroll
-        for (int c = 0; c < P::n; ++c)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) vs[c][i / 4][i % 4] = kv_scale((x.s[i / 4].vs[c][i % 4] >> (8 * h)) & 255u);
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            if (x.page[e] < 0 || x.base[e] + 15 > lim_min) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int key = x.page[e] < 0 ? INT32_MAX : x.base[e] + 4 * i + h;
-                    if (key > lim) t[4 * e + i] = -INFINITY;
-#pragma unroll
-                    for (int c = 0; c < P::n; ++c)
-                        if (key > lim_max) vs[c][e][i] = 1.f;
-                }
-            }
-        }
-        const float mx = max3(max3(t[0], t[1], t[2]), max3(t[3], t[4], t[5]), max3(t[6], t[7], t[7]));
-        if (__ballot(mx > ref + kRaise)) {
-            const float top = fmaxf(ref, max_over_h(mx));
-            const float f = ref == top ? 1.f : exp2_fast(ref - top);
-            ref = top;
-            sub = top == -INFINITY ? 0.f : top - kCarry;
-            sum *= f;
-#pragma unroll
-            for (int i = 0; i < kTiles; ++i) acc[i] *= f;
-        }
-        u32x4 pf;
-#pragma unroll
-        for (int i = 0; i < 8; i += 2) {
-            const float p0 = exp2_fast(t[i] - sub), p1 = exp2_fast(t[i + 1] - sub);
-            sum += p0 + p1;
-            pf[i / 2] = TT::pack(p0, p1);
-        }
-        auto piece = [&](auto piece_c) {
-            constexpr int c = decltype(piece_c)::value, S = P::size(c);
-            u32x2 v0[S / 16], v1[S / 16];
-            value_operands<TT, S>(x.s[0].v[c], vs[c][0], v0);
-            value_operands<TT, S>(x.s[1].v[c], vs[c][1], v1);
-#pragma unroll
-            for (int j = 0; j < S / 16; ++j) {
-                const u32x4 v = {v0[j][0], v0[j][1], v1[j][0], v1[j][1]};
-                acc[P::off(c) / 16 + j] = TT::mfma(v, pf, acc[P::off(c) / 16 + j]);
             }
         };
-        piece(std::integral_constant<int, 0>());
-        if constexpr (P::n > 1) piece(std::integral_constant<int, 1>());
-    };
-    if (step < s_end) {
-        look(step);
+        struct Pair {
+            CodedKeys<D> k[2];
+            Values<D> v[2];
+            int key[2];
+        };
+        auto fetch = [&](Pair &x, int at_step) {
+            if (ahead == 32) {
+                look(at_step);
+                ahead = 0;
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) x.key[e] = __builtin_amdgcn_readlane(keys, 2 * ahead + e);
+            if ((x.key[0] & x.key[1]) >= 0) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const uint64_t off = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)rec_hi, 2 * ahead + e) << 32 |
+                                         (uint32_t)__builtin_amdgcn_readlane((int)rec_lo, 2 * ahead + e);
+                    const uint8_t *rec = a.c.rec + off;
+                    const int strip = (max(x.key[e], 0) >> 4) & strip_mask;
+                    x.k[e].load(rec, a.c.bs, strip, k_offs);
+                    x.v[e].load(rec, a.c.bs, strip, v_offs);
+                }
+            }
+            ++ahead;
+        };
         Pair x, y;
-        fetch(x, step);
-        while (true) {
-            step += kWaves;
+        const bool any = step < s_end;
+        if (any) {
+            look(step);
+            fetch(x, step);
+        }
+        uint8_t *staged = room + (TEAM == 1 ? wave * kQueryBytes : 0);
+        stage.store(team_tid, staged, a.q_flip);
+        if (TEAM > 1) __syncthreads();
+        else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        CodedQuery<TT, D> query;
+        query.load(staged, kUnit, place, h);
+
+        f32x4 acc[kTiles];
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i) acc[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
+        float ref = -INFINITY, sub = 0.f, sum = 0.f;
+        auto work = [&](const Pair &z) {
+            if ((z.key[0] & z.key[1]) < 0) return;  // neither strip is there
+            f32x4 st[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) st[e] = query.scores(z.k[e]);
+            float vs[P::n][2][4];
+#pragma unroll
+            for (int c = 0; c < P::n; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) vs[c][i / 4][i % 4] = scale_of(z.v[i / 4].vs[c][i % 4], sel);
+            constexpr int kOwn = PACK ? 4 : 8;  // scores of this lane
+            float t[kOwn];
+#pragma unroll
+            for (int i = 0; i < kOwn; ++i) t[i] = PACK ? (second ? st[1][i] : st[0][i]) : st[i / 4][i % 4];
+            if ((z.key[0] | z.key[1]) < 0 || max(z.key[0], z.key[1]) + 15 > lim_min) {
+                int key[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    key[e] = z.key[e] < 0 ? INT32_MAX - 16 : z.key[e] + h;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int c = 0; c < P::n; ++c)
+                            if (key[e] + 4 * i > lim_max) vs[c][e][i] = 1.f;
+                }
+#pragma unroll
+                for (int i = 0; i < kOwn; ++i)
+                    if ((PACK ? (second ? key[1] : key[0]) : key[i / 4]) + 4 * (i % 4) > lim) t[i] = -INFINITY;
+            }
+            float mx = max3(t[0], t[1], max3(t[2], t[3], t[3]));
+            if (!PACK) mx = max3(mx, max3(t[kOwn - 4], t[kOwn - 3], t[kOwn - 2]), t[kOwn - 1]);
+            mx *= a.scale;
+            if (__ballot(mx > ref + kRaise)) {
+                const float top = fmaxf(ref, max_over_h(mx));
+                const float f = ref == top ? 1.f : exp2_fast(ref - top);
+                ref = top;
+                sub = top == -INFINITY ? 0.f : top - kCarry;
+                sum *= f;
+#pragma unroll
+                for (int i = 0; i < kTiles; ++i) acc[i] *= f;
+            }
+            uint32_t w[kOwn / 2];
+#pragma unroll
+            for (int i = 0; i < kOwn; i += 2) {
+                const float p0 = exp2_fast(__builtin_fmaf(t[i], a.scale, -sub));
+                const float p1 = exp2_fast(__builtin_fmaf(t[i + 1], a.scale, -sub));
+                sum += p0 + p1;
+                w[i / 2] = TT::pack(p0, p1);
+            }
+            u32x4 pf;
+            if (PACK) {
+                const uint32_t m1 = second ? ~0u : 0u;
+                pf = (u32x4){w[0] & ~m1, w[1] & ~m1, w[0] & m1, w[1] & m1};
+            } else {
+                pf = (u32x4){w[0], w[1], w[kOwn / 2 - 2], w[kOwn / 2 - 1]};
+            }
+            auto piece = [&](auto piece_c) {
+                constexpr int c = decltype(piece_c)::value, S = P::size(c);
+                u32x2 v0[S / 16], v1[S / 16];
+                value_operands<TT, S>(z.v[0].v[c], vs[c][0], v0);
+                value_operands<TT, S>(z.v[1].v[c], vs[c][1], v1);
+#pragma unroll
+                for (int j = 0; j < S / 16; ++j) {
+                    const u32x4 v = {v0[j][0], v0[j][1], v1[j][0], v1[j][1]};
+                    acc[P::off(c) / 16 + j] = TT::mfma(v, pf, acc[P::off(c) / 16 + j]);
+                }
+            };
+            piece(std::integral_constant<int, 0>());
+            if constexpr (P::n > 1) piece(std::integral_constant<int, 1>());
+        };
+        while (any) {
+            step += TEAM;
             if (step < s_end) fetch(y, step);
             work(x);
             if (step >= s_end) break;
-            step += kWaves;
+            step += TEAM;
             if (step < s_end) fetch(x, step);
             work(y);
             if (step >= s_end) break;
         }
-    }
 
-    // join the waves: wave w's sums times exp2(ref_w - max)
-    sum = sum_over_h(sum);
-    if (h == 0) ml[wave][col] = make_float2(ref, sum);
-    __syncthreads();
-    float top = -INFINITY, total = 0.f;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, ml[w][col].x);
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        const float2 x = ml[w][col];
-        if (x.x > -INFINITY || x.y != 0.f) total += x.y * exp2_fast(x.x - top);
-    }
-    const float f = ref > -INFINITY ? exp2_fast(ref - top) : sum != 0.f ? sum : 0.f;
-#pragma unroll
-    for (int i = 0; i < kTiles; ++i) acc[i] *= f;
-    float *buf = merge[wave & 1];
-    if (wave >= 2) {
-#pragma unroll
-        for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) buf[(4 * i + r) * 64 + lane] = acc[i][r];
-    }
-    __syncthreads();
-    if (wave < 2) {
-#pragma unroll
-        for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) acc[i][r] += buf[(4 * i + r) * 64 + lane];
-    }
-    __syncthreads();
-    if (wave == 1) {
-#pragma unroll
-        for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) merge[1][(4 * i + r) * 64 + lane] = acc[i][r];
-    }
-    __syncthreads();
-    if (wave == 0 && have) {
-#pragma unroll
-        for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) acc[i][r] += merge[1][(4 * i + r) * 64 + lane];
-        const int64_t orow = tok * ((int64_t)heads * a.group) + qhead;
-        if (whole) {
-            write_rows<TT, D>(acc, (elem *)a.out + orow * D, total == 0.f ? 0.f : 1.f / total, h);
-            if (a.lse && h == 0) a.lse[orow] = log_of(top, total);
+        // join the waves (and halves of the columns): sums times exp2(ref - max)
+        sum = sum_over_h(sum);
+        float top, total = 0.f;
+        auto add = [&](float r, float s) {
+            if (r > -INFINITY || s != 0.f) total += s * exp2_fast(r - top);
+        };
+        if (TEAM == 1) {
+            const float r2 = PACK ? other_half(ref) : -INFINITY, s2 = PACK ? other_half(sum) : 0.f;
+            top = fmaxf(ref, r2);
+            add(second ? r2 : ref, second ? s2 : sum);
+            add(second ? ref : r2, second ? sum : s2);
         } else {
-            const int64_t at = SPARSE ? orow * a.splits + split
-                                      : ((int64_t)head * a.slots + slot) * a.unit_rows + col;
-            if (h == 0) a.part_ml[at] = make_float2(top, total);
-            write_part<D>(acc, a.part + at * D, h);
+            if (h == 0) ml[wave % TEAM][col] = make_float2(ref, sum);
+            __syncthreads();
+            top = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < TEAM; ++w) {
+                top = fmaxf(top, ml[w][col].x);
+                if (PACK) top = fmaxf(top, ml[w][col ^ 8].x);
+            }
+#pragma unroll
+            for (int w = 0; w < TEAM; ++w) {
+                add(ml[w][place].x, ml[w][place].y);
+                if (PACK) add(ml[w][place + 8].x, ml[w][place + 8].y);
+            }
         }
-    }
-    if (SPARSE || a.splits == 1 || (int)unit + 1 >= a.units || before[unit + 1] >= to) return;
-    __syncthreads();  // the next unit writes ml and merge
+        const float f = ref > -INFINITY ? exp2_fast(ref - top) : sum != 0.f ? sum : 0.f;
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i) acc[i] *= f;
+        if (TEAM > 1) {
+            float(*merge)[kTiles * 4 * 64] = (float(*)[kTiles * 4 * 64])room;
+            float *buf = merge[wave & 1];
+            if (wave >= 2) {
+#pragma unroll
+                for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) buf[(4 * i + r) * 64 + lane] = acc[i][r];
+            }
+            __syncthreads();
+            if (wave < 2) {
+#pragma unroll
+                for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) acc[i][r] += buf[(4 * i + r) * 64 + lane];
+            }
+            __syncthreads();
+            if (wave == 1) {
+#pragma unroll
+                for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) merge[1][(4 * i + r) * 64 + lane] = acc[i][r];
+            }
+            __syncthreads();
+            if (wave == 0) {
+#pragma unroll
+                for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) acc[i][r] += merge[1][(4 * i + r) * 64 + lane];
+            }
+        }
+        if (TEAM == 1 || wave == 0) {
+            if (PACK) {
+#pragma unroll
+                for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) acc[i][r] += other_half(acc[i][r]);
+            }
+            if (have && !second) {
+                const int64_t orow = ((t0 + row_tok) * heads + head) * a.group + (row - row_tok * (uint32_t)a.group);
+                if (whole) {
+                    write_rows<TT, D>(acc, (elem *)a.out + orow * D, total == 0.f ? 0.f : 1.f / total, h);
+                    if (a.lse && h == 0) a.lse[orow] = log_of(top, total);
+                } else {
+                    const int64_t at = SPARSE ? orow * a.splits + split
+                                              : ((int64_t)head * a.slots + slot) * a.unit_rows + place;
+                    if (h == 0) a.part_ml[at] = make_float2(top, total);
+                    write_part<D>(acc, a.part + at * D, h);
+                }
+            }
+        }
+        if (SPARSE || a.splits == 1 || (int)unit + 1 >= a.units || before[unit + 1] >= to) return;
+        __syncthreads();  // the next unit writes room and ml
     }
 }
 
@@ -418,7 +470,7 @@ __global__ __launch_bounds__(kThreads) void kv_combine_kernel(KvAttend a, int64_
         const uint32_t x = (uint32_t)row / (uint32_t)a.c.heads, unit = x / (uint32_t)a.unit_rows;
         const uint32_t b = unit / (uint32_t)a.per_unit;
         const int head = (int)((uint32_t)row - x * (uint32_t)a.c.heads), col = (int)(x - unit * (uint32_t)a.unit_rows);
-        const uint32_t r = (unit - b * (uint32_t)a.per_unit) * 16 + col;
+        const uint32_t r = (unit - b * (uint32_t)a.per_unit) * (uint32_t)a.unit_size + col;
         const int64_t t0 = min(max((int64_t)a.start[b], (int64_t)0), a.T);
         const int64_t m = (min(max((int64_t)a.start[b + 1], t0), a.T) - t0) * a.group;
         if (r >= m || m > a.small_rows) return;
@@ -494,10 +546,18 @@ __global__ __launch_bounds__(kThreads) void kv_combine_kernel(KvAttend a, int64_
 template <typename TT, int D> hipError_t launch_tokens(const KvAttend &a, int64_t groups, hipStream_t s)
 {
     const unsigned grid = (unsigned)(groups * a.c.heads);
-    if (a.blocks)
-        hipLaunchKernelGGL((kv_attend_kernel<TT, D, true>), dim3(grid), dim3(kThreads), 0, s, a);
-    else
-        hipLaunchKernelGGL((kv_attend_kernel<TT, D, false>), dim3(grid), dim3(kThreads), 0, s, a);
+    const dim3 block(kThreads);
+    const bool pack = a.unit_size == 8;
+    if (a.team == 1) {
+        const dim3 waves((unsigned)((groups + kWaves - 1) / kWaves * a.c.heads));
+        if (pack) hipLaunchKernelGGL((kv_attend_kernel<TT, D, true, true, 1>), waves, block, 0, s, a);
+        else hipLaunchKernelGGL((kv_attend_kernel<TT, D, true, false, 1>), waves, block, 0, s, a);
+        return hipGetLastError();
+    }
+    if (a.blocks && pack) hipLaunchKernelGGL((kv_attend_kernel<TT, D, true, true, 4>), dim3(grid), block, 0, s, a);
+    else if (a.blocks) hipLaunchKernelGGL((kv_attend_kernel<TT, D, true, false, 4>), dim3(grid), block, 0, s, a);
+    else if (pack) hipLaunchKernelGGL((kv_attend_kernel<TT, D, false, true, 4>), dim3(grid), block, 0, s, a);
+    else hipLaunchKernelGGL((kv_attend_kernel<TT, D, false, false, 4>), dim3(grid), block, 0, s, a);
     return hipGetLastError();
 }
 
@@ -550,15 +610,19 @@ KvAttendPlan kv_attend_plan(const KvCache &c, int group, int64_t T, int64_t B, i
         rows = std::min(rows, kSmallRows);
     }
     p.token_splits = p.prompt_splits = 1;
+    p.team = kWaves;
     if (p.tokens) {
-        p.per_unit = (int)((rows + 15) / 16);
-        p.unit_rows = (int)std::min<int64_t>(rows, 16);
+        // beside a prompt the other requests' rows are mostly one token's
+        p.unit_size = (p.prompt ? group : rows) <= 8 ? 8 : 16;
+        p.per_unit = (int)((rows + p.unit_size - 1) / p.unit_size);
+        p.unit_rows = (int)std::min<int64_t>(rows, p.unit_size);
         p.units = (count ? T : B) * p.per_unit;
         // as many workgroups as are resident at once (a further round would only begin and join again)
         const int64_t resident = (int64_t)num_cus * (c.dim <= 128 ? 2 : 1);
         if (count) {
             const int64_t most = std::max<int64_t>(1, keys / (32 * kMinSteps));
             p.token_splits = (int)std::max<int64_t>(1, std::min(resident / (p.units * c.heads), most));
+            if (p.units * c.heads >= 12 * (int64_t)num_cus) p.team = 1;
         } else if (keys > kWholeKeys && p.units <= kKvMaxUnits && p.units * c.heads < 16 * (int64_t)num_cus) {
             p.token_splits = (int)std::max<int64_t>(1, resident / c.heads);
         }

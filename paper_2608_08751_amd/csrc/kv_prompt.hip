@@ -80,7 +80,9 @@ __global__ __launch_bounds__(kThreads, 2) void kv_prompt_kernel(KvAttend a, int 
         ref[ct] = -INFINITY;
         sub[ct] = sum[ct] = 0.f;
     }
-    const LaneOffsets<D> offs(lane, a.c.bs);
+    const typename Keys<D>::Offsets k_offs(lane);
+    const typename Values<D>::Offsets v_offs(lane, a.c.bs);
+    const uint32_t sel = scale_selector(h);
     const int strip_mask = (1 << (a.c.shift - 4)) - 1;
     const size_t rec_bytes = a.c.rec_bytes();
 
@@ -137,7 +139,8 @@ __global__ __launch_bounds__(kThreads, 2) void kv_prompt_kernel(KvAttend a, int 
                 if (id >= 0 && id < a.c.blocks) pages = id;
             }
         };
-        Strip<D> s;
+        Keys<D> keys;
+        Values<D> vals;
         int page = -1;
         auto fetch = [&](int k) {
             if (ahead == 64) {
@@ -148,7 +151,8 @@ __global__ __launch_bounds__(kThreads, 2) void kv_prompt_kernel(KvAttend a, int 
             ++ahead;
             if (page >= 0) {
                 const uint8_t *rec = a.c.rec + ((int64_t)page * a.c.heads + head) * rec_bytes;
-                load_strip<D>(s, rec, a.c.bs, (4 * k + wave) & strip_mask, offs);
+                keys.load(rec, a.c.bs, (4 * k + wave) & strip_mask, k_offs);
+                vals.load(rec, a.c.bs, (4 * k + wave) & strip_mask, v_offs);
             }
         };
         auto stage = [&](int k) {
@@ -165,20 +169,20 @@ __global__ __launch_bounds__(kThreads, 2) void kv_prompt_kernel(KvAttend a, int 
             const int key = k * kTileKeys + 16 * wave;
             auto piece = [&](auto piece_c) {
                 constexpr int c = decltype(piece_c)::value, S = P::size(c);
-                const float ks = kv_scale(s.ks[c]);
+                const float ks = kv_scale(keys.ks[c]);
 #pragma unroll
                 for (int d = 0; d < S / 32; ++d)
-                    kbuf[buf][wave][P::off(c) / 32 + d][lane] = decode8<TT>(s.k[P::off(c) / 32 + d], ks);
+                    kbuf[buf][wave][P::off(c) / 32 + d][lane] = decode8<TT>(keys.k[P::off(c) / 32 + d], ks);
                 float vs[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) vs[i] = kv_scale((s.vs[c][i] >> (8 * h)) & 255u);
+                for (int i = 0; i < 4; ++i) vs[i] = scale_of(vals.vs[c][i], sel);
                 if (key + 15 > gmax) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
                         if (key + 4 * i + h > gmax) vs[i] = 1.f;
                 }
                 u32x2 v[S / 16];
-                value_operands<TT, S>(s.v[c], vs, v);
+                value_operands<TT, S>(vals.v[c], vs, v);
 #pragma unroll
                 for (int j = 0; j < S / 16; ++j) vdst[128 * (P::off(c) / 16 + j)] = v[j];
             };

@@ -23,64 +23,215 @@ template <int D> struct Pieces {
     static constexpr int off(int c) { return c == 0 ? 0 : first; }
 };
 
-template <int D> struct Strip {
-    uint32_t k[D / 32];
-    uint32_t ks[Pieces<D>::n];
-    uint32_t v[Pieces<D>::n][4];
-    u32x4 vs[Pieces<D>::n];
-};
-
-// A lane's offsets into the four parts of a strip, whose first bytes are uniform
-// over the wave (scalar base, 32-bit lane offset).
-template <int D> struct LaneOffsets {
-    uint32_t k[Pieces<D>::n], ks[Pieces<D>::n], v[Pieces<D>::n], vs[Pieces<D>::n];
-    __device__ __forceinline__ LaneOffsets(int lane, int bs)
+// The values of a strip, and a lane's offsets into them from the strip's first
+// bytes, which are uniform over the wave (scalar base, 32-bit lane offset).
+template <int D> struct Values {
+    typedef Pieces<D> P;
+    uint32_t v[P::n][4];
+    u32x4 vs[P::n];
+    struct Offsets {
+        uint32_t v[P::n], vs[P::n];
+        __device__ __forceinline__ Offsets(int lane, int bs)
+        {
+            const int m = lane & 15, h = lane >> 4;
+#pragma unroll
+            for (int c = 0; c < P::n; ++c) {
+                const int S = P::size(c), off = P::off(c), g = off / 32;
+                v[c] = h * (D / 2) + off / 2 + m * S / 32;
+                vs[c] = (g + (S == 128 ? m >> 2 : S == 64 ? m >> 3 : 0)) * bs;
+            }
+        }
+    };
+    __device__ __forceinline__ void load(const uint8_t *rec, int bs, int strip, const Offsets &o)
     {
-        typedef Pieces<D> P;
-        const int m = lane & 15, h = lane >> 4, key = 4 * (m & 3) + (m >> 2);
+        const uint8_t *vr = rec + (bs + strip * 16) * (D / 2);
+        const uint8_t *vsr = rec + bs * (D + D / 32) + strip * 16;
 #pragma unroll
         for (int c = 0; c < P::n; ++c) {
-            const int S = P::size(c), off = P::off(c), g = off / 32;
-            k[c] = key * (D / 2) + off / 2 + S / 8 * h;
-            ks[c] = key * (D / 32) + g + (S == 128 ? h : S == 64 ? h >> 1 : 0);
-            v[c] = h * (D / 2) + off / 2 + m * S / 32;
-            vs[c] = (g + (S == 128 ? m >> 2 : S == 64 ? m >> 3 : 0)) * bs;
+            const int S = P::size(c);
+            vs[c] = *(const u32x4 *)(vsr + o.vs[c]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint8_t *p = vr + o.v[c] + 4 * i * (D / 2);
+                v[c][i] = S == 128 ? *(const uint32_t *)p : S == 64 ? *(const uint16_t *)p : *p;
+            }
         }
     }
 };
 
-template <int D>
-__device__ __forceinline__ void load_strip(Strip<D> &s, const uint8_t *rec, int bs, int strip, const LaneOffsets<D> &o)
-{
+// The keys of a strip as 16-bit operands are made of them: S / 32 dwords of a piece.
+template <int D> struct Keys {
     typedef Pieces<D> P;
-    const uint8_t *kr = rec + strip * (16 * (D / 2));
-    const uint8_t *vr = kr + bs * (D / 2);
-    const uint8_t *ksr = rec + bs * D + strip * (16 * (D / 32));
-    const uint8_t *vsr = rec + bs * (D + D / 32) + strip * 16;
+    uint32_t k[D / 32];
+    uint32_t ks[P::n];
+    struct Offsets {
+        uint32_t k[P::n], ks[P::n];
+        __device__ __forceinline__ Offsets(int lane)
+        {
+            const int m = lane & 15, h = lane >> 4, key = 4 * (m & 3) + (m >> 2);
 #pragma unroll
-    for (int c = 0; c < P::n; ++c) {
-        const int S = P::size(c), g = P::off(c) / 32;
-        s.ks[c] = *(ksr + o.ks[c]);
-        s.vs[c] = *(const u32x4 *)(vsr + o.vs[c]);
-        if (S == 128) {
-            const u32x4 x = *(const u32x4 *)(kr + o.k[c]);
+            for (int c = 0; c < P::n; ++c) {
+                const int S = P::size(c), off = P::off(c), g = off / 32;
+                k[c] = key * (D / 2) + off / 2 + S / 8 * h;
+                ks[c] = key * (D / 32) + g + (S == 128 ? h : S == 64 ? h >> 1 : 0);
+            }
+        }
+    };
+    __device__ __forceinline__ void load(const uint8_t *rec, int bs, int strip, const Offsets &o)
+    {
+        const uint8_t *kr = rec + strip * (16 * (D / 2));
+        const uint8_t *ksr = rec + bs * D + strip * (16 * (D / 32));
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s.k[g + i] = x[i];
+        for (int c = 0; c < P::n; ++c) {
+            const int S = P::size(c), g = P::off(c) / 32;
+            ks[c] = *(ksr + o.ks[c]);
+            if (S == 128) {
+                const u32x4 x = *(const u32x4 *)(kr + o.k[c]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s.v[c][i] = *(const uint32_t *)(vr + o.v[c] + 4 * i * (D / 2));
-        } else if (S == 64) {
-            const u32x2 x = *(const u32x2 *)(kr + o.k[c]);
-            s.k[g] = x[0];
-            s.k[g + 1] = x[1];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s.v[c][i] = *(const uint16_t *)(vr + o.v[c] + 4 * i * (D / 2));
-        } else {
-            s.k[g] = *(const uint32_t *)(kr + o.k[c]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s.v[c][i] = *(vr + o.v[c] + 4 * i * (D / 2));
+                for (int i = 0; i < 4; ++i) k[g + i] = x[i];
+            } else if (S == 64) {
+                const u32x2 x = *(const u32x2 *)(kr + o.k[c]);
+                k[g] = x[0];
+                k[g + 1] = x[1];
+            } else {
+                k[g] = *(const uint32_t *)(kr + o.k[c]);
+            }
         }
     }
-}
+};
+
+// The keys of a strip as 4-bit operands: parts of 128 channels, a lane holds the 32
+// channels of group h and their scale (a group beyond the last: the last
+// once more, against zeros of the query).
+template <int D> struct CodedKeys {
+    static constexpr int kParts = (D + 127) / 128;
+    u32x4 k[kParts];
+    uint32_t ks[kParts];
+    struct Offsets {
+        uint32_t k[kParts], ks[kParts];
+        __device__ __forceinline__ Offsets(int lane)
+        {
+            const int m = lane & 15, h = lane >> 4, key = 4 * (m & 3) + (m >> 2);
+#pragma unroll
+            for (int p = 0; p < kParts; ++p) {
+                const int g = min(4 * p + h, D / 32 - 1);
+                k[p] = key * (D / 2) + 16 * g;
+                ks[p] = key * (D / 32) + g;
+            }
+        }
+    };
+    __device__ __forceinline__ void load(const uint8_t *rec, int bs, int strip, const Offsets &o)
+    {
+        const uint8_t *kr = rec + strip * (16 * (D / 2));
+        const uint8_t *ksr = rec + bs * D + strip * (16 * (D / 32));
+#pragma unroll
+        for (int p = 0; p < kParts; ++p) {
+            k[p] = *(const u32x4 *)(kr + o.k[p]);
+            ks[p] = *(ksr + o.ks[p]);
+        }
+    }
+};
+
+// Query rows as sums of fp8 numbers: term t of a channel is the fp8 rounding of what
+// the terms before leave, times 16^t, beside a power of two for each 32 channels (byte t
+// of a scale word: that of term t).
+template <typename TT, int D> struct CodedQuery {
+    static constexpr int kTerms = TT::kTerms, kParts = CodedKeys<D>::kParts;
+    i32x8 q[kParts][kTerms];
+    uint32_t scale[kParts];
+
+    static constexpr int bytes(int rows) { return rows * (kTerms * D + D / 8); }
+    // THREADS threads stage rows r < n by row(r) (their channels; zeros up to ROWS) in
+    // lds: [term][row][D] and then the scale words [row][D / 32]. First the loads,
+    // then, after what the caller has put between, the rounding.
+    template <int THREADS, int ROWS> struct Stage {
+        static constexpr int kLanes = D / 4, kAtOnce = THREADS / kLanes;  // a thread: 4 channels
+        static constexpr int kTurns = (ROWS + kAtOnce - 1) / kAtOnce;
+        u32x2 w[kTurns];
+        template <typename Row> __device__ __forceinline__ void load(int tid, int n, Row row)
+        {
+#pragma unroll
+            for (int i = 0; i < kTurns; ++i) {
+                const int r = tid / kLanes + i * kAtOnce;
+                w[i] = (u32x2){0, 0};
+                if (r < n && tid < kAtOnce * kLanes) w[i] = *(const u32x2 *)(row(r) + 4 * (tid % kLanes));
+            }
+        }
+        __device__ __forceinline__ void store(int tid, uint8_t *lds, uint32_t flip) const
+        {
+            const int c = tid % kLanes;
+            uint32_t *scales = (uint32_t *)(lds + ROWS * kTerms * D);
+#pragma unroll
+            for (int j = 0; j < kTurns; ++j) {
+                const int r = tid / kLanes + j * kAtOnce;
+                const u32x2 y = w[j] ^ flip;
+                float x[4] = {TT::lo(y[0]), TT::hi(y[0]), TT::lo(y[1]), TT::hi(y[1])};
+                float amax = 0.f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (!(fabsf(x[i]) <= 3.402823466e38f)) x[i] = __builtin_nanf("");  // infinities too: fp8 has none
+                    amax = fmaxf(amax, fabsf(x[i]));
+                }
+#pragma unroll
+                for (int d = 1; d < 8; d <<= 1) amax = fmaxf(amax, __shfl_xor(amax, d));
+                if (r >= ROWS || tid >= kAtOnce * kLanes) continue;
+                // largest magnitude in [128, 256): fp8 numbers reach 448
+                const int e = max((int)(__float_as_uint(amax) >> 23) - 7, 4 * (kTerms - 1));
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[i] = __builtin_amdgcn_ldexpf(x[i], 127 - e);
+#pragma unroll
+                for (int t = 0; t < kTerms; ++t) {
+                    int b = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
+                    b = __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], b, true);
+                    *(int *)(lds + (t * ROWS + r) * D + 4 * c) = b;
+                    x[0] = (x[0] - __builtin_amdgcn_cvt_f32_fp8(b, 0)) * 16.f;
+                    x[1] = (x[1] - __builtin_amdgcn_cvt_f32_fp8(b, 1)) * 16.f;
+                    x[2] = (x[2] - __builtin_amdgcn_cvt_f32_fp8(b, 2)) * 16.f;
+                    x[3] = (x[3] - __builtin_amdgcn_cvt_f32_fp8(b, 3)) * 16.f;
+                }
+                if (c % 8 == 0)
+                    scales[r * (D / 32) + c / 8] =
+                        (uint32_t)e | (uint32_t)(e - 4) << 8 | (uint32_t)(kTerms > 2 ? e - 8 : 0) << 16;
+            }
+        }
+    };
+    // The operands of row r for lane (its column, h): bytes 16 h ... and 64 + 16 h ... of a part.
+    __device__ __forceinline__ void load(const uint8_t *lds, int rows, int r, int h)
+    {
+        const uint32_t *scales = (const uint32_t *)(lds + rows * kTerms * D);
+#pragma unroll
+        for (int p = 0; p < kParts; ++p) {
+#pragma unroll
+            for (int t = 0; t < kTerms; ++t)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const int c = 128 * p + 64 * half + 16 * h;
+                    u32x4 x = {0, 0, 0, 0};
+                    if (c < D) x = *(const u32x4 *)(lds + (t * rows + r) * D + c);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) q[p][t][4 * half + i] = (int)x[i];
+                }
+            scale[p] = 4 * p + h < D / 32 ? scales[r * (D / 32) + 4 * p + h] : 0x7f7f7fu;
+        }
+    }
+    template <int T> __device__ __forceinline__ f32x4 term(const CodedKeys<D> &k, int p, f32x4 acc) const
+    {
+        const i32x8 a = {(int)k.k[p][0], (int)k.k[p][1], (int)k.k[p][2], (int)k.k[p][3], 0, 0, 0, 0};
+        return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q[p][T], acc, 4, 0, 0, (int)k.ks[p], T, (int)scale[p]);
+    }
+    // q.k of 16 keys (rows) and the columns' query rows
+    __device__ __forceinline__ f32x4 scores(const CodedKeys<D> &k) const
+    {
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int p = 0; p < kParts; ++p) {
+            if constexpr (kTerms > 2) acc = term<2>(k, p, acc);
+            acc = term<1>(k, p, acc);
+            acc = term<0>(k, p, acc);
+        }
+        return acc;
+    }
+};
 
 template <typename TT> __device__ __forceinline__ u32x4 decode8(uint32_t w, float scale)
 {
@@ -103,6 +254,19 @@ __device__ __forceinline__ float sum_over_h(float x)
 }
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// 2^(e - 127) of byte h of w (sel: scale_selector(h)): the byte goes to bits 23 ... 30.
+__device__ __forceinline__ uint32_t scale_selector(int h) { return (uint32_t)h << 24 | 0x0c0c0cu; }
+__device__ __forceinline__ float scale_of(uint32_t w, uint32_t sel)
+{
+    return __uint_as_float(__builtin_amdgcn_perm(0u, w, sel) >> 1);
+}
+
+// x of the lane 8 columns further on, of 16.
+__device__ __forceinline__ float other_half(float x)
+{
+    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), 0x128, 0xf, 0xf, true));
+}
 
 // The largest of three; a NaN among them makes the result any of the three (a
 // row that holds one is NaN whatever its reference).

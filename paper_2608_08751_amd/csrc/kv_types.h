@@ -10,6 +10,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 struct KvF16 {
@@ -32,6 +33,7 @@ struct KvF16 {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
     }
     static constexpr int kMinExp = -13, kMaxExp = 13;
+    static constexpr int kTerms = 3;  // fp8 numbers (4 significant bits) that a number is the sum of
 };
 
 struct KvBf16 {
@@ -53,6 +55,7 @@ struct KvBf16 {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
     }
     static constexpr int kMinExp = -125, kMaxExp = 125;
+    static constexpr int kTerms = 2;
 };
 
 // 2^(e - 127) of a scale byte (255 gives an infinity, which decodes to NaN)
