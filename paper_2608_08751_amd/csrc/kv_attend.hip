@@ -9,18 +9,16 @@
 //     The query is the sum of two (f16: three) fp8 numbers a channel with a power of two per
 //     32 channels, each the rounding (4 significant bits) of what the ones before
 //     leave: exact for channels down to 2^-13 of the largest of their 32, below that
-//     off by 2^-21 of it at most. Lane (r = lane % 16, h = lane / 16) holds key 4 (r % 4) + r / 4 of the
-//     strip, so that its four results are keys 4 i + h of query row r.
+//     off by 2^-21 of it at most.
 //   * values: O^T = V^T P^T on v_mfma_f32_16x16x32. The results above are the B operand as
-//     they are: lane h's eight probabilities of two strips are keys 4 i + h. A lane reads the
-//     codes of neighbouring channels of those keys (four loads of 256 consecutive bytes a
-//     wave), v_cvt_scalef32 makes pairs of channels with the key's scale, v_perm_b32 pairs of keys.
+//     they are: lane (r, h)'s eight probabilities of two strips are keys 4 h ... 4 h + 3 of each.
+//     It reads the codes of neighbouring channels of those keys, v_cvt_scalef32 makes pairs of channels with the key's scale, v_perm_b32 pairs of keys.
 //   * up to 8 rows (PACK) leave half of the 16 columns free: column r + 8 is row r
 //     again, columns below 8 take the exponentials of the first strip of a step and the others
 //     those of the second, each with a reference, sum and output of its own, joined at the end.
-//   * the reference is raised only when a score passes it by 2^6, for all rows of the
-//     wave at once, so the common step has no exchange between lanes. Probabilities
-//     carry 2^8, which keeps small ones normal in f16 (at most 2^14).
+//   * the reference is raised only when a lane's probabilities of a step sum to more than
+//     2^14, for all rows of the wave at once, so the common step needs no maximum
+//     and no exchange between lanes. Probabilities carry 2^8, which keeps small ones normal in f16.
 // Masked scores are replaced, not added to; values of keys that no row sees get scale
 // 1, so that nothing left in unused slots reaches a sum.
 //
@@ -90,7 +88,6 @@ __global__ __launch_bounds__(kThreads, D == 64 || (SPARSE && D <= 128) ? 3 : D <
     const size_t rec_bytes = a.c.rec_bytes();
     const typename CodedKeys<D>::Offsets k_offs(lane);
     const typename Values<D>::Offsets v_offs(lane, a.c.bs);
-    const uint32_t sel = scale_selector(h);
 
     uint32_t unit = part;
     int split = 0;
@@ -276,7 +273,7 @@ __global__ __launch_bounds__(kThreads, D == 64 || (SPARSE && D <= 128) ? 3 : D <
             fetch(x, step);
         }
         uint8_t *staged = room + (TEAM == 1 ? wave * kQueryBytes : 0);
-        stage.store(team_tid, staged, a.q_flip);
+        stage.store(team_tid, rows_here, staged, a.q_flip);
         if (TEAM > 1) __syncthreads();
         else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         CodedQuery<TT, D> query;
@@ -295,7 +292,7 @@ __global__ __launch_bounds__(kThreads, D == 64 || (SPARSE && D <= 128) ? 3 : D <
 #pragma unroll
             for (int c = 0; c < P::n; ++c)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) vs[c][i / 4][i % 4] = scale_of(z.v[i / 4].vs[c][i % 4], sel);
+                for (int e = 0; e < 2; ++e) four_scales(z.v[e].vs[c], vs[c][e]);
             constexpr int kOwn = PACK ? 4 : 8;  // scores of this lane
             float t[kOwn];
 #pragma unroll
@@ -304,37 +301,45 @@ __global__ __launch_bounds__(kThreads, D == 64 || (SPARSE && D <= 128) ? 3 : D <
                 int key[2];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    key[e] = z.key[e] < 0 ? INT32_MAX - 16 : z.key[e] + h;
+                    key[e] = z.key[e] < 0 ? INT32_MAX - 16 : z.key[e] + 4 * h;
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
 #pragma unroll
                         for (int c = 0; c < P::n; ++c)
-                            if (key[e] + 4 * i > lim_max) vs[c][e][i] = 1.f;
+                            if (key[e] + i > lim_max) vs[c][e][i] = 1.f;
                 }
 #pragma unroll
                 for (int i = 0; i < kOwn; ++i)
-                    if ((PACK ? (second ? key[1] : key[0]) : key[i / 4]) + 4 * (i % 4) > lim) t[i] = -INFINITY;
+                    if ((PACK ? (second ? key[1] : key[0]) : key[i / 4]) + i % 4 > lim) t[i] = -INFINITY;
             }
-            float mx = max3(t[0], t[1], max3(t[2], t[3], t[3]));
-            if (!PACK) mx = max3(mx, max3(t[kOwn - 4], t[kOwn - 3], t[kOwn - 2]), t[kOwn - 1]);
-            mx *= a.scale;
-            if (__ballot(mx > ref + kRaise)) {
-                const float top = fmaxf(ref, max_over_h(mx));
+            float p[kOwn], part_sum;
+            auto probabilities = [&]() {
+                part_sum = 0.f;
+#pragma unroll
+                for (int i = 0; i < kOwn; i += 2) {
+                    p[i] = exp2_fast(__builtin_fmaf(t[i], a.scale, -sub));
+                    p[i + 1] = exp2_fast(__builtin_fmaf(t[i + 1], a.scale, -sub));
+                    part_sum += p[i] + p[i + 1];
+                }
+            };
+            probabilities();
+            if (__ballot(part_sum > kMost || ref == -INFINITY)) {
+                float mx = t[0];
+#pragma unroll
+                for (int i = 1; i < kOwn; ++i) mx = fmaxf(mx, t[i]);
+                const float top = fmaxf(ref, max_over_h(mx * a.scale));
                 const float f = ref == top ? 1.f : exp2_fast(ref - top);
                 ref = top;
                 sub = top == -INFINITY ? 0.f : top - kCarry;
                 sum *= f;
 #pragma unroll
                 for (int i = 0; i < kTiles; ++i) acc[i] *= f;
+                probabilities();
             }
+            sum += part_sum;
             uint32_t w[kOwn / 2];
 #pragma unroll
-            for (int i = 0; i < kOwn; i += 2) {
-                const float p0 = exp2_fast(__builtin_fmaf(t[i], a.scale, -sub));
-                const float p1 = exp2_fast(__builtin_fmaf(t[i + 1], a.scale, -sub));
-                sum += p0 + p1;
-                w[i / 2] = TT::pack(p0, p1);
-            }
+            for (int i = 0; i < kOwn; i += 2) w[i / 2] = TT::pack(p[i], p[i + 1]);
             u32x4 pf;
             if (PACK) {
                 const uint32_t m1 = second ? ~0u : 0u;

@@ -82,7 +82,6 @@ __global__ __launch_bounds__(kThreads, 2) void kv_prompt_kernel(KvAttend a, int 
     }
     const typename Keys<D>::Offsets k_offs(lane);
     const typename Values<D>::Offsets v_offs(lane, a.c.bs);
-    const uint32_t sel = scale_selector(h);
     const int strip_mask = (1 << (a.c.shift - 4)) - 1;
     const size_t rec_bytes = a.c.rec_bytes();
 
@@ -174,12 +173,11 @@ __global__ __launch_bounds__(kThreads, 2) void kv_prompt_kernel(KvAttend a, int 
                 for (int d = 0; d < S / 32; ++d)
                     kbuf[buf][wave][P::off(c) / 32 + d][lane] = decode8<TT>(keys.k[P::off(c) / 32 + d], ks);
                 float vs[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) vs[i] = scale_of(vals.vs[c][i], sel);
+                four_scales(vals.vs[c], vs);
                 if (key + 15 > gmax) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        if (key + 4 * i + h > gmax) vs[i] = 1.f;
+                        if (key + 4 * h + i > gmax) vs[i] = 1.f;
                 }
                 u32x2 v[S / 16];
                 value_operands<TT, S>(vals.v[c], vs, v);
@@ -212,37 +210,41 @@ __global__ __launch_bounds__(kThreads, 2) void kv_prompt_kernel(KvAttend a, int 
                     for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
-                            if ((gone >> e & 1) || k * kTileKeys + 16 * e + 4 * i + h > lim[ct])
+                            if ((gone >> e & 1) || k * kTileKeys + 16 * e + 4 * h + i > lim[ct])
                                 st[e][ct][i] = -INFINITY;
             }
             u32x4 pf[CT][2];
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) {
-                float mx = max3(st[0][ct][0], st[0][ct][1], st[0][ct][2]);
-                mx = max3(mx, st[0][ct][3], st[1][ct][0]);
-                mx = max3(mx, st[1][ct][1], st[1][ct][2]);
-                mx = max3(mx, st[1][ct][3], st[2][ct][0]);
-                mx = max3(mx, st[2][ct][1], st[2][ct][2]);
-                mx = max3(mx, st[2][ct][3], st[3][ct][0]);
-                mx = max3(mx, st[3][ct][1], st[3][ct][2]);
-                mx = max3(mx, st[3][ct][3], st[3][ct][3]) * a.scale;
-                if (__ballot(mx > ref[ct] + kRaise)) {
-                    const float top = fmaxf(ref[ct], max_over_h(mx));
+                float p[4][4], part_sum;
+                auto probabilities = [&]() {
+                    part_sum = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) p[e][i] = exp2_fast(__builtin_fmaf(st[e][ct][i], a.scale, -sub[ct]));
+                        part_sum += (p[e][0] + p[e][1]) + (p[e][2] + p[e][3]);
+                    }
+                };
+                probabilities();
+                if (__ballot(part_sum > kMost || ref[ct] == -INFINITY)) {
+                    float mx = st[0][ct][0];
+#pragma unroll
+                    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, st[i / 4][ct][i % 4]);
+                    const float top = fmaxf(ref[ct], max_over_h(mx * a.scale));
                     const float f = ref[ct] == top ? 1.f : exp2_fast(ref[ct] - top);
                     ref[ct] = top;
                     sub[ct] = top == -INFINITY ? 0.f : top - kCarry;
                     sum[ct] *= f;
 #pragma unroll
                     for (int i = 0; i < kOut; ++i) acc[ct][i] *= f;
+                    probabilities();
                 }
+                sum[ct] += part_sum;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    float p[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) p[i] = exp2_fast(__builtin_fmaf(st[e][ct][i], a.scale, -sub[ct]));
-                    sum[ct] += (p[0] + p[1]) + (p[2] + p[3]);
-                    pf[ct][e >> 1][2 * (e & 1)] = TT::pack(p[0], p[1]);
-                    pf[ct][e >> 1][2 * (e & 1) + 1] = TT::pack(p[2], p[3]);
+                    pf[ct][e >> 1][2 * (e & 1)] = TT::pack(p[e][0], p[e][1]);
+                    pf[ct][e >> 1][2 * (e & 1) + 1] = TT::pack(p[e][2], p[e][3]);
                 }
             }
 #pragma unroll

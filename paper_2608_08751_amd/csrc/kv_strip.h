@@ -1,19 +1,20 @@
 // A strip of 16 keys and values of the 4-bit cache in a wave's registers, as the
 // attention kernels hold it, and its operands for v_mfma_f32_16x16x32.
 //
-// Lane (r = lane % 16, h = lane / 16). Keys: the lane holds key 4 (r % 4) + r / 4, so
-// that row 4 h + i of a product with the keys as A is key 4 i + h; the channels of a
+// Lane (r = lane % 16, h = lane / 16). Keys: the lane holds key r, so that its four
+// results of a product with the keys as A are keys 4 h ... 4 h + 3; the channels of a
 // key are taken as its row of codes lies in memory (any order serves, the query's
 // fragments use the same), 16 bytes a lane at 128 channels. Values: lane (r, h)
-// holds, of keys 4 i + h, the codes of neighbouring channels (dim / 16 of them).
+// holds, of keys 4 h ... 4 h + 3, the codes of neighbouring channels (dim / 16 of them) and
+// their four scales in one word.
 #pragma once
 
 #include "kv_types.h"
 
 namespace ivf {
 
-constexpr float kRaise = 6.f;  // a score may pass its row's reference by this much
-constexpr float kCarry = 8.f;  // probabilities are times 2^kCarry
+constexpr float kCarry = 8.f;      // probabilities are times 2^kCarry
+constexpr float kMost = 0x1p14f;   // what a lane's probabilities of a step may sum to (f16 holds 2^16)
 
 // A row of channels is taken as one or two pieces of 128, 64 or 32.
 template <int D> struct Pieces {
@@ -28,7 +29,7 @@ template <int D> struct Pieces {
 template <int D> struct Values {
     typedef Pieces<D> P;
     uint32_t v[P::n][4];
-    u32x4 vs[P::n];
+    uint32_t vs[P::n];
     struct Offsets {
         uint32_t v[P::n], vs[P::n];
         __device__ __forceinline__ Offsets(int lane, int bs)
@@ -37,8 +38,8 @@ template <int D> struct Values {
 #pragma unroll
             for (int c = 0; c < P::n; ++c) {
                 const int S = P::size(c), off = P::off(c), g = off / 32;
-                v[c] = h * (D / 2) + off / 2 + m * S / 32;
-                vs[c] = (g + (S == 128 ? m >> 2 : S == 64 ? m >> 3 : 0)) * bs;
+                v[c] = 4 * h * (D / 2) + off / 2 + m * S / 32;
+                vs[c] = (g + (S == 128 ? m >> 2 : S == 64 ? m >> 3 : 0)) * bs + 4 * h;
             }
         }
     };
@@ -49,10 +50,10 @@ template <int D> struct Values {
 #pragma unroll
         for (int c = 0; c < P::n; ++c) {
             const int S = P::size(c);
-            vs[c] = *(const u32x4 *)(vsr + o.vs[c]);
+            vs[c] = *(const uint32_t *)(vsr + o.vs[c]);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const uint8_t *p = vr + o.v[c] + 4 * i * (D / 2);
+                const uint8_t *p = vr + o.v[c] + i * (D / 2);
                 v[c][i] = S == 128 ? *(const uint32_t *)p : S == 64 ? *(const uint16_t *)p : *p;
             }
         }
@@ -68,7 +69,7 @@ template <int D> struct Keys {
         uint32_t k[P::n], ks[P::n];
         __device__ __forceinline__ Offsets(int lane)
         {
-            const int m = lane & 15, h = lane >> 4, key = 4 * (m & 3) + (m >> 2);
+            const int key = lane & 15, h = lane >> 4;
 #pragma unroll
             for (int c = 0; c < P::n; ++c) {
                 const int S = P::size(c), off = P::off(c), g = off / 32;
@@ -111,7 +112,7 @@ template <int D> struct CodedKeys {
         uint32_t k[kParts], ks[kParts];
         __device__ __forceinline__ Offsets(int lane)
         {
-            const int m = lane & 15, h = lane >> 4, key = 4 * (m & 3) + (m >> 2);
+            const int key = lane & 15, h = lane >> 4;
 #pragma unroll
             for (int p = 0; p < kParts; ++p) {
                 const int g = min(4 * p + h, D / 32 - 1);
@@ -157,13 +158,20 @@ template <typename TT, int D> struct CodedQuery {
                 if (r < n && tid < kAtOnce * kLanes) w[i] = *(const u32x2 *)(row(r) + 4 * (tid % kLanes));
             }
         }
-        __device__ __forceinline__ void store(int tid, uint8_t *lds, uint32_t flip) const
+        __device__ __forceinline__ void store(int tid, int n, uint8_t *lds, uint32_t flip) const
         {
             const int c = tid % kLanes;
             uint32_t *scales = (uint32_t *)(lds + ROWS * kTerms * D);
 #pragma unroll
             for (int j = 0; j < kTurns; ++j) {
                 const int r = tid / kLanes + j * kAtOnce;
+                if (j * kAtOnce >= n) {  // no rows in this turn: zeros
+                    if (r >= ROWS || tid >= kAtOnce * kLanes) continue;
+#pragma unroll
+                    for (int t = 0; t < kTerms; ++t) *(int *)(lds + (t * ROWS + r) * D + 4 * c) = 0;
+                    if (c % 8 == 0) scales[r * (D / 32) + c / 8] = 0x7f7f7fu;
+                    continue;
+                }
                 const u32x2 y = w[j] ^ flip;
                 float x[4] = {TT::lo(y[0]), TT::hi(y[0]), TT::lo(y[1]), TT::hi(y[1])};
                 float amax = 0.f;
@@ -255,11 +263,17 @@ __device__ __forceinline__ float sum_over_h(float x)
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// 2^(e - 127) of byte h of w (sel: scale_selector(h)): the byte goes to bits 23 ... 30.
-__device__ __forceinline__ uint32_t scale_selector(int h) { return (uint32_t)h << 24 | 0x0c0c0cu; }
-__device__ __forceinline__ float scale_of(uint32_t w, uint32_t sel)
+// 2^(e - 127) of byte i of w, e in bits 23 ... 30.
+template <int I> __device__ __forceinline__ float scale_byte_of(uint32_t w)
 {
-    return __uint_as_float(__builtin_amdgcn_perm(0u, w, sel) >> 1);
+    return __uint_as_float(__builtin_amdgcn_perm(0u, w, (uint32_t)I << 24 | 0x0c0c0cu) >> 1);
+}
+__device__ __forceinline__ void four_scales(uint32_t w, float (&s)[4])
+{
+    s[0] = scale_byte_of<0>(w);
+    s[1] = scale_byte_of<1>(w);
+    s[2] = scale_byte_of<2>(w);
+    s[3] = scale_byte_of<3>(w);
 }
 
 // x of the lane 8 columns further on, of 16.
@@ -268,17 +282,8 @@ __device__ __forceinline__ float other_half(float x)
     return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), 0x128, 0xf, 0xf, true));
 }
 
-// The largest of three; a NaN among them makes the result any of the three (a
-// row that holds one is NaN whatever its reference).
-__device__ __forceinline__ float max3(float a, float b, float c)
-{
-    float r;
-    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-    return r;
-}
-
 // The values' operand of one piece of S channels: out[j] holds channel S / 16 r + j of
-// keys 4 i + h, i = 0 ... 3 (w: their codes, vs: their scales).
+// keys 4 h + i, i = 0 ... 3 (w: their codes, vs: their scales).
 template <typename TT, int S>
 __device__ __forceinline__ void value_operands(const uint32_t (&w)[4], const float (&vs)[4], u32x2 (&out)[S / 16])
 {
