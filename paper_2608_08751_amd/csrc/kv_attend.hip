@@ -86,8 +86,8 @@ __global__ __launch_bounds__(kThreads, D == 64 || (SPARSE && D <= 128) ? 3 : D <
     const int last_key = (int)min((int64_t)a.cols << a.c.shift, (int64_t)INT32_MAX) - 1;
     const int strip_shift = a.c.shift - 4, strip_mask = (1 << strip_shift) - 1;
     const size_t rec_bytes = a.c.rec_bytes();
-    const typename CodedKeys<D>::Offsets k_offs(lane);
-    const typename Values<D>::Offsets v_offs(lane, a.c.bs);
+    typename CodedKeys<D>::Offsets k_offs(lane, a.c.bs);
+    typename Values<D>::Offsets v_offs(lane, a.c.bs);
 
     uint32_t unit = part;
     int split = 0;
@@ -258,10 +258,9 @@ __global__ __launch_bounds__(kThreads, D == 64 || (SPARSE && D <= 128) ? 3 : D <
                 for (int e = 0; e < 2; ++e) {
                     const uint64_t off = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)rec_hi, 2 * ahead + e) << 32 |
                                          (uint32_t)__builtin_amdgcn_readlane((int)rec_lo, 2 * ahead + e);
-                    const uint8_t *rec = a.c.rec + off;
-                    const int strip = (max(x.key[e], 0) >> 4) & strip_mask;
-                    x.k[e].load(rec, a.c.bs, strip, k_offs);
-                    x.v[e].load(rec, a.c.bs, strip, v_offs);
+                    const StripBase base = StripBase::at<D>(a.c.rec + off, (max(x.key[e], 0) >> 4) & strip_mask);
+                    x.k[e].load(base, k_offs);
+                    x.v[e].load(base, v_offs);
                 }
             }
             ++ahead;

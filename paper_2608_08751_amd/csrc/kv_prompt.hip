@@ -80,8 +80,8 @@ __global__ __launch_bounds__(kThreads, 2) void kv_prompt_kernel(KvAttend a, int 
         ref[ct] = -INFINITY;
         sub[ct] = sum[ct] = 0.f;
     }
-    const typename Keys<D>::Offsets k_offs(lane);
-    const typename Values<D>::Offsets v_offs(lane, a.c.bs);
+    typename Keys<D>::Offsets k_offs(lane, a.c.bs);
+    typename Values<D>::Offsets v_offs(lane, a.c.bs);
     const int strip_mask = (1 << (a.c.shift - 4)) - 1;
     const size_t rec_bytes = a.c.rec_bytes();
 
@@ -150,8 +150,9 @@ __global__ __launch_bounds__(kThreads, 2) void kv_prompt_kernel(KvAttend a, int 
             ++ahead;
             if (page >= 0) {
                 const uint8_t *rec = a.c.rec + ((int64_t)page * a.c.heads + head) * rec_bytes;
-                keys.load(rec, a.c.bs, (4 * k + wave) & strip_mask, k_offs);
-                vals.load(rec, a.c.bs, (4 * k + wave) & strip_mask, v_offs);
+                const StripBase base = StripBase::at<D>(rec, (4 * k + wave) & strip_mask);
+                keys.load(base, k_offs);
+                vals.load(base, v_offs);
             }
         };
         auto stage = [&](int k) {
@@ -205,13 +206,18 @@ __global__ __launch_bounds__(kThreads, 2) void kv_prompt_kernel(KvAttend a, int 
             const int gone = absent[buf][0] | absent[buf][1] << 1 | absent[buf][2] << 2 | absent[buf][3] << 3;
             if (k * kTileKeys + kTileKeys - 1 > wmin || __builtin_amdgcn_readfirstlane(gone)) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
+                for (int ct = 0; ct < CT; ++ct) {
+                    const int left = lim[ct] - k * kTileKeys - 4 * h;  // of the lane's keys, the last to be seen
 #pragma unroll
-                    for (int ct = 0; ct < CT; ++ct)
+                    for (int e = 0; e < 4; ++e) {
+                        const int last = (gone >> e & 1) ? -1 : left;
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if ((gone >> e & 1) || k * kTileKeys + 16 * e + 4 * h + i > lim[ct])
-                                st[e][ct][i] = -INFINITY;
+                        for (int i = 0; i < 4; ++i) {
+                            if (last < 16 * e + i) st[e][ct][i] = -INFINITY;
+                            asm volatile("" : "+v"(st[e][ct][i]));  // one comparison at a time: no stack of masks
+                        }
+                    }
+                }
             }
             u32x4 pf[CT][2];
 #pragma unroll

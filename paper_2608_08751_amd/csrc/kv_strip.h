@@ -24,8 +24,34 @@ template <int D> struct Pieces {
     static constexpr int off(int c) { return c == 0 ? 0 : first; }
 };
 
-// The values of a strip, and a lane's offsets into them from the strip's first
-// bytes, which are uniform over the wave (scalar base, 32-bit lane offset).
+// Where a strip's four parts begin: the rows of codes (keys; the values' are
+// bs D / 2 further on, which their lane offsets hold), the keys' scales and the
+// values', each from the record's start. Uniform over the wave: kept in scalar registers, so that a
+// load takes scalar base, 32-bit lane offset and constant.
+typedef const __attribute__((address_space(1))) uint8_t *GlobalBytes;
+template <typename T> __device__ __forceinline__ T load_global(GlobalBytes p)
+{
+    return *(const __attribute__((address_space(1))) T *)p;
+}
+// A lane offset as the load takes it: extended to 64 bits where it is used (taken out of the
+// loop the sum would be a 64-bit vector addition a load). No instruction.
+__device__ __forceinline__ uint32_t here(uint32_t &offset)
+{
+    asm volatile("" : "+v"(offset));
+    return offset;
+}
+struct StripBase {
+    GlobalBytes rows, k_scales, v_scales;
+    template <int D> static __device__ __forceinline__ StripBase at(const uint8_t *rec, int strip)
+    {
+        const GlobalBytes r = (GlobalBytes)rec;
+        StripBase b = {r + strip * (8 * D), r + strip * (D / 2), r + strip * 16};
+        asm("" : "+s"(b.rows), "+s"(b.k_scales), "+s"(b.v_scales));  // no instruction: keeps the sums apart
+        return b;
+    }
+};
+
+// The values of a strip, and a lane's offsets into them.
 template <int D> struct Values {
     typedef Pieces<D> P;
     uint32_t v[P::n][4];
@@ -38,23 +64,22 @@ template <int D> struct Values {
 #pragma unroll
             for (int c = 0; c < P::n; ++c) {
                 const int S = P::size(c), off = P::off(c), g = off / 32;
-                v[c] = 4 * h * (D / 2) + off / 2 + m * S / 32;
-                vs[c] = (g + (S == 128 ? m >> 2 : S == 64 ? m >> 3 : 0)) * bs + 4 * h;
+                v[c] = (bs + 4 * h) * (D / 2) + off / 2 + m * S / 32;
+                vs[c] = bs * (D + D / 32) + (g + (S == 128 ? m >> 2 : S == 64 ? m >> 3 : 0)) * bs + 4 * h;
             }
         }
     };
-    __device__ __forceinline__ void load(const uint8_t *rec, int bs, int strip, const Offsets &o)
+    __device__ __forceinline__ void load(const StripBase &b, Offsets &o)
     {
-        const uint8_t *vr = rec + (bs + strip * 16) * (D / 2);
-        const uint8_t *vsr = rec + bs * (D + D / 32) + strip * 16;
 #pragma unroll
         for (int c = 0; c < P::n; ++c) {
             const int S = P::size(c);
-            vs[c] = *(const uint32_t *)(vsr + o.vs[c]);
+            vs[c] = load_global<uint32_t>(b.v_scales + here(o.vs[c]));
+            const GlobalBytes row = b.rows + here(o.v[c]);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const uint8_t *p = vr + o.v[c] + i * (D / 2);
-                v[c][i] = S == 128 ? *(const uint32_t *)p : S == 64 ? *(const uint16_t *)p : *p;
+                const GlobalBytes p = row + i * (D / 2);
+                v[c][i] = S == 128 ? load_global<uint32_t>(p) : S == 64 ? load_global<uint16_t>(p) : load_global<uint8_t>(p);
             }
         }
     }
@@ -67,35 +92,33 @@ template <int D> struct Keys {
     uint32_t ks[P::n];
     struct Offsets {
         uint32_t k[P::n], ks[P::n];
-        __device__ __forceinline__ Offsets(int lane)
+        __device__ __forceinline__ Offsets(int lane, int bs)
         {
             const int key = lane & 15, h = lane >> 4;
 #pragma unroll
             for (int c = 0; c < P::n; ++c) {
                 const int S = P::size(c), off = P::off(c), g = off / 32;
                 k[c] = key * (D / 2) + off / 2 + S / 8 * h;
-                ks[c] = key * (D / 32) + g + (S == 128 ? h : S == 64 ? h >> 1 : 0);
+                ks[c] = bs * D + key * (D / 32) + g + (S == 128 ? h : S == 64 ? h >> 1 : 0);
             }
         }
     };
-    __device__ __forceinline__ void load(const uint8_t *rec, int bs, int strip, const Offsets &o)
+    __device__ __forceinline__ void load(const StripBase &b, Offsets &o)
     {
-        const uint8_t *kr = rec + strip * (16 * (D / 2));
-        const uint8_t *ksr = rec + bs * D + strip * (16 * (D / 32));
 #pragma unroll
         for (int c = 0; c < P::n; ++c) {
             const int S = P::size(c), g = P::off(c) / 32;
-            ks[c] = *(ksr + o.ks[c]);
+            ks[c] = load_global<uint8_t>(b.k_scales + here(o.ks[c]));
             if (S == 128) {
-                const u32x4 x = *(const u32x4 *)(kr + o.k[c]);
+                const u32x4 x = load_global<u32x4>(b.rows + here(o.k[c]));
 #pragma unroll
                 for (int i = 0; i < 4; ++i) k[g + i] = x[i];
             } else if (S == 64) {
-                const u32x2 x = *(const u32x2 *)(kr + o.k[c]);
+                const u32x2 x = load_global<u32x2>(b.rows + here(o.k[c]));
                 k[g] = x[0];
                 k[g + 1] = x[1];
             } else {
-                k[g] = *(const uint32_t *)(kr + o.k[c]);
+                k[g] = load_global<uint32_t>(b.rows + here(o.k[c]));
             }
         }
     }
@@ -110,25 +133,23 @@ template <int D> struct CodedKeys {
     uint32_t ks[kParts];
     struct Offsets {
         uint32_t k[kParts], ks[kParts];
-        __device__ __forceinline__ Offsets(int lane)
+        __device__ __forceinline__ Offsets(int lane, int bs)
         {
             const int key = lane & 15, h = lane >> 4;
 #pragma unroll
             for (int p = 0; p < kParts; ++p) {
                 const int g = min(4 * p + h, D / 32 - 1);
                 k[p] = key * (D / 2) + 16 * g;
-                ks[p] = key * (D / 32) + g;
+                ks[p] = bs * D + key * (D / 32) + g;
             }
         }
     };
-    __device__ __forceinline__ void load(const uint8_t *rec, int bs, int strip, const Offsets &o)
+    __device__ __forceinline__ void load(const StripBase &b, Offsets &o)
     {
-        const uint8_t *kr = rec + strip * (16 * (D / 2));
-        const uint8_t *ksr = rec + bs * D + strip * (16 * (D / 32));
 #pragma unroll
         for (int p = 0; p < kParts; ++p) {
-            k[p] = *(const u32x4 *)(kr + o.k[p]);
-            ks[p] = *(ksr + o.ks[p]);
+            k[p] = load_global<u32x4>(b.rows + here(o.k[p]));
+            ks[p] = load_global<uint8_t>(b.k_scales + here(o.ks[p]));
         }
     }
 };
