@@ -83,7 +83,7 @@ struct KvAttend {
     // slot and number of parts (1: written to `out` at once). splits 1: no parts.
     int splits;
     int unit_size;  // rows of a unit: 8 or 16
-    int team;       // waves that share a unit: 4, or 1
+    int team;       // waves that share a unit: 8, 4 or 1
     int unit_rows;  // rows that a unit has room for in part[]
     int per_unit;   // units of a request, or of a token with `blocks`
     int units;

@@ -64,18 +64,21 @@ __device__ int64_t unit_steps(const KvAttend &a, uint32_t u, int unit, int last_
     return max(1, (lim + 32) >> 5);
 }
 
+constexpr int attend_threads(int team) { return team == 1 ? kThreads : 64 * team; }
+
 template <typename TT, int D, bool SPARSE, bool PACK, int TEAM>
-__global__ __launch_bounds__(kThreads, D == 64 || (SPARSE && D <= 128) ? 3 : D <= 128 ? 2 : 1) void kv_attend_kernel(KvAttend a)
+__global__ __launch_bounds__(attend_threads(TEAM), TEAM == 8 ? 2 : D == 64 || (SPARSE && D <= 128) ? 3 : D <= 128 ? 2 : 1)
+void kv_attend_kernel(KvAttend a)
 {
     typedef Pieces<D> P;
     typedef typename TT::elem elem;
     constexpr int kTiles = D / 16, kUnit = PACK ? 8 : 16;
-    constexpr int kQueryBytes = CodedQuery<TT, D>::bytes(kUnit), kMergeBytes = 2 * kTiles * 4 * 64 * 4;
-    // TEAM waves share a unit: four join their results in LDS, one needs it for its query only
+    constexpr int kQueryBytes = CodedQuery<TT, D>::bytes(kUnit), kMergeBytes = TEAM / 2 * kTiles * 4 * 64 * 4;
+    // TEAM waves share a unit: several join their results in LDS, one needs it for its query only
     __shared__ __align__(16) uint8_t room[TEAM == 1 ? kWaves * kQueryBytes : kQueryBytes > kMergeBytes ? kQueryBytes : kMergeBytes];
     __shared__ float2 ml[TEAM][16];
     __shared__ int64_t before[SPARSE ? 1 : kKvMaxUnits + 1];  // steps of the units before
-    __shared__ int64_t wave_steps[kWaves];
+    __shared__ int64_t wave_steps[TEAM];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, h = lane >> 4;
@@ -99,13 +102,14 @@ __global__ __launch_bounds__(kThreads, D == 64 || (SPARSE && D <= 128) ? 3 : D <
         unit = part / (uint32_t)a.splits;
         split = (int)(part - unit * (uint32_t)a.splits);
     } else if (a.splits > 1) {
-        constexpr int kPer = kKvMaxUnits / kThreads;
+        constexpr int kPer = kKvMaxUnits / (64 * TEAM);
+        const int per = (a.units + 64 * TEAM - 1) / (64 * TEAM);  // units of a thread: one, as long as that reaches
         int64_t mine[kPer], all = 0;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-            const uint32_t u = tid * kPer + i;
+            const uint32_t u = tid * per + i;
             mine[i] = all;
-            if (u < (uint32_t)a.units) all += unit_steps(a, u, kUnit, last_key);
+            if (i < per && u < (uint32_t)a.units) all += unit_steps(a, u, kUnit, last_key);
         }
         int64_t up = all;
 #pragma unroll
@@ -113,16 +117,17 @@ __global__ __launch_bounds__(kThreads, D == 64 || (SPARSE && D <= 128) ? 3 : D <
             const int64_t x = __shfl_up(up, d);
             if (lane >= d) up += x;
         }
-        if (lane == 63) wave_steps[wave] = up;
+        if (lane == 63) wave_steps[wave % TEAM] = up;
         __syncthreads();
         int64_t base = up - all, total = 0;
-        for (int w = 0; w < kWaves; ++w) {
+        for (int w = 0; w < TEAM; ++w) {
             if (w < wave) base += wave_steps[w];
             total += wave_steps[w];
         }
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) before[tid * kPer + i] = base + mine[i];
-        if (tid == 0) before[kKvMaxUnits] = total;
+        for (int i = 0; i < kPer; ++i)
+            if (i < per && tid * per + i < a.units) before[tid * per + i] = base + mine[i];
+        if (tid == 0) before[a.units] = total;
         __syncthreads();
         chunk = max((total + a.splits - 1) / a.splits, (int64_t)kMinSteps);
         from = chunk * part;
@@ -402,33 +407,23 @@ __global__ __launch_bounds__(kThreads, D == 64 || (SPARSE && D <= 128) ? 3 : D <
         for (int i = 0; i < kTiles; ++i) acc[i] *= f;
         if (TEAM > 1) {
             float(*merge)[kTiles * 4 * 64] = (float(*)[kTiles * 4 * 64])room;
-            float *buf = merge[wave & 1];
-            if (wave >= 2) {
+            // halving: the upper half of the waves that are left hand theirs down
 #pragma unroll
-                for (int i = 0; i < kTiles; ++i)
+            for (int half = TEAM / 2; half >= 1; half /= 2) {
+                if (wave >= half && wave < 2 * half) {
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) buf[(4 * i + r) * 64 + lane] = acc[i][r];
-            }
-            __syncthreads();
-            if (wave < 2) {
+                    for (int i = 0; i < kTiles; ++i)
 #pragma unroll
-                for (int i = 0; i < kTiles; ++i)
+                        for (int r = 0; r < 4; ++r) merge[wave - half][(4 * i + r) * 64 + lane] = acc[i][r];
+                }
+                __syncthreads();
+                if (wave < half) {
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) acc[i][r] += buf[(4 * i + r) * 64 + lane];
-            }
-            __syncthreads();
-            if (wave == 1) {
+                    for (int i = 0; i < kTiles; ++i)
 #pragma unroll
-                for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) merge[1][(4 * i + r) * 64 + lane] = acc[i][r];
-            }
-            __syncthreads();
-            if (wave == 0) {
-#pragma unroll
-                for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) acc[i][r] += merge[1][(4 * i + r) * 64 + lane];
+                        for (int r = 0; r < 4; ++r) acc[i][r] += merge[wave][(4 * i + r) * 64 + lane];
+                }
+                if (half > 1) __syncthreads();
             }
         }
         if (TEAM == 1 || wave == 0) {
@@ -547,22 +542,22 @@ __global__ __launch_bounds__(kThreads) void kv_combine_kernel(KvAttend a, int64_
     if (a.lse && lane == 0) a.lse[orow] = log_of(top, total);
 }
 
+template <typename TT, int D, bool SPARSE, int TEAM>
+hipError_t launch_team(const KvAttend &a, int64_t groups, hipStream_t s)
+{
+    const dim3 grid((unsigned)(groups * a.c.heads)), block(attend_threads(TEAM));
+    if (a.unit_size == 8) hipLaunchKernelGGL((kv_attend_kernel<TT, D, SPARSE, true, TEAM>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((kv_attend_kernel<TT, D, SPARSE, false, TEAM>), grid, block, 0, s, a);
+    return hipGetLastError();
+}
+
 template <typename TT, int D> hipError_t launch_tokens(const KvAttend &a, int64_t groups, hipStream_t s)
 {
-    const unsigned grid = (unsigned)(groups * a.c.heads);
-    const dim3 block(kThreads);
-    const bool pack = a.unit_size == 8;
-    if (a.team == 1) {
-        const dim3 waves((unsigned)((groups + kWaves - 1) / kWaves * a.c.heads));
-        if (pack) hipLaunchKernelGGL((kv_attend_kernel<TT, D, true, true, 1>), waves, block, 0, s, a);
-        else hipLaunchKernelGGL((kv_attend_kernel<TT, D, true, false, 1>), waves, block, 0, s, a);
-        return hipGetLastError();
-    }
-    if (a.blocks && pack) hipLaunchKernelGGL((kv_attend_kernel<TT, D, true, true, 4>), dim3(grid), block, 0, s, a);
-    else if (a.blocks) hipLaunchKernelGGL((kv_attend_kernel<TT, D, true, false, 4>), dim3(grid), block, 0, s, a);
-    else if (pack) hipLaunchKernelGGL((kv_attend_kernel<TT, D, false, true, 4>), dim3(grid), block, 0, s, a);
-    else hipLaunchKernelGGL((kv_attend_kernel<TT, D, false, false, 4>), dim3(grid), block, 0, s, a);
-    return hipGetLastError();
+    if (a.team == 1) return launch_team<TT, D, true, 1>(a, (groups + kWaves - 1) / kWaves, s);
+    if constexpr (D <= 128)
+        if (a.team == 8)
+            return a.blocks ? launch_team<TT, D, true, 8>(a, groups, s) : launch_team<TT, D, false, 8>(a, groups, s);
+    return a.blocks ? launch_team<TT, D, true, 4>(a, groups, s) : launch_team<TT, D, false, 4>(a, groups, s);
 }
 
 template <typename TT> hipError_t launch_combine(const KvAttend &a, bool prompt, hipStream_t s)
@@ -621,13 +616,19 @@ KvAttendPlan kv_attend_plan(const KvCache &c, int group, int64_t T, int64_t B, i
         p.per_unit = (int)((rows + p.unit_size - 1) / p.unit_size);
         p.unit_rows = (int)std::min<int64_t>(rows, p.unit_size);
         p.units = (count ? T : B) * p.per_unit;
-        // as many workgroups as are resident at once (a further round would only begin and join again)
-        const int64_t resident = (int64_t)num_cus * (c.dim <= 128 ? 2 : 1);
+        // Eight waves share a unit where there are at most as many as CUs, four where there
+        // are more, or they are shared out, or a wave takes over 256 registers (dim > 128), one
+        // where there is a unit for every wave that the device holds: one alone joins nothing.
+        const int64_t all = p.units * c.heads;
+        const bool shared = !count && keys > kWholeKeys && p.units <= kKvMaxUnits && all < 16 * (int64_t)num_cus;
+        p.team = c.dim > 128 || shared ? 4 : all <= num_cus ? 8 : count && all >= 12 * (int64_t)num_cus ? 1 : 4;
+        if (c.dim > 128 && count && all >= 4 * (int64_t)num_cus) p.team = 1;
+        // as many workgroups as are resident at once: a further round would only begin and join again
         if (count) {
             const int64_t most = std::max<int64_t>(1, keys / (32 * kMinSteps));
-            p.token_splits = (int)std::max<int64_t>(1, std::min(resident / (p.units * c.heads), most));
-            if (p.units * c.heads >= 12 * (int64_t)num_cus) p.team = 1;
-        } else if (keys > kWholeKeys && p.units <= kKvMaxUnits && p.units * c.heads < 16 * (int64_t)num_cus) {
+            p.token_splits = (int)std::max<int64_t>(1, std::min(num_cus / all, most));
+        } else if (shared) {
+            const int64_t resident = (int64_t)num_cus * (c.dim <= 128 ? 2 : 1);
             p.token_splits = (int)std::max<int64_t>(1, resident / c.heads);
         }
         if (p.token_splits > 1) {
