@@ -109,7 +109,8 @@ KvAttendPlan kv_attend_plan(const KvCache &c, int group, int64_t T, int64_t B, i
 hipError_t launch_kv_tokens(const KvAttend &a, int64_t groups, hipStream_t s);
 hipError_t launch_kv_combine(const KvAttend &a, bool prompt, hipStream_t s);
 
-int kv_prompt_rows(int dim);  // rows of a workgroup
+int kv_prompt_rows(int dim);      // rows of a workgroup
+int kv_prompt_resident(int dim);  // workgroups that a CU holds
 hipError_t launch_kv_prompt(const KvAttend &a, hipStream_t s);
 
 }  // namespace ivf

@@ -642,9 +642,9 @@ KvAttendPlan kv_attend_plan(const KvCache &c, int group, int64_t T, int64_t B, i
     }
     if (p.prompt) {
         const int64_t units = (T * group + kv_prompt_rows(c.dim) - 1) / kv_prompt_rows(c.dim) * c.heads;
-        if (units < num_cus) {
+        if (units < kv_prompt_resident(c.dim) * (int64_t)num_cus / 2) {
             const int64_t most = std::max<int64_t>(1, keys / 256);
-            p.prompt_splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(2 * (int64_t)num_cus / units, most), 32));
+            p.prompt_splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(kv_prompt_resident(c.dim) * (int64_t)num_cus / units, most), 32));
         }
         if (p.prompt_splits > 1) {
             const size_t n = (size_t)T * group * c.heads * p.prompt_splits;

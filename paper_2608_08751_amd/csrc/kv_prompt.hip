@@ -22,19 +22,25 @@
 namespace ivf {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kTileKeys = 64;
+// D <= 128: eight waves, 32 rows each; wider: four waves of 16 rows (registers, LDS).
+template <int D> struct PromptShape {
+    static constexpr int waves = D <= 128 ? 8 : 4, ct = D <= 128 ? 2 : 1;
+    static constexpr int threads = 64 * waves, rows = 16 * ct * waves;
+    static constexpr int keys = 16 * waves;  // of a tile: a strip a wave
+};
 
-template <typename TT, int D, int CT>
-__global__ __launch_bounds__(kThreads, 2) void kv_prompt_kernel(KvAttend a, int tiles)
+template <typename TT, int D>
+__global__ __launch_bounds__(PromptShape<D>::threads, 2) void kv_prompt_kernel(KvAttend a, int tiles)
 {
+    typedef PromptShape<D> Shape;
+    constexpr int CT = Shape::ct, kWaves = Shape::waves, kTileKeys = Shape::keys;
     typedef Pieces<D> P;
     typedef typename TT::elem elem;
-    constexpr int kOut = D / 16, kFrag = D / 32, kRows = 64 * CT;
-    __shared__ u32x4 kbuf[2][4][kFrag][64];
-    __shared__ u32x4 vbuf[2][2][kOut][64];
-    __shared__ int absent[2][4];  // strips that no table entry names
-    __shared__ int lims[4];
+    constexpr int kOut = D / 16, kFrag = D / 32, kRows = Shape::rows;
+    __shared__ u32x4 kbuf[2][kWaves][kFrag][64];
+    __shared__ u32x4 vbuf[2][kWaves / 2][kOut][64];
+    __shared__ int absent[2][kWaves];  // strips that no table entry names
+    __shared__ int lims[kWaves];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, h = lane >> 4;
@@ -119,7 +125,10 @@ __global__ __launch_bounds__(kThreads, 2) void kv_prompt_kernel(KvAttend a, int 
         wmin = __builtin_amdgcn_readfirstlane(wmin);
         if (lane == 0) lims[wave] = wmax;
         __syncthreads();
-        const int gmax = __builtin_amdgcn_readfirstlane(max(max(lims[0], lims[1]), max(lims[2], lims[3])));
+        int gmax = -1;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) gmax = max(gmax, lims[w]);
+        gmax = __builtin_amdgcn_readfirstlane(gmax);
         __syncthreads();
 
         const int ntiles = (gmax + kTileKeys) / kTileKeys;  // 0 where gmax is -1
@@ -150,7 +159,7 @@ __global__ __launch_bounds__(kThreads, 2) void kv_prompt_kernel(KvAttend a, int 
             ++ahead;
             if (page >= 0) {
                 const uint8_t *rec = a.c.rec + ((int64_t)page * a.c.heads + head) * rec_bytes;
-                const StripBase base = StripBase::at<D>(rec, (4 * k + wave) & strip_mask);
+                const StripBase base = StripBase::at<D>(rec, (kWaves * k + wave) & strip_mask);
                 keys.load(base, k_offs);
                 vals.load(base, v_offs);
             }
@@ -188,9 +197,10 @@ __global__ __launch_bounds__(kThreads, 2) void kv_prompt_kernel(KvAttend a, int 
             piece(std::integral_constant<int, 0>());
             if constexpr (P::n > 1) piece(std::integral_constant<int, 1>());
         };
-        auto compute = [&](int k) {
-            const int buf = k & 1;
-            if (k * kTileKeys > wmax) return;  // uniform over the wave
+        // 64 keys of a tile
+        auto compute = [&](int k, int part) {
+            const int buf = k & 1, first = k * kTileKeys + 64 * part;
+            if (first > wmax) return;  // uniform over the wave
             f32x4 st[4][CT];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -198,16 +208,17 @@ __global__ __launch_bounds__(kThreads, 2) void kv_prompt_kernel(KvAttend a, int 
                 for (int ct = 0; ct < CT; ++ct) st[e][ct] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int w = 0; w < kFrag; ++w) {
-                    const u32x4 x = kbuf[buf][e][w][lane];
+                    const u32x4 x = kbuf[buf][4 * part + e][w][lane];
 #pragma unroll
                     for (int ct = 0; ct < CT; ++ct) st[e][ct] = TT::mfma(x, qf[ct][w], st[e][ct]);
                 }
             }
-            const int gone = absent[buf][0] | absent[buf][1] << 1 | absent[buf][2] << 2 | absent[buf][3] << 3;
-            if (k * kTileKeys + kTileKeys - 1 > wmin || __builtin_amdgcn_readfirstlane(gone)) {
+            const int *none = &absent[buf][4 * part];
+            const int gone = none[0] | none[1] << 1 | none[2] << 2 | none[3] << 3;
+            if (first + 63 > wmin || __builtin_amdgcn_readfirstlane(gone)) {
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct) {
-                    const int left = lim[ct] - k * kTileKeys - 4 * h;  // of the lane's keys, the last to be seen
+                    const int left = lim[ct] - first - 4 * h;  // of the lane's keys, the last to be seen
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int last = (gone >> e & 1) ? -1 : left;
@@ -257,7 +268,7 @@ __global__ __launch_bounds__(kThreads, 2) void kv_prompt_kernel(KvAttend a, int 
             for (int p = 0; p < 2; ++p)
 #pragma unroll
                 for (int j = 0; j < kOut; ++j) {
-                    const u32x4 x = vbuf[buf][p][j][lane];
+                    const u32x4 x = vbuf[buf][2 * part + p][j][lane];
 #pragma unroll
                     for (int ct = 0; ct < CT; ++ct) acc[ct][j] = TT::mfma(x, pf[ct][p], acc[ct][j]);
                 }
@@ -272,7 +283,8 @@ __global__ __launch_bounds__(kThreads, 2) void kv_prompt_kernel(KvAttend a, int 
                 stage(k + 1);
                 if (k + 2 < k1) fetch(k + 2);
             }
-            compute(k);
+#pragma unroll 1
+            for (int part = 0; part < kWaves / 4; ++part) compute(k, part);
             __syncthreads();
         }
     }
@@ -293,28 +305,31 @@ __global__ __launch_bounds__(kThreads, 2) void kv_prompt_kernel(KvAttend a, int 
     }
 }
 
-template <typename TT, int D, int CT> hipError_t launch_prompt(const KvAttend &a, hipStream_t s)
+template <typename TT, int D> hipError_t launch_prompt(const KvAttend &a, hipStream_t s)
 {
-    const int64_t tiles = (a.T * a.group + 64 * CT - 1) / (64 * CT);
+    typedef PromptShape<D> Shape;
+    const int64_t tiles = (a.T * a.group + Shape::rows - 1) / Shape::rows;
     const unsigned grid = (unsigned)(tiles * a.splits * a.c.heads);
-    hipLaunchKernelGGL((kv_prompt_kernel<TT, D, CT>), dim3(grid), dim3(kThreads), 0, s, a, (int)tiles);
+    hipLaunchKernelGGL((kv_prompt_kernel<TT, D>), dim3(grid), dim3(Shape::threads), 0, s, a, (int)tiles);
     return hipGetLastError();
 }
 
 template <typename TT> hipError_t launch_prompt_dim(const KvAttend &a, hipStream_t s)
 {
     switch (a.c.dim) {
-    case 64: return launch_prompt<TT, 64, 2>(a, s);
-    case 96: return launch_prompt<TT, 96, 2>(a, s);
-    case 128: return launch_prompt<TT, 128, 2>(a, s);
-    case 192: return launch_prompt<TT, 192, 1>(a, s);
-    default: return launch_prompt<TT, 256, 1>(a, s);
+    case 64: return launch_prompt<TT, 64>(a, s);
+    case 96: return launch_prompt<TT, 96>(a, s);
+    case 128: return launch_prompt<TT, 128>(a, s);
+    case 192: return launch_prompt<TT, 192>(a, s);
+    default: return launch_prompt<TT, 256>(a, s);
     }
 }
 
 }  // namespace
 
-int kv_prompt_rows(int dim) { return dim <= 128 ? 128 : 64; }
+int kv_prompt_rows(int dim) { return dim <= 128 ? PromptShape<128>::rows : PromptShape<256>::rows; }
+
+int kv_prompt_resident(int dim) { return dim <= 128 ? 8 / PromptShape<128>::waves : 1; }
 
 hipError_t launch_kv_prompt(const KvAttend &a, hipStream_t s)
 {
