@@ -17,6 +17,8 @@
 #include "kv.h"
 #include "kv_types.h"
 
+#include <type_traits>
+
 namespace ivf {
 namespace {
 
@@ -59,17 +61,36 @@ __device__ __forceinline__ float wave_max(float m)
     return m;
 }
 
-__device__ __forceinline__ uint32_t wave_min_u32(uint32_t x)
+// The score of a key (the inverse of key_of).
+__device__ __forceinline__ float score_of(uint32_t k)
 {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) x = min(x, (uint32_t)__shfl_xor((int)x, d));
-    return x;
+    return __uint_as_float((k & 0x80000000u) ? k & 0x7fffffffu : ~k);
 }
-__device__ __forceinline__ uint32_t wave_max_u32(uint32_t x)
+
+// x summed over the wave, by lanes of a row of 16 and then over the rows.
+__device__ __forceinline__ float wave_sum(float x)
 {
+    auto step = [&](auto ctrl) {
+        constexpr int c = decltype(ctrl)::value;
+        x += __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), c, 0xf, 0xf, true));
+    };
+    step(std::integral_constant<int, 0xb1>());   // quad_perm 1 0 3 2
+    step(std::integral_constant<int, 0x4e>());   // quad_perm 2 3 0 1
+    step(std::integral_constant<int, 0x141>());  // row_half_mirror
+    step(std::integral_constant<int, 0x140>());  // row_mirror
+    float s = 0.f;
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) x = max(x, (uint32_t)__shfl_xor((int)x, d));
-    return x;
+    for (int r = 0; r < 4; ++r)
+        s += __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), 16 * r));
+    return s;
+}
+
+// The point that a normal variable passes with probability p, for p up to 1/2 to 0.003
+// (Abramowitz and Stegun, Handbook of Mathematical Functions, 26.2.22).
+__device__ __forceinline__ float upper_quantile(float p)
+{
+    const float t = __builtin_amdgcn_sqrtf(-1.38629436f * __builtin_amdgcn_logf(p));  // sqrt(-2 ln p)
+    return t - (0.27061f * t + 2.30753f) * __builtin_amdgcn_rcpf((0.04481f * t + 0.99229f) * t + 1.f);
 }
 
 // What WAVES waves exchange: two counters in turn, so that one barrier an exchange is enough.
@@ -104,22 +125,18 @@ __device__ __forceinline__ void select_best(const uint32_t (&k)[KPT], int wave, 
     int turn = 0;
     uint32_t all[WAVES];
     uint32_t c[KPT];  // candidates: keys that are not forced
-    uint32_t lo = UINT32_MAX, hi = 0;
+    float sum = 0.f, squares = 0.f, count_s = 0.f;  // of a quarter of the scores
 #pragma unroll
     for (int i = 0; i < KPT; ++i) {
         const int j = j0 + 64 * i;
         c[i] = j >= first && j < tail ? k[i] : 0u;
-        lo = min(lo, c[i] - 1u);  // 0 becomes the largest
-        hi = max(hi, c[i]);
+        if (i % 4 == 0 && c[i]) {
+            const float x = score_of(c[i]);
+            sum += x;
+            squares += x * x;
+            count_s += 1.f;
+        }
     }
-    lo = wave_min_u32(lo);
-    hi = wave_max_u32(hi);
-    exchange<WAVES>(ex, turn, wave, lo, all);
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) lo = min(lo, all[w]);
-    exchange<WAVES>(ex, turn, wave, hi, all);
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) hi = max(hi, all[w]);
     auto at_least = [&](uint32_t v) {
         uint32_t x = 0;
 #pragma unroll
@@ -132,18 +149,42 @@ __device__ __forceinline__ void select_best(const uint32_t (&k)[KPT], int wave, 
     };
     // keys above tau are kept, and the first `ties` equal to it
     uint32_t tau = 1;
-    int ties = INT32_MAX;
+    int ties = INT32_MAX, candidates = 0;
     if (want <= 0) {
         tau = UINT32_MAX;
         ties = 0;
-    } else if (hi != 0 && at_least(lo + 1) > want) {
-        uint32_t a = lo + 1, b = hi + 1;  // at_least(a) > want >= at_least(b); no number's key is UINT32_MAX
+    } else if ((candidates = at_least(1)) > want) {
+        // The want-th largest key lies between a and b: at_least(a) > want >= at_least(b) = cb
+        // (no number's key is UINT32_MAX). The first trial value is where a normal
+        // distribution of the scores' mean and variance has `want` keys above, the next ones step away
+        // from it until both sides are known, then the bracket is halved by value (by key where
+        // that leaves it): about seven counts, where halving the keys' range takes twenty.
+        auto over_waves = [&](float x) {
+            exchange<WAVES>(ex, turn, wave, __float_as_uint(wave_sum(x)), all);
+            float s = 0.f;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) s += __uint_as_float(all[w]);
+            return s;
+        };
+        const float per = __builtin_amdgcn_rcpf(over_waves(count_s)), mean = over_waves(sum) * per;
+        const float sigma = __builtin_amdgcn_sqrtf(fmaxf(over_waves(squares) * per - mean * mean, 0.f));
+        const float share = (float)want / (float)candidates;
+        float trial = mean + sigma * (share <= 0.5f ? upper_quantile(share) : -upper_quantile(1.f - share));
+        float step = 0.125f * sigma;
+        uint32_t a = 1, b = UINT32_MAX;
         int cb = 0;
         while (b - a > 1 && cb != want) {
-            const uint32_t mid = a + (b - a) / 2;
+            uint32_t mid = key_of(trial);
+            if (!(mid > a && mid < b)) mid = a + (b - a) / 2;
             const int x = at_least(mid);
             if (x > want) a = mid;
             else b = mid, cb = x;
+            if (a > 1 && b < UINT32_MAX) {
+                trial = 0.5f * score_of(a) + 0.5f * score_of(b);
+            } else {
+                trial += x > want ? step : -step;
+                step *= 2.f;
+            }
         }
         tau = cb == want ? b : a;
         if (cb != want) ties = want - cb;  // b = a + 1: cb keys are above a
