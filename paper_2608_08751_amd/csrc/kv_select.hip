@@ -49,9 +49,12 @@ __device__ __forceinline__ float2 group_sum(const KvSelect &a, int64_t t, int h,
     return u;
 }
 
-__device__ __forceinline__ int code_of(float u, float amax)
+// 127 / amax, or 0 where amax is too small: code = rint(u times it).
+__device__ __forceinline__ float code_scale(float amax) { return amax >= 0x1p-100f ? 127.f / amax : 0.f; }
+__device__ __forceinline__ uint16_t two_codes(float2 u, float scale)
 {
-    return amax >= 0x1p-100f ? (int)rintf(u * (127.f / amax)) : 0;
+    const int c0 = (int)rintf(u.x * scale), c1 = (int)rintf(u.y * scale);
+    return (uint16_t)((c0 & 255) | (c1 & 255) << 8);
 }
 
 __device__ __forceinline__ float wave_max(float m)
@@ -246,17 +249,20 @@ __device__ __forceinline__ Extent extent_of(const KvSelect &a, int64_t t)
 
 constexpr int kOneThreads = 1024, kOneWaves = kOneThreads / 64;
 
-// KPT keys a thread: tables of up to 1024 KPT columns. Dynamic LDS: [cols] block ids, then keys.
-template <typename TT, int KPT>
+// KPT keys a thread: tables of up to 1024 KPT columns. PARTS: 128 channels each.
+// Dynamic LDS: [cols] block ids, then keys.
+template <typename TT, int KPT, int PARTS>
 __global__ __launch_bounds__(kOneThreads) void kv_select_one_kernel(KvSelect a)
 {
     extern __shared__ uint32_t lds[];
-    __shared__ __align__(16) int8_t code[256];
-    __shared__ float top[2];
+    __shared__ __align__(16) int8_t code[128 * PARTS];
+    __shared__ float top[PARTS];
     __shared__ Exchange<kOneWaves> ex;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int h = blockIdx.x % (uint32_t)a.c.heads;
     const int64_t t = blockIdx.x / (uint32_t)a.c.heads;
+    float2 u = make_float2(0.f, 0.f);
+    if (2 * tid < a.c.dim) u = group_sum<TT>(a, t, h, 2 * tid);
     const Extent e = extent_of(a, t);
     int32_t *out = a.out + (t * a.c.heads + h) * a.count;
     const bool ranked = e.n > a.count;
@@ -266,49 +272,47 @@ __global__ __launch_bounds__(kOneThreads) void kv_select_one_kernel(KvSelect a)
         lds[j] = ranked ? (uint32_t)id : (uint32_t)(id >= 0);  // all are kept, but for holes in the table
     }
     if (ranked) {
-        float2 u = make_float2(0.f, 0.f);
-        if (2 * tid < a.c.dim) u = group_sum<TT>(a, t, h, 2 * tid);
-        if (tid < 128) {  // at most 256 channels: two waves hold them
+        if (tid < 64 * PARTS) {  // the waves that hold channels
             const float m = wave_max(fmaxf(fabsf(u.x), fabsf(u.y)));
             if (lane == 0) top[wave] = m;
         }
         __syncthreads();
-        if (tid < 128) {
-            const float amax = fmaxf(top[0], top[1]);
-            const int c0 = code_of(u.x, amax), c1 = code_of(u.y, amax);
-            *(uint16_t *)&code[2 * tid] = (uint16_t)((c0 & 255) | (c1 & 255) << 8);
-        }
+        if (tid < 64 * PARTS)
+            *(uint16_t *)&code[2 * tid] = two_codes(u, code_scale(PARTS > 1 ? fmaxf(top[0], top[PARTS - 1]) : top[0]));
         __syncthreads();
-        const int part = tid & 7;  // 16 bytes of a summary, and 16 more 128 further on
-        const i32x4 q0 = *(const i32x4 *)&code[16 * part], q1 = *(const i32x4 *)&code[128 + 16 * part];
-        const bool has0 = 16 * part < a.c.dim, has1 = 128 + 16 * part < a.c.dim;
-        constexpr int kAhead = 4, kStep = kOneThreads / 8;
+        const int part = tid & 7;  // 16 bytes of every 128 of a summary
+        i32x4 q[PARTS];
+        bool has[PARTS];
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) {
+            q[p] = *(const i32x4 *)&code[128 * p + 16 * part];
+            has[p] = 128 * p + 16 * part < a.c.dim;
+        }
+        constexpr int kAhead = 8 / PARTS, kStep = kOneThreads / 8;
         for (int j0 = tid >> 3; j0 < e.n; j0 += kStep * kAhead) {
-            i32x4 x0[kAhead], x1[kAhead];
+            i32x4 x[kAhead][PARTS];
             float w[kAhead];
             int32_t id[kAhead];
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
                 const int j = j0 + kStep * i;
                 id[i] = j < e.n ? (int32_t)lds[j] : -1;
-                x0[i] = x1[i] = (i32x4){0, 0, 0, 0};
                 w[i] = 0.f;
-                if (id[i] >= 0) {
-                    const int64_t at = (int64_t)id[i] * a.c.heads + h;
-                    const int8_t *p = a.c.summary + at * a.c.dim + 16 * part;
-                    if (has0) x0[i] = *(const i32x4 *)p;
-                    if (has1) x1[i] = *(const i32x4 *)(p + 128);
-                    if (part == 0) w[i] = a.c.weight[at];
+                const int64_t at = (int64_t)max(id[i], 0) * a.c.heads + h;
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p) {
+                    x[i][p] = (i32x4){0, 0, 0, 0};
+                    if (id[i] >= 0 && has[p]) x[i][p] = *(const i32x4 *)(a.c.summary + at * a.c.dim + 128 * p + 16 * part);
                 }
+                if (id[i] >= 0 && part == 0) w[i] = a.c.weight[at];
             }
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
                 int s = 0;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    s = __builtin_amdgcn_sdot4(x0[i][r], q0[r], s, false);
-                    s = __builtin_amdgcn_sdot4(x1[i][r], q1[r], s, false);
-                }
+                for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) s = __builtin_amdgcn_sdot4(x[i][p][r], q[p][r], s, false);
                 s += __shfl_xor(s, 1);
                 s += __shfl_xor(s, 2);
                 s += __shfl_xor(s, 4);
@@ -329,11 +333,14 @@ __global__ __launch_bounds__(kOneThreads) void kv_select_one_kernel(KvSelect a)
 
 constexpr int kTileTokens = 16, kTileThreads = 512;
 
-// KPT keys a lane: tables of up to 64 KPT columns. Dynamic LDS: keys [16][ld], ld >= cols.
+// KPT keys a lane: tables of up to 64 KPT columns. Dynamic LDS: keys [16][ld], then
+// block ids [ld] and weights [ld] of the request at hand, ld >= cols + 4 a multiple of 4.
 template <typename TT, int KPT>
 __global__ __launch_bounds__(kTileThreads) void kv_select_tile_kernel(KvSelect a, int ld)
 {
     extern __shared__ uint32_t lds[];
+    int32_t *ids = (int32_t *)lds + kTileTokens * ld;
+    float *weights = (float *)(ids + ld);
     __shared__ __align__(16) int8_t code[kTileTokens][256];
     __shared__ Extent ext[kTileTokens];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -359,12 +366,9 @@ __global__ __launch_bounds__(kTileThreads) void kv_select_tile_kernel(KvSelect a
             }
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const float amax = wave_max(m[i]);
+            const float scale = code_scale(wave_max(m[i]));
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                const int c0 = code_of(u[i][s].x, amax), c1 = code_of(u[i][s].y, amax);
-                *(uint16_t *)&code[wave + 8 * i][2 * (lane + 64 * s)] = (uint16_t)((c0 & 255) | (c1 & 255) << 8);
-            }
+            for (int s = 0; s < 2; ++s) *(uint16_t *)&code[wave + 8 * i][2 * (lane + 64 * s)] = two_codes(u[i][s], scale);
         }
     }
     __syncthreads();
@@ -377,24 +381,23 @@ __global__ __launch_bounds__(kTileThreads) void kv_select_tile_kernel(KvSelect a
         const int b = ext[i0].b;
         int i1 = i0, n = 0;
         for (; i1 < tokens && ext[i1].b == b; ++i1) n = max(n, ext[i1].n);
+        for (int j = tid; j < (n + 15) / 16 * 16; j += kTileThreads) {
+            int32_t id = j < n ? a.table[(int64_t)b * a.cols + j] : -1;
+            if (id >= a.c.blocks) id = -1;
+            ids[j] = max(id, 0);
+            weights[j] = id >= 0 ? a.c.weight[(int64_t)id * a.c.heads + h] : -1.f;  // weights are not negative
+        }
+        __syncthreads();
         const bool mine = col >= i0 && col < i1;
         constexpr int kAhead = 4, kStep = 16 * (kTileThreads / 64);
         for (int j0 = 16 * wave; j0 < n; j0 += kStep * kAhead) {
-            int32_t id[kAhead];
-#pragma unroll
-            for (int x = 0; x < kAhead; ++x) {
-                const int jr = j0 + kStep * x + col;  // the block that this lane loads
-                id[x] = jr < n ? a.table[(int64_t)b * a.cols + jr] : -1;
-                if (id[x] >= a.c.blocks) id[x] = -1;
-            }
             i32x4 acc[kAhead];
-            float w[kAhead];
 #pragma unroll
             for (int x = 0; x < kAhead; ++x) {
-                const int64_t at = (int64_t)max(id[x], 0) * a.c.heads + h;
-                const int8_t *p = a.c.summary + at * a.c.dim + 16 * hi;
-                w[x] = a.c.weight[at];
                 acc[x] = (i32x4){0, 0, 0, 0};
+                const int j = j0 + kStep * x;
+                const int32_t id = j < n ? ids[j + col] : 0;
+                const int8_t *p = a.c.summary + ((int64_t)id * a.c.heads + h) * a.c.dim + 16 * hi;
 #pragma unroll
                 for (int s = 0; s < 4; ++s) {
                     if (s < steps) {
@@ -406,24 +409,18 @@ __global__ __launch_bounds__(kTileThreads) void kv_select_tile_kernel(KvSelect a
             }
 #pragma unroll
             for (int x = 0; x < kAhead; ++x) {
+                const int j = j0 + kStep * x + 4 * hi;  // the lane's four blocks
                 if (j0 + kStep * x >= n) break;
-                uint32_t k[4];
+                const f32x4 w = *(const f32x4 *)&weights[j];
+                u32x4 k;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int src = 4 * hi + r;  // the block of row src was loaded by lane src
-                    const float wr = __shfl(w[x], src);
-                    const int idr = __shfl(id[x], src);
-                    k[r] = idr >= 0 ? key_of((float)acc[x][r] * wr) : 0u;
-                }
-                if (mine) {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) lds[col * ld + j0 + kStep * x + 4 * hi + r] = k[r];
-                }
+                for (int r = 0; r < 4; ++r) k[r] = w[r] >= 0.f ? key_of((float)acc[x][r] * w[r]) : 0u;
+                if (mine) *(u32x4 *)&lds[col * ld + j] = k;
             }
         }
         i0 = i1;
+        __syncthreads();
     }
-    __syncthreads();
     Exchange<1> ex;
     for (int i = wave; i < tokens; i += kTileThreads / 64) {
         const Extent e = ext[i];
@@ -454,7 +451,7 @@ template <typename TT> hipError_t launch_select(const KvSelect &a, hipStream_t s
     // 16 tokens of a tile share the summaries where a batch brings more tokens than requests
     if (a.T > 2 * a.B && a.cols <= 2048) {
         const int ld = (a.cols + 15) / 16 * 16 + 4;
-        const size_t lds = (size_t)kTileTokens * ld * 4;
+        const size_t lds = (size_t)(kTileTokens + 2) * ld * 4;
         const unsigned grid = (unsigned)((a.T + kTileTokens - 1) / kTileTokens * a.c.heads);
         return a.cols <= 512    ? launch_lds(kv_select_tile_kernel<TT, 8>, grid, kTileThreads, lds, s, a, ld)
                : a.cols <= 1024 ? launch_lds(kv_select_tile_kernel<TT, 16>, grid, kTileThreads, lds, s, a, ld)
@@ -462,9 +459,13 @@ template <typename TT> hipError_t launch_select(const KvSelect &a, hipStream_t s
     }
     const size_t lds = (size_t)a.cols * 4;
     const unsigned grid = (unsigned)(a.T * a.c.heads);
-    return a.cols <= 2048   ? launch_lds(kv_select_one_kernel<TT, 2>, grid, kOneThreads, lds, s, a)
-           : a.cols <= 8192 ? launch_lds(kv_select_one_kernel<TT, 8>, grid, kOneThreads, lds, s, a)
-                            : launch_lds(kv_select_one_kernel<TT, 32>, grid, kOneThreads, lds, s, a);
+    if (a.c.dim <= 128)
+        return a.cols <= 2048   ? launch_lds(kv_select_one_kernel<TT, 2, 1>, grid, kOneThreads, lds, s, a)
+               : a.cols <= 8192 ? launch_lds(kv_select_one_kernel<TT, 8, 1>, grid, kOneThreads, lds, s, a)
+                                : launch_lds(kv_select_one_kernel<TT, 32, 1>, grid, kOneThreads, lds, s, a);
+    return a.cols <= 2048   ? launch_lds(kv_select_one_kernel<TT, 2, 2>, grid, kOneThreads, lds, s, a)
+           : a.cols <= 8192 ? launch_lds(kv_select_one_kernel<TT, 8, 2>, grid, kOneThreads, lds, s, a)
+                            : launch_lds(kv_select_one_kernel<TT, 32, 2>, grid, kOneThreads, lds, s, a);
 }
 
 }  // namespace
