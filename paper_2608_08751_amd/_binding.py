@@ -111,6 +111,7 @@ class Context:
         self.lib = load_library()
         self.device = device
         self._ws = None
+        self._bound = None  # the stream of the last bind()
         h = ctypes.c_void_p()
         if device >= 0:
             with torch.cuda.device(device):
@@ -152,13 +153,15 @@ class Context:
                    "ivf_set_workspace")
 
     def bind_stream(self):
+        self._bound = None
         self.check(self.lib.ivf_set_stream(self.handle, _stream_handle()), "ivf_set_stream")
 
     def bind(self):
         """Binds torch's current stream of the device; the library and the context's handle."""
-        st = self.lib.ivf_set_stream(self.handle, _stream_handle(self.device))
-        if st:
-            self.check(st, "ivf_set_stream")
+        stream = _stream_handle(self.device)
+        if stream != self._bound:
+            self.check(self.lib.ivf_set_stream(self.handle, stream), "ivf_set_stream")
+            self._bound = stream
         return self.lib, self.handle
 
     def sync(self):

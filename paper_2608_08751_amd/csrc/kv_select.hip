@@ -96,23 +96,39 @@ __device__ __forceinline__ float upper_quantile(float p)
     return t - (0.27061f * t + 2.30753f) * __builtin_amdgcn_rcpf((0.04481f * t + 0.99229f) * t + 1.f);
 }
 
-// What WAVES waves exchange: two counters in turn, so that one barrier an exchange is enough.
+// Sums over WAVES waves: two rows in turn, so that one barrier a sum is enough.
 template <int WAVES> struct Exchange {
     uint32_t v[2][WAVES];
 };
-// The waves' values x (uniform in each), in all of them.
-template <int WAVES>
-__device__ __forceinline__ void exchange(Exchange<WAVES> &e, int &turn, int wave, uint32_t x, uint32_t (&all)[WAVES])
+template <typename T, int WAVES>
+__device__ __forceinline__ T add_rows16(T x)  // over lanes 0 ... 15, in lane 0
 {
+    auto step = [&](auto ctrl) {
+        constexpr int c = decltype(ctrl)::value;
+        x += __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), c, 0xf, 0xf, true));
+    };
+    step(std::integral_constant<int, 0xb1>());
+    step(std::integral_constant<int, 0x4e>());
+    step(std::integral_constant<int, 0x141>());
+    step(std::integral_constant<int, 0x140>());
+    return __builtin_bit_cast(T, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x)));
+}
+// The sum of the waves' x (uniform in each); *before: of the waves before this one.
+template <typename T, int WAVES>
+__device__ __forceinline__ T sum_waves(Exchange<WAVES> &e, int &turn, int wave, T x, T *before = nullptr)
+{
+    static_assert(WAVES <= 16, "a lane a wave");
     if (WAVES == 1) {
-        all[0] = x;
-        return;
+        if (before) *before = 0;
+        return x;
     }
-    if ((threadIdx.x & 63) == 0) e.v[turn][wave] = x;
+    const int lane = threadIdx.x & 63;
+    if (lane == 0) e.v[turn][wave] = __builtin_bit_cast(uint32_t, x);
     __syncthreads();
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) all[w] = e.v[turn][w];
+    const T y = lane < WAVES ? __builtin_bit_cast(T, e.v[turn][lane % WAVES]) : T(0);
     turn ^= 1;
+    if (before) *before = add_rows16<T, WAVES>(lane < wave ? y : T(0));
+    return add_rows16<T, WAVES>(y);
 }
 
 // Keeps of keys 0 ... n - 1 those of forced places (j < first or j >= tail) and the
@@ -126,52 +142,46 @@ __device__ __forceinline__ void select_best(const uint32_t (&k)[KPT], int wave, 
 {
     const int lane = threadIdx.x & 63, j0 = wave * KPT * 64 + lane;
     int turn = 0;
-    uint32_t all[WAVES];
-    uint32_t c[KPT];  // candidates: keys that are not forced
+    uint32_t c[KPT];  // keys; forced ones the largest
     float sum = 0.f, squares = 0.f, count_s = 0.f;  // of a quarter of the scores
+    int forced = 0;
 #pragma unroll
     for (int i = 0; i < KPT; ++i) {
         const int j = j0 + 64 * i;
-        c[i] = j >= first && j < tail ? k[i] : 0u;
-        if (i % 4 == 0 && c[i]) {
-            const float x = score_of(c[i]);
+        const bool kept = (j < first || j >= tail) && k[i] != 0;
+        c[i] = kept ? UINT32_MAX : k[i];
+        forced += __popcll(__ballot(kept));
+        if (i % 4 == 0) {
+            const bool sample = k[i] != 0 && !kept;
+            const float x = sample ? score_of(k[i]) : 0.f;
             sum += x;
             squares += x * x;
-            count_s += 1.f;
+            count_s += sample ? 1.f : 0.f;
         }
     }
+    forced = sum_waves<int, WAVES>(ex, turn, wave, forced);
+    // keys at or above v (no number's key is UINT32_MAX), the forced ones left out
     auto at_least = [&](uint32_t v) {
-        uint32_t x = 0;
+        int x = 0;
 #pragma unroll
-        for (int i = 0; i < KPT; ++i) x += (uint32_t)__popcll(__ballot(c[i] >= v));
-        exchange<WAVES>(ex, turn, wave, x, all);
-        x = 0;
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) x += all[w];
-        return (int)x;
+        for (int i = 0; i < KPT; ++i) x += __popcll(__ballot(c[i] >= v));
+        return sum_waves<int, WAVES>(ex, turn, wave, x) - forced;
     };
-    // keys above tau are kept, and the first `ties` equal to it
+    // kept are keys at or above tau, and the first `ties` equal to tau - 1
     uint32_t tau = 1;
-    int ties = INT32_MAX, candidates = 0;
+    int ties = 0, candidates = 0;
     if (want <= 0) {
         tau = UINT32_MAX;
-        ties = 0;
     } else if ((candidates = at_least(1)) > want) {
-        // The want-th largest key lies between a and b: at_least(a) > want >= at_least(b) = cb
-        // (no number's key is UINT32_MAX). The first trial value is where a normal
+        // The want-th largest key lies between a and b: at_least(a) > want >= at_least(b) = cb.
+        // The first trial value is where a normal
         // distribution of the scores' mean and variance has `want` keys above, the next ones step away
         // from it until both sides are known, then the bracket is halved by value (by key where
         // that leaves it): about seven counts, where halving the keys' range takes twenty.
-        auto over_waves = [&](float x) {
-            exchange<WAVES>(ex, turn, wave, __float_as_uint(wave_sum(x)), all);
-            float s = 0.f;
-#pragma unroll
-            for (int w = 0; w < WAVES; ++w) s += __uint_as_float(all[w]);
-            return s;
-        };
+        auto over_waves = [&](float x) { return sum_waves<float, WAVES>(ex, turn, wave, wave_sum(x)); };
         const float per = __builtin_amdgcn_rcpf(over_waves(count_s)), mean = over_waves(sum) * per;
         const float sigma = __builtin_amdgcn_sqrtf(fmaxf(over_waves(squares) * per - mean * mean, 0.f));
-        const float share = (float)want / (float)candidates;
+        const float share = (float)want * __builtin_amdgcn_rcpf((float)candidates);
         float trial = mean + sigma * (share <= 0.5f ? upper_quantile(share) : -upper_quantile(1.f - share));
         float step = 0.125f * sigma;
         uint32_t a = 1, b = UINT32_MAX;
@@ -189,37 +199,37 @@ __device__ __forceinline__ void select_best(const uint32_t (&k)[KPT], int wave, 
                 step *= 2.f;
             }
         }
-        tau = cb == want ? b : a;
-        if (cb != want) ties = want - cb;  // b = a + 1: cb keys are above a
+        tau = b;
+        ties = want - cb;  // where more than 0, b = a + 1
     }
-    uint32_t eq = 0;
-#pragma unroll
-    for (int i = 0; i < KPT; ++i) eq += (uint32_t)__popcll(__ballot(c[i] == tau));
-    exchange<WAVES>(ex, turn, wave, eq, all);
-    int used = 0;
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w)
-        if (w < wave) used += (int)all[w];
     const uint64_t below = ((uint64_t)1 << lane) - 1;
-    uint32_t take = 0, kept = 0;
+    uint32_t take = 0;
+    int kept = 0;
     static_assert(KPT <= 32, "a bit a key");
+    if (ties > 0) {
+        int eq = 0, used = 0;
 #pragma unroll
-    for (int i = 0; i < KPT; ++i) {
-        const int j = j0 + 64 * i;
-        const bool same = c[i] == tau;
-        const uint64_t me = __ballot(same);
-        const bool t = ((j < first || j >= tail) && k[i] != 0) || c[i] > tau || (same && used + __popcll(me & below) < ties);
-        used += __popcll(me);
-        take |= (uint32_t)t << i;
-        kept += (uint32_t)__popcll(__ballot(t));
-    }
-    exchange<WAVES>(ex, turn, wave, kept, all);
-    int at = 0, total = 0;
+        for (int i = 0; i < KPT; ++i) eq += __popcll(__ballot(c[i] == tau - 1));
+        sum_waves<int, WAVES>(ex, turn, wave, eq, &used);
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
-        if (w < wave) at += (int)all[w];
-        total += (int)all[w];
+        for (int i = 0; i < KPT; ++i) {
+            const bool same = c[i] == tau - 1;
+            const uint64_t me = __ballot(same);
+            const bool t = c[i] >= tau || (same && used + __popcll(me & below) < ties);
+            used += __popcll(me);
+            take |= (uint32_t)t << i;
+            kept += __popcll(__ballot(t));
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < KPT; ++i) {
+            const bool t = c[i] >= tau;
+            take |= (uint32_t)t << i;
+            kept += __popcll(__ballot(t));
+        }
     }
+    int at = 0;
+    const int total = sum_waves<int, WAVES>(ex, turn, wave, kept, &at);
 #pragma unroll
     for (int i = 0; i < KPT; ++i) {
         const bool t = take >> i & 1;
@@ -249,15 +259,16 @@ __device__ __forceinline__ Extent extent_of(const KvSelect &a, int64_t t)
 
 constexpr int kOneThreads = 1024, kOneWaves = kOneThreads / 64;
 
-// KPT keys a thread: tables of up to 1024 KPT columns. PARTS: 128 channels each.
-// Dynamic LDS: [cols] block ids, then keys.
-template <typename TT, int KPT, int PARTS>
+// KPT keys a lane of the TEAM waves that select: tables of up to 64 KPT TEAM columns. PARTS: 128
+// channels each. Dynamic LDS: [cols] block ids, then keys. One wave selects among up to 2,048 keys
+// (a count is three instructions for 64 keys there, and no barrier), all 16 beyond.
+template <typename TT, int KPT, int PARTS, int TEAM>
 __global__ __launch_bounds__(kOneThreads) void kv_select_one_kernel(KvSelect a)
 {
     extern __shared__ uint32_t lds[];
     __shared__ __align__(16) int8_t code[128 * PARTS];
     __shared__ float top[PARTS];
-    __shared__ Exchange<kOneWaves> ex;
+    __shared__ Exchange<TEAM> ex;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int h = blockIdx.x % (uint32_t)a.c.heads;
     const int64_t t = blockIdx.x / (uint32_t)a.c.heads;
@@ -322,16 +333,17 @@ __global__ __launch_bounds__(kOneThreads) void kv_select_one_kernel(KvSelect a)
         }
     }
     __syncthreads();
+    if (wave >= TEAM) return;
     uint32_t k[KPT];
 #pragma unroll
     for (int i = 0; i < KPT; ++i) {
         const int j = (wave * KPT + i) * 64 + lane;
         k[i] = j < e.n ? lds[j] : 0u;
     }
-    select_best<kOneWaves, KPT>(k, wave, e.n, e.first, e.tail, e.want, a.count, out, ex);
+    select_best<TEAM, KPT>(k, wave, e.n, e.first, e.tail, e.want, a.count, out, ex);
 }
 
-constexpr int kTileTokens = 16, kTileThreads = 512;
+constexpr int kTileTokens = 16, kTileThreads = 1024;  // a wave a token
 
 // KPT keys a lane: tables of up to 64 KPT columns. Dynamic LDS: keys [16][ld], then
 // block ids [ld] and weights [ld] of the request at hand, ld >= cols + 4 a multiple of 4.
@@ -352,24 +364,19 @@ __global__ __launch_bounds__(kTileThreads) void kv_select_tile_kernel(KvSelect a
         if (tid < tokens) e = extent_of(a, t0 + tid);
         ext[tid] = e;
     }
-    // codes of two tokens a wave (missing ones are zero)
+    // the code of a token a wave (missing ones are zero)
     {
-        float2 u[2][2];
-        float m[2] = {0.f, 0.f};
+        float2 u[2];
+        float m = 0.f;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                const int d = 2 * (lane + 64 * s), x = wave + 8 * i;
-                u[i][s] = d < a.c.dim && x < tokens ? group_sum<TT>(a, t0 + x, h, d) : make_float2(0.f, 0.f);
-                m[i] = fmaxf(m[i], fmaxf(fabsf(u[i][s].x), fabsf(u[i][s].y)));
-            }
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const float scale = code_scale(wave_max(m[i]));
-#pragma unroll
-            for (int s = 0; s < 2; ++s) *(uint16_t *)&code[wave + 8 * i][2 * (lane + 64 * s)] = two_codes(u[i][s], scale);
+        for (int s = 0; s < 2; ++s) {
+            const int d = 2 * (lane + 64 * s);
+            u[s] = d < a.c.dim && wave < tokens ? group_sum<TT>(a, t0 + wave, h, d) : make_float2(0.f, 0.f);
+            m = fmaxf(m, fmaxf(fabsf(u[s].x), fabsf(u[s].y)));
         }
+        const float scale = code_scale(wave_max(m));
+#pragma unroll
+        for (int s = 0; s < 2; ++s) *(uint16_t *)&code[wave][2 * (lane + 64 * s)] = two_codes(u[s], scale);
     }
     __syncthreads();
     // scores, request by request (the tokens of one follow each other)
@@ -421,18 +428,16 @@ __global__ __launch_bounds__(kTileThreads) void kv_select_tile_kernel(KvSelect a
         i0 = i1;
         __syncthreads();
     }
+    if (wave >= tokens) return;
     Exchange<1> ex;
-    for (int i = wave; i < tokens; i += kTileThreads / 64) {
-        const Extent e = ext[i];
-        uint32_t k[KPT];
+    const Extent e = ext[wave];
+    uint32_t k[KPT];
 #pragma unroll
-        for (int x = 0; x < KPT; ++x) {
-            const int j = 64 * x + lane;
-            k[x] = j < e.n ? lds[i * ld + j] : 0u;
-        }
-        select_best<1, KPT>(k, 0, e.n, e.first, e.tail, e.want, a.count,
-                            a.out + ((t0 + i) * a.c.heads + h) * a.count, ex);
+    for (int x = 0; x < KPT; ++x) {
+        const int j = 64 * x + lane;
+        k[x] = j < e.n ? lds[wave * ld + j] : 0u;
     }
+    select_best<1, KPT>(k, 0, e.n, e.first, e.tail, e.want, a.count, a.out + ((t0 + wave) * a.c.heads + h) * a.count, ex);
 }
 
 template <typename F, typename... A>
@@ -444,6 +449,15 @@ hipError_t launch_lds(F *f, unsigned grid, int threads, size_t lds, hipStream_t 
     }
     hipLaunchKernelGGL(f, dim3(grid), dim3(threads), lds, s, args...);
     return hipGetLastError();
+}
+
+template <typename TT, int PARTS> hipError_t launch_one(const KvSelect &a, unsigned grid, size_t lds, hipStream_t s)
+{
+    return a.cols <= 512    ? launch_lds(kv_select_one_kernel<TT, 8, PARTS, 1>, grid, kOneThreads, lds, s, a)
+           : a.cols <= 1024 ? launch_lds(kv_select_one_kernel<TT, 16, PARTS, 1>, grid, kOneThreads, lds, s, a)
+           : a.cols <= 2048 ? launch_lds(kv_select_one_kernel<TT, 32, PARTS, 1>, grid, kOneThreads, lds, s, a)
+           : a.cols <= 8192 ? launch_lds(kv_select_one_kernel<TT, 8, PARTS, 16>, grid, kOneThreads, lds, s, a)
+                            : launch_lds(kv_select_one_kernel<TT, 32, PARTS, 16>, grid, kOneThreads, lds, s, a);
 }
 
 template <typename TT> hipError_t launch_select(const KvSelect &a, hipStream_t s)
@@ -459,13 +473,7 @@ template <typename TT> hipError_t launch_select(const KvSelect &a, hipStream_t s
     }
     const size_t lds = (size_t)a.cols * 4;
     const unsigned grid = (unsigned)(a.T * a.c.heads);
-    if (a.c.dim <= 128)
-        return a.cols <= 2048   ? launch_lds(kv_select_one_kernel<TT, 2, 1>, grid, kOneThreads, lds, s, a)
-               : a.cols <= 8192 ? launch_lds(kv_select_one_kernel<TT, 8, 1>, grid, kOneThreads, lds, s, a)
-                                : launch_lds(kv_select_one_kernel<TT, 32, 1>, grid, kOneThreads, lds, s, a);
-    return a.cols <= 2048   ? launch_lds(kv_select_one_kernel<TT, 2, 2>, grid, kOneThreads, lds, s, a)
-           : a.cols <= 8192 ? launch_lds(kv_select_one_kernel<TT, 8, 2>, grid, kOneThreads, lds, s, a)
-                            : launch_lds(kv_select_one_kernel<TT, 32, 2>, grid, kOneThreads, lds, s, a);
+    return a.c.dim <= 128 ? launch_one<TT, 1>(a, grid, lds, s) : launch_one<TT, 2>(a, grid, lds, s);
 }
 
 }  // namespace
