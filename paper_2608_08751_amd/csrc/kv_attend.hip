@@ -6,10 +6,9 @@
 //   * scores: S^T = K Q^T with 16 keys (a strip) as rows, on
 //     v_mfma_scale_f32_16x16x128_f8f6f4: 32 channels of 4-bit codes with a power of two
 //     are its A operand as they lie in memory, 16 bytes of codes and a scale byte a lane.
-//     The query is the sum of two (f16: three) fp8 numbers a channel with a power of two per
-//     32 channels, each the rounding (4 significant bits) of what the ones before
-//     leave: exact for channels down to 2^-13 of the largest of their 32, below that
-//     off by 2^-21 of it at most.
+//     The query is the sum of four 6-bit numbers a channel with a power of two per
+//     32 channels: digits of a fixed-point number, off by 2^-19 of the largest of the 32 at
+//     most (numbers of 8 significant bits: exact down to 2^-11 of it, of 11 bits to 2^-8).
 //   * values: O^T = V^T P^T on v_mfma_f32_16x16x32. The results above are the B operand as
 //     they are: lane (r, h)'s eight probabilities of two strips are keys 4 h ... 4 h + 3 of each.
 //     It reads the codes of neighbouring channels of those keys, v_cvt_scalef32 makes pairs of channels with the key's scale, v_perm_b32 pairs of keys.

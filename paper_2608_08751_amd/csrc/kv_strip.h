@@ -154,17 +154,22 @@ template <int D> struct CodedKeys {
     }
 };
 
-// Query rows as sums of fp8 numbers: term t of a channel is the fp8 rounding of what
-// the terms before leave, times 16^t, beside a power of two for each 32 channels (byte t
-// of a scale word: that of term t).
+// Query rows as sums of 6-bit numbers (e2m3): a channel is a fixed-point number, the
+// largest of its 32 in [8, 16), of four digits to the base 32 from -16 to 16: term t is digit t,
+// beside a power of two for each 32 channels (byte t of a scale word: that of term t).
+// The matrix instruction drops bits of a product that lie more than about 14 below the
+// largest one it adds up: whole numbers times 4-bit codes have none there, the terms of a
+// floating-point split (fp8) do (scores off by up to 2^-16 of sum |q k|, now 2^-22).
 template <typename TT, int D> struct CodedQuery {
-    static constexpr int kTerms = TT::kTerms, kParts = CodedKeys<D>::kParts;
-    i32x8 q[kParts][kTerms];
+    static constexpr int kTerms = 4, kParts = CodedKeys<D>::kParts;
+    static constexpr int kGroups = D / 32, kGroupBytes = 24, kRowBytes = kGroups * kGroupBytes;
+    typedef int i32x6 __attribute__((ext_vector_type(6)));
+    i32x6 q[kParts][kTerms];
     uint32_t scale[kParts];
 
-    static constexpr int bytes(int rows) { return rows * (kTerms * D + D / 8); }
+    static constexpr int bytes(int rows) { return rows * (kTerms * kRowBytes + 4 * kGroups); }
     // THREADS threads stage rows r < n by row(r) (their channels; zeros up to ROWS) in
-    // lds: [term][row][D] and then the scale words [row][D / 32]. First the loads,
+    // lds: [term][row][kRowBytes] and then the scale words [row][kGroups]. First the loads,
     // then, after what the caller has put between, the rounding.
     template <int THREADS, int ROWS> struct Stage {
         static constexpr int kLanes = D / 4, kAtOnce = THREADS / kLanes;  // a thread: 4 channels
@@ -181,83 +186,90 @@ template <typename TT, int D> struct CodedQuery {
         }
         __device__ __forceinline__ void store(int tid, int n, uint8_t *lds, uint32_t flip) const
         {
-            const int c = tid % kLanes;
-            uint32_t *scales = (uint32_t *)(lds + ROWS * kTerms * D);
+            const int c = tid % kLanes, at = c % 4;  // four threads: the 12 bytes of 16 channels
+            uint32_t *scales = (uint32_t *)(lds + ROWS * kTerms * kRowBytes);
 #pragma unroll
             for (int j = 0; j < kTurns; ++j) {
                 const int r = tid / kLanes + j * kAtOnce;
+                const bool mine = r < ROWS && tid < kAtOnce * kLanes;
+                uint8_t *put = lds + r * kRowBytes + 12 * (c / 4) + 4 * at;
                 if (j * kAtOnce >= n) {  // no rows in this turn: zeros
-                    if (r >= ROWS || tid >= kAtOnce * kLanes) continue;
 #pragma unroll
-                    for (int t = 0; t < kTerms; ++t) *(int *)(lds + (t * ROWS + r) * D + 4 * c) = 0;
-                    if (c % 8 == 0) scales[r * (D / 32) + c / 8] = 0x7f7f7fu;
+                    for (int t = 0; t < kTerms; ++t)
+                        if (mine && at < 3) *(uint32_t *)(put + t * ROWS * kRowBytes) = 0;
+                    if (mine && c % 8 == 0) scales[r * kGroups + c / 8] = 0x7f7f7f7fu;
                     continue;
                 }
                 const u32x2 y = w[j] ^ flip;
                 float x[4] = {TT::lo(y[0]), TT::hi(y[0]), TT::lo(y[1]), TT::hi(y[1])};
-                float amax = 0.f;
+                uint32_t top = 0;  // bits of the largest magnitude; of infinities and NaN: larger still
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (!(fabsf(x[i]) <= 3.402823466e38f)) x[i] = __builtin_nanf("");  // infinities too: fp8 has none
-                    amax = fmaxf(amax, fabsf(x[i]));
-                }
+                for (int i = 0; i < 4; ++i) top = max(top, __float_as_uint(fabsf(x[i])));
 #pragma unroll
-                for (int d = 1; d < 8; d <<= 1) amax = fmaxf(amax, __shfl_xor(amax, d));
-                if (r >= ROWS || tid >= kAtOnce * kLanes) continue;
-                // largest magnitude in [128, 256): fp8 numbers reach 448
-                const int e = max((int)(__float_as_uint(amax) >> 23) - 7, 4 * (kTerms - 1));
+                for (int d = 1; d < 8; d <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
+                const int e = max((int)(top >> 23), 15);  // 255 makes the group's products NaN
 #pragma unroll
-                for (int i = 0; i < 4; ++i) x[i] = __builtin_amdgcn_ldexpf(x[i], 127 - e);
+                for (int i = 0; i < 4; ++i) x[i] = e == 255 ? 0.f : __builtin_amdgcn_ldexpf(x[i], 130 - e);  // below 16
 #pragma unroll
                 for (int t = 0; t < kTerms; ++t) {
-                    int b = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
-                    b = __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], b, true);
-                    *(int *)(lds + (t * ROWS + r) * D + 4 * c) = b;
-                    x[0] = (x[0] - __builtin_amdgcn_cvt_f32_fp8(b, 0)) * 16.f;
-                    x[1] = (x[1] - __builtin_amdgcn_cvt_f32_fp8(b, 1)) * 16.f;
-                    x[2] = (x[2] - __builtin_amdgcn_cvt_f32_fp8(b, 2)) * 16.f;
-                    x[3] = (x[3] - __builtin_amdgcn_cvt_f32_fp8(b, 3)) * 16.f;
+                    uint32_t four = 0;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float whole = rintf(x[i]);  // 0 ... 16 are the 6-bit numbers 0 ... 2 in eighths
+                        four |= ((uint32_t)fabsf(whole) | (__float_as_uint(x[i]) >> 31) << 5) << 6 * i;
+                        x[i] = (x[i] - whole) * 32.f;
+                    }
+                    const uint32_t next = (uint32_t)__shfl_down((int)four, 1);
+                    if (mine && at < 3)
+                        *(uint32_t *)(put + t * ROWS * kRowBytes) = four >> 8 * at | next << (24 - 8 * at);
                 }
-                if (c % 8 == 0)
-                    scales[r * (D / 32) + c / 8] =
-                        (uint32_t)e | (uint32_t)(e - 4) << 8 | (uint32_t)(kTerms > 2 ? e - 8 : 0) << 16;
+                if (mine && c % 8 == 0)
+                    scales[r * kGroups + c / 8] =
+                        (uint32_t)e | (uint32_t)(e - 5) << 8 | (uint32_t)(e - 10) << 16 | (uint32_t)(e - 15) << 24;
             }
         }
     };
-    // The operands of row r for lane (its column, h): bytes 16 h ... and 64 + 16 h ... of a part.
+    // The operands of row r for lane (its column, h): group 4 p + h of a part.
     __device__ __forceinline__ void load(const uint8_t *lds, int rows, int r, int h)
     {
-        const uint32_t *scales = (const uint32_t *)(lds + rows * kTerms * D);
+        const uint32_t *scales = (const uint32_t *)(lds + rows * kTerms * kRowBytes);
 #pragma unroll
         for (int p = 0; p < kParts; ++p) {
+            const int g = 4 * p + h;
 #pragma unroll
-            for (int t = 0; t < kTerms; ++t)
+            for (int t = 0; t < kTerms; ++t) {
+                const u32x2 *from = (const u32x2 *)(lds + (t * rows + r) * kRowBytes + kGroupBytes * g);
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const int c = 128 * p + 64 * half + 16 * h;
-                    u32x4 x = {0, 0, 0, 0};
-                    if (c < D) x = *(const u32x4 *)(lds + (t * rows + r) * D + c);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) q[p][t][4 * half + i] = (int)x[i];
+                for (int i = 0; i < 3; ++i) {
+                    u32x2 x = {0, 0};
+                    if (g < kGroups) x = from[i];
+                    q[p][t][2 * i] = (int)x[0];
+                    q[p][t][2 * i + 1] = (int)x[1];
                 }
-            scale[p] = 4 * p + h < D / 32 ? scales[r * (D / 32) + 4 * p + h] : 0x7f7f7fu;
+            }
+            scale[p] = g < kGroups ? scales[r * kGroups + g] : 0x7f7f7f7fu;
         }
     }
     template <int T> __device__ __forceinline__ f32x4 term(const CodedKeys<D> &k, int p, f32x4 acc) const
     {
         const i32x8 a = {(int)k.k[p][0], (int)k.k[p][1], (int)k.k[p][2], (int)k.k[p][3], 0, 0, 0, 0};
-        return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q[p][T], acc, 4, 0, 0, (int)k.ks[p], T, (int)scale[p]);
+        const i32x6 y = q[p][T];
+        const i32x8 b = {y[0], y[1], y[2], y[3], y[4], y[5], 0, 0};
+        return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc, 4, 2, 0, (int)k.ks[p], T, (int)scale[p]);
     }
-    // q.k of 16 keys (rows) and the columns' query rows
+    // q.k of 16 keys (rows) and the columns' query rows, the smallest terms first
     __device__ __forceinline__ f32x4 scores(const CodedKeys<D> &k) const
     {
         f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+        acc = add<3>(k, acc);
+        acc = add<2>(k, acc);
+        acc = add<1>(k, acc);
+        return add<0>(k, acc);
+    }
+    template <int T> __device__ __forceinline__ f32x4 add(const CodedKeys<D> &k, f32x4 acc) const
+    {
 #pragma unroll
-        for (int p = 0; p < kParts; ++p) {
-            if constexpr (kTerms > 2) acc = term<2>(k, p, acc);
-            acc = term<1>(k, p, acc);
-            acc = term<0>(k, p, acc);
-        }
+        for (int p = 0; p < kParts; ++p) acc = term<T>(k, p, acc);
         return acc;
     }
 };

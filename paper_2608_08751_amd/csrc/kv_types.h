@@ -33,7 +33,6 @@ struct KvF16 {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
     }
     static constexpr int kMinExp = -13, kMaxExp = 13;
-    static constexpr int kTerms = 3;  // fp8 numbers (4 significant bits) that a number is the sum of
 };
 
 struct KvBf16 {
@@ -55,7 +54,6 @@ struct KvBf16 {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
     }
     static constexpr int kMinExp = -125, kMaxExp = 125;
-    static constexpr int kTerms = 2;
 };
 
 // 2^(e - 127) of a scale byte (255 gives an infinity, which decodes to NaN)

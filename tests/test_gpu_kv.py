@@ -548,3 +548,103 @@ def test_other_stream_and_graph_replay(ctx):
         assert (blocks.cpu().numpy() == want_b).all()
         want, want_lse = M.attend(as_np(fresh), keys, values, 2, request, position, table, 16, 0.1, want_b)
         check_attend(out, lse, want, want_lse, "bf16", np.nanmax(np.abs(values)), 30.0)
+
+
+# ---- precision and the forms that larger batches take ------------------------------
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dim,new", [(64, 1), (128, 1), (256, 1), (128, 70)])
+def test_scores_of_channels_far_apart(ctx, kind, dim, new):
+    # One key a row, so that the log-sum-exp is its score. In each group of 32 one channel of the
+    # query is large, the others 2^-7 ... 2^-13 of it. A score may be off by a query rounding of 2^-19 of the largest
+    # channel of a group for each of the group's channels, and by fp32 sums: 2^-20 of sum |q k|.
+    import paper_2608_08751_amd as ivf
+
+    B, rng = 64 if new == 1 else 1, np.random.default_rng(dim)
+    cache, table, keys, _ = make(ctx, kind, [1] * B, 2, dim, 16, 70)
+    start, request = np.arange(B + 1) * new, np.repeat(np.arange(B), new)
+    T = B * new
+    x = rng.standard_normal((T, 6, dim)) * np.exp2(-rng.integers(7, 14, (T, 6, dim)).astype(float))
+    x[..., rng.integers(0, 32, dim // 32) + np.arange(0, dim, 32)] = rng.standard_normal((T, 6, dim // 32)) + 2
+    q = dev(x.astype(np.float32), dtype_of(kind))
+    _, lse = ivf.ivf_kv_attend(ctx, cache, q, ints(start), ints(request), ints(np.zeros(T)), ints(table), 1.0, new)
+    qn = as_np(q).reshape(T, 2, 3, dim)
+    k = np.stack([keys[table[b, 0], :, 0] for b in request])[:, :, None]
+    want = (qn * k).sum(-1)
+    grouped = lambda a: np.abs(a).reshape(*a.shape[:-1], -1, 32)  # noqa: E731
+    allowed = (2.0**-19 * (grouped(qn).max(-1) * grouped(k).sum(-1)).sum(-1) + 2.0**-20 * np.abs(qn * k).sum(-1)
+               + 2.0**-21 * (1 + np.abs(want)))
+    assert (np.abs(as_np(lse).reshape(T, 2, 3) - want) <= allowed).all()
+
+
+@pytest.mark.parametrize("count", [0, 4])
+@pytest.mark.parametrize("new", [2, 70])
+def test_attend_queries_that_are_not_finite(ctx, count, new):
+    # their rows are NaN where they see a key, empty where they see none; no other row changes
+    import paper_2608_08751_amd as ivf
+
+    cache, table, keys, values = make(ctx, "bf16", [100], 2, 64, 16, 71)
+    start, request, position = batch([100], [new])
+    position[1] = -1
+    q = queries(new, 4, 64, "bf16", 5)
+    q[0, 1, 3], q[0, 2, 40], q[1, :, 0] = float("nan"), float("inf"), float("nan")
+    blocks = np.tile(np.arange(count, dtype=np.int32), (new, 2, 1)) if count else None
+    out, lse = ivf.ivf_kv_attend(ctx, cache, q, ints(start), ints(request), ints(position), ints(table), 0.125, new,
+                                 blocks=None if blocks is None else ints(blocks))
+    clean = as_np(q)
+    bad = ~np.isfinite(clean).all(-1)
+    want, want_lse = M.attend(np.where(bad[..., None], 0.0, clean), keys, values, 2, request, position, table, 16, 0.125,
+                              blocks)
+    bad[position < 0] = False
+    want[bad], want_lse[bad] = np.nan, np.nan
+    check_attend(out, lse, want, want_lse, "bf16", np.nanmax(np.abs(values)), 30.0)
+
+
+# tokens with blocks of their own: four waves a unit, one wave a unit, rows beyond 8, wide channels
+@pytest.mark.parametrize("kind,heads,group,dim,bs,new,count", [
+    ("bf16", 8, 2, 64, 16, 100, 4), ("f16", 8, 12, 128, 32, 90, 3), ("bf16", 8, 2, 128, 16, 400, 5),
+    ("f16", 8, 12, 64, 16, 390, 4), ("bf16", 8, 1, 96, 64, 400, 2), ("f16", 8, 3, 192, 16, 130, 3),
+    ("bf16", 8, 9, 256, 16, 130, 3)])
+def test_many_tokens_with_selected_blocks(ctx, kind, heads, group, dim, bs, new, count):
+    run_attend(ctx, kind, [new + 300, 40], [new, 3], heads, group, dim, bs, seed=80, count=count)
+
+
+# many requests: a unit for every wave, more units than are shared out, each beside a long table
+@pytest.mark.parametrize("kind,B,heads,group,dim,longest", [
+    ("bf16", 150, 2, 4, 128, 60), ("f16", 1040, 1, 1, 64, 1100), ("bf16", 520, 8, 2, 64, 1100),
+    ("f16", 140, 2, 11, 96, 1300), ("bf16", 130, 3, 2, 256, 1200)])
+def test_many_requests(ctx, kind, B, heads, group, dim, longest):
+    lens = np.random.default_rng(B).integers(1, 40, B)
+    lens[B // 2] = longest
+    run_attend(ctx, kind, lens.tolist(), [1] * B, heads, group, dim, 16, seed=81)
+
+
+@pytest.mark.parametrize("kind,lens,new,heads,group,dim,bs", [
+    ("bf16", [5000], [100], 1, 2, 128, 64),  # few rows, long: the keys are split
+    ("f16", [260, 9, 300, 1, 1, 400], [200, 1, 3, 1, 1, 90], 2, 4, 64, 16),  # small requests between prompts
+    ("bf16", [150, 3, 200], [150, 3, 200], 2, 3, 192, 32),
+    ("f16", [140, 2, 1, 180], [140, 2, 1, 180], 1, 5, 256, 16),
+])
+def test_prompts_beside_small_requests(ctx, kind, lens, new, heads, group, dim, bs):
+    run_attend(ctx, kind, lens, new, heads, group, dim, bs, seed=82)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dim", [64, 96, 128, 192, 256])
+def test_append_read_of_many_tokens(ctx, kind, dim):
+    # scattered slots, some outside the cache
+    import paper_2608_08751_amd as ivf
+
+    T, heads, bs, blocks = 2500, 2, 32, 90
+    rng = np.random.default_rng(dim)
+    slots = rng.permutation(blocks * bs)[:T]
+    slots[::97] = -1
+    x = rng.standard_normal((T, 2, heads, dim)) * np.exp2(rng.integers(-6, 7, (T, 2, heads, 1)).astype(float))
+    kv = dev(x.astype(np.float32), dtype_of(kind))
+    kv[7, 0, 0, 5], kv[9, 1, 1, dim - 1] = float("nan"), float("inf")
+    cache = ivf.KVCache.empty(blocks, heads, dim, bs, dtype_of(kind))
+    ivf.ivf_kv_append(ctx, cache, kv[:, 0], kv[:, 1], dev(slots.astype(np.int64)))
+    k, v, _ = ivf.ivf_kv_read(ctx, cache, dev(slots.astype(np.int64)))
+    wk, wv = M.store(as_np(kv[:, 0]), as_np(kv[:, 1]), kind)
+    wk[slots < 0], wv[slots < 0] = np.nan, np.nan
+    assert np.array_equal(as_np(k), wk, equal_nan=True) and np.array_equal(as_np(v), wv, equal_nan=True)
