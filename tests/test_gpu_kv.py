@@ -648,3 +648,20 @@ def test_append_read_of_many_tokens(ctx, kind, dim):
     wk, wv = M.store(as_np(kv[:, 0]), as_np(kv[:, 1]), kind)
     wk[slots < 0], wv[slots < 0] = np.nan, np.nan
     assert np.array_equal(as_np(k), wk, equal_nan=True) and np.array_equal(as_np(v), wv, equal_nan=True)
+
+
+@pytest.mark.parametrize("dtype", KINDS)
+def test_example_runs_and_agrees_with_fp64(ctx, dtype):
+    # relative to the largest output: (u / 2) (1 + vmax / outmax), with vmax / outmax below 12 here
+    import importlib.util
+    import os
+
+    path = os.path.join(os.path.dirname(__file__), "..", "examples", "paged_decode.py")
+    spec = importlib.util.spec_from_file_location("paged_decode", path)
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    _, _, error, in_use = module.run(requests=5, prompt=200, steps=20, heads=2, group=3, dim=64, block_size=16, count=6,
+                                     dtype=dtype_of(dtype))
+    assert error <= 13 * {"bf16": 2.0**-9, "f16": 2.0**-12}[dtype]
+    lengths = [int(100 + 25 * i) for i in range(5)]
+    assert in_use == sum(-(-(n + 21) // 16) for n in lengths)
