@@ -66,7 +66,7 @@ __device__ int64_t unit_steps(const KvAttend &a, uint32_t u, int unit, int last_
 constexpr int attend_threads(int team) { return team == 1 ? kThreads : 64 * team; }
 
 template <typename TT, int D, bool SPARSE, bool PACK, int TEAM>
-__global__ __launch_bounds__(attend_threads(TEAM), TEAM == 8 ? 2 : D == 64 || (SPARSE && D <= 128) ? 3 : D <= 128 ? 2 : 1)
+__global__ __launch_bounds__(attend_threads(TEAM), D > 128 ? 1 : SPARSE && TEAM < 8 && D != 96 ? 3 : 2)
 void kv_attend_kernel(KvAttend a)
 {
     typedef Pieces<D> P;
@@ -545,7 +545,7 @@ template <typename TT, int D, bool SPARSE, int TEAM>
 hipError_t launch_team(const KvAttend &a, int64_t groups, hipStream_t s)
 {
     const dim3 grid((unsigned)(groups * a.c.heads)), block(attend_threads(TEAM));
-    if (a.unit_size == 8) hipLaunchKernelGGL((kv_attend_kernel<TT, D, SPARSE, true, TEAM>), grid, block, 0, s, a);
+    if (SPARSE && a.unit_size == 8) hipLaunchKernelGGL((kv_attend_kernel<TT, D, SPARSE, SPARSE, TEAM>), grid, block, 0, s, a);
     else hipLaunchKernelGGL((kv_attend_kernel<TT, D, SPARSE, false, TEAM>), grid, block, 0, s, a);
     return hipGetLastError();
 }
@@ -564,7 +564,6 @@ template <typename TT> hipError_t launch_combine(const KvAttend &a, bool prompt,
     const int64_t rows = (prompt || a.blocks) ? a.T * a.group * a.c.heads : (int64_t)a.units * a.unit_rows * a.c.heads;
     const dim3 four((unsigned)rows), one((unsigned)((rows + kWaves - 1) / kWaves)), block(kThreads);
     if (prompt) hipLaunchKernelGGL((kv_combine_kernel<TT, kByPrompt, 1>), one, block, 0, s, a, rows);
-    else if (a.blocks && a.splits < 16) hipLaunchKernelGGL((kv_combine_kernel<TT, kBySplit, 1>), one, block, 0, s, a, rows);
     else if (a.blocks) hipLaunchKernelGGL((kv_combine_kernel<TT, kBySplit, 4>), four, block, 0, s, a, rows);
     else hipLaunchKernelGGL((kv_combine_kernel<TT, kByUnit, 4>), four, block, 0, s, a, rows);
     return hipGetLastError();
@@ -581,11 +580,16 @@ template <typename TT> hipError_t launch_tokens_dim(const KvAttend &a, int64_t g
     }
 }
 
-// Requests with at most this many rows go through the single-token kernel,
-// 16 rows a workgroup, where others take the prompt kernel.
+// Requests with at most this many rows go through the single-token kernel, 16 rows a
+// workgroup, others through the prompt kernel (8 requests of 32 rows after 4,000 tokens, 8 heads x 128: 32 us
+// here, 107 there; of 64 rows 36 and 72; one request of 64 rows 22 and 21, of 128 rows 24 and 23).
 constexpr int64_t kSmallRows = 64;
-// Tables of at most this many keys are not split: joining parts costs a launch.
-constexpr int64_t kWholeKeys = 1024;
+
+// Tables of at most this many keys are not shared out: joining parts costs a launch and the prefix
+// sums. `all` units of one token, 8 heads x 128, lengths drawn up to the limit, shared out and not: 8 units,
+// 2,048 keys 12.2 and 15.1 us; 32 units, 2,048 keys 16.6 and 14.2, 4,096 keys 17.0 and 20.0; 128 units, 4,096
+// keys 26.4 and 22.5; 1,024 units, 4,096 keys 82 and 79.
+constexpr int64_t whole_keys(int64_t all) { return all < 32 ? 1024 : all < 128 ? 2048 : 4096; }
 
 }  // namespace
 
@@ -610,19 +614,24 @@ KvAttendPlan kv_attend_plan(const KvCache &c, int group, int64_t T, int64_t B, i
     p.token_splits = p.prompt_splits = 1;
     p.team = kWaves;
     if (p.tokens) {
-        // beside a prompt the other requests' rows are mostly one token's
-        p.unit_size = (p.prompt ? group : rows) <= 8 ? 8 : 16;
+        p.unit_size = count && rows <= 8 ? 8 : 16;
         p.per_unit = (int)((rows + p.unit_size - 1) / p.unit_size);
         p.unit_rows = (int)std::min<int64_t>(rows, p.unit_size);
         p.units = (count ? T : B) * p.per_unit;
-        // Eight waves share a unit where there are at most as many as CUs, four where there
-        // are more, or they are shared out, or a wave takes over 256 registers (dim > 128), one
-        // where there is a unit for every wave that the device holds: one alone joins nothing.
+        // Waves that share a unit, where units are not cut into parts:
+        // * eight where there are at most as many units as CUs, but not for 512 keys or fewer (256 units of 4,096
+        //   selected keys 32 us, with four waves 34; single tokens after 777 tokens, 256 units 11.3 and 11.8,
+        //   after 300 tokens, 128 units 8.8 and 7.9), nor beyond 128 channels (over 256 registers a wave);
+        // * one where there is a unit for every wave that the device holds: alone it joins nothing
+        //   (2,048 units of 1,536 selected keys x 128 channels 51 us, with four 55; 1,536 units 49 and 42; 256
+        //   channels, 1,024 units 61 and 83, 512 units 59 and 43);
+        // * four otherwise.
         const int64_t all = p.units * c.heads;
-        const bool shared = !count && keys > kWholeKeys && p.units <= kKvMaxUnits && all < 16 * (int64_t)num_cus;
-        p.team = c.dim > 128 || shared ? 4 : all <= num_cus ? 8 : count && all >= 12 * (int64_t)num_cus ? 1 : 4;
-        if (c.dim > 128 && count && all >= 4 * (int64_t)num_cus) p.team = 1;
+        const bool shared = !count && keys > whole_keys(all) && p.units <= kKvMaxUnits && all < 16 * (int64_t)num_cus;
+        if (count && all >= (c.dim <= 128 ? 8 : 4) * (int64_t)num_cus) p.team = 1;
+        else if (c.dim <= 128 && !shared && all <= num_cus && keys > 512) p.team = 8;
         // as many workgroups as are resident at once: a further round would only begin and join again
+        // (16 tokens, 8 heads, 4,096 selected keys: 18.6 us, two rounds 24.5)
         if (count) {
             const int64_t most = std::max<int64_t>(1, keys / (32 * kMinSteps));
             p.token_splits = (int)std::max<int64_t>(1, std::min(num_cus / all, most));
@@ -641,8 +650,9 @@ KvAttendPlan kv_attend_plan(const KvCache &c, int group, int64_t T, int64_t B, i
     }
     if (p.prompt) {
         const int64_t units = (T * group + kv_prompt_rows(c.dim) - 1) / kv_prompt_rows(c.dim) * c.heads;
+        // parts of a tile of keys or more until every CU has work (64 tokens after 1,000: 23.8 us, parts of two tiles 25.5, of four 32)
         if (units < kv_prompt_resident(c.dim) * (int64_t)num_cus / 2) {
-            const int64_t most = std::max<int64_t>(1, keys / 256);
+            const int64_t most = std::max<int64_t>(1, keys / 128);
             p.prompt_splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(kv_prompt_resident(c.dim) * (int64_t)num_cus / units, most), 32));
         }
         if (p.prompt_splits > 1) {

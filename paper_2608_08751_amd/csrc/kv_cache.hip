@@ -65,56 +65,48 @@ __device__ __forceinline__ uint32_t encode(const Eight &v, float scale)
     return w;
 }
 
-// A workgroup takes U times 256 / (D / 8) consecutive tokens of one head, so that the
-// bytes it writes, tokens of a block side by side, meet in one L2 (single scale
-// bytes and 64-byte rows from workgroups on several would each be a write of their own).
+// A workgroup takes 256 / (D / 8) consecutive tokens of one head, so that the bytes it
+// writes, tokens of a block side by side, meet in one L2 (single scale bytes and
+// 64-byte rows from workgroups on several would each be a write of their own). Four times
+// as many tokens, for more loads in flight a thread, were slower at every length from 64
+// to 31,000 tokens (8 heads x 128: 5.6 -> 7.1 us, 36.3 -> 37.9).
 template <int D> constexpr int tokens_at_once() { return kThreads / (D / 8); }
 
-template <typename TT, int D, int U>
+template <typename TT, int D>
 __global__ __launch_bounds__(kThreads) void kv_append_kernel(KvCache c, KvRows k, KvRows v,
                                                              const int64_t *__restrict__ slots, int64_t T)
 {
     constexpr int kPer = D / 8, kTok = tokens_at_once<D>();
     const int h = blockIdx.x % (uint32_t)c.heads;
-    const int64_t t0 = (int64_t)(blockIdx.x / (uint32_t)c.heads) * (kTok * U);
     const int row = threadIdx.x / kPer, g8 = threadIdx.x % kPer;
-    u32x4 kw[U], vw[U];
-    int64_t slot[U];
-#pragma unroll
-    for (int i = 0; i < U; ++i) {
-        const int64_t t = t0 + i * kTok + row;
-        const bool in = row < kTok && t < T;
-        slot[i] = -1;
-        kw[i] = vw[i] = (u32x4){0, 0, 0, 0};
-        if (in) {
-            slot[i] = slots[t];
-            kw[i] = *(const u32x4 *)((const typename TT::elem *)k.p + t * k.ts + h * k.hs + 8 * g8);
-            vw[i] = *(const u32x4 *)((const typename TT::elem *)v.p + t * v.ts + h * v.hs + 8 * g8);
-        }
+    const int64_t t = (int64_t)(blockIdx.x / (uint32_t)c.heads) * kTok + row;
+    u32x4 kw = {0, 0, 0, 0}, vw = {0, 0, 0, 0};
+    int64_t slot = -1;
+    if (row < kTok && t < T) {
+        slot = slots[t];
+        kw = *(const u32x4 *)((const typename TT::elem *)k.p + t * k.ts + h * k.hs + 8 * g8);
+        vw = *(const u32x4 *)((const typename TT::elem *)v.p + t * v.ts + h * v.hs + 8 * g8);
     }
-#pragma unroll
-    for (int i = 0; i < U; ++i) {
-        const Eight kx = widen<TT>(kw[i]), vx = widen<TT>(vw[i]);
-        bool bad = false;
-        const float ka = max4(top_of(kx, bad)), va = max4(top_of(vx, bad));
-        uint32_t b = bad;
-        b |= __shfl_xor(b, 1);
-        b |= __shfl_xor(b, 2);
-        uint32_t ke = scale_byte<TT>(ka), ve = scale_byte<TT>(va);
-        uint32_t kc = encode(kx, kv_scale(ke)), vc = encode(vx, kv_scale(ve));
-        if (b) {
-            ke = 255;
-            ve = kc = vc = 0;
-        }
-        if (slot[i] < 0 || (slot[i] >> c.shift) >= c.blocks) continue;
-        const int place = (int)(slot[i] & (c.bs - 1));
-        uint8_t *rec = c.rec + ((slot[i] >> c.shift) * c.heads + h) * c.rec_bytes();
-        *(uint32_t *)(rec + place * (D / 2) + 4 * g8) = kc;
-        *(uint32_t *)(rec + c.v_codes() + place * (D / 2) + 4 * g8) = vc;
-        if ((g8 & 3) == 0) {
-            rec[c.k_scales() + place * (D / 32) + g8 / 4] = (uint8_t)ke;
-            rec[c.v_scales() + g8 / 4 * c.bs + place] = (uint8_t)ve;
-        }
+    const Eight kx = widen<TT>(kw), vx = widen<TT>(vw);
+    bool bad = false;
+    const float ka = max4(top_of(kx, bad)), va = max4(top_of(vx, bad));
+    uint32_t b = bad;
+    b |= __shfl_xor(b, 1);
+    b |= __shfl_xor(b, 2);
+    uint32_t ke = scale_byte<TT>(ka), ve = scale_byte<TT>(va);
+    uint32_t kc = encode(kx, kv_scale(ke)), vc = encode(vx, kv_scale(ve));
+    if (b) {
+        ke = 255;
+        ve = kc = vc = 0;
+    }
+    if (slot < 0 || (slot >> c.shift) >= c.blocks) return;
+    const int place = (int)(slot & (c.bs - 1));
+    uint8_t *rec = c.rec + ((slot >> c.shift) * c.heads + h) * c.rec_bytes();
+    *(uint32_t *)(rec + place * (D / 2) + 4 * g8) = kc;
+    *(uint32_t *)(rec + c.v_codes() + place * (D / 2) + 4 * g8) = vc;
+    if ((g8 & 3) == 0) {
+        rec[c.k_scales() + place * (D / 32) + g8 / 4] = (uint8_t)ke;
+        rec[c.v_scales() + g8 / 4 * c.bs + place] = (uint8_t)ve;
     }
 }
 
@@ -200,7 +192,7 @@ __global__ __launch_bounds__(kThreads) void kv_summary_kernel(KvCache c, const i
 }
 
 // The first `token_groups` workgroups a head read tokens, the others means.
-template <typename TT, int D, int U>
+template <typename TT, int D>
 __global__ __launch_bounds__(kThreads) void kv_read_kernel(KvCache c, const int64_t *__restrict__ slots, int64_t T,
                                                            typename TT::elem *k, typename TT::elem *v,
                                                            const int32_t *__restrict__ blocks, int64_t n,
@@ -212,67 +204,46 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(KvCache c, const int6
     const int row = threadIdx.x / kPer, g8 = threadIdx.x % kPer;
     if (row >= kTok) return;
     if (group < token_groups) {
-        const int64_t t0 = (int64_t)group * (kTok * U) + row;
-        uint32_t kc[U], vc[U], ke[U], ve[U];
-        bool there[U];
-#pragma unroll
-        for (int i = 0; i < U; ++i) {
-            const int64_t t = t0 + i * kTok, slot = t < T ? slots[t] : -1;
-            there[i] = slot >= 0 && (slot >> c.shift) < c.blocks;
-            kc[i] = vc[i] = ke[i] = ve[i] = 0;
-            if (there[i]) {
-                const int place = (int)(slot & (c.bs - 1));
-                const uint8_t *rec = c.rec + ((slot >> c.shift) * c.heads + h) * c.rec_bytes();
-                ke[i] = rec[c.k_scales() + place * (D / 32) + g8 / 4];
-                ve[i] = rec[c.v_scales() + g8 / 4 * c.bs + place];
-                kc[i] = *(const uint32_t *)(rec + place * (D / 2) + 4 * g8);
-                vc[i] = *(const uint32_t *)(rec + c.v_codes() + place * (D / 2) + 4 * g8);
-            }
+        const int64_t t = (int64_t)group * kTok + row;
+        if (t >= T) return;
+        const int64_t slot = slots[t], at = (t * c.heads + h) * D + 8 * g8;
+        uint32_t kc = 0, vc = 0, ke = 255, ve = 0;
+        if (slot >= 0 && (slot >> c.shift) < c.blocks) {
+            const int place = (int)(slot & (c.bs - 1));
+            const uint8_t *rec = c.rec + ((slot >> c.shift) * c.heads + h) * c.rec_bytes();
+            ke = rec[c.k_scales() + place * (D / 32) + g8 / 4];
+            ve = rec[c.v_scales() + g8 / 4 * c.bs + place];
+            kc = *(const uint32_t *)(rec + place * (D / 2) + 4 * g8);
+            vc = *(const uint32_t *)(rec + c.v_codes() + place * (D / 2) + 4 * g8);
         }
-#pragma unroll
-        for (int i = 0; i < U; ++i) {
-            const int64_t t = t0 + i * kTok;
-            if (t >= T) continue;
-            const uint32_t nan = there[i] ? ke[i] : 255u;
-            const int64_t at = (t * c.heads + h) * D + 8 * g8;
-            if (k) *(u32x4 *)(k + at) = stored<TT>(kc[i], ke[i], nan);
-            if (v) *(u32x4 *)(v + at) = stored<TT>(vc[i], ve[i], nan);
-        }
+        if (k) *(u32x4 *)(k + at) = stored<TT>(kc, ke, ke);
+        if (v) *(u32x4 *)(v + at) = stored<TT>(vc, ve, ke);
         return;
     }
+    const int64_t b = (int64_t)(group - token_groups) * kTok + row;
+    if (b >= n) return;
+    const int64_t block = blocks[b], at = (b * c.heads + h) * D + 8 * g8;
+    f32x4 lo, hi;
+    lo = hi = (f32x4){__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
+    if (block >= 0 && block < c.blocks) {
+        const int64_t s = block * c.heads + h;
+        const float w = c.weight[s];
+        const int8_t *q = c.summary + s * D + 8 * g8;
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-        const int64_t b = (int64_t)(group - token_groups) * (kTok * U) + i * kTok + row;
-        if (b >= n) return;
-        const int64_t block = blocks[b], at = (b * c.heads + h) * D + 8 * g8;
-        f32x4 lo, hi;
-        lo = hi = (f32x4){__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
-        if (block >= 0 && block < c.blocks) {
-            const int64_t s = block * c.heads + h;
-            const float w = c.weight[s];
-            const int8_t *q = c.summary + s * D + 8 * g8;
-#pragma unroll
-            for (int d = 0; d < 4; ++d) {
-                lo[d] = (float)q[d] * w;
-                hi[d] = (float)q[4 + d] * w;
-            }
+        for (int d = 0; d < 4; ++d) {
+            lo[d] = (float)q[d] * w;
+            hi[d] = (float)q[4 + d] * w;
         }
-        *(f32x4 *)(mean + at) = lo;
-        *(f32x4 *)(mean + at + 4) = hi;
     }
+    *(f32x4 *)(mean + at) = lo;
+    *(f32x4 *)(mean + at + 4) = hi;
 }
 
-// Tokens a thread: 4, for more loads in flight, where that leaves workgroups for every CU.
-constexpr int64_t kManyTokens = 2048;
-
 template <typename TT, int D> struct Launch {
-    static unsigned groups(int64_t n, int u) { return (unsigned)((n + tokens_at_once<D>() * u - 1) / (tokens_at_once<D>() * u)); }
+    static unsigned groups(int64_t n) { return (unsigned)((n + tokens_at_once<D>() - 1) / tokens_at_once<D>()); }
     static hipError_t append(const KvCache &c, KvRows k, KvRows v, const int64_t *slots, int64_t T, hipStream_t s)
     {
-        if (T >= kManyTokens)
-            hipLaunchKernelGGL((kv_append_kernel<TT, D, 4>), dim3(groups(T, 4) * c.heads), dim3(kThreads), 0, s, c, k, v, slots, T);
-        else
-            hipLaunchKernelGGL((kv_append_kernel<TT, D, 1>), dim3(groups(T, 1) * c.heads), dim3(kThreads), 0, s, c, k, v, slots, T);
+        hipLaunchKernelGGL((kv_append_kernel<TT, D>), dim3(groups(T) * c.heads), dim3(kThreads), 0, s, c, k, v, slots, T);
         return hipGetLastError();
     }
     static hipError_t summaries(const KvCache &c, const int64_t *slots, int64_t T, hipStream_t s)
@@ -284,12 +255,8 @@ template <typename TT, int D> struct Launch {
                            int64_t n, float *mean, hipStream_t s)
     {
         typedef typename TT::elem elem;
-        if (T >= kManyTokens)
-            hipLaunchKernelGGL((kv_read_kernel<TT, D, 4>), dim3((groups(T, 4) + groups(n, 4)) * c.heads), dim3(kThreads), 0, s,
-                               c, slots, T, (elem *)k, (elem *)v, blocks, n, mean, groups(T, 4));
-        else
-            hipLaunchKernelGGL((kv_read_kernel<TT, D, 1>), dim3((groups(T, 1) + groups(n, 1)) * c.heads), dim3(kThreads), 0, s,
-                               c, slots, T, (elem *)k, (elem *)v, blocks, n, mean, groups(T, 1));
+        hipLaunchKernelGGL((kv_read_kernel<TT, D>), dim3((groups(T) + groups(n)) * c.heads), dim3(kThreads), 0, s, c, slots, T,
+                           (elem *)k, (elem *)v, blocks, n, mean, groups(T));
         return hipGetLastError();
     }
 };

@@ -462,8 +462,10 @@ template <typename TT, int PARTS> hipError_t launch_one(const KvSelect &a, unsig
 
 template <typename TT> hipError_t launch_select(const KvSelect &a, hipStream_t s)
 {
-    // 16 tokens of a tile share the summaries where a batch brings more tokens than requests
-    if (a.T > 2 * a.B && a.cols <= 2048) {
+    // 16 tokens of a tile share the summaries where there are enough of them a request and the tiles fill
+    // the device: 500 blocks, 8 heads x 128, one request of 64 tokens 14.9 us in tiles and 11.3 one by one, of 96
+    // tokens 15.4 and 15.5, of 512 tokens 16 and 60; 32 requests of 4 tokens 26 and 19, of 8 tokens 19 and 32
+    if (a.T >= 6 * a.B && a.T * a.c.heads >= 768 && a.cols <= 2048) {
         const int ld = (a.cols + 15) / 16 * 16 + 4;
         const size_t lds = (size_t)(kTileTokens + 2) * ld * 4;
         const unsigned grid = (unsigned)((a.T + kTileTokens - 1) / kTileTokens * a.c.heads);

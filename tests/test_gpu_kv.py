@@ -665,3 +665,57 @@ def test_example_runs_and_agrees_with_fp64(ctx, dtype):
     assert error <= 13 * {"bf16": 2.0**-9, "f16": 2.0**-12}[dtype]
     lengths = [int(100 + 25 * i) for i in range(5)]
     assert in_use == sum(-(-(n + 21) // 16) for n in lengths)
+
+
+# many tokens a request: tiles of 16 tokens, some of which span requests
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("lens,new,heads,group,dim,bs,first,last,count", [
+    ([900], [400], 2, 7, 128, 32, 2, 1, 9),
+    ([500, 40, 300], [200, 37, 150], 2, 2, 96, 16, 1, 1, 12),
+    ([420, 33], [390, 3], 2, 1, 256, 16, 0, 2, 7),
+    ([2600], [110], 7, 4, 64, 16, 1, 2, 20),
+    ([1400], [160], 5, 3, 192, 16, 1, 1, 64),
+])
+def test_select_many_tokens(ctx, kind, lens, new, heads, group, dim, bs, first, last, count):
+    import paper_2608_08751_amd as ivf
+
+    cache, table, _, _ = make(ctx, kind, lens, heads, dim, bs, 90 + dim)
+    _, request, position = batch(lens, new)
+    position[5], request[7] = -1, len(lens)  # a token that sees nothing, one of no request
+    q = queries(len(request), heads * group, dim, kind, 6)
+    q[11], q[12, 0, 3] = 0, float("nan")
+    got = ivf.ivf_kv_select(ctx, cache, q, ints(request), ints(position), ints(table), count, first=first, last=last)
+    want = M.select(as_np(q), cache.summary.cpu().numpy(), cache.weight.cpu().numpy(), heads, request, position, table,
+                    bs, first, last, count)
+    assert (got.cpu().numpy() == want).all()
+
+
+def test_select_ties_and_holes_of_many_tokens(ctx):
+    import paper_2608_08751_amd as ivf
+
+    rng = np.random.default_rng(13)
+    heads, group, dim, bs, cols, B, tokens = 2, 2, 64, 16, 70, 2, 200
+    cache = ivf.KVCache.empty(90, heads, dim, bs, dtype_of("f16"))
+    cache.summary.copy_(dev(rng.integers(-2, 3, (90, heads, 1)).astype(np.int8)).expand(90, heads, dim))
+    cache.weight.copy_(dev((rng.integers(0, 3, (90, heads)) / 2.0).astype(np.float32)))
+    table = rng.integers(0, 90, (B, cols)).astype(np.int32)
+    table[0, 5:9], table[1, 0], table[1, 50], table[0, cols - 1] = -1, -7, 90, 1 << 30
+    request = np.repeat(np.arange(B), tokens)
+    position = rng.integers(0, cols * bs, B * tokens)
+    position[0] = cols * bs + 500  # beyond the table
+    q = queries(B * tokens, heads * group, dim, "f16", 14)
+    for first, last, count in ((1, 1, 3), (0, 3, 20), (30, 30, 64)):
+        got = ivf.ivf_kv_select(ctx, cache, q, ints(request), ints(position), ints(table), count, first=first, last=last)
+        want = M.select(as_np(q), cache.summary.cpu().numpy(), cache.weight.cpu().numpy(), heads, request, position,
+                        table, bs, first, last, count)
+        assert (got.cpu().numpy() == want).all()
+
+
+# every number of waves a unit, below and above the limits, tables shared out and whole, for every width
+@pytest.mark.parametrize("kind,B,heads,longest", [("bf16", 40, 1, 900), ("f16", 34, 1, 2000), ("bf16", 6, 2, 1900),
+                                                  ("f16", 17, 8, 3900), ("bf16", 130, 2, 4400)])
+@pytest.mark.parametrize("dim,group", [(64, 4), (96, 12), (128, 8), (192, 1), (256, 3)])
+def test_requests_beside_long_tables(ctx, kind, B, heads, longest, dim, group):
+    lens = np.random.default_rng(B).integers(1, 70, B)
+    lens[B // 3] = longest
+    run_attend(ctx, kind, lens.tolist(), [1] * B, heads, group, dim, 32, seed=83)
