@@ -180,7 +180,6 @@ ivf_status ivf_kv_append(ivf_ctx *ctx, const ivf_kv_cache *cache, const void *k,
         if (!g.ok) return fail(ctx, IVF_EDEVICE, "no usable device (context device %d)", ctx->device);
         TIMED("kv_append", launch_kv_append(c, {k, k_token_stride, k_head_stride}, {v, v_token_stride, v_head_stride},
                                             slots, T, ctx->stream));
-        TIMED("kv_summaries", launch_kv_summaries(c, slots, T, ctx->stream));
         ctx->last_stats = nullptr;
         return IVF_OK;
     });

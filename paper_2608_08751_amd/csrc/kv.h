@@ -41,7 +41,6 @@ hipError_t launch_kv_plan(const int32_t *cached, const int32_t *added, int B, in
                           int32_t *request, int32_t *position, int64_t *info, int num_cus, hipStream_t s);
 
 hipError_t launch_kv_append(const KvCache &c, KvRows k, KvRows v, const int64_t *slots, int64_t T, hipStream_t s);
-hipError_t launch_kv_summaries(const KvCache &c, const int64_t *slots, int64_t T, hipStream_t s);
 hipError_t launch_kv_read(const KvCache &c, const int64_t *slots, int64_t T, void *k, void *v, const int32_t *blocks,
                           int64_t n, float *mean, hipStream_t s);
 

@@ -8,7 +8,7 @@
 // to move, 4 bytes read and 17 / 16 written per channel of key and value together,
 // bounds a prompt: 29,000 tokens of 8 heads x 128 f16 (120 MB in, 32 MB out) 28 us,
 // 5.4 TB/s, reading them back 24 us, 6.2 TB/s, their summaries (fp64 sums, from L2)
-// 11 us. A single token is one launch, 3 us.
+// 11 us. A call of few tokens is one launch, 3 us.
 #include "kv.h"
 #include "kv_types.h"
 
@@ -74,14 +74,31 @@ __device__ __forceinline__ uint32_t encode(const Eight &v, float scale)
 // to 31,000 tokens (8 heads x 128: 5.6 -> 7.1 us, 36.3 -> 37.9).
 template <int D> constexpr int tokens_at_once() { return kThreads / (D / 8); }
 
+// The codes and scale bytes of 8 channels of a token's key and value; four lanes that share a
+// scale call it together.
+struct Coded {
+    uint32_t kc, vc, ke, ve;
+};
+template <typename TT> __device__ __forceinline__ Coded code_token(u32x4 kw, u32x4 vw)
+{
+    const Eight kx = widen<TT>(kw), vx = widen<TT>(vw);
+    bool bad = false;
+    const float ka = max4(top_of(kx, bad)), va = max4(top_of(vx, bad));
+    uint32_t b = bad;
+    b |= __shfl_xor(b, 1);
+    b |= __shfl_xor(b, 2);
+    const uint32_t ke = scale_byte<TT>(ka), ve = scale_byte<TT>(va);
+    if (b) return {0, 0, 255, 0};
+    return {encode(kx, kv_scale(ke)), encode(vx, kv_scale(ve)), ke, ve};
+}
+
 template <typename TT, int D>
-__global__ __launch_bounds__(kThreads) void kv_append_kernel(KvCache c, KvRows k, KvRows v,
-                                                             const int64_t *__restrict__ slots, int64_t T)
+__device__ __forceinline__ void append_tokens(const KvCache &c, const KvRows &k, const KvRows &v,
+                                              const int64_t *__restrict__ slots, int64_t T, uint32_t group, int h)
 {
     constexpr int kPer = D / 8, kTok = tokens_at_once<D>();
-    const int h = blockIdx.x % (uint32_t)c.heads;
     const int row = threadIdx.x / kPer, g8 = threadIdx.x % kPer;
-    const int64_t t = (int64_t)(blockIdx.x / (uint32_t)c.heads) * kTok + row;
+    const int64_t t = (int64_t)group * kTok + row;
     u32x4 kw = {0, 0, 0, 0}, vw = {0, 0, 0, 0};
     int64_t slot = -1;
     if (row < kTok && t < T) {
@@ -89,27 +106,23 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(KvCache c, KvRows k
         kw = *(const u32x4 *)((const typename TT::elem *)k.p + t * k.ts + h * k.hs + 8 * g8);
         vw = *(const u32x4 *)((const typename TT::elem *)v.p + t * v.ts + h * v.hs + 8 * g8);
     }
-    const Eight kx = widen<TT>(kw), vx = widen<TT>(vw);
-    bool bad = false;
-    const float ka = max4(top_of(kx, bad)), va = max4(top_of(vx, bad));
-    uint32_t b = bad;
-    b |= __shfl_xor(b, 1);
-    b |= __shfl_xor(b, 2);
-    uint32_t ke = scale_byte<TT>(ka), ve = scale_byte<TT>(va);
-    uint32_t kc = encode(kx, kv_scale(ke)), vc = encode(vx, kv_scale(ve));
-    if (b) {
-        ke = 255;
-        ve = kc = vc = 0;
-    }
+    const Coded x = code_token<TT>(kw, vw);
     if (slot < 0 || (slot >> c.shift) >= c.blocks) return;
     const int place = (int)(slot & (c.bs - 1));
     uint8_t *rec = c.rec + ((slot >> c.shift) * c.heads + h) * c.rec_bytes();
-    *(uint32_t *)(rec + place * (D / 2) + 4 * g8) = kc;
-    *(uint32_t *)(rec + c.v_codes() + place * (D / 2) + 4 * g8) = vc;
+    *(uint32_t *)(rec + place * (D / 2) + 4 * g8) = x.kc;
+    *(uint32_t *)(rec + c.v_codes() + place * (D / 2) + 4 * g8) = x.vc;
     if ((g8 & 3) == 0) {
-        rec[c.k_scales() + place * (D / 32) + g8 / 4] = (uint8_t)ke;
-        rec[c.v_scales() + g8 / 4 * c.bs + place] = (uint8_t)ve;
+        rec[c.k_scales() + place * (D / 32) + g8 / 4] = (uint8_t)x.ke;
+        rec[c.v_scales() + g8 / 4 * c.bs + place] = (uint8_t)x.ve;
     }
+}
+
+template <typename TT, int D>
+__global__ __launch_bounds__(kThreads) void kv_append_kernel(KvCache c, KvRows k, KvRows v,
+                                                             const int64_t *__restrict__ slots, int64_t T)
+{
+    append_tokens<TT, D>(c, k, v, slots, T, blockIdx.x / (uint32_t)c.heads, blockIdx.x % (uint32_t)c.heads);
 }
 
 // Eight stored values: codes w, scale byte e of the key beside them 255 = NaN.
@@ -125,15 +138,18 @@ template <typename TT> __device__ __forceinline__ u32x4 stored(uint32_t w, uint3
 // Summaries of the blocks whose last slot is among 64 consecutive tokens, one
 // head: the workgroup sums such a block's keys, thread (token row, 8 channels),
 // in fp64 (exact for all but keys of far more than 2^40 different magnitudes,
-// so the order does not show).
-template <typename TT, int D>
-__global__ __launch_bounds__(kThreads) void kv_summary_kernel(KvCache c, const int64_t *__restrict__ slots, int64_t T)
+// so the order does not show). FRESH: the tokens of this call are not in the cache yet;
+// the workgroup finds the block's ones among the slots and codes them itself.
+template <typename TT, int D, bool FRESH>
+__device__ __forceinline__ void summarise(const KvCache &c, const KvRows &k, const KvRows &v,
+                                          const int64_t *__restrict__ slots, int64_t T, uint32_t group, int h)
 {
     constexpr int kPer = D / 8, kTok = tokens_at_once<D>(), kAhead = 4;
     __shared__ double sums[kTok * D];
     __shared__ float top[kThreads / 64];
-    const int tid = threadIdx.x, h = blockIdx.x % (uint32_t)c.heads;
-    const int64_t t = (int64_t)(blockIdx.x / (uint32_t)c.heads) * 64 + (tid & 63);
+    __shared__ int from[FRESH ? 128 : 1];  // the token of this call in each slot of the block, or -1
+    const int tid = threadIdx.x;
+    const int64_t t = (int64_t)group * 64 + (tid & 63);
     const int64_t mine = t < T ? slots[t] : -1;
     uint64_t full = __ballot(mine >= 0 && (mine & (c.bs - 1)) == c.bs - 1 && (mine >> c.shift) < c.blocks);
     const int row = tid / kPer, g8 = tid % kPer;
@@ -143,18 +159,43 @@ __global__ __launch_bounds__(kThreads) void kv_summary_kernel(KvCache c, const i
         const int64_t block = __shfl(mine, l) >> c.shift;
         const int64_t at = block * c.heads + h;
         const uint8_t *rec = c.rec + at * c.rec_bytes();
+        if (FRESH) {
+            if (tid < 128) from[tid] = -1;
+            __syncthreads();
+            for (int64_t i = tid; i < T; i += kThreads) {
+                const int64_t slot = slots[i];
+                if (slot >= 0 && slot >> c.shift == block) from[slot & (c.bs - 1)] = (int)i;
+            }
+            __syncthreads();
+        }
         if (row < kTok) {
             double s[8] = {};
             for (int p0 = row; p0 < c.bs; p0 += kTok * kAhead) {
                 uint32_t w[kAhead], e[kAhead];
+                u32x4 kw[kAhead], vw[kAhead];
+                bool fresh[kAhead];
 #pragma unroll
                 for (int i = 0; i < kAhead; ++i) {
                     const int p = p0 + i * kTok;
                     w[i] = 0;
                     e[i] = 127;
-                    if (p < c.bs) {
+                    const int64_t x = FRESH && p < c.bs ? from[p] : -1;
+                    fresh[i] = x >= 0;
+                    if (fresh[i]) {
+                        kw[i] = *(const u32x4 *)((const typename TT::elem *)k.p + x * k.ts + h * k.hs + 8 * g8);
+                        vw[i] = *(const u32x4 *)((const typename TT::elem *)v.p + x * v.ts + h * v.hs + 8 * g8);
+                    } else if (p < c.bs) {
                         w[i] = *(const uint32_t *)(rec + p * (D / 2) + 4 * g8);
                         e[i] = rec[c.k_scales() + p * (D / 32) + g8 / 4];
+                    }
+                }
+                if (FRESH) {
+#pragma unroll
+                    for (int i = 0; i < kAhead; ++i) {
+                        if (!fresh[i]) continue;  // the same for the lanes that share a scale
+                        const Coded x = code_token<TT>(kw[i], vw[i]);
+                        w[i] = x.kc;
+                        e[i] = x.ke;
                     }
                 }
 #pragma unroll
@@ -191,6 +232,24 @@ __global__ __launch_bounds__(kThreads) void kv_summary_kernel(KvCache c, const i
         if (tid == 0) c.weight[at] = live ? amax / 127.f : 0.f;
         __syncthreads();
     }
+}
+
+template <typename TT, int D>
+__global__ __launch_bounds__(kThreads) void kv_summary_kernel(KvCache c, const int64_t *__restrict__ slots, int64_t T)
+{
+    summarise<TT, D, false>(c, {}, {}, slots, T, blockIdx.x / (uint32_t)c.heads, blockIdx.x % (uint32_t)c.heads);
+}
+
+// Tokens and summaries in one launch: the first `token_groups` workgroups a head write, the others sum.
+template <typename TT, int D>
+__global__ __launch_bounds__(kThreads) void kv_append_few_kernel(KvCache c, KvRows k, KvRows v,
+                                                                 const int64_t *__restrict__ slots, int64_t T,
+                                                                 uint32_t token_groups)
+{
+    const uint32_t group = blockIdx.x / (uint32_t)c.heads;
+    const int h = blockIdx.x % (uint32_t)c.heads;
+    if (group < token_groups) append_tokens<TT, D>(c, k, v, slots, T, group, h);
+    else summarise<TT, D, true>(c, k, v, slots, T, group - token_groups, h);
 }
 
 // The first `token_groups` workgroups a head read tokens, the others means.
@@ -241,16 +300,26 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(KvCache c, const int6
     *(f32x4 *)(mean + at + 4) = hi;
 }
 
+// Calls of at most this many tokens take one launch: a workgroup that sums a block codes the call's
+// tokens in it anew and scans the call's slots for them. 8 heads x 128, consecutive tokens (every
+// block of 64 full): 1 token 2.8 us in one launch and 4.0 in two, 64 tokens 5.3 and 5.6, 512 tokens 5.8 and 5.9,
+// 1,024 tokens 6.5 and 6.0, 4,096 tokens 11.1 and 8.5; the host's share 4.0 and 6.0.
+constexpr int64_t kFewTokens = 512;
+
 template <typename TT, int D> struct Launch {
     static unsigned groups(int64_t n) { return (unsigned)((n + tokens_at_once<D>() - 1) / tokens_at_once<D>()); }
     static hipError_t append(const KvCache &c, KvRows k, KvRows v, const int64_t *slots, int64_t T, hipStream_t s)
     {
+        const unsigned sixties = (unsigned)((T + 63) / 64);
+        if (T <= kFewTokens) {
+            hipLaunchKernelGGL((kv_append_few_kernel<TT, D>), dim3((groups(T) + sixties) * c.heads), dim3(kThreads), 0, s, c, k,
+                               v, slots, T, groups(T));
+            return hipGetLastError();
+        }
         hipLaunchKernelGGL((kv_append_kernel<TT, D>), dim3(groups(T) * c.heads), dim3(kThreads), 0, s, c, k, v, slots, T);
-        return hipGetLastError();
-    }
-    static hipError_t summaries(const KvCache &c, const int64_t *slots, int64_t T, hipStream_t s)
-    {
-        hipLaunchKernelGGL((kv_summary_kernel<TT, D>), dim3((unsigned)((T + 63) / 64) * c.heads), dim3(kThreads), 0, s, c, slots, T);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL((kv_summary_kernel<TT, D>), dim3(sixties * c.heads), dim3(kThreads), 0, s, c, slots, T);
         return hipGetLastError();
     }
     static hipError_t read(const KvCache &c, const int64_t *slots, int64_t T, void *k, void *v, const int32_t *blocks,
@@ -284,11 +353,6 @@ template <typename F> hipError_t by_cache(const KvCache &c, F f)
 hipError_t launch_kv_append(const KvCache &c, KvRows k, KvRows v, const int64_t *slots, int64_t T, hipStream_t s)
 {
     return by_cache(c, [&](auto l) { return decltype(l)::append(c, k, v, slots, T, s); });
-}
-
-hipError_t launch_kv_summaries(const KvCache &c, const int64_t *slots, int64_t T, hipStream_t s)
-{
-    return by_cache(c, [&](auto l) { return decltype(l)::summaries(c, slots, T, s); });
 }
 
 hipError_t launch_kv_read(const KvCache &c, const int64_t *slots, int64_t T, void *k, void *v, const int32_t *blocks,

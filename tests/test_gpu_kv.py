@@ -719,3 +719,32 @@ def test_requests_beside_long_tables(ctx, kind, B, heads, longest, dim, group):
     lens = np.random.default_rng(B).integers(1, 70, B)
     lens[B // 3] = longest
     run_attend(ctx, kind, lens.tolist(), [1] * B, heads, group, dim, 32, seed=83)
+
+
+@pytest.mark.parametrize("kind,T,heads,dim,bs", [("bf16", 300, 2, 64, 128), ("f16", 1000, 1, 96, 16),
+                                                 ("bf16", 2500, 2, 128, 64), ("f16", 5000, 1, 256, 32),
+                                                 ("bf16", 900, 3, 192, 16)])
+def test_summaries_of_scattered_tokens(ctx, kind, T, heads, dim, bs):
+    # half of every block by an earlier call, the rest, in any order, by this one; some tokens are not finite
+    import paper_2608_08751_amd as ivf
+
+    rng = np.random.default_rng(T)
+    blocks = T // (bs // 2)
+    order = rng.permutation(blocks * bs)
+    first = order[order % bs < bs // 2]  # the slots before the middle, and then the others
+    second = order[order % bs >= bs // 2]
+    cache = ivf.KVCache.empty(blocks, heads, dim, bs, dtype_of(kind))
+    cache.summary.fill_(77)
+    stored = np.zeros((blocks * bs, heads, dim))
+    for slots in (first, second):
+        x = rng.standard_normal((len(slots), 2, heads, dim)) * np.exp2(rng.integers(-6, 7, (len(slots), 2, heads, 1)))
+        kv = dev(x.astype(np.float32), dtype_of(kind))
+        kv[3, 0, 0, 5], kv[11, 1, 0, dim - 1] = float("nan"), float("inf")
+        assert (cache.summary == 77).all()  # nothing full yet
+        ivf.ivf_kv_append(ctx, cache, kv[:, 0], kv[:, 1], dev(slots.astype(np.int64)))
+        stored[slots], _ = M.store(as_np(kv[:, 0]), as_np(kv[:, 1]), kind)
+    codes, weight = cache.summary.cpu().numpy(), cache.weight.cpu().numpy()
+    for b in range(blocks):
+        for h in range(heads):
+            want, w = M.summary(stored[b * bs:(b + 1) * bs, h])
+            assert (codes[b, h] == want).all() and weight[b, h] == w
