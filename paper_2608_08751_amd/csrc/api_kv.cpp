@@ -345,6 +345,7 @@ ivf_status ivf_kv_attend(ivf_ctx *ctx, const ivf_kv_cache *cache, const void *q,
         a.per_unit = p.per_unit;
         a.units = (int)p.units;
         a.slots = (int)p.slots;
+        KvAttend prompts = a;
         if (p.tokens) {
             char *ws = (char *)ctx->ws;
             a.splits = p.token_splits;
@@ -352,16 +353,17 @@ ivf_status ivf_kv_attend(ivf_ctx *ctx, const ivf_kv_cache *cache, const void *q,
             a.part_ml = (float2 *)(ws + p.token_ml);
             a.unit_parts = (int2 *)(ws + p.token_parts);
             TIMED("kv_attend", launch_kv_tokens(a, p.token_groups, ctx->stream));
-            if (a.splits > 1) TIMED("kv_combine", launch_kv_combine(a, false, ctx->stream));
         }
         if (p.prompt) {
             char *ws = (char *)ctx->ws + p.token_bytes;
-            a.splits = p.prompt_splits;
-            a.part = (float *)ws;
-            a.part_ml = (float2 *)(ws + p.prompt_ml);
-            TIMED("kv_prompt", launch_kv_prompt(a, ctx->stream));
-            if (a.splits > 1) TIMED("kv_combine", launch_kv_combine(a, true, ctx->stream));
+            prompts.splits = p.prompt_splits;
+            prompts.part = (float *)ws;
+            prompts.part_ml = (float2 *)(ws + p.prompt_ml);
+            TIMED("kv_prompt", launch_kv_prompt(prompts, ctx->stream));
         }
+        const KvAttend *join_prompts = p.prompt && p.prompt_splits > 1 ? &prompts : nullptr;
+        const KvAttend *join_units = p.tokens && p.token_splits > 1 ? &a : nullptr;
+        if (join_prompts || join_units) TIMED("kv_combine", launch_kv_combine(join_prompts, join_units, ctx->stream));
         ctx->last_stats = nullptr;
         return IVF_OK;
     });

@@ -106,7 +106,8 @@ struct KvAttendPlan {
 KvAttendPlan kv_attend_plan(const KvCache &c, int group, int64_t T, int64_t B, int64_t cols, int64_t count,
                             int64_t longest, int num_cus);
 hipError_t launch_kv_tokens(const KvAttend &a, int64_t groups, hipStream_t s);
-hipError_t launch_kv_combine(const KvAttend &a, bool prompt, hipStream_t s);
+// joins the parts of prompts and of the single-token kernel's calls; either may be null
+hipError_t launch_kv_combine(const KvAttend *prompts, const KvAttend *units, hipStream_t s);
 
 int kv_prompt_rows(int dim);      // rows of a workgroup
 int kv_prompt_resident(int dim);  // workgroups that a CU holds
