@@ -592,9 +592,9 @@ def ivf_kv_plan(ctx: Context, cached, added, block_size: int, table, free_blocks
     if tokens < 0:
         raise ValueError("tokens must be >= 0, got %d" % tokens)
     n_free = free_blocks.numel()
-    # slots (two words each) come first: 8-byte aligned
+    # slots (two words each) come first: 8-byte aligned; parts without gradients, at half the cost of views
     whole = torch.empty(4 * tokens + B + 1, dtype=i32, device=cached.device)
-    slots, request, position, start = whole.split((2 * tokens, tokens, tokens, B + 1))
+    slots, request, position, start = torch.unsafe_split_with_sizes(whole, (2 * tokens, tokens, tokens, B + 1))
     info = torch.empty(4, dtype=torch.int64, device=cached.device) if want_info else None
     at = whole.data_ptr()
     lib, handle = ctx.bind()
@@ -628,13 +628,13 @@ def ivf_kv_read(ctx: Context, cache: KVCache, slots, blocks=None):
     import torch
 
     T = slots.shape[0]
-    k = torch.empty((T, cache.heads, cache.dim), dtype=cache.dtype, device=slots.device)
+    k = torch.empty(T, cache.heads, cache.dim, dtype=cache.dtype, device=slots.device)
     v = torch.empty_like(k)
     mean, n, p_blocks, p_mean = None, 0, None, None
     if blocks is not None:
         n = blocks.shape[0]
         p_blocks = _ints(blocks, "blocks", (n,), torch.int32)
-        mean = torch.empty((n, cache.heads, cache.dim), dtype=torch.float32, device=slots.device)
+        mean = torch.empty(n, cache.heads, cache.dim, dtype=torch.float32, device=slots.device)
         p_mean = mean.data_ptr()
     lib, handle = ctx.bind()
     st = lib.ivf_kv_read(handle, cache.ref, _ints(slots, "slots", (T,), torch.int64), T, k.data_ptr(), v.data_ptr(),
@@ -654,7 +654,7 @@ def ivf_kv_select(ctx: Context, cache: KVCache, q, request, position, table, cou
     qp, qt, qh = _rows(q, "q", cache)
     T, Hq, _ = q.shape
     B, cols = table.shape
-    out = torch.empty((T, cache.heads, max(count, 0)), dtype=i32, device=q.device)
+    out = torch.empty(T, cache.heads, max(count, 0), dtype=i32, device=q.device)
     lib, handle = ctx.bind()
     st = lib.ivf_kv_select(handle, cache.ref, qp, qt, qh, Hq, T, _ints(request, "request", (T,), i32),
                            _ints(position, "position", (T,), i32), _ints(table, "table", (B, cols), i32), B, cols, first,
@@ -681,12 +681,12 @@ def ivf_kv_attend(ctx: Context, cache: KVCache, q, start, request, position, tab
         count = blocks.shape[-1]
         p_blocks = _ints(blocks, "blocks", (T, cache.heads, count), i32)
     if out is None:
-        out = torch.empty((T, Hq, dim), dtype=cache.dtype, device=q.device)
+        out = q.new_empty(T, Hq, dim)
     elif not out.is_cuda or not out.is_contiguous() or out.dtype != cache.dtype or out.shape != (T, Hq, dim):
         raise ValueError("out must be contiguous %s %s on the device" % ((T, Hq, dim), cache.dtype))
     if out_lse is None:
         if want_lse:
-            out_lse = torch.empty((T, Hq), dtype=torch.float32, device=q.device)
+            out_lse = torch.empty(T, Hq, dtype=torch.float32, device=q.device)
     elif (not out_lse.is_cuda or not out_lse.is_contiguous() or out_lse.dtype != torch.float32
           or out_lse.shape != (T, Hq)):
         raise ValueError("out_lse must be contiguous %s fp32 on the device" % ((T, Hq),))
