@@ -565,8 +565,9 @@ ivf_status ivf_kv_read(ivf_ctx *ctx, const ivf_kv_cache *cache, const int64_t *s
  * ascending). The score is <c, summary> * weight in fp32, with the integer
  * product exact and c the int8 code rint(u * (127 / amax)) of u, the sum of
  * the head's group of query rows (fp64, rounded to fp32 once; non-finite
- * channels, and all where amax is below 2^-100, count 0). Blocks without a
- * table entry are not selected.
+ * channels, and all where amax is below 2^-100, count 0). A weight that is not
+ * finite or below 0 (of a block whose last slot was never written) counts 0.
+ * Blocks without a table entry are not selected.
  *   q        [T][q_heads][dim] by strides
  *   request, position [T] int32     table [B][table_cols] int32
  *   first >= 0, last >= 1, first + last <= count <= 4096

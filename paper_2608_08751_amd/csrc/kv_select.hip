@@ -54,6 +54,10 @@ __device__ __forceinline__ float2 group_sum(const KvSelect &a, int64_t t, int h,
     return u;
 }
 
+// A block's weight as its score takes it. That of a block whose last slot has not been written
+// may be anything: no number, or one below 0, counts 0.
+__device__ __forceinline__ float weight_of(float w) { return w >= 0.f && w <= 3.402823466e38f ? w : 0.f; }
+
 // 127 / amax, or 0 where amax is too small: code = rint(u times it).
 __device__ __forceinline__ float code_scale(float amax) { return amax >= 0x1p-100f ? 127.f / amax : 0.f; }
 __device__ __forceinline__ uint16_t two_codes(float2 u, float scale)
@@ -333,7 +337,7 @@ __global__ __launch_bounds__(kOneThreads) void kv_select_one_kernel(KvSelect a)
                 s += __shfl_xor(s, 2);
                 s += __shfl_xor(s, 4);
                 const int j = j0 + kStep * i;
-                if (part == 0 && j < e.n) lds[j] = id[i] >= 0 ? key_of((float)s * w[i]) : 0u;
+                if (part == 0 && j < e.n) lds[j] = id[i] >= 0 ? key_of((float)s * weight_of(w[i])) : 0u;
             }
         }
     }
@@ -397,7 +401,7 @@ __global__ __launch_bounds__(kTileThreads) void kv_select_tile_kernel(KvSelect a
             int32_t id = j < n ? a.table[(int64_t)b * a.cols + j] : -1;
             if (id >= a.c.blocks) id = -1;
             ids[j] = max(id, 0);
-            weights[j] = id >= 0 ? a.c.weight[(int64_t)id * a.c.heads + h] : -1.f;  // weights are not negative
+            weights[j] = id >= 0 ? weight_of(a.c.weight[(int64_t)id * a.c.heads + h]) : -1.f;  // below 0: no block
         }
         __syncthreads();
         const bool mine = col >= i0 && col < i1;

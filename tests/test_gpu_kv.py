@@ -748,3 +748,25 @@ def test_summaries_of_scattered_tokens(ctx, kind, T, heads, dim, bs):
         for h in range(heads):
             want, w = M.summary(stored[b * bs:(b + 1) * bs, h])
             assert (codes[b, h] == want).all() and weight[b, h] == w
+
+
+@pytest.mark.parametrize("new", [3, 200])  # one by one; in tiles
+@pytest.mark.parametrize("junk", [float("nan"), -float("inf"), float("inf"), -2.0])
+def test_select_weights_never_written(ctx, new, junk):
+    # a token's own block is among the selected whatever its weight holds before its last slot is written
+    import paper_2608_08751_amd as ivf
+
+    heads, n, bs = 4, 1003, 16
+    cache, table, _, _ = make(ctx, "bf16", [n], heads, 64, bs, 21)
+    open_block = int(table[0, (n - 1) // bs])
+    cache.weight[open_block] = junk
+    cache.weight[int(table[0, 20])] = junk  # and one that is ranked
+    cache.summary[open_block] = -77
+    weights = cache.weight.cpu().numpy().copy()
+    weights[~(np.isfinite(weights) & (weights >= 0))] = 0
+    _, request, position = batch([n], [new])
+    q = queries(new, 2 * heads, 64, "bf16", 4)
+    got = ivf.ivf_kv_select(ctx, cache, q, ints(request), ints(position), ints(table), 7).cpu().numpy()
+    want = M.select(as_np(q), cache.summary.cpu().numpy(), weights, heads, request, position, table, bs, 1, 1, 7)
+    assert (got == want).all()
+    assert (got.max(-1) == position[:, None] // bs).all()
