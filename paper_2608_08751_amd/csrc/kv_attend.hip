@@ -66,7 +66,7 @@ __device__ int64_t unit_steps(const KvAttend &a, uint32_t u, int unit, int last_
     int lim = -1;
     for (int64_t t = t0 + (uint32_t)r0 / (uint32_t)a.group; t <= t0 + (uint32_t)r1 / (uint32_t)a.group; ++t)
         lim = max(lim, min(a.position[t], last_key));
-    return max(1, (lim + 32) >> 5);
+    return max(1, (lim >> 5) + 1);
 }
 
 constexpr int attend_threads(int team) { return team == 1 ? kThreads : 64 * team; }

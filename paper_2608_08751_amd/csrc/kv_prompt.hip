@@ -134,7 +134,7 @@ __global__ __launch_bounds__(PromptShape<D>::threads, 2) void kv_prompt_kernel(K
         gmax = __builtin_amdgcn_readfirstlane(gmax);
         __syncthreads();
 
-        const int ntiles = (gmax + kTileKeys) / kTileKeys;  // 0 where gmax is -1
+        const int ntiles = (int)(((int64_t)gmax + kTileKeys) / kTileKeys);  // 0 where gmax is -1
         const int per = (ntiles + a.splits - 1) / a.splits;
         const int k0 = min((int64_t)ntiles, (int64_t)split * per), k1 = min(ntiles, k0 + per);
         if (k0 >= k1) continue;

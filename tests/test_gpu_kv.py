@@ -770,3 +770,28 @@ def test_select_weights_never_written(ctx, new, junk):
     want = M.select(as_np(q), cache.summary.cpu().numpy(), weights, heads, request, position, table, bs, 1, 1, 7)
     assert (got == want).all()
     assert (got.max(-1) == position[:, None] // bs).all()
+
+
+@pytest.mark.parametrize("new", [2, 70])
+def test_positions_up_to_the_last_of_a_table(ctx, new):
+    # a table of 2^31 - 16 keys that names its first block and its last ones: the rows of the last tokens equal
+    # those of a short request with the same blocks
+    import torch
+
+    import paper_2608_08751_amd as ivf
+
+    heads, group, dim, bs, far = 1, 2, 64, 16, 6
+    n = (1 + far) * bs
+    cache, table, keys, values = make(ctx, "bf16", [n], heads, dim, bs, 33)
+    cols = (1 << 27) - 1
+    wide = torch.full((1, cols), -1, dtype=torch.int32, device="cuda")
+    wide[0, 0] = int(table[0, 0])
+    wide[0, cols - far:] = ints(table[0, 1:1 + far])
+    start, request, position = batch([n], [new])
+    q = queries(new, heads * group, dim, "bf16", 5)
+    out, lse = ivf.ivf_kv_attend(ctx, cache, q, ints(start), ints(request), ints(position + (cols - far - 1) * bs), wide,
+                                 0.125, new)
+    want, want_lse = M.attend(as_np(q), keys, values, heads, request, position, table, bs, 0.125)
+    vmax = np.nanmax(np.abs(values))
+    smax = 0.125 * np.abs(as_np(q)).sum(-1).max() * np.nanmax(np.abs(keys))
+    check_attend(out, lse, want, want_lse, "bf16", vmax, smax)
