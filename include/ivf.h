@@ -591,6 +591,8 @@ ivf_status ivf_kv_select(ivf_ctx *ctx, const ivf_kv_cache *cache, const void *q,
  *            with `blocks` the requests' ranges are not read, without it
  *            request[] is not, and rows outside every range are not written
  *   longest  at least the largest number of tokens of one request, 1 ... T
+ *            (where it is less, rows of requests that have more may be left
+ *            unwritten)
  *   blocks   [T][heads][count] int32 (ivf_kv_select), or NULL (count 0)
  *   out      [T][q_heads][dim] of the cache's type
  *   out_lse  [T][q_heads] fp32, log of the sum of exp(scale * q.k); may be NULL

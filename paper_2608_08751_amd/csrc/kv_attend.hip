@@ -165,7 +165,7 @@ void kv_attend_kernel(KvAttend a)
                 if (a.splits == 1 || (int)unit + 1 >= a.units || before[unit + 1] >= to) return;
                 continue;
             }
-            rows_here = (int)min((int64_t)kUnit, rows - r0);
+            rows_here = (int)min((int64_t)a.unit_rows, rows - r0);  // never more than part[] has room for
         }
         const bool live = b >= 0 && b < a.B;
 

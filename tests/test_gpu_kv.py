@@ -795,3 +795,39 @@ def test_positions_up_to_the_last_of_a_table(ctx, new):
     vmax = np.nanmax(np.abs(values))
     smax = 0.125 * np.abs(as_np(q)).sum(-1).max() * np.nanmax(np.abs(keys))
     check_attend(out, lse, want, want_lse, "bf16", vmax, smax)
+
+
+@pytest.mark.parametrize("group,new", [(4, 3), (2, 50), (16, 4)])
+def test_requests_of_more_tokens_than_longest_says(ctx, group, new):
+    # nothing is written past the workspace or the outputs, and requests that keep to `longest` are right
+    import ctypes
+
+    import torch
+
+    import paper_2608_08751_amd as ivf
+    from paper_2608_08751_amd import _binding as B
+
+    heads, dim, bs, lens = 2, 64, 16, [5000, 700, 4800]
+    cache, table, keys, values = make(ctx, "bf16", lens, heads, dim, bs, 61)
+    start, request, position = batch(lens, [1, new, 1])
+    T, Hq = len(request), heads * group
+    q = queries(T, Hq, dim, "bf16", 3)
+    own = ivf.Context(0)
+    need = own.lib.ivf_kv_attend_bytes(cache.ref, Hq, T, 3, table.shape[1], 0, 1)
+    assert need > 0  # the key ranges are shared out
+    ws = torch.full((need + 65536,), 0x5A, dtype=torch.uint8, device="cuda")
+    out = torch.zeros(T + 64, Hq, dim, dtype=q.dtype, device="cuda")
+    lse = torch.zeros(T + 64, Hq, device="cuda")
+    args = [ints(start), ints(request), ints(position), ints(table)]
+    lib, handle = own.bind()
+    assert lib.ivf_set_workspace(handle, B._ptr(ws), need) == B.IVF_OK
+    st = lib.ivf_kv_attend(handle, cache.ref, B._ptr(q), q.stride(0), q.stride(1), Hq, T, *map(B._ptr, args), 3,
+                           table.shape[1], None, 0, ctypes.c_float(0.125), 1, B._ptr(out), B._ptr(lse))
+    assert st == B.IVF_OK
+    torch.cuda.synchronize()
+    own.close()
+    assert (ws[need:] == 0x5A).all() and not out[T:].any() and not lse[T:].any()
+    want, want_lse = M.attend(as_np(q), keys, values, heads, request, position, table, bs, 0.125)
+    kept = [0, T - 1]
+    check_attend(out[kept], lse[kept], want[kept], want_lse[kept], "bf16", np.nanmax(np.abs(values)),
+                 0.125 * np.abs(as_np(q)).sum(-1).max() * np.nanmax(np.abs(keys)))
