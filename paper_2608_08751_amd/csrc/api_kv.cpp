@@ -99,6 +99,13 @@ ivf_status check_tokens(ivf_ctx *ctx, const KvCache &c, int64_t T, int64_t heads
     return IVF_OK;
 }
 
+// A launch holds fewer than 2^32 threads.
+ivf_status check_threads(ivf_ctx *ctx, int64_t threads)
+{
+    if (threads >= (int64_t)UINT32_MAX) return fail(ctx, IVF_EUNSUPPORTED, "too many tokens for one call");
+    return IVF_OK;
+}
+
 ivf_status check_table(ivf_ctx *ctx, int64_t B, int32_t cols, int shift)
 {
     if (B < 1 || B > INT32_MAX) return fail(ctx, IVF_EINVAL, "B must be in [1, 2^31)");
@@ -168,6 +175,7 @@ ivf_status ivf_kv_append(ivf_ctx *ctx, const ivf_kv_cache *cache, const void *k,
         if (st != IVF_OK) return st;
         if ((st = check_tokens(ctx, c, T, c.heads)) != IVF_OK) return st;
         if (T == 0) return IVF_OK;
+        if ((st = check_threads(ctx, kv_cache_threads(c, T, T <= kKvFewTokens ? T : 0))) != IVF_OK) return st;
         size_t kb, vb;
         if ((st = check_rows(ctx, "k", k, k_token_stride, k_head_stride, T, c.heads, c.dim, &kb)) != IVF_OK) return st;
         if ((st = check_rows(ctx, "v", v, v_token_stride, v_head_stride, T, c.heads, c.dim, &vb)) != IVF_OK) return st;
@@ -196,6 +204,7 @@ ivf_status ivf_kv_read(ivf_ctx *ctx, const ivf_kv_cache *cache, const int64_t *s
         if ((st = check_tokens(ctx, c, n, c.heads)) != IVF_OK) return st;
         if (!out_k && !out_v) T = 0;
         if (T == 0 && n == 0) return IVF_OK;
+        if ((st = check_threads(ctx, kv_cache_threads(c, T, n))) != IVF_OK) return st;
         if ((T && !slots) || (n && (!blocks || !out_mean))) return fail(ctx, IVF_EINVAL, "null pointer argument");
         const void *i32[] = {blocks}, *i64[] = {slots};
         if ((st = check_elements(ctx, i32, 4)) != IVF_OK || (st = check_elements(ctx, i64, 8)) != IVF_OK) return st;
@@ -315,9 +324,11 @@ ivf_status ivf_kv_attend(ivf_ctx *ctx, const ivf_kv_cache *cache, const void *q,
         const int group = q_heads / a.c.heads;
         const KvAttendPlan p = kv_attend_plan(a.c, group, T, B, table_cols, count, longest, ctx->num_cus);
         const int64_t tiles = (T * group + kv_prompt_rows(a.c.dim) - 1) / kv_prompt_rows(a.c.dim);
-        if (p.token_groups * a.c.heads > INT32_MAX || p.units * 16 * a.c.heads > INT32_MAX ||
-            tiles * p.prompt_splits * a.c.heads > INT32_MAX)
-            return fail(ctx, IVF_EUNSUPPORTED, "too many rows for one call");
+        if (p.units * 16 * a.c.heads > INT32_MAX) return fail(ctx, IVF_EUNSUPPORTED, "too many rows for one call");
+        // a team of one: four units a workgroup
+        if ((st = check_threads(ctx, (p.token_groups + 3) * a.c.heads * 64 * p.team)) != IVF_OK ||
+            (st = check_threads(ctx, tiles * p.prompt_splits * a.c.heads * 512)) != IVF_OK)
+            return st;
         const size_t need = p.token_bytes + p.prompt_bytes;
         if (need && (st = check_ws(ctx, need)) != IVF_OK) return st;
         DeviceGuard g(ctx->device);

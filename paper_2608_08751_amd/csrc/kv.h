@@ -40,6 +40,16 @@ hipError_t launch_kv_plan(const int32_t *cached, const int32_t *added, int B, in
                           const int32_t *free_blocks, int64_t n_free, int64_t T, int32_t *start, int64_t *slots,
                           int32_t *request, int32_t *position, int64_t *info, int num_cus, hipStream_t s);
 
+// Threads of the launch that writes or reads T tokens and sums or reads n blocks (at most: 2048 / dim
+// tokens or blocks take 256 threads a head).
+inline int64_t kv_cache_threads(const KvCache &c, int64_t T, int64_t n)
+{
+    const int64_t at_once = 2048 / c.dim;
+    return ((T + at_once - 1) / at_once + (n + at_once - 1) / at_once) * c.heads * 256;
+}
+// Appending up to this many tokens takes one launch (kv_cache.hip).
+constexpr int64_t kKvFewTokens = 512;
+
 hipError_t launch_kv_append(const KvCache &c, KvRows k, KvRows v, const int64_t *slots, int64_t T, hipStream_t s);
 hipError_t launch_kv_read(const KvCache &c, const int64_t *slots, int64_t T, void *k, void *v, const int32_t *blocks,
                           int64_t n, float *mean, hipStream_t s);

@@ -300,18 +300,16 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(KvCache c, const int6
     *(f32x4 *)(mean + at + 4) = hi;
 }
 
-// Calls of at most this many tokens take one launch: a workgroup that sums a block codes the call's
+// Calls of at most kKvFewTokens tokens take one launch: a workgroup that sums a block codes the call's
 // tokens in it anew and scans the call's slots for them. 8 heads x 128, consecutive tokens (every
 // block of 64 full): 1 token 2.8 us in one launch and 4.0 in two, 64 tokens 5.3 and 5.6, 512 tokens 5.8 and 5.9,
 // 1,024 tokens 6.5 and 6.0, 4,096 tokens 11.1 and 8.5; the host's share 4.0 and 6.0.
-constexpr int64_t kFewTokens = 512;
-
 template <typename TT, int D> struct Launch {
     static unsigned groups(int64_t n) { return (unsigned)((n + tokens_at_once<D>() - 1) / tokens_at_once<D>()); }
     static hipError_t append(const KvCache &c, KvRows k, KvRows v, const int64_t *slots, int64_t T, hipStream_t s)
     {
         const unsigned sixties = (unsigned)((T + 63) / 64);
-        if (T <= kFewTokens) {
+        if (T <= kKvFewTokens) {
             hipLaunchKernelGGL((kv_append_few_kernel<TT, D>), dim3((groups(T) + sixties) * c.heads), dim3(kThreads), 0, s, c, k,
                                v, slots, T, groups(T));
             return hipGetLastError();

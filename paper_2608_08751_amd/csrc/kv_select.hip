@@ -491,7 +491,19 @@ template <typename TT> hipError_t launch_select(const KvSelect &a, hipStream_t s
 
 hipError_t launch_kv_select(const KvSelect &a, hipStream_t s)
 {
-    return a.c.bf16 ? launch_select<KvBf16>(a, s) : launch_select<KvF16>(a, s);
+    // a launch holds fewer than 2^32 threads: at most this many tokens of 1,024 threads a head
+    const int64_t most = (int64_t)UINT32_MAX / kOneThreads / a.c.heads / kTileTokens * kTileTokens;
+    for (int64_t t = 0; t < a.T; t += most) {
+        KvSelect part = a;
+        part.T = a.T - t < most ? a.T - t : most;
+        part.q.p = (const uint16_t *)a.q.p + t * a.q.ts;
+        part.request += t;
+        part.position += t;
+        part.out += t * a.c.heads * a.count;
+        const hipError_t e = a.c.bf16 ? launch_select<KvBf16>(part, s) : launch_select<KvF16>(part, s);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace ivf

@@ -156,3 +156,21 @@ def test_attend_workspace(vctx):
     assert str(need) in vctx.error()
     vctx.lib.ivf_set_workspace(vctx.handle, P(64 * GB), need)
     assert attend(vctx, **small) == B.IVF_EDEVICE
+
+
+def test_calls_beyond_a_launch(vctx):
+    # a launch holds fewer than 2^32 threads: 2048 / dim tokens of a head take 256, a wave attends for a token
+    far = [P(n << 40) for n in range(1, 6)]
+    big = dict(c=cache(heads=1), T=(1 << 28) - 16)  # 2^32 - 256 threads
+    assert append(vctx, k=far[0], v=far[1], slots=far[2], kt=128, vt=128, **big) == B.IVF_EDEVICE
+    assert read(vctx, slots=far[0], k=far[1], v=far[2], n=0, **big) == B.IVF_EDEVICE
+    assert read(vctx, slots=far[0], k=far[1], v=far[2], n=17, **big) == B.IVF_EUNSUPPORTED
+    big["T"] += 1
+    assert append(vctx, k=far[0], v=far[1], slots=far[2], kt=128, vt=128, **big) == B.IVF_EUNSUPPORTED
+    assert read(vctx, slots=far[0], k=far[1], v=far[2], n=0, **big) == B.IVF_EUNSUPPORTED
+    rows = dict(c=cache(heads=1), heads=1, q=far[0], qt=128, request=far[1], position=P((2 << 40) + (4 << 30)),
+                start=far[4], blocks=far[2], count=2, out=far[3], lse=None, longest=1)
+    assert attend(vctx, T=(1 << 26) - 16, **rows) == B.IVF_EDEVICE
+    assert attend(vctx, T=1 << 26, **rows) == B.IVF_EUNSUPPORTED
+    assert select(vctx, c=cache(heads=1), heads=1, q=far[0], qt=128, request=far[1], position=far[2], out=far[3],
+                  T=1 << 28) == B.IVF_EDEVICE  # several launches

@@ -831,3 +831,28 @@ def test_requests_of_more_tokens_than_longest_says(ctx, group, new):
     kept = [0, T - 1]
     check_attend(out[kept], lse[kept], want[kept], want_lse[kept], "bf16", np.nanmax(np.abs(values)),
                  0.125 * np.abs(as_np(q)).sum(-1).max() * np.nanmax(np.abs(keys)))
+
+
+def test_select_more_tokens_than_a_launch_holds(ctx):
+    # 2^32 threads are 4,194,304 workgroups: tokens on both sides of where the second launch begins
+    import torch
+
+    import paper_2608_08751_amd as ivf
+
+    n, bs, T = 300, 16, 4_200_000
+    cache, table, _, _ = make(ctx, "bf16", [n], 1, 64, bs, 12)
+    # a table of more columns than the tiles hold: a workgroup a token
+    wide = np.full((1, 2100), -1, np.int32)
+    wide[0, : table.shape[1]] = table[0]
+    few = queries(997, 1, 64, "bf16", 8, strided=False)
+    q = few.repeat(T // 997 + 1, 1, 1)[:T]
+    position = ints(np.arange(T) * 7 % n)
+    request = torch.zeros(T, dtype=torch.int32, device="cuda")
+    got = ivf.ivf_kv_select(ctx, cache, q, request, position, ints(wide), 4)
+    period = 997 * n  # tokens after which queries and positions are the same again
+    want = ivf.ivf_kv_select(ctx, cache, q[:period], request[:period], position[:period], ints(wide), 4)
+    assert (got == want.repeat(T // period + 1, 1, 1)[:T]).all()
+    some = np.arange(0, period, 4001)
+    ref = M.select(as_np(q[some]), cache.summary.cpu().numpy(), cache.weight.cpu().numpy(), 1, [0] * len(some),
+                   position.cpu().numpy()[some], wide, bs, 1, 1, 4)
+    assert (want.cpu().numpy()[some] == ref).all()
