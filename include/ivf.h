@@ -517,7 +517,8 @@ typedef struct {
 /* Block tables and slots from request lengths. Request b has cached[b] tokens
  * in the cache and brings added[b] more (negative lengths count as 0). Its
  * ceil((cached + added) / block_size) - ceil(cached / block_size) further
- * blocks are taken from free_blocks in order, requests in order.
+ * blocks (those within table_cols) are taken from free_blocks in order,
+ * requests in order.
  *   cached, added [B] int32, B <= 16384
  *   table       [B][table_cols] int32 (rows table_cols apart), updated: the
  *               entries of blocks that were there stay, the new blocks'
@@ -542,7 +543,8 @@ ivf_status ivf_kv_plan(ivf_ctx *ctx, const int32_t *cached, const int32_t *added
  * them.
  *   k, v  [T][heads][dim] by strides, type of the cache
  * Errors: IVF_EINVAL (sizes, NULL pointers, misalignment, aliasing),
- * IVF_EUNSUPPORTED (block size, dim, type), IVF_EDEVICE. */
+ * IVF_EUNSUPPORTED (block size, dim, type, more tokens than one launch holds:
+ * about 2^35 / dim, tokens times heads), IVF_EDEVICE. */
 ivf_status ivf_kv_append(ivf_ctx *ctx, const ivf_kv_cache *cache, const void *k,
                          int64_t k_token_stride, int64_t k_head_stride, const void *v,
                          int64_t v_token_stride, int64_t v_head_stride, const int64_t *slots,
