@@ -310,7 +310,7 @@ void kv_attend_kernel(KvAttend a)
                 int key[2];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    key[e] = z.key[e] < 0 ? INT32_MAX - 16 : z.key[e] + 4 * h;
+                    key[e] = z.key[e] < 0 ? INT32_MAX - 3 : z.key[e] + 4 * h;  // a strip that is not there: past every position
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
 #pragma unroll
