@@ -22,6 +22,7 @@
 #include "kv.h"
 #include "kv_types.h"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace ivf {
@@ -140,6 +141,12 @@ __device__ __forceinline__ T sum_waves(Exchange<WAVES> &e, int &turn, int wave, 
     return add_rows16<T, WAVES>(y);
 }
 
+// `from` and the number of lanes below this one in the mask.
+__device__ __forceinline__ int lanes_below(uint64_t mask, int from)
+{
+    return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, (uint32_t)from));
+}
+
 // Keeps of keys 0 ... n - 1 those of forced places (j < first or j >= tail) and the
 // best `want` of the others (key descending, index ascending), and writes their
 // indexes, ascending, to out[0, count), -1 behind; a key of 0 is never kept. WAVES
@@ -156,12 +163,16 @@ __device__ __forceinline__ void select_best(const uint32_t (&k)[KPT], int wave, 
     int forced = 0;
 #pragma unroll
     for (int i = 0; i < KPT; ++i) {
-        const int j = j0 + 64 * i;
-        const bool kept = (j < first || j >= tail) && k[i] != 0;
-        c[i] = kept ? UINT32_MAX : k[i];
-        forced += __popcll(__ballot(kept));
+        c[i] = k[i];
+        const int base = (wave * KPT + i) * 64;
+        if (base < first || base + 64 > tail) {  // the same for the wave: most 64 keys have no forced one
+            const int j = j0 + 64 * i;
+            const bool kept = (j < first || j >= tail) && k[i] != 0;
+            c[i] = kept ? UINT32_MAX : k[i];
+            forced += __popcll(__ballot(kept));
+        }
         if (i % 4 == 0) {
-            const bool sample = k[i] != 0 && !kept;
+            const bool sample = c[i] + 1 > 1;  // neither 0 nor forced
             const float x = sample ? score_of(k[i]) : 0.f;
             sum += x;
             squares += x * x;
@@ -196,7 +207,7 @@ __device__ __forceinline__ void select_best(const uint32_t (&k)[KPT], int wave, 
         uint32_t a = 1, b = UINT32_MAX;
         int cb = 0;
         while (b - a > 1 && cb != want) {
-            uint32_t mid = key_of(trial);
+            uint32_t mid = (uint32_t)__builtin_amdgcn_readfirstlane((int)key_of(trial));
             if (!(mid > a && mid < b)) mid = a + (b - a) / 2;
             const int x = at_least(mid);
             if (x > want) a = mid;
@@ -211,10 +222,9 @@ __device__ __forceinline__ void select_best(const uint32_t (&k)[KPT], int wave, 
         tau = b;
         ties = want - cb;  // where more than 0, b = a + 1
     }
-    const uint64_t below = ((uint64_t)1 << lane) - 1;
-    uint32_t take = 0;
+    uint64_t take[KPT];  // lanes whose key i is kept, in scalar registers
     int kept = 0;
-    static_assert(KPT <= 32, "a bit a key");
+    static_assert(KPT <= 32, "two scalar registers a key");
     if (ties > 0) {
         int eq = 0, used = 0;
 #pragma unroll
@@ -224,28 +234,24 @@ __device__ __forceinline__ void select_best(const uint32_t (&k)[KPT], int wave, 
         for (int i = 0; i < KPT; ++i) {
             const bool same = c[i] == tau - 1;
             const uint64_t me = __ballot(same);
-            const bool t = c[i] >= tau || (same && used + __popcll(me & below) < ties);
+            take[i] = __ballot(c[i] >= tau || (same && lanes_below(me, used) < ties));
             used += __popcll(me);
-            take |= (uint32_t)t << i;
-            kept += __popcll(__ballot(t));
+            kept += __popcll(take[i]);
         }
     } else {
 #pragma unroll
         for (int i = 0; i < KPT; ++i) {
-            const bool t = c[i] >= tau;
-            take |= (uint32_t)t << i;
-            kept += __popcll(__ballot(t));
+            take[i] = __ballot(c[i] >= tau);
+            kept += __popcll(take[i]);
         }
     }
     int at = 0;
     const int total = sum_waves<int, WAVES>(ex, turn, wave, kept, &at);
 #pragma unroll
     for (int i = 0; i < KPT; ++i) {
-        const bool t = take >> i & 1;
-        const uint64_t mt = __ballot(t);
-        const int to = at + __popcll(mt & below);
-        if (t && to < count) out[to] = j0 + 64 * i;
-        at += __popcll(mt);
+        const int to = lanes_below(take[i], at);
+        if (__builtin_amdgcn_inverse_ballot_w64(take[i]) && to < count) out[to] = j0 + 64 * i;
+        at += __popcll(take[i]);
     }
     for (int i = total + wave * 64 + lane; i < count; i += WAVES * 64) out[i] = -1;
 }
@@ -439,12 +445,14 @@ __global__ __launch_bounds__(kTileThreads) void kv_select_tile_kernel(KvSelect a
     }
     if (wave >= tokens) return;
     Exchange<1> ex;
-    const Extent e = ext[wave];
+    const Extent x = ext[wave];
+    const auto same = [](int v) { return __builtin_amdgcn_readfirstlane(v); };  // the lanes agree: scalar registers
+    const Extent e = {same(x.b), same(x.n), same(x.first), same(x.tail), same(x.want)};
     uint32_t k[KPT];
 #pragma unroll
-    for (int x = 0; x < KPT; ++x) {
-        const int j = 64 * x + lane;
-        k[x] = j < e.n ? lds[wave * ld + j] : 0u;
+    for (int i = 0; i < KPT; ++i) {
+        const uint32_t y = lds[wave * ld + 64 * i + lane];  // past the row's end: another row, or what the launch adds
+        k[i] = 64 * i + lane < e.n ? y : 0u;
     }
     select_best<1, KPT>(k, 0, e.n, e.first, e.tail, e.want, a.count, a.out + ((t0 + wave) * a.c.heads + h) * a.count, ex);
 }
@@ -476,7 +484,8 @@ template <typename TT> hipError_t launch_select(const KvSelect &a, hipStream_t s
     // tokens 15.4 and 15.5, of 512 tokens 16 and 60; 32 requests of 4 tokens 26 and 19, of 8 tokens 19 and 32
     if (a.T >= 6 * a.B && a.T * a.c.heads >= 768 && a.cols <= 2048) {
         const int ld = (a.cols + 15) / 16 * 16 + 4;
-        const size_t lds = (size_t)(kTileTokens + 2) * ld * 4;
+        const int keys = a.cols <= 512 ? 512 : a.cols <= 1024 ? 1024 : 2048;  // that a wave reads from its row on
+        const size_t lds = (size_t)std::max((kTileTokens + 2) * ld, (kTileTokens - 1) * ld + keys) * 4;
         const unsigned grid = (unsigned)((a.T + kTileTokens - 1) / kTileTokens * a.c.heads);
         return a.cols <= 512    ? launch_lds(kv_select_tile_kernel<TT, 8>, grid, kTileThreads, lds, s, a, ld)
                : a.cols <= 1024 ? launch_lds(kv_select_tile_kernel<TT, 16>, grid, kTileThreads, lds, s, a, ld)
