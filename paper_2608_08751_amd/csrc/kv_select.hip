@@ -17,7 +17,7 @@
 //
 // 32 tokens x 8 heads over up to 1,016 blocks of 128 channels take 12 us, of which the
 // scores (17 MB of summaries) are a third and the rounds of the selection the rest;
-// 2,048 tokens x 8 heads over 1,000 blocks of 96 channels 57 us, bound by the selection's
+// 2,048 tokens x 8 heads over 1,000 blocks of 96 channels 55 us, bound by the selection's
 // vector instructions (16,384 times the best 48 of 1,000; the products are 4 us).
 #include "kv.h"
 #include "kv_types.h"
