@@ -143,7 +143,8 @@ size_t ivf_workspace_bytes(int op, int64_t rows, int64_t C, int32_t D, int32_t k
 
 /* Hands the context a caller-owned device buffer (256-byte aligned) used as
  * scratch by later calls. The buffer must stay allocated while calls that use
- * it are in flight. NULL/0 detaches it. */
+ * it are in flight, and as long as a graph may be replayed that captured one
+ * (it holds the buffer's address). NULL/0 detaches it. */
 ivf_status ivf_set_workspace(ivf_ctx *ctx, void *dev_ptr, size_t bytes);
 
 /* Waits for the context's stream. IVF_EDEVICE if the device reported an error. */

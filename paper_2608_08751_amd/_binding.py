@@ -103,7 +103,12 @@ def _stream_handle(device=None):
 
 class Context:
     """An ivf_ctx bound to a device and to torch's current stream, plus a
-    grow-only workspace tensor allocated through torch."""
+    grow-only workspace tensor allocated through torch.
+
+    Calls may be captured into graphs. A graph keeps the address of the
+    workspace that its calls were captured with, so a workspace that a capture
+    has used lives as long as the context, also where a later call replaces it by
+    a larger one, and the context has to outlive its graphs."""
 
     def __init__(self, device: int = 0):
         import torch
@@ -111,6 +116,9 @@ class Context:
         self.lib = load_library()
         self.device = device
         self._ws = None
+        self._ws_captured = False  # a captured call holds its address
+        self._ws_streams = set()  # the streams that torch knows to use it
+        self._kept = []  # replaced workspaces of captured calls
         self._bound = None  # the stream of the last bind()
         h = ctypes.c_void_p()
         if device >= 0:
@@ -146,9 +154,19 @@ class Context:
     def ensure_workspace(self, nbytes: int):
         import torch
 
+        stream = _stream_handle(self.device)
         if self._ws is None or self._ws.numel() < nbytes:
-            self._ws = None
+            if self._ws_captured:
+                self._kept.append(self._ws)
+            self._ws, self._ws_captured = None, False
             self._ws = torch.empty(max(nbytes, 1 << 20), dtype=torch.uint8, device="cuda:%d" % self.device)
+            self._ws_streams = {stream}
+        if torch.cuda.is_current_stream_capturing():
+            self._ws_captured = True
+        elif stream not in self._ws_streams:
+            # its memory is handed on only after what this stream does with it
+            self._ws.record_stream(torch.cuda.current_stream(self.device))
+            self._ws_streams.add(stream)
         self.check(self.lib.ivf_set_workspace(self.handle, _ptr(self._ws), self._ws.numel()),
                    "ivf_set_workspace")
 
