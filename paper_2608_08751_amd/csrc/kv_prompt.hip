@@ -67,7 +67,7 @@ __global__ __launch_bounds__(PromptShape<D>::threads, 2) void kv_prompt_kernel(K
         const bool have = r < all_rows;
         tok[ct] = have ? r / a.group : -1;
         qhead[ct] = head * a.group + (int)(have ? r - tok[ct] * a.group : 0);
-        pos[ct] = have ? min(a.position[tok[ct]], last_key) : -1;
+        pos[ct] = have ? max(min(a.position[tok[ct]], last_key), -1) : -1;  // keys are subtracted from it
         mine[ct] = false;
         const elem *q = (const elem *)a.q.p + (have ? tok[ct] * a.q.ts + (int64_t)qhead[ct] * a.q.hs : 0);
 #pragma unroll

@@ -12,6 +12,21 @@ pytestmark = pytest.mark.gpu
 KINDS = ["bf16", "f16"]
 
 
+def attend_held(ctx, kind, cache, table, keys, values, start, request, position, q, bs, scale, longest):  # noqa: F811
+    """Attention of a batch held to the model; query rows that are not finite are NaN where they see a key."""
+    import paper_2608_08751_amd as ivf
+
+    out, lse = ivf.ivf_kv_attend(ctx, cache, q, ints(start), ints(request), ints(position), ints(table), scale, longest)
+    clean = as_np(q)
+    spoilt = ~np.isfinite(clean).all(-1)
+    clean = np.where(spoilt[..., None], 0.0, clean)
+    want, want_lse = M.attend(clean, keys, values, cache.heads, request, position, table, bs, scale)
+    spoilt &= want_lse > -np.inf
+    want[spoilt], want_lse[spoilt] = np.nan, np.nan
+    smax = abs(scale) * np.abs(clean).sum(-1).max() * np.nanmax(np.abs(keys))
+    check_attend(out, lse, want, want_lse, kind, np.nanmax(np.abs(values)), smax)
+
+
 def test_a_captured_call_survives_a_larger_workspace():
     # a decoding step whose key ranges are split is captured; then a call that needs more replaces the workspace.
     # Replays write their parts into memory that is nobody else's.
@@ -56,3 +71,16 @@ def test_a_captured_call_survives_a_larger_workspace():
         check_attend(out, lse, want, want_lse, "bf16", np.nanmax(np.abs(values)), 50.0)
         check_attend(out2, lse2, want2, want_lse2, "bf16", np.nanmax(np.abs(values)), 50.0)
     own.close()
+
+
+# the single-token kernel; the prompt kernel, its key range whole and split
+@pytest.mark.parametrize("kind,new,group,dim,bs", [("bf16", 9, 2, 64, 16), ("f16", 300, 2, 64, 16), ("bf16", 200, 1, 128, 64),
+                                                   ("f16", 90, 3, 256, 32)])
+def test_the_most_negative_positions_see_nothing(ctx, kind, new, group, dim, bs):  # noqa: F811
+    n = new + 500
+    cache, table, keys, values = make(ctx, kind, [n], 2, dim, bs, 91)
+    start, request, position = batch([n], [new])
+    for i, p in enumerate((-(2**31), -(2**31) + 5, -(2**31) + 70, -(2**31) + 4000, -1, -64)):
+        position[(i + 1) * new // 8] = p
+    q = queries(new, 2 * group, dim, kind, 92)
+    attend_held(ctx, kind, cache, table, keys, values, start, request, position, q, bs, dim**-0.5, new)
