@@ -599,7 +599,8 @@ ivf_status ivf_kv_select(ivf_ctx *ctx, const ivf_kv_cache *cache, const void *q,
  *   blocks   [T][heads][count] int32 (ivf_kv_select), or NULL (count 0)
  *   out      [T][q_heads][dim] of the cache's type
  *   out_lse  [T][q_heads] fp32, log of the sum of exp(scale * q.k); may be NULL
- * A row that sees nothing is 0 with -infinity.
+ * A row that sees nothing is 0 with -infinity; a row whose query holds a NaN or
+ * an infinity is NaN where it sees a key.
  * Workspace: ivf_kv_attend_bytes(). Errors: as ivf_kv_append, IVF_ENOMEM. */
 ivf_status ivf_kv_attend(ivf_ctx *ctx, const ivf_kv_cache *cache, const void *q,
                          int64_t q_token_stride, int64_t q_head_stride, int32_t q_heads, int64_t T,

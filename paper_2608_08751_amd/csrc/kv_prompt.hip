@@ -76,6 +76,9 @@ __global__ __launch_bounds__(PromptShape<D>::threads, 2) void kv_prompt_kernel(K
             for (int d = 0; d < P::size(c) / 32; ++d) {
                 u32x4 x = {0, 0, 0, 0};
                 if (have) x = *(const u32x4 *)(q + P::off(c) + P::size(c) / 4 * h + 8 * d);
+                // a channel that is not finite makes every score NaN, as in the single-token kernel: an
+                // infinity alone may score -infinity with all keys, which is how masked ones look
+                if (!TT::finite(x)) x = (u32x4){0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu};
                 qf[ct][P::off(c) / 32 + d] = x ^ a.q_flip;
             }
     }

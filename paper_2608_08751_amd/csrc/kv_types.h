@@ -13,6 +13,16 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
+// Whether none of 8 numbers is an infinity or NaN; exponent: the bits of both halves' exponents.
+__device__ __forceinline__ bool all_finite(u32x4 w, uint32_t exponent)
+{
+    const uint32_t lo = exponent & 0xffffu, hi = exponent & 0xffff0000u;
+    bool ok = true;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) ok &= (w[i] & lo) != lo && (w[i] & hi) != hi;
+    return ok;
+}
+
 struct KvF16 {
     typedef _Float16 elem;
     typedef _Float16 x8 __attribute__((ext_vector_type(8)));
@@ -32,6 +42,7 @@ struct KvF16 {
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
     }
+    static __device__ __forceinline__ bool finite(u32x4 w) { return all_finite(w, 0x7c007c00u); }
     static constexpr int kMinExp = -13, kMaxExp = 13;
 };
 
@@ -53,6 +64,7 @@ struct KvBf16 {
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
     }
+    static __device__ __forceinline__ bool finite(u32x4 w) { return all_finite(w, 0x7f807f80u); }
     static constexpr int kMinExp = -125, kMaxExp = 125;
 };
 

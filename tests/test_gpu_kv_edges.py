@@ -84,3 +84,32 @@ def test_the_most_negative_positions_see_nothing(ctx, kind, new, group, dim, bs)
         position[(i + 1) * new // 8] = p
     q = queries(new, 2 * group, dim, kind, 92)
     attend_held(ctx, kind, cache, table, keys, values, start, request, position, q, bs, dim**-0.5, new)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("scale", [0.125, -0.125])
+@pytest.mark.parametrize("new,dim", [(2, 64), (70, 64), (70, 96), (200, 128), (70, 192), (70, 256)])
+def test_queries_of_infinity_whose_scores_are_all_the_lowest(ctx, kind, scale, new, dim):  # noqa: F811
+    # one channel of the keys is negative in every token: an infinity there scores -infinity (or, by the scale's
+    # sign, +infinity) with every key, the softmax of which is no number
+    import paper_2608_08751_amd as ivf
+
+    heads, n, bs = 2, new + 40, 16
+    rng = np.random.default_rng(dim)
+    kv = rng.standard_normal((n, 2, heads, dim))
+    kv[:, 0, :, dim - 9] = -2.0
+    kv = dev(kv.astype(np.float32), dtype_of(kind))
+    blocks = -(-n // bs)
+    cache = ivf.KVCache.empty(blocks, heads, dim, bs, kv.dtype)
+    ivf.ivf_kv_append(ctx, cache, kv[:, 0], kv[:, 1], dev(np.arange(n, dtype=np.int64)))
+    k, v = M.store(as_np(kv[:, 0]), as_np(kv[:, 1]), kind)
+    assert (k[:, :, dim - 9] < 0).all()
+    pad = lambda x: np.concatenate([x, np.zeros((blocks * bs - n, heads, dim))])  # noqa: E731
+    keys, values = (pad(x).reshape(blocks, bs, heads, dim).transpose(0, 2, 1, 3) for x in (k, v))
+    table = np.arange(blocks, dtype=np.int32)[None]
+    start, request, position = batch([n], [new])
+    position[1] = -1  # a row that sees nothing stays empty whatever its query holds
+    q = queries(new, heads * 2, dim, kind, 93)
+    q[0, 1, dim - 9], q[1, :, dim - 9] = float("inf"), float("inf")
+    q[new // 2, 3, dim - 9], q[new - 1, 0, dim - 9] = float("inf"), -float("inf")
+    attend_held(ctx, kind, cache, table, keys, values, start, request, position, q, bs, scale, new)
