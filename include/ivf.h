@@ -532,6 +532,8 @@ typedef struct {
  *   out_request, out_position [T] int32; past the last token -1
  *   out_info    [4] int64: tokens, blocks asked for, blocks taken, requests
  *               that the table's columns do not hold; may be NULL
+ * B = 0 writes the outputs too, those that are not NULL; its inputs and table
+ * may be NULL.
  * Errors: IVF_EINVAL, IVF_EUNSUPPORTED (B, sizes), IVF_EDEVICE. */
 ivf_status ivf_kv_plan(ivf_ctx *ctx, const int32_t *cached, const int32_t *added, int64_t B,
                        int32_t block_size, int32_t *table, int32_t table_cols,

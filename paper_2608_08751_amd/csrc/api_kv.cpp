@@ -139,25 +139,27 @@ ivf_status ivf_kv_plan(ivf_ctx *ctx, const int32_t *cached, const int32_t *added
         const int shift = block_shift(block_size);
         if (!shift) return fail(ctx, IVF_EUNSUPPORTED, "block_size must be 16, 32, 64 or 128 (got %d)", block_size);
         if (B < 0 || T < 0 || n_free < 0) return fail(ctx, IVF_EINVAL, "B, T and n_free must be >= 0");
-        if (B == 0) return IVF_OK;
+        // an empty batch fills the outputs that are there; it needs no table (and a validation-only context, nothing)
+        if (B == 0 && (ctx->device < 0 || (!out_start && !out_slots && !out_request && !out_position && !out_info)))
+            return IVF_OK;
         if (B > kKvMaxRequests) return fail(ctx, IVF_EUNSUPPORTED, "at most %d requests", kKvMaxRequests);
         if (T > INT32_MAX) return fail(ctx, IVF_EUNSUPPORTED, "T must be < 2^31");
-        ivf_status st = check_table(ctx, B, table_cols, shift);
+        ivf_status st = B == 0 ? IVF_OK : check_table(ctx, B, table_cols, shift);
         if (st != IVF_OK) return st;
-        if (!cached || !added || !table || !out_start || (n_free && !free_blocks) ||
-            (T && (!out_slots || !out_request || !out_position)))
+        if (B && (!cached || !added || !table || !out_start || (n_free && !free_blocks) ||
+                  (T && (!out_slots || !out_request || !out_position))))
             return fail(ctx, IVF_EINVAL, "null pointer argument");
         const void *i32[] = {cached, added, table, free_blocks, out_start, out_request, out_position};
         const void *i64[] = {out_slots, out_info};
         if ((st = check_elements(ctx, i32, 4)) != IVF_OK || (st = check_elements(ctx, i64, 8)) != IVF_OK) return st;
         const Span ins[] = {{cached, (size_t)B * 4}, {added, (size_t)B * 4}, {free_blocks, (size_t)n_free * 4}};
-        const Span outs[] = {{table, (size_t)B * table_cols * 4}, {out_start, (size_t)(B + 1) * 4},
+        const Span outs[] = {{table, B ? (size_t)B * table_cols * 4 : 0}, {out_start, (size_t)(B + 1) * 4},
                              {out_slots, (size_t)T * 8}, {out_request, (size_t)T * 4}, {out_position, (size_t)T * 4},
                              {out_info, 32}};
         if ((st = no_overlap(ctx, outs, 6, ins, 3)) != IVF_OK) return st;
         DeviceGuard g(ctx->device);
         if (!g.ok) return fail(ctx, IVF_EDEVICE, "no usable device (context device %d)", ctx->device);
-        TIMED("kv_plan", launch_kv_plan(cached, added, (int)B, shift, table, table_cols, free_blocks, n_free, T,
+        TIMED("kv_plan", launch_kv_plan(cached, added, (int)B, shift, table, B ? table_cols : 1, free_blocks, n_free, T,
                                         out_start, out_slots, out_request, out_position, out_info, ctx->num_cus,
                                         ctx->stream));
         ctx->last_stats = nullptr;

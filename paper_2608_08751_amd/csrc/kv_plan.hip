@@ -75,7 +75,7 @@ __global__ __launch_bounds__(THREADS) void kv_plan_kernel(
     if (blockIdx.x == 0) {
         for (int b = tid; b < B; b += THREADS) start[b] = first[b];
         if (tid == 0) {
-            start[B] = (int32_t)total;
+            if (start) start[B] = (int32_t)total;
             if (info) {
                 info[0] = tall;
                 info[1] = ball;
@@ -112,9 +112,9 @@ __global__ __launch_bounds__(THREADS) void kv_plan_kernel(
             }
             pos = min(pos, (int64_t)INT32_MAX);
         }
-        slots[t] = slot;
-        request[t] = b;
-        position[t] = (int32_t)pos;
+        if (slots) slots[t] = slot;  // null in an empty batch only
+        if (request) request[t] = b;
+        if (position) position[t] = (int32_t)pos;
     }
 
     // table rows, a wave each: columns from the first new block on

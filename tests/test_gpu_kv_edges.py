@@ -113,3 +113,31 @@ def test_queries_of_infinity_whose_scores_are_all_the_lowest(ctx, kind, scale, n
     q[0, 1, dim - 9], q[1, :, dim - 9] = float("inf"), float("inf")
     q[new // 2, 3, dim - 9], q[new - 1, 0, dim - 9] = float("inf"), -float("inf")
     attend_held(ctx, kind, cache, table, keys, values, start, request, position, q, bs, scale, new)
+
+
+@pytest.mark.parametrize("tokens", [0, 5, 1000])
+def test_plan_of_no_requests(ctx, tokens):  # noqa: F811
+    import torch
+
+    import paper_2608_08751_amd as ivf
+
+    none = torch.empty(0, dtype=torch.int32, device="cuda")
+    torch.full((4 * tokens + 64,), 77, dtype=torch.int32, device="cuda")  # what the outputs' memory may hold before
+    plan = ivf.ivf_kv_plan(ctx, none, none, 16, none.view(0, 9), ints([4, 2]), tokens, want_info=True)
+    assert plan.start.tolist() == [0] and plan.info.tolist() == [0, 0, 0, 0]
+    for x in (plan.slots, plan.request, plan.position):
+        assert x.shape == (tokens,) and (x == -1).all()
+
+
+def test_plan_of_no_requests_writes_what_is_asked_for(ctx):  # noqa: F811
+    import torch
+
+    import paper_2608_08751_amd as ivf
+    from paper_2608_08751_amd import _binding as B
+
+    lib, handle = ctx.bind()
+    start = torch.full((3,), 77, dtype=torch.int32, device="cuda")
+    assert lib.ivf_kv_plan(handle, None, None, 0, 16, None, 0, None, 0, 0, B._ptr(start), None, None, None,
+                           None) == ivf.IVF_OK
+    assert lib.ivf_kv_plan(handle, None, None, 0, 16, None, 0, None, 0, 0, None, None, None, None, None) == ivf.IVF_OK
+    assert start.tolist() == [0, 77, 77]
