@@ -114,6 +114,27 @@ ivf_status check_table(ivf_ctx *ctx, int64_t B, int32_t cols, int shift)
     return IVF_OK;
 }
 
+// The sizes of an attention call, and how it is carried out (T above 0).
+ivf_status plan_attend(ivf_ctx *ctx, const KvCache &c, int32_t q_heads, int64_t T, int64_t B, int32_t cols, int32_t count,
+                       int64_t longest, int num_cus, KvAttendPlan &p)
+{
+    if (q_heads < 1 || q_heads > 65536 || q_heads % c.heads)
+        return fail(ctx, IVF_EINVAL, "q_heads must be a multiple of the cache's heads (got %d, %d)", q_heads, c.heads);
+    ivf_status st = check_tokens(ctx, c, T, q_heads);
+    if (st != IVF_OK || T == 0) return st;
+    if ((st = check_table(ctx, B, cols, c.shift)) != IVF_OK) return st;
+    if (count < 0 || count > kKvMaxCount)
+        return fail(ctx, IVF_EINVAL, "count must be in [1, %d] with blocks, 0 without", kKvMaxCount);
+    if (longest < 1) return fail(ctx, IVF_EINVAL, "longest must be >= 1");
+    const int group = q_heads / c.heads;
+    p = kv_attend_plan(c, group, T, B, cols, count, std::min(longest, T), num_cus);
+    const int64_t tiles = (T * group + kv_prompt_rows(c.dim) - 1) / kv_prompt_rows(c.dim);
+    if (p.units * 16 * c.heads > INT32_MAX) return fail(ctx, IVF_EUNSUPPORTED, "too many rows for one call");
+    // a team of one: four units a workgroup
+    if ((st = check_threads(ctx, (p.token_groups + 3) * c.heads * 64 * p.team)) != IVF_OK) return st;
+    return check_threads(ctx, tiles * p.prompt_splits * c.heads * 512);
+}
+
 ivf_status no_overlap(ivf_ctx *ctx, const Span *outs, int no, const Span *ins, int ni)
 {
     for (int i = 0; i < no; ++i) {
@@ -278,15 +299,14 @@ size_t ivf_kv_attend_bytes(const ivf_kv_cache *cache, int32_t q_heads, int64_t T
                            int32_t count, int64_t longest)
 {
     KvCache c;
-    if (check_cache(nullptr, cache, c) != IVF_OK || q_heads < 1 || q_heads % c.heads || T < 1 || B < 1 ||
-        table_cols < 1 || count < 0 || longest < 1)
-        return 0;
+    if (check_cache(nullptr, cache, c) != IVF_OK) return 0;
     int num_cus = 256, dev = 0;
     if (hipGetDevice(&dev) == hipSuccess) {
         int n = 0;
         if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && n > 0) num_cus = n;
     }
-    const KvAttendPlan p = kv_attend_plan(c, q_heads / c.heads, T, B, table_cols, count, std::min(longest, T), num_cus);
+    KvAttendPlan p = {};
+    if (plan_attend(nullptr, c, q_heads, T, B, table_cols, count, longest, num_cus, p) != IVF_OK) return 0;
     return p.token_bytes + p.prompt_bytes;
 }
 
@@ -300,14 +320,11 @@ ivf_status ivf_kv_attend(ivf_ctx *ctx, const ivf_kv_cache *cache, const void *q,
         KvAttend a;
         ivf_status st = check_cache(ctx, cache, a.c);
         if (st != IVF_OK) return st;
-        if (q_heads < 1 || q_heads > 65536 || q_heads % a.c.heads)
-            return fail(ctx, IVF_EINVAL, "q_heads must be a multiple of the cache's heads (got %d, %d)", q_heads, a.c.heads);
-        if ((st = check_tokens(ctx, a.c, T, q_heads)) != IVF_OK) return st;
+        KvAttendPlan p = {};
+        if ((st = plan_attend(ctx, a.c, q_heads, T, B, table_cols, count, longest, ctx->num_cus, p)) != IVF_OK) return st;
         if (T == 0) return IVF_OK;
-        if ((st = check_table(ctx, B, table_cols, a.c.shift)) != IVF_OK) return st;
-        if (blocks ? count < 1 || count > kKvMaxCount : count != 0)
+        if (blocks ? count < 1 : count != 0)
             return fail(ctx, IVF_EINVAL, "count must be in [1, %d] with blocks, 0 without", kKvMaxCount);
-        if (longest < 1) return fail(ctx, IVF_EINVAL, "longest must be >= 1");
         if (!isfinite(scale)) return fail(ctx, IVF_EINVAL, "scale must be finite");
         size_t qb;
         if ((st = check_rows(ctx, "q", q, q_token_stride, q_head_stride, T, q_heads, a.c.dim, &qb)) != IVF_OK) return st;
@@ -322,21 +339,12 @@ ivf_status ivf_kv_attend(ivf_ctx *ctx, const ivf_kv_cache *cache, const void *q,
         if ((st = no_overlap(ctx, outs, 2, ins, 6)) != IVF_OK) return st;
         for (const Span &o : outs)
             if (overlaps_cache(a.c, o.p, o.n)) return fail(ctx, IVF_EINVAL, "outputs overlap the cache");
-        longest = std::min(longest, T);
-        const int group = q_heads / a.c.heads;
-        const KvAttendPlan p = kv_attend_plan(a.c, group, T, B, table_cols, count, longest, ctx->num_cus);
-        const int64_t tiles = (T * group + kv_prompt_rows(a.c.dim) - 1) / kv_prompt_rows(a.c.dim);
-        if (p.units * 16 * a.c.heads > INT32_MAX) return fail(ctx, IVF_EUNSUPPORTED, "too many rows for one call");
-        // a team of one: four units a workgroup
-        if ((st = check_threads(ctx, (p.token_groups + 3) * a.c.heads * 64 * p.team)) != IVF_OK ||
-            (st = check_threads(ctx, tiles * p.prompt_splits * a.c.heads * 512)) != IVF_OK)
-            return st;
         const size_t need = p.token_bytes + p.prompt_bytes;
         if (need && (st = check_ws(ctx, need)) != IVF_OK) return st;
         DeviceGuard g(ctx->device);
         if (!g.ok) return fail(ctx, IVF_EDEVICE, "no usable device (context device %d)", ctx->device);
         a.q = {q, q_token_stride, q_head_stride};
-        a.group = group;
+        a.group = q_heads / a.c.heads;
         a.T = T;
         a.start = start;
         a.request = request;
