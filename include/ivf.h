@@ -592,6 +592,7 @@ ivf_status ivf_kv_select(ivf_ctx *ctx, const ivf_kv_cache *cache, const void *q,
  * listed twice counts twice).
  *   out = sum_j softmax_j(scale * q.k_j) v_j, sums in fp32, probabilities
  *   rounded to the cache's type for their product with the values.
+ *   scale    of magnitude below 2.3e38
  *   start    [B + 1] int32, request, position [T] int32 as in ivf_kv_plan;
  *            with `blocks` the requests' ranges are not read, without it
  *            request[] is not, and rows outside every range are not written

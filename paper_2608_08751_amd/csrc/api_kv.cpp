@@ -325,7 +325,8 @@ ivf_status ivf_kv_attend(ivf_ctx *ctx, const ivf_kv_cache *cache, const void *q,
         if (T == 0) return IVF_OK;
         if (blocks ? count < 1 : count != 0)
             return fail(ctx, IVF_EINVAL, "count must be in [1, %d] with blocks, 0 without", kKvMaxCount);
-        if (!isfinite(scale)) return fail(ctx, IVF_EINVAL, "scale must be finite");
+        const float scale2 = fabsf(scale) * 1.44269504089f;  // of exponents to the base 2
+        if (!isfinite(scale2)) return fail(ctx, IVF_EINVAL, "scale must be finite, and of magnitude below 2.3e38");
         size_t qb;
         if ((st = check_rows(ctx, "q", q, q_token_stride, q_head_stride, T, q_heads, a.c.dim, &qb)) != IVF_OK) return st;
         if (!position || !table || !out || (blocks ? !request : !start)) return fail(ctx, IVF_EINVAL, "null pointer argument");
@@ -355,7 +356,7 @@ ivf_status ivf_kv_attend(ivf_ctx *ctx, const ivf_kv_cache *cache, const void *q,
         a.blocks = blocks;
         a.count = count;
         // a scale of 0 as the least number above it: masked scores stay -infinity
-        a.scale = std::max(fabsf(scale) * 1.44269504089f, 0x1p-149f);
+        a.scale = std::max(scale2, 0x1p-149f);
         a.q_flip = scale < 0.f ? 0x80008000u : 0u;
         a.out = out;
         a.lse = out_lse;

@@ -36,3 +36,13 @@ def test_attend_bytes_are_what_the_call_asks_for(vctx):  # noqa: F811
         got = attend(vctx, T=T, n=n, cols=cols, longest=longest)
         assert got == (B.IVF_ENOMEM if need else B.IVF_EDEVICE)
         assert not need or str(need) in vctx.error()
+
+
+def test_attend_scales_beyond_fp32_to_the_base_2(vctx):  # noqa: F811
+    # scale log2(e) is an fp32 factor: infinite, it would make a score of 0 no number
+    vctx.lib.ivf_set_workspace(vctx.handle, (1 << 46) + (1 << 40), 1 << 36)
+    for scale in (2.3e38, -2.3e38, 0.0, 1e-45):
+        assert attend(vctx, scale=scale) == B.IVF_EDEVICE  # every check passed
+    for scale in (2.4e38, -3.4e38, float("inf")):
+        assert attend(vctx, scale=scale) == B.IVF_EINVAL
+        assert "scale" in vctx.error()
