@@ -119,7 +119,6 @@ class Context:
         self._ws_captured = False  # a captured call holds its address
         self._ws_streams = set()  # the streams that torch knows to use it
         self._kept = []  # replaced workspaces of captured calls
-        self._bound = None  # the stream of the last bind()
         h = ctypes.c_void_p()
         if device >= 0:
             with torch.cuda.device(device):
@@ -171,15 +170,12 @@ class Context:
                    "ivf_set_workspace")
 
     def bind_stream(self):
-        self._bound = None
         self.check(self.lib.ivf_set_stream(self.handle, _stream_handle()), "ivf_set_stream")
 
     def bind(self):
         """Binds torch's current stream of the device; the library and the context's handle."""
-        stream = _stream_handle(self.device)
-        if stream != self._bound:
-            self.check(self.lib.ivf_set_stream(self.handle, stream), "ivf_set_stream")
-            self._bound = stream
+        # each time: the handle may have been given another stream since
+        self.lib.ivf_set_stream(self.handle, _stream_handle(self.device))
         return self.lib, self.handle
 
     def sync(self):

@@ -1,4 +1,5 @@
-"""Which workspaces a context keeps (CPU: torch's allocations and streams are stand-ins)."""
+"""Which workspaces a context keeps and which stream it binds (CPU: torch's allocations
+and streams are stand-ins)."""
 import gc
 import weakref
 
@@ -88,3 +89,24 @@ def test_every_stream_that_uses_a_workspace_is_known(vctx, device):
     for device.stream in (3, 1):
         vctx.ensure_workspace(1 << 20)
     assert ws.streams == [1]
+
+
+def test_bind_follows_torch_after_the_handle_was_given_another_stream(vctx, device):
+    class Recorder:
+        def __init__(self, lib):
+            self.lib, self.stream = lib, None
+
+        def __getattr__(self, name):
+            return getattr(self.lib, name)
+
+        def ivf_set_stream(self, handle, stream):
+            self.stream = stream
+            return self.lib.ivf_set_stream(handle, stream)
+
+    lib = vctx.lib = Recorder(vctx.lib)
+    device.stream = 64
+    vctx.bind()
+    assert lib.stream == 64
+    vctx.lib.ivf_set_stream(vctx.handle, 128)
+    vctx.bind()
+    assert lib.stream == 64
