@@ -535,6 +535,9 @@ class KVCache:
         if tuple(records.shape) != (blocks, heads, block_size * dim * 17 // 16) or tuple(weight.shape) != (blocks, heads):
             raise ValueError("records %s, summary %s and weight %s do not belong together (block_size %d)" % (
                 tuple(records.shape), tuple(summary.shape), tuple(weight.shape), block_size))
+        if not records.device == summary.device == weight.device:
+            raise ValueError("records, summary and weight must lie on one device")
+        self.device = records.get_device()
         self.records, self.summary, self.weight = records, summary, weight
         self.blocks, self.heads, self.dim, self.block_size, self.dtype = blocks, heads, dim, block_size, dtype
         self.struct = _KvCacheStruct(records.data_ptr(), summary.data_ptr(), weight.data_ptr(), blocks, block_size,
@@ -564,10 +567,17 @@ class KVCache:
 KVPlan = collections.namedtuple("KVPlan", "start slots request position info")
 
 
-def _rows(t, name, cache, heads=None):
+def _same_device(ctx, cache):
+    if cache.device != ctx.device:
+        raise TypeError("the cache must be on the context's device %d, is on %s" % (ctx.device, cache.records.device))
+
+
+def _rows(ctx, t, name, cache, heads=None):
     """(pointer, token stride, head stride) of rows [tokens, heads, dim]."""
-    if not t.is_cuda or t.dtype != cache.dtype:
-        raise TypeError("%s must be a device tensor of the cache's type %s" % (name, cache.dtype))
+    _same_device(ctx, cache)
+    if t.get_device() != ctx.device or t.dtype != cache.dtype:
+        raise TypeError("%s must be of the cache's type %s on device %d, got %s on %s" % (
+            name, cache.dtype, ctx.device, t.dtype, t.device))
     shape = t.shape
     if len(shape) != 3 or shape[2] != cache.dim or (heads is not None and shape[1] != heads):
         raise ValueError("%s must be [tokens, %s, %d], got %s" % (name, heads or "heads", cache.dim, tuple(shape)))
@@ -579,10 +589,10 @@ def _rows(t, name, cache, heads=None):
     return t.data_ptr(), st if shape[0] > 1 else 0, sh if shape[1] > 1 else 0
 
 
-def _ints(t, name, shape, kind):
-    """The pointer of a contiguous device tensor of whole numbers of this shape."""
-    if t.dtype != kind or not t.is_cuda:
-        raise TypeError("%s must be a device tensor of %s, got %s on %s" % (name, kind, t.dtype, t.device))
+def _ints(ctx, t, name, shape, kind):
+    """The pointer of a contiguous tensor of whole numbers of this shape on the context's device."""
+    if t.dtype != kind or t.get_device() != ctx.device:
+        raise TypeError("%s must be %s on device %d, got %s on %s" % (name, kind, ctx.device, t.dtype, t.device))
     if t.shape != shape:
         raise ValueError("%s must be %s, got %s" % (name, tuple(shape), tuple(t.shape)))
     if not t.is_contiguous():
@@ -606,15 +616,16 @@ def ivf_kv_plan(ctx: Context, cached, added, block_size: int, table, free_blocks
     if tokens < 0:
         raise ValueError("tokens must be >= 0, got %d" % tokens)
     n_free = free_blocks.numel()
+    ins = (_ints(ctx, cached, "cached", (B,), i32), _ints(ctx, added, "added", (B,), i32), B, block_size,
+           _ints(ctx, table, "table", shape, i32), shape[1], _ints(ctx, free_blocks, "free_blocks", (n_free,), i32),
+           n_free, tokens)
     # slots (two words each) come first: 8-byte aligned; parts without gradients, at half the cost of views
     whole = torch.empty(4 * tokens + B + 1, dtype=i32, device=cached.device)
     slots, request, position, start = torch.unsafe_split_with_sizes(whole, (2 * tokens, tokens, tokens, B + 1))
     info = torch.empty(4, dtype=torch.int64, device=cached.device) if want_info else None
     at = whole.data_ptr()
     lib, handle = ctx.bind()
-    st = lib.ivf_kv_plan(handle, _ints(cached, "cached", (B,), i32), _ints(added, "added", (B,), i32), B, block_size,
-                         _ints(table, "table", shape, i32), shape[1], _ints(free_blocks, "free_blocks", (n_free,), i32),
-                         n_free, tokens, at + 16 * tokens, at, at + 8 * tokens, at + 12 * tokens,
+    st = lib.ivf_kv_plan(handle, *ins, at + 16 * tokens, at, at + 8 * tokens, at + 12 * tokens,
                          info.data_ptr() if want_info else None)
     if st:
         ctx.check(st, "ivf_kv_plan")
@@ -626,12 +637,12 @@ def ivf_kv_append(ctx: Context, cache: KVCache, k, v, slots):
     import torch
 
     T = slots.shape[0]
-    kp, kt, kh = _rows(k, "k", cache, cache.heads)
-    vp, vt, vh = _rows(v, "v", cache, cache.heads)
+    kp, kt, kh = _rows(ctx, k, "k", cache, cache.heads)
+    vp, vt, vh = _rows(ctx, v, "v", cache, cache.heads)
     if k.shape[0] != T or v.shape[0] != T:
         raise ValueError("k and v must hold one row per slot (%d)" % T)
     lib, handle = ctx.bind()
-    st = lib.ivf_kv_append(handle, cache.ref, kp, kt, kh, vp, vt, vh, _ints(slots, "slots", (T,), torch.int64), T)
+    st = lib.ivf_kv_append(handle, cache.ref, kp, kt, kh, vp, vt, vh, _ints(ctx, slots, "slots", (T,), torch.int64), T)
     if st:
         ctx.check(st, "ivf_kv_append")
 
@@ -641,17 +652,18 @@ def ivf_kv_read(ctx: Context, cache: KVCache, slots, blocks=None):
     and, of `blocks` (int32 [n]), the key means [n, heads, dim] fp32 (else None)."""
     import torch
 
+    _same_device(ctx, cache)
     T = slots.shape[0]
     k = torch.empty(T, cache.heads, cache.dim, dtype=cache.dtype, device=slots.device)
     v = torch.empty_like(k)
     mean, n, p_blocks, p_mean = None, 0, None, None
     if blocks is not None:
         n = blocks.shape[0]
-        p_blocks = _ints(blocks, "blocks", (n,), torch.int32)
+        p_blocks = _ints(ctx, blocks, "blocks", (n,), torch.int32)
         mean = torch.empty(n, cache.heads, cache.dim, dtype=torch.float32, device=slots.device)
         p_mean = mean.data_ptr()
     lib, handle = ctx.bind()
-    st = lib.ivf_kv_read(handle, cache.ref, _ints(slots, "slots", (T,), torch.int64), T, k.data_ptr(), v.data_ptr(),
+    st = lib.ivf_kv_read(handle, cache.ref, _ints(ctx, slots, "slots", (T,), torch.int64), T, k.data_ptr(), v.data_ptr(),
                          p_blocks, n, p_mean)
     if st:
         ctx.check(st, "ivf_kv_read")
@@ -665,14 +677,14 @@ def ivf_kv_select(ctx: Context, cache: KVCache, q, request, position, table, cou
     import torch
 
     i32 = torch.int32
-    qp, qt, qh = _rows(q, "q", cache)
+    qp, qt, qh = _rows(ctx, q, "q", cache)
     T, Hq, _ = q.shape
     B, cols = table.shape
     out = torch.empty(T, cache.heads, max(count, 0), dtype=i32, device=q.device)
     lib, handle = ctx.bind()
-    st = lib.ivf_kv_select(handle, cache.ref, qp, qt, qh, Hq, T, _ints(request, "request", (T,), i32),
-                           _ints(position, "position", (T,), i32), _ints(table, "table", (B, cols), i32), B, cols, first,
-                           last, count, out.data_ptr())
+    st = lib.ivf_kv_select(handle, cache.ref, qp, qt, qh, Hq, T, _ints(ctx, request, "request", (T,), i32),
+                           _ints(ctx, position, "position", (T,), i32), _ints(ctx, table, "table", (B, cols), i32), B,
+                           cols, first, last, count, out.data_ptr())
     if st:
         ctx.check(st, "ivf_kv_select")
     return out
@@ -687,30 +699,31 @@ def ivf_kv_attend(ctx: Context, cache: KVCache, q, start, request, position, tab
     import torch
 
     i32 = torch.int32
-    qp, qt, qh = _rows(q, "q", cache)
+    qp, qt, qh = _rows(ctx, q, "q", cache)
     T, Hq, dim = q.shape
     B, cols = table.shape
     p_blocks, count = None, 0
     if blocks is not None:
         count = blocks.shape[-1]
-        p_blocks = _ints(blocks, "blocks", (T, cache.heads, count), i32)
+        p_blocks = _ints(ctx, blocks, "blocks", (T, cache.heads, count), i32)
     if out is None:
         out = q.new_empty(T, Hq, dim)
-    elif not out.is_cuda or not out.is_contiguous() or out.dtype != cache.dtype or out.shape != (T, Hq, dim):
-        raise ValueError("out must be contiguous %s %s on the device" % ((T, Hq, dim), cache.dtype))
+    elif (out.get_device() != ctx.device or not out.is_contiguous() or out.dtype != cache.dtype
+          or out.shape != (T, Hq, dim)):
+        raise ValueError("out must be contiguous %s %s on the context's device" % ((T, Hq, dim), cache.dtype))
     if out_lse is None:
         if want_lse:
             out_lse = torch.empty(T, Hq, dtype=torch.float32, device=q.device)
-    elif (not out_lse.is_cuda or not out_lse.is_contiguous() or out_lse.dtype != torch.float32
+    elif (out_lse.get_device() != ctx.device or not out_lse.is_contiguous() or out_lse.dtype != torch.float32
           or out_lse.shape != (T, Hq)):
-        raise ValueError("out_lse must be contiguous %s fp32 on the device" % ((T, Hq),))
+        raise ValueError("out_lse must be contiguous %s fp32 on the context's device" % ((T, Hq),))
     need = cache.attend_bytes(ctx, Hq, T, B, cols, count, longest)
     if need:
         ctx.ensure_workspace(need)
     lib, handle = ctx.bind()
-    st = lib.ivf_kv_attend(handle, cache.ref, qp, qt, qh, Hq, T, _ints(start, "start", (B + 1,), i32),
-                           _ints(request, "request", (T,), i32), _ints(position, "position", (T,), i32),
-                           _ints(table, "table", (B, cols), i32), B, cols, p_blocks, count, scale, longest,
+    st = lib.ivf_kv_attend(handle, cache.ref, qp, qt, qh, Hq, T, _ints(ctx, start, "start", (B + 1,), i32),
+                           _ints(ctx, request, "request", (T,), i32), _ints(ctx, position, "position", (T,), i32),
+                           _ints(ctx, table, "table", (B, cols), i32), B, cols, p_blocks, count, scale, longest,
                            out.data_ptr(), None if out_lse is None else out_lse.data_ptr())
     if st:
         ctx.check(st, "ivf_kv_attend")

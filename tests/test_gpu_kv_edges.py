@@ -141,3 +141,55 @@ def test_plan_of_no_requests_writes_what_is_asked_for(ctx):  # noqa: F811
                            None) == ivf.IVF_OK
     assert lib.ivf_kv_plan(handle, None, None, 0, 16, None, 0, None, 0, 0, None, None, None, None, None) == ivf.IVF_OK
     assert start.tolist() == [0, 77, 77]
+
+
+USES = {"plan": ("cached", "added", "table", "free"), "append": ("k", "v", "slots"), "read": ("slots", "free"),
+        "select": ("q", "request", "position", "table"),
+        "attend": ("q", "start", "request", "position", "table", "blocks", "out", "lse")}
+
+
+def arguments():
+    """Tensors for a call each on a cache of 4 blocks of 16 tokens, 2 heads of 64 channels."""
+    import torch
+
+    return {"q": queries(3, 4, 64, "bf16", 1), "k": queries(3, 2, 64, "bf16", 2), "v": queries(3, 2, 64, "bf16", 3),
+            "slots": dev(np.arange(3, dtype=np.int64)), "start": ints([0, 3]), "request": ints([0, 0, 0]),
+            "position": ints([0, 1, 2]), "table": ints([[0, 1]]), "blocks": ints(np.zeros((3, 2, 1))),
+            "cached": ints([0]), "added": ints([3]), "free": ints([1]),
+            "out": torch.empty(3, 4, 64, device="cuda", dtype=torch.bfloat16), "lse": torch.empty(3, 4, device="cuda")}
+
+
+def call(name, ctx, cache, a):  # noqa: F811
+    import paper_2608_08751_amd as ivf
+
+    if name == "plan":
+        ivf.ivf_kv_plan(ctx, a["cached"], a["added"], 16, a["table"], a["free"], 3)
+    elif name == "append":
+        ivf.ivf_kv_append(ctx, cache, a["k"], a["v"], a["slots"])
+    elif name == "read":
+        ivf.ivf_kv_read(ctx, cache, a["slots"], a["free"])
+    elif name == "select":
+        ivf.ivf_kv_select(ctx, cache, a["q"], a["request"], a["position"], a["table"], 2)
+    else:
+        ivf.ivf_kv_attend(ctx, cache, a["q"], a["start"], a["request"], a["position"], a["table"], 0.1, 3,
+                          blocks=a["blocks"], out=a["out"], out_lse=a["lse"])
+
+
+def test_tensors_of_another_device_are_refused(ctx):  # noqa: F811
+    # arguments on the host; all of device 0 with a context that says it is device 1's
+    import paper_2608_08751_amd as ivf
+
+    cache = ivf.KVCache.empty(4, 2, 64, 16, dtype_of("bf16"))
+    other = ivf.Context(0)
+    other.device = 1
+    for name, used in USES.items():
+        good = arguments()
+        call(name, ctx, cache, good)
+        with pytest.raises((TypeError, ValueError), match="device"):
+            call(name, other, cache, good)
+        for x in used:
+            with pytest.raises((TypeError, ValueError), match="device"):
+                call(name, ctx, cache, {**good, x: good[x].cpu()})
+    other.close()
+    with pytest.raises(ValueError, match="device"):
+        ivf.KVCache(cache.records, cache.summary, cache.weight.cpu(), 16, dtype_of("bf16"))
