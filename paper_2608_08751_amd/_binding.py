@@ -574,10 +574,15 @@ def _same_device(ctx, cache):
 
 def _rows(ctx, t, name, cache, heads=None):
     """(pointer, token stride, head stride) of rows [tokens, heads, dim]."""
+    import torch
+
     _same_device(ctx, cache)
     if t.get_device() != ctx.device or t.dtype != cache.dtype:
         raise TypeError("%s must be of the cache's type %s on device %d, got %s on %s" % (
             name, cache.dtype, ctx.device, t.dtype, t.device))
+    if t.requires_grad and torch.is_grad_enabled():
+        raise RuntimeError("%s requires a gradient, and the cache's calls have no backward pass: detach it, or call "
+                           "under torch.no_grad()" % name)
     shape = t.shape
     if len(shape) != 3 or shape[2] != cache.dim or (heads is not None and shape[1] != heads):
         raise ValueError("%s must be [tokens, %s, %d], got %s" % (name, heads or "heads", cache.dim, tuple(shape)))

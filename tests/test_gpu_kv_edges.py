@@ -193,3 +193,18 @@ def test_tensors_of_another_device_are_refused(ctx):  # noqa: F811
     other.close()
     with pytest.raises(ValueError, match="device"):
         ivf.KVCache(cache.records, cache.summary, cache.weight.cpu(), 16, dtype_of("bf16"))
+
+
+@pytest.mark.parametrize("name,x", [("select", "q"), ("attend", "q"), ("append", "k"), ("append", "v")])
+def test_rows_that_require_a_gradient_are_refused(ctx, name, x):  # noqa: F811
+    import torch
+
+    import paper_2608_08751_amd as ivf
+
+    cache = ivf.KVCache.empty(4, 2, 64, 16, dtype_of("bf16"))
+    a = arguments()
+    a[x] = a[x].clone().requires_grad_()
+    with pytest.raises(RuntimeError, match="gradient"):
+        call(name, ctx, cache, a)
+    with torch.no_grad():
+        call(name, ctx, cache, a)
