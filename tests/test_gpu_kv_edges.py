@@ -208,3 +208,32 @@ def test_rows_that_require_a_gradient_are_refused(ctx, name, x):  # noqa: F811
         call(name, ctx, cache, a)
     with torch.no_grad():
         call(name, ctx, cache, a)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("form", ["tokens", "prompt", "selected"])
+def test_key_ranges_whole_and_in_parts(ctx, kind, form):  # noqa: F811
+    # the same rows with a short table (or list of blocks), whole, and with one padded far beyond it, in parts
+    import paper_2608_08751_amd as ivf
+
+    heads, group, dim, bs = 2, 4, 64, 16
+    lens, new = ([200], [100]) if form == "prompt" else ([900, 3, 960], [1, 1, 1])
+    cache, table, keys, values = make(ctx, kind, lens, heads, dim, bs, 96)
+    start, request, position = batch(lens, new)
+    T, B = len(request), len(lens)
+    q = queries(T, heads * group, dim, kind, 97)
+    wide = np.pad(table, ((0, 0), (0, 4000 - table.shape[1])), constant_values=-1)
+    short, long = None, None
+    if form == "selected":
+        short = np.full((T, heads, 20), -1, np.int32)
+        for t, p in enumerate(position):
+            kept = np.random.default_rng(t).permutation(p // bs + 1)[:18]
+            short[t, :, : len(kept)] = np.sort(kept)
+        long = np.pad(short, ((0, 0), (0, 0), (0, 300)), constant_values=-1)
+    want, want_lse = M.attend(as_np(q), keys, values, heads, request, position, table, bs, 0.125, short)
+    for t, blocks, parts in ((table, short, False), (table if form == "selected" else wide, long, True)):
+        need = cache.attend_bytes(ctx, heads * group, T, B, t.shape[1], 0 if blocks is None else blocks.shape[2], max(new))
+        assert (need > 0) == parts
+        out, lse = ivf.ivf_kv_attend(ctx, cache, q, ints(start), ints(request), ints(position), ints(t), 0.125, max(new),
+                                     blocks=None if blocks is None else ints(blocks))
+        check_attend(out, lse, want, want_lse, kind, np.nanmax(np.abs(values)), 50.0)
