@@ -91,14 +91,22 @@ def _ptr(t):
     return ctypes.c_void_p(t.data_ptr()) if t is not None else None
 
 
-def _stream_handle(device=None):
-    import torch
+_raw_stream = None
 
-    # torch.cuda.current_stream() builds a Stream object (3 us); the raw query is 0.1 us
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    if raw is not None:
-        return raw(torch.cuda.current_device() if device is None else device)
-    return torch.cuda.current_stream(device).cuda_stream
+
+def _stream_handle(device=None):
+    global _raw_stream
+    if _raw_stream is None:
+        import torch
+
+        # torch.cuda.current_stream() builds a Stream object (3 us); the raw query is 0.1 us
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
+                              lambda device: torch.cuda.current_stream(device).cuda_stream)
+    if device is None:
+        import torch
+
+        device = torch.cuda.current_device()
+    return _raw_stream(device)
 
 
 class Context:
@@ -567,20 +575,21 @@ class KVCache:
 KVPlan = collections.namedtuple("KVPlan", "start slots request position info")
 
 
-def _same_device(ctx, cache):
-    if cache.device != ctx.device:
-        raise TypeError("the cache must be on the context's device %d, is on %s" % (ctx.device, cache.records.device))
+def _grad_enabled():
+    import torch
+
+    return torch.is_grad_enabled()
 
 
 def _rows(ctx, t, name, cache, heads=None):
     """(pointer, token stride, head stride) of rows [tokens, heads, dim]."""
-    import torch
-
-    _same_device(ctx, cache)
-    if t.get_device() != ctx.device or t.dtype != cache.dtype:
+    device = ctx.device
+    if cache.device != device:
+        raise TypeError("the cache must be on the context's device %d, is on %s" % (device, cache.records.device))
+    if t.get_device() != device or t.dtype != cache.dtype:
         raise TypeError("%s must be of the cache's type %s on device %d, got %s on %s" % (
-            name, cache.dtype, ctx.device, t.dtype, t.device))
-    if t.requires_grad and torch.is_grad_enabled():
+            name, cache.dtype, device, t.dtype, t.device))
+    if t.requires_grad and _grad_enabled():
         raise RuntimeError("%s requires a gradient, and the cache's calls have no backward pass: detach it, or call "
                            "under torch.no_grad()" % name)
     shape = t.shape
@@ -657,7 +666,8 @@ def ivf_kv_read(ctx: Context, cache: KVCache, slots, blocks=None):
     and, of `blocks` (int32 [n]), the key means [n, heads, dim] fp32 (else None)."""
     import torch
 
-    _same_device(ctx, cache)
+    if cache.device != ctx.device:
+        raise TypeError("the cache must be on the context's device %d, is on %s" % (ctx.device, cache.records.device))
     T = slots.shape[0]
     k = torch.empty(T, cache.heads, cache.dim, dtype=cache.dtype, device=slots.device)
     v = torch.empty_like(k)
