@@ -590,8 +590,14 @@ ivf_status ivf_kv_select(ivf_ctx *ctx, const ivf_kv_cache *cache, const void *q,
  * names), with `blocks` only those of the blocks listed for its token and
  * key/value head (entries outside [0, table_cols) list nothing; a block
  * listed twice counts twice).
- *   out = sum_j softmax_j(scale * q.k_j) v_j, sums in fp32, probabilities
- *   rounded to the cache's type for their product with the values.
+ *   out = sum_j softmax_j(scale * q.k_j) v_j, sums in fp32 (a score beyond its
+ *   range is an infinity, and -infinity counts as masked), probabilities
+ *   rounded to the cache's type for their product with the values; their sum
+ *   is of the unrounded ones. Without `blocks`, requests of more than 64 rows
+ *   (tokens times q_heads / heads) take the query as it is; all other rows
+ *   take its channels as fixed-point numbers, off by at most 2^-19 of the
+ *   largest of their 32, so that a query's scores may differ by that much with
+ *   the number of tokens beside it.
  *   scale    of magnitude below 2.3e38
  *   start    [B + 1] int32, request, position [T] int32 as in ivf_kv_plan;
  *            with `blocks` the requests' ranges are not read, without it

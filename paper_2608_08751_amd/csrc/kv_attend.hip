@@ -8,17 +8,26 @@
 //     are its A operand as they lie in memory, 16 bytes of codes and a scale byte a lane.
 //     The query is the sum of four 6-bit numbers a channel with a power of two per
 //     32 channels: digits of a fixed-point number, off by 2^-19 of the largest of the 32 at
-//     most (numbers of 8 significant bits: exact down to 2^-11 of it, of 11 bits to 2^-8).
+//     most (numbers of 8 significant bits: exact down to 2^-11 of it, of 11 bits to 2^-8). A choice: keys
+//     decoded to 16 bits would take the query as it is (the prompt kernel's do), at four vector
+//     instructions more for 8 channels of a key; scores are off by 2e-7 of sum |q k|, far less than the
+//     probabilities' rounding.
 //   * values: O^T = V^T P^T on v_mfma_f32_16x16x32. The results above are the B operand as
 //     they are: lane (r, h)'s eight probabilities of two strips are keys 4 h ... 4 h + 3 of each.
 //     It reads the codes of neighbouring channels of those keys, v_cvt_scalef32 makes pairs of
-//     channels with the key's scale, v_perm_b32 pairs of keys.
+//     channels with the key's scale, v_perm_b32 pairs of keys. Probabilities are rounded to the
+//     cache's type, which is what this product takes; a second product with what the rounding leaves
+//     would double the matrix work of the values and take away a sixth of the error (relative to fp64:
+//     bf16 0.0020, of which the outputs' own rounding alone makes 0.0017; f16 0.00026 and 0.00021). The sum of
+//     the probabilities is of the unrounded ones.
 //   * with selected blocks and up to 8 rows (PACK), which leave half of the 16 columns free,
 //     column r + 8 is row r again: columns below 8 take the exponentials of the first strip of a
 //     step and the others those of the second, each with a reference, sum and output of its
-//     own, joined at the end (512 tokens x 8 heads over 24 blocks of 64 keys, 64 channels 71.6 us and 73.4
-//     without, 256 channels 219 and 230). Whole contexts are bound by memory, and the joining costs more than
-//     it gives: one request of 700 keys x 128 channels 10.6 us with it, 9.6 without.
+//     own, joined at the end. 512 tokens x 8 heads over 24 blocks of 64 keys, with it and without, caches cold:
+//     64, 96, 128, 192, 256 channels 81.3 and 84.9, 104 and 108, 99.7 and 102, 210 and 214, 238 and 245 us; 32 single
+//     tokens over 64 blocks: 38.8 and 36.6, 52.2 and 49.0, 66.3 and 65.5, 89.1 and 92.2, 112 and 115 us. Whole contexts
+//     are bound by memory, and the joining costs more than it gives: one request of 700 keys x 128 channels
+//     10.6 us with it, 9.6 without.
 //   * the reference is raised only when a lane's probabilities of a step sum to more than
 //     2^14, for all rows of the wave at once, so the common step needs no maximum
 //     and no exchange between lanes. Probabilities carry 2^8, which keeps small ones normal in f16.
@@ -28,11 +37,14 @@
 // A team of 1, 4 or 8 waves takes a range of steps of 32 keys, each wave every 1st, 4th or 8th
 // step with its own reference, sums and output, joined in LDS. What bounds single tokens is
 // the read of the cache, 17 / 16 bytes per channel of key and value: 64 requests of up to 32,000
-// tokens, 8 heads x 128, 915 MB: 167 us and 6 for joining, 5.3 TB/s (a large copy 5.2). Many tokens with
+// tokens, 8 heads x 128, 912 MB: 173 us with the joining, 5.3 TB/s (a plain read of 8 GB 6.0; calls one after the
+// other 186 us and 8). 256 channels hold one wave a SIMD, with accumulation registers to spill into: 949 MB 222 us
+// and 7. Many tokens with
 // blocks of their own are bound by the decoding of values, a vector instruction a value with its
 // share of scales, 1/4 of which serve a query row where a group is four rows: 2,048
-// tokens x 8 heads over 24 blocks of 64 keys 287 us, vector units 77 % and matrix
-// units 29 % busy, 11 TB/s from L2.
+// tokens x 8 heads over 24 blocks of 64 keys 286 us (calls one after the other 343), vector units 77 % and matrix
+// units 29 % busy, 11 TB/s from L2. Its launch bound of three waves a SIMD costs one or two spilled registers at
+// 128 channels.
 #include "kv.h"
 #include "kv_strip.h"
 
@@ -613,12 +625,14 @@ template <typename TT> hipError_t launch_tokens_dim(const KvAttend &a, int64_t g
 }
 
 // Requests with at most this many rows go through the single-token kernel, 16 rows a
-// workgroup, others through the prompt kernel (8 requests of 32 rows after 4,000 tokens, 8 heads x 128: 32 us
-// here, 107 there; of 64 rows 36 and 72; one request of 64 rows 22 and 21, of 128 rows 24 and 23).
+// workgroup, others through the prompt kernel. After 4,000 tokens, 8 heads x 128, caches cold, here and there, for 64,
+// 128, 256 and 512 rows: one request 28.0 and 30.8, 30.0 and 35.4, 35.9 and 47.1, 47.1 and 44.5 us; 8 requests 51.8
+// and 72.4, 75.6 and 69.5, 117 and 80.0, 202 and 151; 32 requests 134 and 157, 222 and 237, 357 and 175, 679 and 323. So
+// the two cross between 64 and 256 rows, later for one request, of which the limit takes no note.
 constexpr int64_t kSmallRows = 64;
 
 // Tables of at most this many keys are not shared out: joining parts costs a launch and the prefix
-// sums. `all` units of one token, 8 heads x 128, lengths drawn up to the limit, shared out and not: 8 units,
+// sums. Measured at 128 channels, and taken for every width. `all` units of one token, 8 heads x 128, lengths drawn up to the limit, shared out and not: 8 units,
 // 2,048 keys 12.2 and 15.1 us; 32 units, 2,048 keys 16.6 and 14.2, 4,096 keys 17.0 and 20.0; 128 units, 4,096
 // keys 26.4 and 22.5; 1,024 units, 4,096 keys 82 and 79.
 constexpr int64_t whole_keys(int64_t all) { return all < 32 ? 1024 : all < 128 ? 2048 : 4096; }

@@ -8,10 +8,10 @@
 // bytes a request to read, from L2) and then takes its share of the tokens,
 // each of which finds its request by bisection, and of the table rows. What it
 // writes, 16 bytes a token and the tables, bounds a large call; a small one is
-// one launch long: 16 requests of one token 4.7 us, 2,000 requests with 300
-// prompts of up to 700 tokens (149,000 tokens, 4.5 MB) 11.4 us.
+// one launch long: 16 requests of one token 4.8 us, 2,000 requests with 300
+// prompts of up to 700 tokens (149,000 tokens, 4.5 MB) 11.7 us.
 // Up to 2,048 requests 256 threads hold 8 each; with 1,024 threads of 16, which
-// 16,384 requests need, 16 requests take 8.3 us and 2,000 take 11.1 instead of 8.7.
+// 16,384 requests need, these two calls take 8.2 and 13.0 us.
 #include "kv.h"
 
 #include <algorithm>

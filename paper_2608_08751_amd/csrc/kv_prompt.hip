@@ -13,8 +13,11 @@
 // slots a score, four of them the exponential): 64 keys x 32 rows x 128 channels
 // take 64 products of 16 cycles and about 340 vector issues of 4 (46 % and 48 % of the
 // time, hardly at once). 2,048 tokens after
-// 8,192, 32 query heads on 8 of 128 channels: 306 us, 1,011 TFLOP/s, 89 % of what a
-// bf16 product of 8,192^3 reaches here.
+// 8,192, 32 query heads on 8 of 128 channels: 304 us, 1,020 TFLOP/s, 92 % of what one
+// bf16 product of 8,192^3 reaches here; calls one after the other 358 us, 64 % of such products
+// (1,340 TFLOP/s). 256 channels: 1,370 us, 450 TFLOP/s: an operand from LDS serves one product of 16 rows, and
+// one wave a SIMD has nothing to do meanwhile (matrix units 19 %, vector units 21 % busy).
+// Probabilities are rounded to the cache's type, as in the single-token kernel.
 #include "kv.h"
 #include "kv_strip.h"
 
@@ -24,8 +27,8 @@
 namespace ivf {
 namespace {
 
-// D <= 128: eight waves, 32 rows each (four waves over tiles of 64 keys: 327 us instead of
-// the 306 above); wider: four waves of 16 rows (registers, LDS).
+// D <= 128: eight waves, 32 rows each (four waves over tiles of 64 keys: 327 us where this took
+// 306); wider: four waves of 16 rows (registers, LDS).
 template <int D> struct PromptShape {
     static constexpr int waves = D <= 128 ? 8 : 4, ct = D <= 128 ? 2 : 1;
     static constexpr int threads = 64 * waves, rows = 16 * ct * waves;

@@ -15,7 +15,7 @@
 // request share every summary through v_mfma_i32_16x16x64_i8, each wave then selects
 // for its own tokens. Both keep the keys in LDS.
 //
-// 32 tokens x 8 heads over up to 1,016 blocks of 128 channels take 12 us, of which the
+// 32 tokens x 8 heads over up to 1,016 blocks of 128 channels take 13 us, of which the
 // scores (17 MB of summaries) are a third and the rounds of the selection the rest;
 // 2,048 tokens x 8 heads over 1,000 blocks of 96 channels 55 us, bound by the selection's
 // vector instructions (16,384 times the best 48 of 1,000; the products are 4 us).
@@ -197,7 +197,8 @@ __device__ __forceinline__ void select_best(const uint32_t (&k)[KPT], int wave, 
         // The first trial value is where a normal
         // distribution of the scores' mean and variance has `want` keys above, the next ones step away
         // from it until both sides are known, then the bracket is halved by value (by key where
-        // that leaves it): about seven counts, where halving the keys' range takes twenty.
+        // that leaves it): for the best 45 of 1,000 normal scores 6.8 counts on average, at most 11 in 95 of
+        // 100 (of 400, run on the host), where halving the keys' range takes 16.5.
         auto over_waves = [&](float x) { return sum_waves<float, WAVES>(ex, turn, wave, wave_sum(x)); };
         const float per = __builtin_amdgcn_rcpf(over_waves(count_s)), mean = over_waves(sum) * per;
         const float sigma = __builtin_amdgcn_sqrtf(fmaxf(over_waves(squares) * per - mean * mean, 0.f));
