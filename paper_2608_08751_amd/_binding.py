@@ -710,7 +710,8 @@ def ivf_kv_attend(ctx: Context, cache: KVCache, q, start, request, position, tab
     """Attention of queries q [T, query heads, dim] over their requests' tokens in
     the cache, or over the selected `blocks` (int32 [T, heads, count]) only:
     outputs like q and the log-sum-exps fp32 [T, query heads]. `longest` is at
-    least the largest number of tokens that one request has in the batch."""
+    least the largest number of tokens that one request has in the batch. Without
+    `blocks`, rows past start[B] (padding of the batch) are left unwritten."""
     import torch
 
     i32 = torch.int32

@@ -237,3 +237,42 @@ def test_key_ranges_whole_and_in_parts(ctx, kind, form):  # noqa: F811
         out, lse = ivf.ivf_kv_attend(ctx, cache, q, ints(start), ints(request), ints(position), ints(t), 0.125, max(new),
                                      blocks=None if blocks is None else ints(blocks))
         check_attend(out, lse, want, want_lse, kind, np.nanmax(np.abs(values)), 50.0)
+
+
+@pytest.mark.parametrize("new", [3, 70])  # the single-token kernel, the prompt kernel
+@pytest.mark.parametrize("scale", [0.0, -0.0, 1e-45])
+def test_scales_of_zero(ctx, new, scale):  # noqa: F811
+    # every key that a row sees weighs the same, a masked one nothing
+    n, heads, bs = new + 90, 2, 16
+    cache, table, keys, values = make(ctx, "bf16", [n], heads, 64, bs, 98)
+    start, request, position = batch([n], [new])
+    position[1] = -1
+    table[0, 2] = -1
+    q = queries(new, 2 * heads, 64, "bf16", 99)
+    attend_held(ctx, "bf16", cache, table, keys, values, start, request, position, q, bs, scale, new)
+
+
+@pytest.mark.parametrize("new", [3, 70])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_scores_beyond_fp32(ctx, new, dim):  # noqa: F811
+    # of magnitude 2^200: -infinity counts as masked, +infinity is no number
+    import paper_2608_08751_amd as ivf
+
+    n, bs, big = new + 20, 16, 2.0**100
+    kv = np.full((n, 2, 1, dim), big)
+    kv[:, 1] = np.random.default_rng(dim).standard_normal((n, 1, dim))
+    kv[5, 0] = 0.0  # a key whose score is 0
+    kv = dev(kv.astype(np.float32), dtype_of("bf16"))
+    cache = ivf.KVCache.empty(-(-n // bs), 1, dim, bs, dtype_of("bf16"))
+    ivf.ivf_kv_append(ctx, cache, kv[:, 0], kv[:, 1], dev(np.arange(n, dtype=np.int64)))
+    _, v = M.store(as_np(kv[:, 0]), as_np(kv[:, 1]), "bf16")
+    start, request, position = batch([n], [new])
+    position[1] = 4  # does not see it
+    q = np.full((new, 2, dim), -big, np.float32)
+    q[2, 1] = big
+    out, lse = ivf.ivf_kv_attend(ctx, cache, dev(q, dtype_of("bf16")), ints(start), ints(request), ints(position),
+                                 ints(np.arange(-(-n // bs))[None]), 1.0, new)
+    want, want_lse = np.tile(v[5, 0], (new, 2, 1)), np.zeros((new, 2))
+    want[1], want_lse[1] = 0.0, -np.inf
+    want[2, 1], want_lse[2, 1] = np.nan, np.nan
+    check_attend(out, lse, want, want_lse, "bf16", np.abs(v).max(), 1.0)
