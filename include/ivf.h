@@ -541,6 +541,62 @@ ivf_status ivf_kv_plan(ivf_ctx *ctx, const int32_t *cached, const int32_t *added
                        int64_t *out_slots, int32_t *out_request, int32_t *out_position,
                        int64_t *out_info);
 
+/* Requests that go on from another's tokens (several samples of one prompt,
+ * beams): fork i makes row child[i] of the table a copy of row parent[i],
+ * with cached[child[i]] = cached[parent[i]]. The blocks are shared but for the
+ * last one, where that is partly filled: in its place the child gets the next
+ * of free_blocks (forks in order; -1 where they do not suffice), and the pair
+ * (out_source[i], out_to[i]) says what ivf_kv_copy has to copy in every cache that
+ * the table serves (-1, -1: nothing). Columns past the tokens become -1.
+ *   parent, child [n] int32, n <= 16384: rows. A fork whose rows are the same
+ *               or outside [0, B), whose child a later such fork names too, or
+ *               is the parent of one, is left out: it changes nothing and its
+ *               pair is (-1, -1).
+ *   cached      [B] int32 tokens that requests have, updated; B <= 16384
+ *   table       [B][table_cols] int32, updated
+ *   out_source, out_to [n] int32
+ *   out_info    [2] int64: blocks asked for, blocks taken; may be NULL
+ * A parent's last block without a table entry stays without one.
+ * Errors: as ivf_kv_plan. */
+ivf_status ivf_kv_fork(ivf_ctx *ctx, const int32_t *parent, const int32_t *child, int64_t n, int32_t *cached,
+                       int64_t B, int32_t block_size, int32_t *table, int32_t table_cols,
+                       const int32_t *free_blocks, int64_t n_free, int32_t *out_source, int32_t *out_to,
+                       int64_t *out_info);
+
+/* Copies whole blocks: block source[i] of source_cache becomes block to[i] of
+ * cache, keys, values and summary, for n pairs. A pair with a block outside its
+ * cache (-1) is skipped. The caches may be one; they differ in `blocks` at
+ * most. Where a block is written by two pairs, or written by one and read by another, what
+ * the written one holds afterwards is unspecified.
+ * Errors: as ivf_kv_append. */
+ivf_status ivf_kv_copy(ivf_ctx *ctx, const ivf_kv_cache *cache, const ivf_kv_cache *source_cache,
+                       const int32_t *to, const int32_t *source, int64_t n);
+
+/* The blocks that no request holds, and moving those together that requests
+ * hold. Request b holds the blocks that the first ceil(cached[b] / block_size)
+ * columns of its table row name (a request that has ended: cached[b] = 0 or
+ * less); a block may be held by several, and entries outside [0, blocks) hold
+ * nothing. Let U blocks be held. Up to `moves` of those with numbers from U on,
+ * lowest first, move into the free numbers below U, lowest first: the table's
+ * entries for them are changed (those that requests hold), and ivf_kv_copy has
+ * to copy the pairs (out_source[i], out_to[i]) in every cache that the table
+ * serves, before out_free is used. With as many moves as there are such blocks the
+ * held ones are 0 ... U - 1 afterwards.
+ *   cached      [B] int32        table [B][table_cols] int32, updated
+ *   out_free    [blocks] int32: the blocks that are free after the moves,
+ *               ascending, -1 behind them; may be NULL
+ *   out_source, out_to [moves] int32, -1 behind the pairs; NULL when moves is 0
+ *   out_info    [3] int64: U, moves made, blocks - U; may be NULL
+ * B = 0: all are free, cached and table may be NULL.
+ * Workspace: ivf_kv_reclaim_bytes() (0 for small tables).
+ * Errors: as ivf_kv_plan, IVF_ENOMEM. */
+ivf_status ivf_kv_reclaim(ivf_ctx *ctx, const int32_t *cached, int64_t B, int32_t block_size, int32_t *table,
+                          int32_t table_cols, int64_t blocks, int64_t moves, int32_t *out_free,
+                          int32_t *out_source, int32_t *out_to, int64_t *out_info);
+
+/* Workspace of ivf_kv_reclaim (0 where it needs none, or for arguments that it refuses). */
+size_t ivf_kv_reclaim_bytes(int64_t B, int32_t block_size, int32_t table_cols, int64_t blocks, int64_t moves);
+
 /* Writes T tokens into the cache at slots[t] (distinct; a slot outside the
  * cache is skipped) and the summaries of the blocks whose last slot is among
  * them.

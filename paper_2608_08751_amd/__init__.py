@@ -11,7 +11,10 @@ and the benchmark:
 * ``ivf_build_lists``   the inverted-list build alone;
 * ``ivf_kv_plan``, ``ivf_kv_append``, ``ivf_kv_read``, ``ivf_kv_select``, ``ivf_kv_attend``
                         a paged key/value cache held in 4 bits (``KVCache``): its tables, writing
-                        and reading it, the blocks that queries select, attention over it.
+                        and reading it, the blocks that queries select, attention over it;
+* ``ivf_kv_fork``, ``ivf_kv_copy``, ``ivf_kv_reclaim``
+                        requests that share a context's blocks, copies of blocks, the free blocks
+                        and moving the others together.
 """
 from ._binding import (  # noqa: F401
     IVF_BF16,
@@ -45,7 +48,9 @@ from ._binding import (  # noqa: F401
     Context,
     IvfError,
     KVCache,
+    KVFork,
     KVPlan,
+    KVReclaim,
     ivf_assign_build,
     ivf_adc_scan,
     ivf_assign_cells,
@@ -54,8 +59,11 @@ from ._binding import (  # noqa: F401
     ivf_kmeans_step,
     ivf_kv_append,
     ivf_kv_attend,
+    ivf_kv_copy,
+    ivf_kv_fork,
     ivf_kv_plan,
     ivf_kv_read,
+    ivf_kv_reclaim,
     ivf_kv_select,
     ivf_list_major,
     ivf_pq_encode,

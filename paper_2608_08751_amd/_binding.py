@@ -51,6 +51,10 @@ SIGNATURES = [
     ("ivf_adc_scan", _INT, [_P, _P, _I64, _I32, _P, _I64, _P, _I32, _P, _P, _I64, _P, _I32, _P, _I32, _P, _P]),
     ("ivf_pq_train_step", _INT, [_P, _P, _I64, _I32, _I32, _P, _U64, _I32, _P, _P, _P]),
     ("ivf_kv_plan", _INT, [_P, _P, _P, _I64, _I32, _P, _I32, _P, _I64, _I64, _P, _P, _P, _P, _P]),
+    ("ivf_kv_fork", _INT, [_P, _P, _P, _I64, _P, _I64, _I32, _P, _I32, _P, _I64, _P, _P, _P]),
+    ("ivf_kv_copy", _INT, [_P, _P, _P, _P, _P, _I64]),
+    ("ivf_kv_reclaim", _INT, [_P, _P, _I64, _I32, _P, _I32, _I64, _I64, _P, _P, _P, _P]),
+    ("ivf_kv_reclaim_bytes", _SZ, [_I64, _I32, _I32, _I64, _I64]),
     ("ivf_kv_append", _INT, [_P, _P, _P, _I64, _I64, _P, _I64, _I64, _P, _I64]),
     ("ivf_kv_read", _INT, [_P, _P, _P, _I64, _P, _P, _P, _I64, _P]),
     ("ivf_kv_select", _INT, [_P, _P, _P, _I64, _I64, _I32, _I64, _P, _P, _P, _I64, _I32, _I32, _I32, _I32, _P]),
@@ -573,6 +577,8 @@ class KVCache:
 
 
 KVPlan = collections.namedtuple("KVPlan", "start slots request position info")
+KVFork = collections.namedtuple("KVFork", "source to info")
+KVReclaim = collections.namedtuple("KVReclaim", "free source to info")
 
 
 def _grad_enabled():
@@ -644,6 +650,78 @@ def ivf_kv_plan(ctx: Context, cached, added, block_size: int, table, free_blocks
     if st:
         ctx.check(st, "ivf_kv_plan")
     return KVPlan(start, slots.view(torch.int64), request, position, info)
+
+
+def ivf_kv_fork(ctx: Context, parent, child, cached, block_size: int, table, free_blocks, want_info: bool = False):
+    """Requests that go on from another's tokens: rows child (int32 [n]) of `table`
+    (int32 [B, columns]) and `cached` (int32 [B]) become those of `parent`, in place, a
+    partly filled last block replaced by one of free_blocks (int32, taken in order).
+    Returns KVFork(source [n], to [n], info int64 [2] or None): the pairs that
+    ivf_kv_copy has to copy, -1 where there is nothing to copy."""
+    import torch
+
+    i32 = torch.int32
+    shape = table.shape
+    if len(shape) != 2:
+        raise ValueError("table must be [requests, columns], got %s" % (tuple(shape),))
+    n, n_free = parent.numel(), free_blocks.numel()
+    ins = (_ints(ctx, parent, "parent", (n,), i32), _ints(ctx, child, "child", (n,), i32), n,
+           _ints(ctx, cached, "cached", shape[:1], i32), shape[0], block_size, _ints(ctx, table, "table", shape, i32),
+           shape[1], _ints(ctx, free_blocks, "free_blocks", (n_free,), i32), n_free)
+    source, to = torch.unsafe_split_with_sizes(torch.empty(2 * n, dtype=i32, device=table.device), (n, n))
+    info = torch.empty(2, dtype=torch.int64, device=table.device) if want_info else None
+    lib, handle = ctx.bind()
+    st = lib.ivf_kv_fork(handle, *ins, source.data_ptr(), to.data_ptr(), info.data_ptr() if want_info else None)
+    if st:
+        ctx.check(st, "ivf_kv_fork")
+    return KVFork(source, to, info)
+
+
+def ivf_kv_copy(ctx: Context, cache: KVCache, to, source, source_cache: KVCache | None = None):
+    """Copies blocks `source` (int32 [n]) of source_cache (default: the cache
+    itself) into blocks `to` (int32 [n]) of cache. Pairs of -1 are skipped."""
+    import torch
+
+    other = cache if source_cache is None else source_cache
+    for c in (cache, other):
+        if c.device != ctx.device:
+            raise TypeError("the cache must be on the context's device %d, is on %s" % (ctx.device, c.records.device))
+    n = to.numel()
+    args = _ints(ctx, to, "to", (n,), torch.int32), _ints(ctx, source, "source", (n,), torch.int32), n
+    lib, handle = ctx.bind()
+    st = lib.ivf_kv_copy(handle, cache.ref, other.ref, *args)
+    if st:
+        ctx.check(st, "ivf_kv_copy")
+
+
+def ivf_kv_reclaim(ctx: Context, cached, block_size: int, table, blocks: int, moves: int = 0):
+    """The blocks (of `blocks`) that no request holds: request b holds those of the
+    first ceil(cached[b] / block_size) columns of its row of `table` (int32 [B, columns]).
+    With `moves`, up to so many held blocks are first moved into free ones of lower
+    numbers, in `table`. Returns KVReclaim(free [blocks] ascending, -1 behind them,
+    source [moves], to [moves]: the pairs that ivf_kv_copy has to copy before the free
+    blocks are used, -1 behind them, info int64 [3]: blocks held, moves made, blocks free)."""
+    import torch
+
+    i32 = torch.int32
+    shape = table.shape
+    if len(shape) != 2:
+        raise ValueError("table must be [requests, columns], got %s" % (tuple(shape),))
+    if moves < 0 or blocks < 1:
+        raise ValueError("blocks >= 1 and moves >= 0 are wanted, got %d and %d" % (blocks, moves))
+    B, cols = shape
+    ins = (_ints(ctx, cached, "cached", (B,), i32), B, block_size, _ints(ctx, table, "table", shape, i32), cols, blocks, moves)
+    whole = torch.empty(6 + blocks + 2 * moves, dtype=i32, device=table.device)  # info (two words each) comes first
+    info, free, source, to = torch.unsafe_split_with_sizes(whole, (6, blocks, moves, moves))
+    need = ctx.lib.ivf_kv_reclaim_bytes(B, block_size, cols, blocks, moves)
+    if need:
+        ctx.ensure_workspace(need)
+    at = whole.data_ptr()
+    lib, handle = ctx.bind()
+    st = lib.ivf_kv_reclaim(handle, *ins, at + 24, at + 24 + 4 * blocks, at + 24 + 4 * (blocks + moves), at)
+    if st:
+        ctx.check(st, "ivf_kv_reclaim")
+    return KVReclaim(free, source, to, info.view(torch.int64))
 
 
 def ivf_kv_append(ctx: Context, cache: KVCache, k, v, slots):

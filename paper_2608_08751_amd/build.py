@@ -19,7 +19,7 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libivf.so")
 
 SOURCES = ["api.cpp", "screen.hip", "screen_i8.hip", "screen_f16.hip", "select.hip", "fallback.hip", "resolve.hip", "lists.hip", "lists_radix.hip", "kmeans.hip", "layout.hip", "pq.hip", "assign_graph.hip", "adc.hip", "probe.hip",
-           "api_kv.cpp", "kv_plan.hip", "kv_cache.hip", "kv_select.hip", "kv_attend.hip", "kv_prompt.hip"]
+           "api_kv.cpp", "kv_plan.hip", "kv_pages.hip", "kv_cache.hip", "kv_select.hip", "kv_attend.hip", "kv_prompt.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

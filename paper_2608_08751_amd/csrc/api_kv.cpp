@@ -14,28 +14,9 @@ using namespace ivf;
 
 namespace {
 
-// Runs f(); what a C++ library throws on the host becomes a status.
-template <typename F> ivf_status guarded(ivf_ctx *ctx, const char *call, F f)
-{
-    if (!ctx) return IVF_EINVAL;
-    try {
-        ctx->err.clear();
-        ctx->cur_call = call;
-        return f();
-    } catch (...) {
-        return IVF_EDEVICE;
-    }
-}
-
 int block_shift(int32_t bs) { return bs == 16 ? 4 : bs == 32 ? 5 : bs == 64 ? 6 : bs == 128 ? 7 : 0; }
 
 bool kv_dim(int32_t d) { return d == 64 || d == 96 || d == 128 || d == 192 || d == 256; }
-
-// The cache's arrays for overlap checks.
-struct Span {
-    const void *p;
-    size_t n;
-};
 
 ivf_status check_cache(ivf_ctx *ctx, const ivf_kv_cache *c, KvCache &k)
 {
@@ -70,14 +51,6 @@ bool overlaps_cache(const KvCache &c, const void *p, size_t n)
            overlap(p, n, c.weight, bh * 4);
 }
 
-// Arrays of whole numbers and fp32 outputs lie at multiples of their elements.
-template <int N> ivf_status check_elements(ivf_ctx *ctx, const void *const (&p)[N], size_t element)
-{
-    for (const void *x : p)
-        if ((uintptr_t)x % element) return fail(ctx, IVF_EINVAL, "arrays must be aligned to their elements");
-    return IVF_OK;
-}
-
 // Rows [T][heads][dim] of 16-bit elements by strides; *bytes: from the first to
 // past the last.
 ivf_status check_rows(ivf_ctx *ctx, const char *name, const void *p, int64_t ts, int64_t hs, int64_t T, int64_t heads,
@@ -96,13 +69,6 @@ ivf_status check_tokens(ivf_ctx *ctx, const KvCache &c, int64_t T, int64_t heads
     if (T < 0) return fail(ctx, IVF_EINVAL, "T must be >= 0");
     if (T > INT32_MAX || T * heads > INT32_MAX)
         return fail(ctx, IVF_EUNSUPPORTED, "too many tokens for one call");
-    return IVF_OK;
-}
-
-// A launch holds fewer than 2^32 threads.
-ivf_status check_threads(ivf_ctx *ctx, int64_t threads)
-{
-    if (threads >= (int64_t)UINT32_MAX) return fail(ctx, IVF_EUNSUPPORTED, "too many tokens for one call");
     return IVF_OK;
 }
 
@@ -133,18 +99,6 @@ ivf_status plan_attend(ivf_ctx *ctx, const KvCache &c, int32_t q_heads, int64_t 
     // a team of one: four units a workgroup
     if ((st = check_threads(ctx, (p.token_groups + 3) * c.heads * 64 * p.team)) != IVF_OK) return st;
     return check_threads(ctx, tiles * p.prompt_splits * c.heads * 512);
-}
-
-ivf_status no_overlap(ivf_ctx *ctx, const Span *outs, int no, const Span *ins, int ni)
-{
-    for (int i = 0; i < no; ++i) {
-        for (int j = 0; j < ni; ++j)
-            if (overlap(outs[i].p, outs[i].n, ins[j].p, ins[j].n))
-                return fail(ctx, IVF_EINVAL, "outputs overlap inputs");
-        for (int j = i + 1; j < no; ++j)
-            if (overlap(outs[i].p, outs[i].n, outs[j].p, outs[j].n)) return fail(ctx, IVF_EINVAL, "outputs overlap");
-    }
-    return IVF_OK;
 }
 
 }  // namespace
@@ -183,6 +137,129 @@ ivf_status ivf_kv_plan(ivf_ctx *ctx, const int32_t *cached, const int32_t *added
         TIMED("kv_plan", launch_kv_plan(cached, added, (int)B, shift, table, B ? table_cols : 1, free_blocks, n_free, T,
                                         out_start, out_slots, out_request, out_position, out_info, ctx->num_cus,
                                         ctx->stream));
+        ctx->last_stats = nullptr;
+        return IVF_OK;
+    });
+}
+
+ivf_status ivf_kv_fork(ivf_ctx *ctx, const int32_t *parent, const int32_t *child, int64_t n, int32_t *cached, int64_t B,
+                       int32_t block_size, int32_t *table, int32_t table_cols, const int32_t *free_blocks,
+                       int64_t n_free, int32_t *out_source, int32_t *out_to, int64_t *out_info)
+{
+    return guarded(ctx, "kv_fork", [&]() -> ivf_status {
+        const int shift = block_shift(block_size);
+        if (!shift) return fail(ctx, IVF_EUNSUPPORTED, "block_size must be 16, 32, 64 or 128 (got %d)", block_size);
+        if (n < 0 || n_free < 0) return fail(ctx, IVF_EINVAL, "n and n_free must be >= 0");
+        if (n == 0 && !out_info) return IVF_OK;
+        ivf_status st = check_table(ctx, B, table_cols, shift);
+        if (st != IVF_OK) return st;
+        if (n > kKvMaxRequests || B > kKvMaxRequests)
+            return fail(ctx, IVF_EUNSUPPORTED, "at most %d forks and requests", kKvMaxRequests);
+        if (!cached || !table || (n_free && !free_blocks) || (n && (!parent || !child || !out_source || !out_to)))
+            return fail(ctx, IVF_EINVAL, "null pointer argument");
+        const void *i32[] = {parent, child, cached, table, free_blocks, out_source, out_to};
+        const void *i64[] = {out_info};
+        if ((st = check_elements(ctx, i32, 4)) != IVF_OK || (st = check_elements(ctx, i64, 8)) != IVF_OK) return st;
+        const Span ins[] = {{parent, (size_t)n * 4}, {child, (size_t)n * 4}, {free_blocks, (size_t)n_free * 4}};
+        const Span outs[] = {{table, (size_t)B * table_cols * 4}, {cached, (size_t)B * 4}, {out_source, (size_t)n * 4},
+                             {out_to, (size_t)n * 4}, {out_info, 16}};
+        if ((st = no_overlap(ctx, outs, 5, ins, 3)) != IVF_OK) return st;
+        DeviceGuard g(ctx->device);
+        if (!g.ok) return fail(ctx, IVF_EDEVICE, "no usable device (context device %d)", ctx->device);
+        TIMED("kv_fork", launch_kv_fork(parent, child, (int)n, cached, (int)B, shift, table, table_cols, free_blocks, n_free,
+                                        out_source, out_to, out_info, ctx->num_cus, ctx->stream));
+        ctx->last_stats = nullptr;
+        return IVF_OK;
+    });
+}
+
+ivf_status ivf_kv_copy(ivf_ctx *ctx, const ivf_kv_cache *cache, const ivf_kv_cache *source_cache, const int32_t *to,
+                       const int32_t *source, int64_t n)
+{
+    return guarded(ctx, "kv_copy", [&]() -> ivf_status {
+        KvCache dst, src;
+        ivf_status st = check_cache(ctx, cache, dst);
+        if (st != IVF_OK || (st = check_cache(ctx, source_cache, src)) != IVF_OK) return st;
+        if (dst.bs != src.bs || dst.heads != src.heads || dst.dim != src.dim || dst.bf16 != src.bf16)
+            return fail(ctx, IVF_EINVAL, "the caches' block_size, heads, dim and type must be the same");
+        const bool same = dst.rec == src.rec && dst.summary == src.summary && dst.weight == src.weight;
+        const size_t sh = (size_t)src.blocks * src.heads;
+        if (!same && (overlaps_cache(dst, src.rec, sh * src.rec_bytes()) || overlaps_cache(dst, src.summary, sh * src.dim) ||
+                      overlaps_cache(dst, src.weight, sh * 4)))
+            return fail(ctx, IVF_EINVAL, "the caches overlap");
+        if (n < 0) return fail(ctx, IVF_EINVAL, "n must be >= 0");
+        if (n > INT32_MAX) return fail(ctx, IVF_EUNSUPPORTED, "n must be < 2^31");
+        if (n == 0) return IVF_OK;
+        if (!to || !source) return fail(ctx, IVF_EINVAL, "null pointer argument");
+        const void *i32[] = {to, source};
+        if ((st = check_elements(ctx, i32, 4)) != IVF_OK) return st;
+        if (overlaps_cache(dst, to, (size_t)n * 4) || overlaps_cache(dst, source, (size_t)n * 4))
+            return fail(ctx, IVF_EINVAL, "inputs overlap the cache");
+        DeviceGuard g(ctx->device);
+        if (!g.ok) return fail(ctx, IVF_EDEVICE, "no usable device (context device %d)", ctx->device);
+        TIMED("kv_copy", launch_kv_copy(dst, src, to, source, n, ctx->num_cus, ctx->stream));
+        ctx->last_stats = nullptr;
+        return IVF_OK;
+    });
+}
+
+size_t ivf_kv_reclaim_bytes(int64_t B, int32_t block_size, int32_t table_cols, int64_t blocks, int64_t moves)
+{
+    const int shift = block_shift(block_size);
+    if (!shift || B < 0 || (B && check_table(nullptr, B, table_cols, shift) != IVF_OK) || blocks < 1 || blocks > INT32_MAX ||
+        moves < 0 || moves > INT32_MAX)
+        return 0;
+    size_t counts, rank;
+    return kv_reclaim_workspace(blocks, B ? B * table_cols : 0, moves, &counts, &rank);
+}
+
+ivf_status ivf_kv_reclaim(ivf_ctx *ctx, const int32_t *cached, int64_t B, int32_t block_size, int32_t *table,
+                          int32_t table_cols, int64_t blocks, int64_t moves, int32_t *out_free, int32_t *out_source,
+                          int32_t *out_to, int64_t *out_info)
+{
+    return guarded(ctx, "kv_reclaim", [&]() -> ivf_status {
+        const int shift = block_shift(block_size);
+        if (!shift) return fail(ctx, IVF_EUNSUPPORTED, "block_size must be 16, 32, 64 or 128 (got %d)", block_size);
+        if (B < 0) return fail(ctx, IVF_EINVAL, "B must be >= 0");
+        ivf_status st = B == 0 ? IVF_OK : check_table(ctx, B, table_cols, shift);
+        if (st != IVF_OK) return st;
+        if (blocks < 1 || blocks > INT32_MAX)
+            return fail(ctx, IVF_EINVAL, "blocks must be in [1, 2^31) (got %lld)", (long long)blocks);
+        if (moves < 0 || moves > INT32_MAX) return fail(ctx, IVF_EINVAL, "moves must be in [0, 2^31)");
+        if ((B && (!cached || !table)) || (moves && (!out_source || !out_to)))
+            return fail(ctx, IVF_EINVAL, "null pointer argument");
+        if (!moves) out_source = out_to = nullptr;
+        if (!moves && !out_free && !out_info) return IVF_OK;
+        const void *i32[] = {cached, table, out_free, out_source, out_to};
+        const void *i64[] = {out_info};
+        if ((st = check_elements(ctx, i32, 4)) != IVF_OK || (st = check_elements(ctx, i64, 8)) != IVF_OK) return st;
+        const Span ins[] = {{cached, (size_t)B * 4}};
+        const Span outs[] = {{table, B ? (size_t)B * table_cols * 4 : 0}, {out_free, (size_t)blocks * 4},
+                             {out_source, (size_t)moves * 4}, {out_to, (size_t)moves * 4}, {out_info, 24}};
+        if ((st = no_overlap(ctx, outs, 5, ins, 1)) != IVF_OK) return st;
+        KvReclaim a = {};
+        a.cached = cached;
+        a.B = B;
+        a.shift = shift;
+        a.table = table;
+        a.cols = B ? table_cols : 1;
+        a.blocks = blocks;
+        a.moves = moves;
+        a.free = out_free;
+        a.source = out_source;
+        a.to = out_to;
+        a.info = out_info;
+        size_t counts = 0, rank = 0;
+        const size_t need = kv_reclaim_workspace(blocks, a.B * a.cols, moves, &counts, &rank);
+        if (need) {
+            if ((st = check_ws(ctx, need)) != IVF_OK) return st;
+            a.bits = (uint32_t *)ctx->ws;
+            a.counts = (uint32_t *)((char *)ctx->ws + counts);
+            a.rank = (int32_t *)((char *)ctx->ws + rank);
+        }
+        DeviceGuard g(ctx->device);
+        if (!g.ok) return fail(ctx, IVF_EDEVICE, "no usable device (context device %d)", ctx->device);
+        TIMED("kv_reclaim", launch_kv_reclaim(a, ctx->num_cus, ctx->stream));
         ctx->last_stats = nullptr;
         return IVF_OK;
     });

@@ -153,4 +153,50 @@ inline void prof_stop(ivf_ctx *ctx, int slot)
         prof_stop(ctx, slot_);                   \
     } while (0)
 
+// Runs f(); what a C++ library throws on the host becomes a status.
+template <typename F> ivf_status guarded(ivf_ctx *ctx, const char *call, F f)
+{
+    if (!ctx) return IVF_EINVAL;
+    try {
+        ctx->err.clear();
+        ctx->cur_call = call;
+        return f();
+    } catch (...) {
+        return IVF_EDEVICE;
+    }
+}
+
+// An array for overlap checks.
+struct Span {
+    const void *p;
+    size_t n;
+};
+
+// Arrays of whole numbers and fp32 outputs lie at multiples of their elements.
+template <int N> ivf_status check_elements(ivf_ctx *ctx, const void *const (&p)[N], size_t element)
+{
+    for (const void *x : p)
+        if ((uintptr_t)x % element) return fail(ctx, IVF_EINVAL, "arrays must be aligned to their elements");
+    return IVF_OK;
+}
+
+// A launch holds fewer than 2^32 threads.
+inline ivf_status check_threads(ivf_ctx *ctx, int64_t threads)
+{
+    if (threads >= (int64_t)UINT32_MAX) return fail(ctx, IVF_EUNSUPPORTED, "too many tokens for one call");
+    return IVF_OK;
+}
+
+inline ivf_status no_overlap(ivf_ctx *ctx, const Span *outs, int no, const Span *ins, int ni)
+{
+    for (int i = 0; i < no; ++i) {
+        for (int j = 0; j < ni; ++j)
+            if (overlap(outs[i].p, outs[i].n, ins[j].p, ins[j].n))
+                return fail(ctx, IVF_EINVAL, "outputs overlap inputs");
+        for (int j = i + 1; j < no; ++j)
+            if (overlap(outs[i].p, outs[i].n, outs[j].p, outs[j].n)) return fail(ctx, IVF_EINVAL, "outputs overlap");
+    }
+    return IVF_OK;
+}
+
 }  // namespace ivf

@@ -1,6 +1,6 @@
 // The paged 4-bit key/value cache: its layout and the launch parameters of the
-// kernels that build its tables (kv_plan.hip), write and read it
-// (kv_cache.hip), select blocks (kv_select.hip) and attend (kv_attend.hip).
+// kernels that build its tables (kv_plan.hip), share and move its blocks
+// (kv_pages.hip), write and read it (kv_cache.hip), select blocks (kv_select.hip) and attend (kv_attend.hip).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -11,6 +11,7 @@ namespace ivf {
 constexpr int kKvMaxRequests = 16384;  // of one plan: their prefix sums lie in LDS
 constexpr int kKvMaxSelectCols = 32768;  // block scores of a row lie in LDS
 constexpr int kKvMaxCount = 4096;
+constexpr int kKvFewBlocks = 1 << 18;    // whose bits lie in one workgroup's LDS
 constexpr int kKvMaxUnits = 1024;  // whose key ranges are shared out evenly (prefix sums in LDS)
 
 struct KvCache {
@@ -53,6 +54,29 @@ constexpr int64_t kKvFewTokens = 512;
 hipError_t launch_kv_append(const KvCache &c, KvRows k, KvRows v, const int64_t *slots, int64_t T, hipStream_t s);
 hipError_t launch_kv_read(const KvCache &c, const int64_t *slots, int64_t T, void *k, void *v, const int32_t *blocks,
                           int64_t n, float *mean, hipStream_t s);
+
+// Blocks that requests share, give back and move (kv_pages.hip).
+hipError_t launch_kv_fork(const int32_t *parent, const int32_t *child, int n, int32_t *cached, int B, int shift,
+                          int32_t *table, int cols, const int32_t *free_blocks, int64_t n_free, int32_t *source,
+                          int32_t *to, int64_t *info, int num_cus, hipStream_t s);
+hipError_t launch_kv_copy(const KvCache &dst, const KvCache &src, const int32_t *to, const int32_t *source, int64_t n,
+                          int num_cus, hipStream_t s);
+struct KvReclaim {
+    const int32_t *cached;
+    int64_t B;
+    int shift;
+    int32_t *table;
+    int cols;
+    int64_t blocks, moves;
+    int32_t *free, *source, *to;
+    int64_t *info;
+    // workspace: the used blocks as bits, counts of them, and where blocks move (with moves)
+    uint32_t *bits, *counts;
+    int32_t *rank;
+};
+// Bytes of the workspace, and where counts and rank begin in it; 0: none is used.
+size_t kv_reclaim_workspace(int64_t blocks, int64_t entries, int64_t moves, size_t *counts, size_t *rank);
+hipError_t launch_kv_reclaim(const KvReclaim &a, int num_cus, hipStream_t s);
 
 struct KvSelect {
     KvCache c;
