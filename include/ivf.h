@@ -673,6 +673,41 @@ ivf_status ivf_kv_attend(ivf_ctx *ctx, const ivf_kv_cache *cache, const void *q,
                          const int32_t *table, int64_t B, int32_t table_cols, const int32_t *blocks,
                          int32_t count, float scale, int64_t longest, void *out, float *out_lse);
 
+/* What a call may put into the scores of ivf_kv_attend. The score of a query
+ * at position p of its request and a key at position j, x = scale * q.k,
+ * becomes
+ *     cap * tanh(x / cap)          with a cap (0: none), and then
+ *     x - slopes[head] * |p - j|   with slopes, one a query head,
+ * and a row sees the keys with
+ *     first[t] <= j <= p  or  j < prefix[t],
+ * each token its own (NULL: 0): a sliding window (first = p - w + 1) with the
+ * context's first tokens (prefix), documents that see themselves and a shared
+ * head alone, a prefix that sees itself in both directions. Keys that no row of
+ * a group sees are not read.
+ *   cap      0, or from 2^-40 to 2^40, with scale / cap 0 or a normal number
+ *   slopes   [q_heads] fp32, finite, or NULL
+ *   first    [T] int32 or NULL; above p: only the prefix is seen
+ *   prefix   [T] int32 or NULL; at most the request's tokens in the cache (slots
+ *            behind them hold whatever they hold), and not of a token whose
+ *            position is negative, which sees nothing
+ * A struct of zeros changes nothing. */
+typedef struct {
+    float cap;
+    const float *slopes;
+    const int32_t *first;
+    const int32_t *prefix;
+} ivf_kv_terms;
+
+/* ivf_kv_attend with `terms` in the scores (NULL: none); everything else, with
+ * selected blocks too, is as there, with the same workspace: a selected block's
+ * keys are seen where the terms let them be. */
+ivf_status ivf_kv_attend_terms(ivf_ctx *ctx, const ivf_kv_cache *cache, const void *q,
+                               int64_t q_token_stride, int64_t q_head_stride, int32_t q_heads, int64_t T,
+                               const int32_t *start, const int32_t *request, const int32_t *position,
+                               const int32_t *table, int64_t B, int32_t table_cols, const int32_t *blocks,
+                               int32_t count, float scale, int64_t longest, const ivf_kv_terms *terms,
+                               void *out, float *out_lse);
+
 /* Workspace of ivf_kv_attend (the rows' parts where long key ranges are split
  * over workgroups; 0 where none are, or for arguments that it refuses). */
 size_t ivf_kv_attend_bytes(const ivf_kv_cache *cache, int32_t q_heads, int64_t T, int64_t B,

@@ -61,6 +61,8 @@ SIGNATURES = [
     ("ivf_kv_attend_bytes", _SZ, [_P, _I32, _I64, _I64, _I32, _I32, _I64]),
     ("ivf_kv_attend", _INT, [_P, _P, _P, _I64, _I64, _I32, _I64, _P, _P, _P, _P, _I64, _I32, _P, _I32,
                              ctypes.c_float, _I64, _P, _P]),
+    ("ivf_kv_attend_terms", _INT, [_P, _P, _P, _I64, _I64, _I32, _I64, _P, _P, _P, _P, _I64, _I32, _P, _I32,
+                                   ctypes.c_float, _I64, _P, _P, _P]),
 ]
 
 _lib = None
@@ -524,6 +526,11 @@ class _KvCacheStruct(ctypes.Structure):
                 ("heads", _I32), ("dim", _I32), ("dtype", _I32)]
 
 
+class _KvTermsStruct(ctypes.Structure):
+    """ivf_kv_terms."""
+    _fields_ = [("cap", ctypes.c_float), ("slopes", _P), ("first", _P), ("prefix", _P)]
+
+
 class KVCache:
     """A paged key/value cache held in 4 bits: `records` uint8 [blocks, heads,
     block_size * dim * 17 / 16], `summary` int8 [blocks, heads, dim] and
@@ -610,7 +617,7 @@ def _rows(ctx, t, name, cache, heads=None):
 
 
 def _ints(ctx, t, name, shape, kind):
-    """The pointer of a contiguous tensor of whole numbers of this shape on the context's device."""
+    """The pointer of a contiguous tensor of this type and shape on the context's device."""
     if t.dtype != kind or t.get_device() != ctx.device:
         raise TypeError("%s must be %s on device %d, got %s on %s" % (name, kind, ctx.device, t.dtype, t.device))
     if t.shape != shape:
@@ -784,12 +791,18 @@ def ivf_kv_select(ctx: Context, cache: KVCache, q, request, position, table, cou
 
 
 def ivf_kv_attend(ctx: Context, cache: KVCache, q, start, request, position, table, scale: float, longest: int,
-                  blocks=None, out=None, out_lse=None, want_lse: bool = True):
+                  blocks=None, out=None, out_lse=None, want_lse: bool = True, cap: float = 0.0, slopes=None,
+                  first=None, prefix=None):
     """Attention of queries q [T, query heads, dim] over their requests' tokens in
     the cache, or over the selected `blocks` (int32 [T, heads, count]) only:
     outputs like q and the log-sum-exps fp32 [T, query heads]. `longest` is at
     least the largest number of tokens that one request has in the batch. Without
-    `blocks`, rows past start[B] (padding of the batch) are left unwritten."""
+    `blocks`, rows past start[B] (padding of the batch) are left unwritten.
+
+    With `cap` a score x is cap * tanh(x / cap); with `slopes` (fp32 [query heads])
+    it then loses slope * |p - j| for the positions p of the query and j of the key;
+    with `first` and `prefix` (int32 [T]) a token sees the keys first <= j <= p and
+    j < prefix (ivf_kv_terms in include/ivf.h)."""
     import torch
 
     i32 = torch.int32
@@ -814,11 +827,22 @@ def ivf_kv_attend(ctx: Context, cache: KVCache, q, start, request, position, tab
     need = cache.attend_bytes(ctx, Hq, T, B, cols, count, longest)
     if need:
         ctx.ensure_workspace(need)
-    lib, handle = ctx.bind()
-    st = lib.ivf_kv_attend(handle, cache.ref, qp, qt, qh, Hq, T, _ints(ctx, start, "start", (B + 1,), i32),
-                           _ints(ctx, request, "request", (T,), i32), _ints(ctx, position, "position", (T,), i32),
-                           _ints(ctx, table, "table", (B, cols), i32), B, cols, p_blocks, count, scale, longest,
-                           out.data_ptr(), None if out_lse is None else out_lse.data_ptr())
+    args = (cache.ref, qp, qt, qh, Hq, T, _ints(ctx, start, "start", (B + 1,), i32),
+            _ints(ctx, request, "request", (T,), i32), _ints(ctx, position, "position", (T,), i32),
+            _ints(ctx, table, "table", (B, cols), i32), B, cols, p_blocks, count, scale, longest)
+    outs = out.data_ptr(), None if out_lse is None else out_lse.data_ptr()
+    if cap or slopes is not None or first is not None or prefix is not None:
+        if slopes is not None and slopes.requires_grad and _grad_enabled():
+            raise RuntimeError("slopes require a gradient, and the cache's calls have no backward pass: detach them, or "
+                               "call under torch.no_grad()")
+        terms = _KvTermsStruct(cap, None if slopes is None else _ints(ctx, slopes, "slopes", (Hq,), torch.float32),
+                               None if first is None else _ints(ctx, first, "first", (T,), i32),
+                               None if prefix is None else _ints(ctx, prefix, "prefix", (T,), i32))
+        lib, handle = ctx.bind()
+        st = lib.ivf_kv_attend_terms(handle, *args, ctypes.byref(terms), *outs)
+    else:
+        lib, handle = ctx.bind()
+        st = lib.ivf_kv_attend(handle, *args, *outs)
     if st:
         ctx.check(st, "ivf_kv_attend")
     return out, out_lse

@@ -101,6 +101,100 @@ ivf_status plan_attend(ivf_ctx *ctx, const KvCache &c, int32_t q_heads, int64_t 
     return check_threads(ctx, tiles * p.prompt_splits * c.heads * 512);
 }
 
+// The attention calls. terms: null, or what goes into the scores.
+ivf_status attend(ivf_ctx *ctx, const ivf_kv_cache *cache, const void *q, int64_t q_token_stride, int64_t q_head_stride,
+                  int32_t q_heads, int64_t T, const int32_t *start, const int32_t *request, const int32_t *position,
+                  const int32_t *table, int64_t B, int32_t table_cols, const int32_t *blocks, int32_t count, float scale,
+                  int64_t longest, const ivf_kv_terms *terms, void *out, float *out_lse)
+{
+    return guarded(ctx, "kv_attend", [&]() -> ivf_status {
+        KvAttend a;
+        ivf_status st = check_cache(ctx, cache, a.c);
+        if (st != IVF_OK) return st;
+        KvAttendPlan p = {};
+        if ((st = plan_attend(ctx, a.c, q_heads, T, B, table_cols, count, longest, ctx->num_cus, p)) != IVF_OK) return st;
+        if (T == 0) return IVF_OK;
+        if (blocks ? count < 1 : count != 0)
+            return fail(ctx, IVF_EINVAL, "count must be in [1, %d] with blocks, 0 without", kKvMaxCount);
+        const float scale2 = fabsf(scale) * 1.44269504089f;  // of exponents to the base 2
+        if (!isfinite(scale2)) return fail(ctx, IVF_EINVAL, "scale must be finite, and of magnitude below 2.3e38");
+        const ivf_kv_terms none = {}, &given = terms ? *terms : none;
+        KvTerms x = {given.cap, given.slopes, given.first, given.prefix};
+        if (x.cap != 0.f) {
+            if (!(x.cap >= 0x1p-40f && x.cap <= 0x1p40f)) return fail(ctx, IVF_EINVAL, "cap must be 0, or from 2^-40 to 2^40");
+            const float by_cap = fabsf(scale) / x.cap;
+            if (!isfinite(by_cap) || (by_cap < 0x1p-126f && scale != 0.f))
+                return fail(ctx, IVF_EINVAL, "scale / cap must be 0 or a normal number");
+        }
+        size_t qb;
+        if ((st = check_rows(ctx, "q", q, q_token_stride, q_head_stride, T, q_heads, a.c.dim, &qb)) != IVF_OK) return st;
+        if (!position || !table || !out || (blocks ? !request : !start)) return fail(ctx, IVF_EINVAL, "null pointer argument");
+        const void *i32[] = {start, request, position, table, blocks, out_lse, x.slopes, x.first, x.prefix};
+        if ((st = check_elements(ctx, i32, 4)) != IVF_OK) return st;
+        if (!aligned16(out)) return fail(ctx, IVF_EINVAL, "out must be 16-byte aligned");
+        const size_t rows = (size_t)T * q_heads;
+        const Span ins[] = {{q, qb}, {start, (size_t)(B + 1) * 4}, {request, (size_t)T * 4}, {position, (size_t)T * 4},
+                            {table, (size_t)B * table_cols * 4}, {blocks, (size_t)T * a.c.heads * count * 4}, {x.slopes, (size_t)q_heads * 4},
+                            {x.first, (size_t)T * 4}, {x.prefix, (size_t)T * 4}};
+        const Span outs[] = {{out, rows * a.c.dim * 2}, {out_lse, rows * 4}};
+        if ((st = no_overlap(ctx, outs, 2, ins, 9)) != IVF_OK) return st;
+        for (const Span &o : outs)
+            if (overlaps_cache(a.c, o.p, o.n)) return fail(ctx, IVF_EINVAL, "outputs overlap the cache");
+        const size_t need = p.token_bytes + p.prompt_bytes;
+        if (need && (st = check_ws(ctx, need)) != IVF_OK) return st;
+        DeviceGuard g(ctx->device);
+        if (!g.ok) return fail(ctx, IVF_EDEVICE, "no usable device (context device %d)", ctx->device);
+        a.q = {q, q_token_stride, q_head_stride};
+        a.group = q_heads / a.c.heads;
+        a.T = T;
+        a.start = start;
+        a.request = request;
+        a.position = position;
+        a.table = table;
+        a.B = B;
+        a.cols = table_cols;
+        a.blocks = blocks;
+        a.count = count;
+        // a scale of 0 as the least number above it: masked scores stay -infinity
+        a.scale = std::max(scale2, 0x1p-149f);
+        a.q_flip = scale < 0.f ? 0x80008000u : 0u;
+        const bool has_terms = x.cap != 0.f || x.slopes || x.first || x.prefix;
+        if (x.cap != 0.f) a.scale = std::max(fabsf(scale) / x.cap, 0x1p-149f);
+        x.cap *= 1.44269504089f;
+        a.out = out;
+        a.lse = out_lse;
+        a.small_rows = p.small_rows;
+        a.unit_size = p.unit_size;
+        a.team = p.team;
+        a.unit_rows = p.unit_rows;
+        a.per_unit = p.per_unit;
+        a.units = (int)p.units;
+        a.slots = (int)p.slots;
+        KvAttend prompts = a;
+        if (p.tokens) {
+            char *ws = (char *)ctx->ws;
+            a.splits = p.token_splits;
+            a.part = (float *)ws;
+            a.part_ml = (float2 *)(ws + p.token_ml);
+            a.unit_parts = (int2 *)(ws + p.token_parts);
+            TIMED("kv_attend", has_terms ? launch_kv_tokens_terms(a, x, p.token_groups, ctx->stream)
+                                         : launch_kv_tokens(a, p.token_groups, ctx->stream));
+        }
+        if (p.prompt) {
+            char *ws = (char *)ctx->ws + p.token_bytes;
+            prompts.splits = p.prompt_splits;
+            prompts.part = (float *)ws;
+            prompts.part_ml = (float2 *)(ws + p.prompt_ml);
+            TIMED("kv_prompt", has_terms ? launch_kv_prompt_terms(prompts, x, ctx->stream) : launch_kv_prompt(prompts, ctx->stream));
+        }
+        const KvAttend *join_prompts = p.prompt && p.prompt_splits > 1 ? &prompts : nullptr;
+        const KvAttend *join_units = p.tokens && p.token_splits > 1 ? &a : nullptr;
+        if (join_prompts || join_units) TIMED("kv_combine", launch_kv_combine(join_prompts, join_units, ctx->stream));
+        ctx->last_stats = nullptr;
+        return IVF_OK;
+    });
+}
+
 }  // namespace
 
 extern "C" {
@@ -393,79 +487,18 @@ ivf_status ivf_kv_attend(ivf_ctx *ctx, const ivf_kv_cache *cache, const void *q,
                          int32_t table_cols, const int32_t *blocks, int32_t count, float scale, int64_t longest,
                          void *out, float *out_lse)
 {
-    return guarded(ctx, "kv_attend", [&]() -> ivf_status {
-        KvAttend a;
-        ivf_status st = check_cache(ctx, cache, a.c);
-        if (st != IVF_OK) return st;
-        KvAttendPlan p = {};
-        if ((st = plan_attend(ctx, a.c, q_heads, T, B, table_cols, count, longest, ctx->num_cus, p)) != IVF_OK) return st;
-        if (T == 0) return IVF_OK;
-        if (blocks ? count < 1 : count != 0)
-            return fail(ctx, IVF_EINVAL, "count must be in [1, %d] with blocks, 0 without", kKvMaxCount);
-        const float scale2 = fabsf(scale) * 1.44269504089f;  // of exponents to the base 2
-        if (!isfinite(scale2)) return fail(ctx, IVF_EINVAL, "scale must be finite, and of magnitude below 2.3e38");
-        size_t qb;
-        if ((st = check_rows(ctx, "q", q, q_token_stride, q_head_stride, T, q_heads, a.c.dim, &qb)) != IVF_OK) return st;
-        if (!position || !table || !out || (blocks ? !request : !start)) return fail(ctx, IVF_EINVAL, "null pointer argument");
-        const void *i32[] = {start, request, position, table, blocks, out_lse};
-        if ((st = check_elements(ctx, i32, 4)) != IVF_OK) return st;
-        if (!aligned16(out)) return fail(ctx, IVF_EINVAL, "out must be 16-byte aligned");
-        const size_t rows = (size_t)T * q_heads;
-        const Span ins[] = {{q, qb}, {start, (size_t)(B + 1) * 4}, {request, (size_t)T * 4}, {position, (size_t)T * 4},
-                            {table, (size_t)B * table_cols * 4}, {blocks, (size_t)T * a.c.heads * count * 4}};
-        const Span outs[] = {{out, rows * a.c.dim * 2}, {out_lse, rows * 4}};
-        if ((st = no_overlap(ctx, outs, 2, ins, 6)) != IVF_OK) return st;
-        for (const Span &o : outs)
-            if (overlaps_cache(a.c, o.p, o.n)) return fail(ctx, IVF_EINVAL, "outputs overlap the cache");
-        const size_t need = p.token_bytes + p.prompt_bytes;
-        if (need && (st = check_ws(ctx, need)) != IVF_OK) return st;
-        DeviceGuard g(ctx->device);
-        if (!g.ok) return fail(ctx, IVF_EDEVICE, "no usable device (context device %d)", ctx->device);
-        a.q = {q, q_token_stride, q_head_stride};
-        a.group = q_heads / a.c.heads;
-        a.T = T;
-        a.start = start;
-        a.request = request;
-        a.position = position;
-        a.table = table;
-        a.B = B;
-        a.cols = table_cols;
-        a.blocks = blocks;
-        a.count = count;
-        // a scale of 0 as the least number above it: masked scores stay -infinity
-        a.scale = std::max(scale2, 0x1p-149f);
-        a.q_flip = scale < 0.f ? 0x80008000u : 0u;
-        a.out = out;
-        a.lse = out_lse;
-        a.small_rows = p.small_rows;
-        a.unit_size = p.unit_size;
-        a.team = p.team;
-        a.unit_rows = p.unit_rows;
-        a.per_unit = p.per_unit;
-        a.units = (int)p.units;
-        a.slots = (int)p.slots;
-        KvAttend prompts = a;
-        if (p.tokens) {
-            char *ws = (char *)ctx->ws;
-            a.splits = p.token_splits;
-            a.part = (float *)ws;
-            a.part_ml = (float2 *)(ws + p.token_ml);
-            a.unit_parts = (int2 *)(ws + p.token_parts);
-            TIMED("kv_attend", launch_kv_tokens(a, p.token_groups, ctx->stream));
-        }
-        if (p.prompt) {
-            char *ws = (char *)ctx->ws + p.token_bytes;
-            prompts.splits = p.prompt_splits;
-            prompts.part = (float *)ws;
-            prompts.part_ml = (float2 *)(ws + p.prompt_ml);
-            TIMED("kv_prompt", launch_kv_prompt(prompts, ctx->stream));
-        }
-        const KvAttend *join_prompts = p.prompt && p.prompt_splits > 1 ? &prompts : nullptr;
-        const KvAttend *join_units = p.tokens && p.token_splits > 1 ? &a : nullptr;
-        if (join_prompts || join_units) TIMED("kv_combine", launch_kv_combine(join_prompts, join_units, ctx->stream));
-        ctx->last_stats = nullptr;
-        return IVF_OK;
-    });
+    return attend(ctx, cache, q, q_token_stride, q_head_stride, q_heads, T, start, request, position, table, B, table_cols,
+                  blocks, count, scale, longest, nullptr, out, out_lse);
+}
+
+ivf_status ivf_kv_attend_terms(ivf_ctx *ctx, const ivf_kv_cache *cache, const void *q, int64_t q_token_stride,
+                               int64_t q_head_stride, int32_t q_heads, int64_t T, const int32_t *start,
+                               const int32_t *request, const int32_t *position, const int32_t *table, int64_t B,
+                               int32_t table_cols, const int32_t *blocks, int32_t count, float scale, int64_t longest,
+                               const ivf_kv_terms *terms, void *out, float *out_lse)
+{
+    return attend(ctx, cache, q, q_token_stride, q_head_stride, q_heads, T, start, request, position, table, B, table_cols,
+                  blocks, count, scale, longest, terms, out, out_lse);
 }
 
 }  // extern "C"

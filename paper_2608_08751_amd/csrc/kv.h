@@ -1,6 +1,7 @@
 // The paged 4-bit key/value cache: its layout and the launch parameters of the
 // kernels that build its tables (kv_plan.hip), share and move its blocks
-// (kv_pages.hip), write and read it (kv_cache.hip), select blocks (kv_select.hip) and attend (kv_attend.hip).
+// (kv_pages.hip), write and read it (kv_cache.hip), select blocks (kv_select.hip) and attend
+// (kv_attend_kernel.h, kv_prompt_kernel.h).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -126,6 +127,16 @@ struct KvAttend {
     int2 *unit_parts;
 };
 
+// The terms of a call's scores (kv_terms.h): they are cap * tanh(scale * q.k), the cap to the base 2 and the
+// scale by the cap, or with a cap of 0 scale * q.k, less slope |p - j|. (An argument of its own: with
+// these as members of KvAttend the kernels without terms spilled 17 registers.)
+struct KvTerms {
+    float cap;
+    const float *slopes;            // [query heads], or null
+    const int32_t *first, *prefix;  // [T], or null
+};
+struct KvNoTerms {};
+
 // Which kernels take a call, in how many parts, and what those need.
 struct KvAttendPlan {
     bool tokens, prompt;
@@ -140,11 +151,13 @@ struct KvAttendPlan {
 KvAttendPlan kv_attend_plan(const KvCache &c, int group, int64_t T, int64_t B, int64_t cols, int64_t count,
                             int64_t longest, int num_cus);
 hipError_t launch_kv_tokens(const KvAttend &a, int64_t groups, hipStream_t s);
+hipError_t launch_kv_tokens_terms(const KvAttend &a, const KvTerms &x, int64_t groups, hipStream_t s);
 // joins the parts of prompts and of the single-token kernel's calls; either may be null
 hipError_t launch_kv_combine(const KvAttend *prompts, const KvAttend *units, hipStream_t s);
 
 int kv_prompt_rows(int dim);      // rows of a workgroup
 int kv_prompt_resident(int dim);  // workgroups that a CU holds
 hipError_t launch_kv_prompt(const KvAttend &a, hipStream_t s);
+hipError_t launch_kv_prompt_terms(const KvAttend &a, const KvTerms &x, hipStream_t s);
 
 }  // namespace ivf
