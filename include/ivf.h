@@ -713,6 +713,37 @@ ivf_status ivf_kv_attend_terms(ivf_ctx *ctx, const ivf_kv_cache *cache, const vo
 size_t ivf_kv_attend_bytes(const ivf_kv_cache *cache, int32_t q_heads, int64_t T, int64_t B,
                            int32_t table_cols, int32_t count, int64_t longest);
 
+/* The token that follows, of T rows of V logits each (what a decoding step
+ * does with the model's output). A row's logits x, largest m, weigh
+ * w = exp((x - m) / temperature). In the order (x descending, index ascending)
+ * there remain
+ *   the first top_k (0 or less, or V and more: all);
+ *   of these the shortest leading part whose weights reach top_p of theirs
+ *     (1 and more, or no number: all; at least the first);
+ *   of that the weights of at least min_p (0 or less, or no number: all; above 1:
+ *     as 1).
+ * The token is the first index at which the running sum, over the indexes in
+ * their order, of what remains is above u times its whole, u = uniform[t] kept
+ * within [0, 1). A temperature that is not above 0 takes the first of
+ * the largest logits, one above 2^60 counts as 2^60. Weights and their sums are whole numbers of 2^-43 of the
+ * largest weight, so that results do not depend on the order of additions, and
+ * less than 2^-44 counts 0.
+ *   logits      [T][V] of type dt (IVF_F32, IVF_F16, IVF_BF16), rows row_stride
+ *               elements apart; V <= 2^20. No number counts as -infinity,
+ *               which is never drawn, and +infinity as the largest fp32 number.
+ *   uniform     [T] fp32
+ *   temperature, top_p, min_p [T] fp32, top_k [T] int32; each may be NULL (1, 1,
+ *               0, 0)
+ *   out_token   [T] int32; -1 where a row has no logit above -infinity
+ *   out_logprob [T] fp32 logarithm of the token's share of what remains (0 for a
+ *               row that takes the largest, -infinity with a token of -1); may be NULL
+ * The conventions are those of the cache's calls; rows need only be aligned to their
+ * elements. No workspace. Errors: IVF_EINVAL, IVF_EUNSUPPORTED (type, V, T above
+ * 4194303), IVF_EDEVICE. */
+ivf_status ivf_sample(ivf_ctx *ctx, const void *logits, int dt, int64_t row_stride, int64_t T, int64_t V,
+                      const float *uniform, const float *temperature, const int32_t *top_k,
+                      const float *top_p, const float *min_p, int32_t *out_token, float *out_logprob);
+
 /* Measures the fp32 MFMA pipe for reporting: enqueues a probe kernel that
  * runs only v_mfma_f32_32x32x2_f32 (register operands, two waves per SIMD on
  * every CU) for `iters` rounds of 16 instructions per wave (after one

@@ -14,7 +14,8 @@ and the benchmark:
                         and reading it, the blocks that queries select, attention over it;
 * ``ivf_kv_fork``, ``ivf_kv_copy``, ``ivf_kv_reclaim``
                         requests that share a context's blocks, copies of blocks, the free blocks
-                        and moving the others together.
+                        and moving the others together;
+* ``ivf_sample``        the tokens that follow, from logits.
 """
 from ._binding import (  # noqa: F401
     IVF_BF16,
@@ -70,6 +71,7 @@ from ._binding import (  # noqa: F401
     ivf_pq_train_step,
     ivf_route,
     ivf_route_noalloc,
+    ivf_sample,
     load_library,
 )
 

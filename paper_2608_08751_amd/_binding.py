@@ -61,6 +61,7 @@ SIGNATURES = [
     ("ivf_kv_attend_bytes", _SZ, [_P, _I32, _I64, _I64, _I32, _I32, _I64]),
     ("ivf_kv_attend", _INT, [_P, _P, _P, _I64, _I64, _I32, _I64, _P, _P, _P, _P, _I64, _I32, _P, _I32,
                              ctypes.c_float, _I64, _P, _P]),
+    ("ivf_sample", _INT, [_P, _P, _INT, _I64, _I64, _I64, _P, _P, _P, _P, _P, _P, _P]),
     ("ivf_kv_attend_terms", _INT, [_P, _P, _P, _I64, _I64, _I32, _I64, _P, _P, _P, _P, _I64, _I32, _P, _I32,
                                    ctypes.c_float, _I64, _P, _P, _P]),
 ]
@@ -846,3 +847,49 @@ def ivf_kv_attend(ctx: Context, cache: KVCache, q, start, request, position, tab
     if st:
         ctx.check(st, "ivf_kv_attend")
     return out, out_lse
+
+
+# ---- the token that follows ---------------------------------------------------
+
+_logit_types = None
+
+
+def ivf_sample(ctx: Context, logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None):
+    """The token that follows, for each row of logits [T, V] (fp32, fp16 or bf16,
+    V contiguous), drawn by uniform (fp32 [T], in [0, 1)): weights
+    exp((x - max) / temperature), of which the first top_k remain (int32 [T], 0: all), of
+    those the shortest part that reaches top_p (fp32 [T]), of that those of at least min_p
+    (fp32 [T]) times the largest. A temperature (fp32 [T]) of 0 takes the largest logit.
+    Returns (tokens int32 [T], their log-probabilities fp32 [T])."""
+    import torch
+
+    global _logit_types
+    if _logit_types is None:
+        _logit_types = {torch.float32: IVF_F32, torch.float16: IVF_F16, torch.bfloat16: IVF_BF16}
+    dt = _logit_types.get(logits.dtype)
+    if dt is None or logits.get_device() != ctx.device:
+        raise TypeError("logits must be float32, float16 or bfloat16 on device %d, got %s on %s" % (
+            ctx.device, logits.dtype, logits.device))
+    if logits.requires_grad and _grad_enabled():
+        raise RuntimeError("logits require a gradient, and sampling has no backward pass: detach them, or call under "
+                           "torch.no_grad()")
+    if logits.dim() != 2 or logits.shape[1] < 1:
+        raise ValueError("logits must be [T, V] with V >= 1, got %s" % (tuple(logits.shape),))
+    T, V = logits.shape
+    stride, one = logits.stride()
+    if one != 1 and V > 1:
+        raise ValueError("logits: a row must be contiguous")
+    f32, shape = torch.float32, (T,)
+    args = (_ints(ctx, uniform, "uniform", shape, f32),
+            None if temperature is None else _ints(ctx, temperature, "temperature", shape, f32),
+            None if top_k is None else _ints(ctx, top_k, "top_k", shape, torch.int32),
+            None if top_p is None else _ints(ctx, top_p, "top_p", shape, f32),
+            None if min_p is None else _ints(ctx, min_p, "min_p", shape, f32))
+    token, logprob = torch.unsafe_split_with_sizes(torch.empty(2 * T, dtype=torch.int32, device=logits.device), (T, T))
+    logprob = logprob.view(f32)
+    lib, handle = ctx.bind()
+    st = lib.ivf_sample(handle, logits.data_ptr(), dt, stride if T > 1 else 0, T, V, *args, token.data_ptr(),
+                        logprob.data_ptr())
+    if st:
+        ctx.check(st, "ivf_sample")
+    return token, logprob

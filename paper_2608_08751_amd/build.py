@@ -20,7 +20,7 @@ LIB = os.path.join(HERE, "libivf.so")
 
 SOURCES = ["api.cpp", "screen.hip", "screen_i8.hip", "screen_f16.hip", "select.hip", "fallback.hip", "resolve.hip", "lists.hip", "lists_radix.hip", "kmeans.hip", "layout.hip", "pq.hip", "assign_graph.hip", "adc.hip", "probe.hip",
            "api_kv.cpp", "kv_plan.hip", "kv_pages.hip", "kv_cache.hip", "kv_select.hip", "kv_attend.hip", "kv_attend_terms.hip", "kv_prompt.hip",
-           "kv_prompt_terms.hip"]
+           "kv_prompt_terms.hip", "api_sample.cpp", "sample.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
