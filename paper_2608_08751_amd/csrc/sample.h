@@ -7,6 +7,8 @@
 namespace ivf {
 
 constexpr int64_t kSampleMaxVocab = 1 << 20;  // weights of 2^43 at most: their sums stay below 2^63
+constexpr int kSampleMaxParts = 8;               // workgroups that share a row
+constexpr int kSampleList = 2048;
 
 struct Sample {
     const void *logits;
@@ -20,8 +22,9 @@ struct Sample {
     const float *top_p, *min_p;
     int32_t *token;
     float *logprob;  // may be null
+    int parts, per;  // workgroups a row; groups of eight logits a wave
 };
 
-hipError_t launch_sample(const Sample &a, hipStream_t s);
+hipError_t launch_sample(Sample a, hipStream_t s);
 
 }  // namespace ivf

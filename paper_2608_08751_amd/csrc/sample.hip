@@ -10,6 +10,15 @@
 // sums are exact, so that no order of additions matters (atomics included), and
 // a border between two tokens, or of top_p, is off by at most 2^-43 a weight. With fp32
 // sums one in some hundred draws from 128,000 tokens would take a neighbour of the right token.
+//
+// A row is gone over two to four times (from the caches after the first):
+//   ends     the largest and the least logit;
+//   bins     with top_k or top_p: numbers and weights of 2,048 bins by distance to the largest
+//            (of 31 temperatures at most), from which follows the bin in which the kept part ends;
+//   collect  the elements of the bins up to it, where they are few, which are then put in order
+//            and drawn from in LDS; else those of that bin alone, with the sums of all before it;
+//   draw     the range of the row that the running sum ends in, once more.
+// Rows without top_k and top_p take their weights' sums, range by range, in place of bins and collect.
 #include "sample.h"
 
 #include "ivf.h"
@@ -20,18 +29,18 @@ namespace ivf {
 namespace {
 
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
-constexpr int kTile = kThreads * 8;      // elements of a step: eight a thread
-constexpr int kSegments = ((int)kSampleMaxVocab / kTile + 2) * kWaves;  // of 512 elements, a wave's share of a step
 constexpr int kBins = 2048;              // the last one holds what weighs nothing
-constexpr int kList = 1024;              // elements of a bin that are put in order one by one
+constexpr int kList = kSampleList;       // elements that are put in order in LDS
+constexpr int kTile = kThreads * 8;
+constexpr int kSegments = ((int)kSampleMaxVocab / kTile + 2) * kWaves;  // of 512 elements, a wave's share of a tile
 constexpr double kUnit = 8796093022208.0;  // 2^43
 
 typedef unsigned long long u64;
 
-// Numbers as unsigned ones of the same order, and back.
+// Numbers as unsigned ones of the same order (0 and -0 as one), and back.
 __device__ __forceinline__ uint32_t order_of(float x)
 {
-    const uint32_t b = __float_as_uint(x);
+    const uint32_t b = __float_as_uint(x + 0.f);
     return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float number_of(uint32_t o)
@@ -42,22 +51,34 @@ __device__ __forceinline__ float number_of(uint32_t o)
 __device__ __forceinline__ u64 place_of(float x, int i) { return (u64)order_of(x) << 32 | (uint32_t)~i; }
 __device__ __forceinline__ int index_of(u64 place) { return (int)~(uint32_t)place; }
 
-// A logit as it counts: no number as -infinity, +infinity as the largest number, -0 as 0.
-__device__ __forceinline__ float clean(float x) { return fminf(fmaxf(x, -INFINITY), 3.40282347e38f) + 0.f; }
+// A logit as it counts: no number as -infinity, +infinity as the largest number.
+__device__ __forceinline__ float clean(float x) { return fminf(x == x ? x : -INFINITY, 3.40282347e38f); }
 
 __device__ __forceinline__ float widen(float x) { return x; }
 __device__ __forceinline__ float widen(_Float16 x) { return (float)x; }
 __device__ __forceinline__ float widen(__bf16 x) { return (float)x; }
 
-// A row of V logits, taken in groups of eight that begin at multiples of 16 bytes.
+// A row of V logits, taken in groups of eight that begin at multiples of 16 bytes. A range is the groups that one
+// wave goes over, `per` of them; a row has parts * kWaves ranges.
 template <typename E> struct Row {
     const E *p;
     int V, pad;  // elements of the first group that lie before the row
-    __device__ __forceinline__ int end() const { return V + pad; }
-    // x[j]: element v + j - pad, -infinity outside the row
-    __device__ __forceinline__ void load(int v, float (&x)[8]) const
+    int per, parts;
+    __device__ __forceinline__ Row(const Sample &a, int64_t t)
     {
-        const int i = v - pad;
+        p = (const E *)a.logits + t * a.stride;
+        V = a.V;
+        pad = (int)((uintptr_t)p % 16 / sizeof(E));
+        per = a.per;
+        parts = a.parts;
+    }
+    __device__ __forceinline__ int groups() const { return (V + pad + 7) >> 3; }
+    __device__ __forceinline__ int first_of(int g) const { return 8 * g - pad; }
+    __device__ __forceinline__ int range_of(int i) const { return ((i + pad) >> 3) / per; }
+    // the elements of group g, -infinity outside the row
+    __device__ __forceinline__ void load(int g, float (&x)[8]) const
+    {
+        const int i = first_of(g);
         if (i >= 0 && i + 8 <= V) {
             union {
                 uint4 w[sizeof(E) / 2];
@@ -72,15 +93,30 @@ template <typename E> struct Row {
             for (int j = 0; j < 8; ++j) x[j] = i + j >= 0 && i + j < V ? clean(widen(p[i + j])) : -INFINITY;
         }
     }
+    // Calls f(x[8], index of x[0]) for the groups of range r, all lanes each time (-infinity past its end).
+    template <typename F> __device__ __forceinline__ void for_range(int r, F f) const
+    {
+        const int lane = threadIdx.x & 63, end = min((r + 1) * per, groups());
+        for (int g = r * per; g < end; g += 64) {
+            float x[8];
+            if (g + lane < end) {
+                load(g + lane, x);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] = -INFINITY;
+            }
+            f(x, first_of(g + lane));
+        }
+    }
 };
 
 // w = 2^43 exp((x - m) / t) to the nearest whole number; 2^f by a polynomial of degree 9 in f (fitted on
-// [-1/2, 1/2] with 2^0 = 1, relative error 2^-44.6).
-__device__ __forceinline__ u64 weight(float x, float m, double inv_t)
+// [-1/2, 1/2] with 2^0 = 1, relative error 2^-44.6). -infinity weighs nothing.
+__device__ __forceinline__ u64 weight(float x, double m, double inv_t)
 {
-    // -infinity with any temperature (no number with an infinite one) weighs nothing
-    const double d = fmax(((double)x - (double)m) * inv_t, -60.0);
-    const double n = rint(d), f = d - n;
+    constexpr double kRound = 6755399441055744.0;  // 1.5 2^52: the sum's low bits are the nearest whole number
+    const double d = fmax(((double)x - m) * inv_t, -60.0);
+    const double n = d + kRound, f = d - (n - kRound);
     double r = 1.020312117214188e-07;
     r = fma(r, f, 1.325522487405178e-06);
     r = fma(r, f, 1.5252686845751567e-05);
@@ -91,8 +127,9 @@ __device__ __forceinline__ u64 weight(float x, float m, double inv_t)
     r = fma(r, f, 0.2402265069581299);
     r = fma(r, f, 0.6931471805599453);
     r = fma(r, f, 1.0);
-    const double w = ldexp(r, (int)n + 43) + 4503599627370496.0;  // 2^52: rounds, the whole number in the low bits
-    return (u64)__double_as_longlong(w) & 0xfffffffffffffull;
+    // times 2^(n + 43) in the exponent; + 2^52 rounds
+    const u64 b = (u64)__double_as_longlong(r) + ((u64)(uint32_t)((int)__double_as_longlong(n) + 43) << 52);
+    return (u64)__double_as_longlong(__longlong_as_double((long long)b) + 4503599627370496.0) & 0xfffffffffffffull;
 }
 
 __device__ __forceinline__ u64 shfl_up64(u64 x, int d) { return (u64)__shfl_up((long long)x, d); }
@@ -103,15 +140,25 @@ __device__ __forceinline__ u64 wave_sum(u64 x)
     return x;
 }
 
+// How the kept part of a row ends: nowhere; in the last of few elements, all listed; in a listed bin; or in one that
+// has more elements than a list.
+enum Mode { kWhole, kFew, kInBin, kMany };
+
 struct Shared {
     uint32_t count[kBins];
-    u64 sum[kBins];       // weights
-    u64 segment[kSegments];
-    u64 list[kList], sorted[kList];
+    u64 sum[kBins];          // weights
+    u64 list[kList];         // places
+    u64 segment[kSegments];  // or, of a list, indexes and weights
+    u64 range[kSampleMaxParts * kWaves];
     u64 waves[kWaves];
-    uint32_t cursor, bin;
-    u64 cut, before, through;
+    float low[kWaves], high[kWaves];
+    // the bin where a leading part ends, and what comes before it
+    int bin;
     uint32_t rest;
+    u64 before;
+    uint32_t cursor;
+    u64 cut, through;
+    int mode, token;
 };
 
 // The sum of x over the threads before this one; *all: over all of them.
@@ -136,87 +183,416 @@ __device__ __forceinline__ u64 sum_before(Shared &s, u64 x, u64 *all)
     return before;
 }
 
-// Calls f(x[8], index of x[0], segment) for all of the row; indexes outside it come with -infinity.
-template <typename E, typename F> __device__ __forceinline__ void for_row(const Row<E> &row, F f)
+// What a row asks for, with its largest and least logit.
+struct Limits {
+    float m;
+    double md, inv_t;
+    float per;  // bins a unit of distance to the largest
+    bool none, greedy, by_k, by_p;
+    int top_k;
+    float top_p;
+    double least_w;
+    __device__ __forceinline__ Limits(const Sample &a, int64_t t, float high, float low)
+    {
+        // (beyond 2^60 the range of the bins would not hold in fp32; no number stays none)
+        const float given = a.temperature ? a.temperature[t] : 1.f, temp = given > 0x1p60f ? 0x1p60f : given;
+        m = high;
+        md = (double)high;
+        none = high == -INFINITY;
+        greedy = !(temp > 0.f);
+        inv_t = 1.4426950408889634 / (double)temp;
+        // beyond 31 temperatures a weight is below 2^-44
+        per = ((float)(kBins - 1) - 0.5f) / fmaxf(fminf(high - low, 31.f * temp), 1e-30f);
+        top_k = a.top_k ? a.top_k[t] : 0;
+        top_p = a.top_p ? a.top_p[t] : 1.f;
+        by_k = top_k > 0 && top_k < a.V;
+        by_p = top_p < 1.f;
+        least_w = (a.min_p ? (double)fminf(fmaxf(a.min_p[t], 0.f), 1.f) : 0.0) * kUnit;
+    }
+    __device__ __forceinline__ bool cuts() const { return !none && !greedy && (by_k || by_p); }
+    __device__ __forceinline__ int bin(float x) const { return (int)fminf((m - x) * per, (float)(kBins - 1)); }
+    __device__ __forceinline__ u64 weigh(float x) const { return weight(x, md, inv_t); }
+    // the weight of an element that is kept, else 0
+    __device__ __forceinline__ u64 kept(float x, int i, u64 cut) const
+    {
+        if (cut && place_of(x, i) < cut) return 0;
+        const u64 w = weigh(x);
+        return (double)w >= least_w ? w : 0;
+    }
+    // the weights that top_p of `whole` asks for
+    __device__ __forceinline__ u64 need(u64 whole) const
+    {
+        return max((u64)1, (u64)ceil((double)fmaxf(top_p, 0.f) * (double)whole));
+    }
+};
+
+// The largest and the least logit of a part (16 ranges), the least of those above -infinity; all threads get them.
+template <typename E> __device__ float2 ends_of(Shared &s, const Row<E> &row, int part)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    float high = -INFINITY, low = INFINITY;
+    row.for_range(part * kWaves + wave, [&](const float (&x)[8], int) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            high = fmaxf(high, x[j]);
+            low = fminf(low, x[j] > -INFINITY ? x[j] : INFINITY);
+        }
+    });
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        high = fmaxf(high, __shfl_xor(high, d));
+        low = fminf(low, __shfl_xor(low, d));
+    }
+    if (lane == 0) {
+        s.low[wave] = low;
+        s.high[wave] = high;
+    }
+    __syncthreads();
+    for (int w = 0; w < kWaves; ++w) {
+        high = fmaxf(high, s.high[w]);
+        low = fminf(low, s.low[w]);
+    }
+    return make_float2(high, low);
+}
+
+// The lowest index of the part at which the largest logit stands; thread 0 gets it.
+template <typename E> __device__ int first_of(Shared &s, const Row<E> &row, float m, int part)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int first = INT32_MAX;
+    row.for_range(part * kWaves + wave, [&](const float (&x)[8], int i) {
+#pragma unroll
+        for (int j = 7; j >= 0; --j)
+            if (x[j] == m) first = min(first, i + j);
+    });
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) first = min(first, __shfl_xor(first, d));
+    if (lane == 0) s.waves[wave] = (u64)first;
+    __syncthreads();
+    for (int w = 0; w < kWaves; ++w) first = min(first, (int)s.waves[w]);
+    return first;
+}
+
+// Kept weights of range r (a wave); those of bins from `bin` on apart.
+template <typename E> __device__ u64 sum_of(const Row<E> &row, const Limits &l, int r, u64 cut, int bin)
+{
+    u64 sum = 0;
+    row.for_range(r, [&](const float (&x)[8], int i) {
+        if (bin < kBins - 1 || cut) {
+            float most = x[0];
+#pragma unroll
+            for (int j = 1; j < 8; ++j) most = fmaxf(most, x[j]);
+            if (!__any(l.bin(most) < bin && order_of(most) >= (uint32_t)(cut >> 32))) return;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const u64 w = l.kept(x[j], i + j, cut);
+            if (l.bin(x[j]) < bin) sum += w;
+        }
+    });
+    return wave_sum(sum);
+}
+
+// Numbers and weights of the part's bins, in LDS.
+template <typename E> __device__ void fill_bins(Shared &s, const Row<E> &row, const Limits &l, int part)
 {
     const int tid = threadIdx.x;
-    for (int v0 = 0; v0 < row.end(); v0 += kTile) {
-        float x[8];
-        row.load(v0 + 8 * tid, x);
-        f(x, v0 + 8 * tid - row.pad, v0 / kTile * kWaves + (tid >> 6));
+    for (int b = tid; b < kBins; b += kThreads) {
+        s.count[b] = 0;
+        s.sum[b] = 0;
+    }
+    __syncthreads();
+    row.for_range(part * kWaves + (tid >> 6), [&](const float (&x)[8], int) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int b = l.bin(x[j]);
+            if (b < kBins - 1) {
+                atomicAdd(&s.count[b], 1u);
+                if (l.by_p) atomicAdd(&s.sum[b], l.weigh(x[j]));
+            }
+        }
+    });
+    __syncthreads();
+}
+
+// The bin where a leading part ends that has `need` elements, or weights: s.bin, and what comes before it, s.rest and
+// s.before. c, w: two bins of this thread, cn, wn: what comes before them.
+struct Scan {
+    uint32_t c[kBins / kThreads];
+    u64 w[kBins / kThreads], cn, wn, all_c, all_w;
+    __device__ __forceinline__ explicit Scan(Shared &s)
+    {
+        u64 cs = 0, ws = 0;
+#pragma unroll
+        for (int k = 0; k < kBins / kThreads; ++k) {
+            c[k] = s.count[threadIdx.x * (kBins / kThreads) + k];
+            w[k] = s.sum[threadIdx.x * (kBins / kThreads) + k];
+            cs += c[k];
+            ws += w[k];
+        }
+        cn = sum_before(s, cs, &all_c);
+        wn = sum_before(s, ws, &all_w);
+    }
+    __device__ __forceinline__ void find(Shared &s, u64 need, bool by_weight) const
+    {
+        u64 a = cn, b = wn;
+#pragma unroll
+        for (int k = 0; k < kBins / kThreads; ++k) {
+            if (by_weight ? b < need && b + w[k] >= need : a < need && a + c[k] >= need) {
+                s.bin = threadIdx.x * (kBins / kThreads) + k;
+                s.rest = (uint32_t)a;
+                s.before = b;
+            }
+            a += c[k];
+            b += w[k];
+        }
+        __syncthreads();
+    }
+};
+
+// Where the kept part ends (without min_p), from the row's bins: s.mode, s.bin, s.rest, s.before. Returns whether top_k
+// cuts (else there are no more elements that weigh something).
+__device__ bool decide(Shared &s, const Limits &l, const Scan &scan)
+{
+    const bool k_cuts = l.by_k && (u64)l.top_k <= scan.all_c;
+    if (k_cuts) scan.find(s, (u64)l.top_k, false);
+    else if (l.by_p) scan.find(s, l.need(scan.all_w), true);
+    if (threadIdx.x == 0) {
+        if (!k_cuts && !l.by_p) {
+            s.mode = kWhole;
+            s.bin = kBins - 1;
+        } else if (s.rest + s.count[s.bin] <= kList) {
+            s.mode = kFew;
+        } else {
+            // (with both, top_p goes by what top_k leaves)
+            s.mode = !(k_cuts && l.by_p) && s.count[s.bin] <= kList ? kInBin : kMany;
+        }
+    }
+    __syncthreads();
+    return k_cuts;
+}
+
+// The part's elements of bins lo ... hi, in no order. `cursor` and `list` are in LDS or device memory.
+template <typename E>
+__device__ void collect(const Row<E> &row, const Limits &l, int part, int lo, int hi, uint32_t *cursor, u64 *list)
+{
+    const int lane = threadIdx.x & 63;
+    row.for_range(part * kWaves + (threadIdx.x >> 6), [&](const float (&x)[8], int i) {
+        float most = x[0];
+#pragma unroll
+        for (int j = 1; j < 8; ++j) most = fmaxf(most, x[j]);
+        if (!__any(l.bin(most) <= hi)) return;
+        uint32_t hits = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int b = l.bin(x[j]);
+            hits |= (uint32_t)(b >= lo && b <= hi) << j;
+        }
+        const uint32_t n = __popc(hits);
+        uint32_t up = n;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const uint32_t y = __shfl_up(up, d);
+            if (lane >= d) up += y;
+        }
+        const uint32_t all = __builtin_amdgcn_readlane(up, 63);
+        if (!all) return;
+        uint32_t at = 0;
+        if (lane == 0) at = atomicAdd(cursor, all);
+        at = __builtin_amdgcn_readfirstlane(at) + up - n;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (hits >> j & 1) {
+                if (at < kList) list[at] = place_of(x[j], i + j);
+                ++at;
+            }
+    });
+}
+
+// Sorts list[0, n), descending, in LDS; up to the next power of two it is filled with zeros. Strides of up to 64
+// stay inside what a wave holds.
+__device__ void sort_list(u64 *list, int n)
+{
+    const int tid = threadIdx.x;
+    int m = 2;
+    while (m < n) m <<= 1;
+    for (int i = n + tid; i < m; i += kThreads) list[i] = 0;
+    __syncthreads();
+    for (int k = 2; k <= m; k <<= 1)
+        for (int j = k >> 1; j > 0; j >>= 1) {
+            if (tid < m / 2) {
+                const int i = 2 * tid - (tid & (j - 1));
+                const u64 a = list[i], b = list[i + j];
+                if ((a < b) == ((i & k) == 0)) {
+                    list[i] = b;
+                    list[i + j] = a;
+                }
+            }
+            if (j > 64 || (j == 1 && k >= 128)) {
+                __syncthreads();
+            } else {
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+            }
+        }
+    __syncthreads();
+}
+
+// Finds the token whose running sum passes `goal` among a wave's or workgroup's elements, in the order of threads
+// and of w[8]: called with the sum before this thread's.
+template <int N>
+__device__ __forceinline__ void pick(Shared &s, const Sample &a, const Limits &l, int64_t t, u64 running, u64 goal, u64 whole,
+                                     const u64 (&w)[N], const float (&x)[N], const int (&index)[N])
+{
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        if (running <= goal && running + w[j] > goal) {
+            a.token[t] = index[j];
+            if (a.logprob)
+                a.logprob[t] = (float)(((double)x[j] - l.md) * l.inv_t * 0.6931471805599453 - log((double)whole / kUnit));
+            s.token = index[j];
+        }
+        running += w[j];
     }
 }
 
-// What a row's elements are put into bins by: the distance to the largest, in steps.
-struct Binning {
-    float m, per;
-    __device__ __forceinline__ int operator()(float x) const { return (int)fminf((m - x) * per, (float)(kBins - 1)); }
-};
-
-// The element at which a leading part of the order ends: the first whose elements number `need`, or
-// whose weights reach `need` (by_weight), which lies in `bin` (`count` and `sum` come before it).
-// Writes s.cut (its place) and s.through (the weights up to it). All threads call it.
-template <typename E>
-__device__ void find_cut(Shared &s, const Row<E> &row, Binning bins, double inv_t, int bin, uint32_t count, u64 sum, u64 need,
-                         bool by_weight)
+// The running sum that the row's number asks for: the first above it is the token's.
+__device__ __forceinline__ u64 goal_of(const Sample &a, int64_t t, u64 whole)
 {
-    const int tid = threadIdx.x, lane = tid & 63;
-    const uint32_t n = s.count[bin];
-    if (n <= kList) {
-        // put the bin's elements in order, each by the number of larger ones
-        if (tid == 0) s.cursor = 0;
-        __syncthreads();
-        for_row(row, [&](const float (&x)[8], int i, int) {
+    const float u = fmaxf(a.uniform[t], 0.f);
+    return u < 1.f ? min((u64)((double)u * (double)whole), whole - 1) : whole - 1;
+}
+
+// kFew: all that can be kept is listed, n elements.
+__device__ void draw_listed(Shared &s, const Sample &a, const Limits &l, int64_t t, int n, bool k_cuts, u64 all_w)
+{
+    const int tid = threadIdx.x;
+    sort_list(s.list, n);
+    u64 place[2], w[2], all;
+    int i2[2];
+    float x2[2];
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (bins(x[j]) == bin && i + j >= 0 && i + j < row.V) s.list[atomicAdd(&s.cursor, 1u)] = place_of(x[j], i + j);
-        });
-        __syncthreads();
-        u64 mine = 0;
-        if (tid < (int)n) {
-            mine = s.list[tid];
-            int larger = 0;
-            for (uint32_t j = 0; j < n; ++j) larger += s.list[j] > mine;
-            s.sorted[larger] = mine;
-        }
-        __syncthreads();
-        mine = tid < (int)n ? s.sorted[tid] : 0;
-        const u64 w = tid < (int)n ? weight(number_of((uint32_t)(mine >> 32)), bins.m, inv_t) : 0;
-        u64 all;
-        const u64 before = sum + sum_before(s, w, &all);
-        const bool here = by_weight ? before < need && before + w >= need : count + tid + 1 == need;
-        if (here && tid < (int)n) {
-            s.cut = mine;
-            s.through = before + w;
-        }
-        __syncthreads();
-        return;
+    for (int k = 0; k < 2; ++k) {
+        place[k] = 2 * tid + k < n ? s.list[2 * tid + k] : 0;
+        w[k] = place[k] ? l.weigh(number_of((uint32_t)(place[k] >> 32))) : 0;
     }
-    // many elements: the cut's number eight bits at a time, then its index among equal ones
+    if (tid == 0) s.rest = n;
+    const u64 before = sum_before(s, w[0] + w[1], &all);
+    const int most = k_cuts ? l.top_k : n;  // elements that top_k leaves
+    if (l.by_p) {
+        u64 whole = all_w;
+        if (k_cuts) {
+            if ((most - 1) / 2 == tid) s.through = before + w[0] + (most % 2 ? 0 : w[1]);
+            __syncthreads();
+            whole = s.through;
+        }
+        const u64 need = l.need(whole);
+        if (before < need && before + w[0] >= need) s.rest = 2 * tid + 1;
+        else if (before + w[0] < need && before + w[0] + w[1] >= need) s.rest = 2 * tid + 2;
+    }
+    __syncthreads();
+    // what is kept, in the order of the indexes: a weight takes 44 bits, an index 20
+    const int keep = min(most, (int)s.rest);
+    if (tid == 0) s.cursor = 0;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+        if (2 * tid + k < keep && (double)w[k] >= l.least_w)
+            s.segment[atomicAdd(&s.cursor, 1u)] = (u64)(uint32_t)(kSampleMaxVocab - 1 - index_of(place[k])) << 44 | w[k];
+    __syncthreads();
+    const int kept = (int)s.cursor;
+    sort_list(s.segment, kept);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const u64 e = 2 * tid + k < kept ? s.segment[2 * tid + k] : 0;
+        w[k] = e & 0xfffffffffffull;
+        i2[k] = e ? min((int)(kSampleMaxVocab - 1) - (int)(e >> 44), a.V - 1) : 0;  // (no entry: weighs nothing)
+    }
+    u64 whole;
+    const u64 running = sum_before(s, w[0] + w[1], &whole);
+    const u64 goal = goal_of(a, t, whole);
+    if (running <= goal && running + w[0] + w[1] > goal) {
+        // the logit from its weight would lose what small ones have: from the row
+        const int64_t at = t * a.stride;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            x2[k] = clean(a.dt == IVF_F32   ? ((const float *)a.logits)[at + i2[k]]
+                          : a.dt == IVF_F16 ? widen(((const _Float16 *)a.logits)[at + i2[k]])
+                                            : widen(((const __bf16 *)a.logits)[at + i2[k]]));
+        }
+        pick(s, a, l, t, running, goal, whole, w, x2, i2);
+    }
+}
+
+// The token from the ranges' kept weights (s.range): the range where the running sum passes the goal, once more.
+template <typename E> __device__ void draw_ranges(Shared &s, const Sample &a, const Row<E> &row, const Limits &l, int64_t t, u64 cut)
+{
+    const int tid = threadIdx.x, ranges = row.parts * kWaves;
+    u64 whole, x = tid < ranges ? s.range[tid] : 0;
+    const u64 at = sum_before(s, x, &whole);
+    const u64 goal = goal_of(a, t, whole);
+    if (at <= goal && at + x > goal) {
+        s.bin = tid;
+        s.before = at;
+    }
+    if (tid == 0) s.token = -1;
+    __syncthreads();
+    u64 base = s.before;
+    const int end = min((s.bin + 1) * row.per, row.groups());
+    for (int g0 = s.bin * row.per; g0 < end; g0 += kThreads) {
+        float y[8];
+        int index[8];
+        u64 w[8], sum = 0, all;
+        if (g0 + tid < end) {
+            row.load(g0 + tid, y);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = -INFINITY;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            index[j] = row.first_of(g0 + tid) + j;
+            w[j] = l.kept(y[j], index[j], cut);
+            sum += w[j];
+        }
+        const u64 before = base + sum_before(s, sum, &all);
+        if (before <= goal && before + sum > goal) pick(s, a, l, t, before, goal, whole, w, y, index);
+        base += all;
+        if (base > goal) break;  // uniform
+    }
+}
+
+// kMany: the cut of one limit by going over the row, in one workgroup. It is the first element whose elements number
+// `need`, or whose weights reach `need` (by_weight), and lies in s.bin (s.rest and s.before come before it).
+// Writes s.cut (its place) and s.through (the weights up to it). All threads call it.
+template <typename E> __device__ void find_cut(Shared &s, const Row<E> &row, const Limits &l, u64 need, bool by_weight)
+{
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, ranges = row.parts * kWaves;
+    const int bin = s.bin;
+    u64 count = s.rest, sum = s.before;
+    u64 *number = s.list, *heavy = s.list + 256;
+    // its number eight bits at a time, then its index among equal ones
     uint32_t prefix = 0;
     for (int shift = 24; shift >= 0; shift -= 8) {
-        if (tid < 256) {
-            s.list[tid] = 0;
-            s.sorted[tid] = 0;
-        }
         __syncthreads();
-        for_row(row, [&](const float (&x)[8], int i, int) {
+        if (tid < 256) number[tid] = heavy[tid] = 0;
+        __syncthreads();
+        for (int r = wave; r < ranges; r += kWaves)
+            row.for_range(r, [&](const float (&x)[8], int) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const uint32_t o = order_of(x[j]);
-                if (bins(x[j]) == bin && i + j >= 0 && i + j < row.V && (shift == 24 || (o ^ prefix) >> (shift + 8) == 0)) {
-                    atomicAdd(&s.list[o >> shift & 255], 1ull);
-                    atomicAdd(&s.sorted[o >> shift & 255], weight(x[j], bins.m, inv_t));
+                for (int j = 0; j < 8; ++j) {
+                    const uint32_t o = order_of(x[j]);
+                    if (l.bin(x[j]) == bin && (shift == 24 || (o ^ prefix) >> (shift + 8) == 0)) {
+                        atomicAdd(&number[o >> shift & 255], 1ull);
+                        if (l.by_p) atomicAdd(&heavy[o >> shift & 255], l.weigh(x[j]));
+                    }
                 }
-            }
-        });
+            });
         __syncthreads();
         // digits from the largest down
-        const u64 c = tid < 256 ? s.list[255 - tid] : 0;
+        const u64 c = tid < 256 ? number[255 - tid] : 0, w = tid < 256 ? heavy[255 - tid] : 0;
         u64 all;
-        const u64 cb = count + sum_before(s, c, &all);
-        const u64 w = tid < 256 ? s.sorted[255 - tid] : 0;
-        const u64 wb = sum + sum_before(s, w, &all);
+        const u64 cb = count + sum_before(s, c, &all), wb = sum + sum_before(s, w, &all);
         if (c && (by_weight ? wb < need && wb + w >= need : cb < need && cb + c >= need)) {
             s.cursor = 255 - tid;
             s.rest = (uint32_t)cb;
@@ -226,20 +602,26 @@ __device__ void find_cut(Shared &s, const Row<E> &row, Binning bins, double inv_
         prefix |= s.cursor << shift;
         count = s.rest;
         sum = s.before;
-        __syncthreads();
     }
     // the elements equal to it weigh the same
-    const u64 w = weight(number_of(prefix), bins.m, inv_t);
+    const u64 w = l.weigh(number_of(prefix));
     const uint32_t rank = by_weight ? (uint32_t)((need - sum + w - 1) / w) : (uint32_t)(need - count);  // from 1
-    for_row(row, [&](const float (&x)[8], int i, int seg) {
-        int equal = 0;
+    const int segments = (row.groups() + 63) / 64, per = (segments + kThreads - 1) / kThreads;
+    auto equal_of = [&](int seg, float (&x)[8]) {
+        u64 equal = 0;
+        if (64 * seg + lane < row.groups()) {
+            row.load(64 * seg + lane, x);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) equal += order_of(x[j]) == prefix && i + j >= 0 && i + j < row.V;
-        const u64 of_wave = wave_sum(equal);
+            for (int j = 0; j < 8; ++j) equal += order_of(x[j]) == prefix;
+        }
+        return equal;
+    };
+    float x[8];
+    for (int seg = wave; seg < segments; seg += kWaves) {
+        const u64 of_wave = wave_sum(equal_of(seg, x));
         if (lane == 0) s.segment[seg] = of_wave;
-    });
+    }
     __syncthreads();
-    const int segments = (row.end() + kTile - 1) / kTile * kWaves, per = (segments + kThreads - 1) / kThreads;
     u64 mine = 0, all;
     for (int k = 0; k < per; ++k)
         if (tid * per + k < segments) mine += s.segment[tid * per + k];
@@ -254,13 +636,8 @@ __device__ void find_cut(Shared &s, const Row<E> &row, Binning bins, double inv_
             at += c;
         }
     __syncthreads();
-    if (tid < 64) {
-        const int v = (int)s.bin * 512 + 8 * lane;
-        float x[8];
-        row.load(v, x);
-        int equal = 0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) equal += order_of(x[j]) == prefix && v - row.pad + j >= 0 && v - row.pad + j < row.V;
+    if (wave == 0) {
+        const u64 equal = equal_of(s.bin, x);
         u64 up = equal;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
@@ -268,194 +645,117 @@ __device__ void find_cut(Shared &s, const Row<E> &row, Binning bins, double inv_
             if (lane >= d) up += y;
         }
         u64 n = s.before + up - equal;
+        if (equal)
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (order_of(x[j]) == prefix && v - row.pad + j >= 0 && v - row.pad + j < row.V && ++n == rank) {
-                s.cut = place_of(x[j], v - row.pad + j);
-                s.through = sum + rank * w;
-            }
+            for (int j = 0; j < 8; ++j)
+                if (order_of(x[j]) == prefix && ++n == rank) {
+                    s.cut = place_of(x[j], row.first_of(64 * s.bin + lane) + j);
+                    s.through = sum + rank * w;
+                }
     }
     __syncthreads();
 }
 
-template <typename E> __global__ __launch_bounds__(kThreads) void sample_kernel(Sample a)
+// The row's token once its bins are in LDS and what `decide` asks for is collected: s.list and s.cursor, and s.range.
+template <typename E>
+__device__ void finish(Shared &s, const Sample &a, const Row<E> &row, const Limits &l, int64_t t, const Scan &scan, bool k_cuts)
 {
-    __shared__ Shared s;
-    const int64_t t = blockIdx.x;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    Row<E> row;
-    row.p = (const E *)a.logits + t * a.stride;
-    row.V = a.V;
-    row.pad = (int)((uintptr_t)row.p % 16 / sizeof(E));
-    // (beyond 2^60 the range of the bins would not hold in fp32; no number stays none)
-    const float given = a.temperature ? a.temperature[t] : 1.f, temp = given > 0x1p60f ? 0x1p60f : given;
-    const int top_k = a.top_k ? a.top_k[t] : 0;
-    const float top_p = a.top_p ? a.top_p[t] : 1.f, min_p = a.min_p ? a.min_p[t] : 0.f;
-    const double inv_t = 1.4426950408889634 / (double)temp;
-
-    // the largest logit, the first of its value, and the least finite one
-    u64 top = 0;
-    float least = INFINITY;
-    for_row(row, [&](const float (&x)[8], int i, int) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const u64 p = place_of(x[j], i + j);
-            if (i + j >= 0 && i + j < row.V && p > top) top = p;
-            if (x[j] > -INFINITY) least = fminf(least, x[j]);
-        }
-    });
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        top = max(top, (u64)__shfl_xor((long long)top, d));
-        least = fminf(least, __shfl_xor(least, d));
-    }
-    if (lane == 0) {
-        s.list[wave] = top;
-        s.sorted[wave] = __float_as_uint(least);
-    }
-    __syncthreads();
-    for (int w = 0; w < kWaves; ++w) {
-        top = max(top, s.list[w]);
-        least = fminf(least, __uint_as_float((uint32_t)s.sorted[w]));
-    }
-    __syncthreads();
-    const float m = number_of((uint32_t)(top >> 32));
-    if (m == -INFINITY || !(temp > 0.f)) {
-        if (tid == 0) {
-            a.token[t] = m == -INFINITY ? -1 : index_of(top);
-            if (a.logprob) a.logprob[t] = m == -INFINITY ? -INFINITY : 0.f;
-        }
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, ranges = row.parts * kWaves;
+    const int mode = s.mode;
+    if (mode == kFew) {
+        draw_listed(s, a, l, t, (int)min(s.cursor, (uint32_t)kList), k_cuts, scan.all_w);
         return;
     }
-
-    u64 cut = 0;  // what is kept has this place or a larger one
-    const bool by_k = top_k > 0 && top_k < a.V, by_p = top_p < 1.f;
-    if (by_k || by_p) {
-        Binning bins;
-        bins.m = m;
-        // beyond 31 temperatures a weight is below 2^-44
-        bins.per = ((float)(kBins - 1) - 0.5f) / fmaxf(fminf(m - least, 31.f * temp), 1e-30f);
-        for (int b = tid; b < kBins; b += kThreads) {
-            s.count[b] = 0;
-            s.sum[b] = 0;
+    u64 cut = 0;
+    if (mode == kInBin) {
+        const int n = (int)min(s.cursor, (uint32_t)kList);
+        const u64 need = k_cuts ? (u64)l.top_k - s.rest : l.need(scan.all_w) - s.before;  // of the list
+        sort_list(s.list, n);
+        u64 place[2], w[2], all;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            place[k] = 2 * tid + k < n ? s.list[2 * tid + k] : 0;
+            w[k] = place[k] ? l.weigh(number_of((uint32_t)(place[k] >> 32))) : 0;
+        }
+        u64 before = sum_before(s, w[0] + w[1], &all);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            if (place[k] && (k_cuts ? (u64)(2 * tid + k + 1) <= need : before < need)) {
+                if (k_cuts ? (u64)(2 * tid + k + 1) == need : before + w[k] >= need) s.cut = place[k];
+                if ((double)w[k] >= l.least_w) atomicAdd(&s.range[row.range_of(index_of(place[k]))], w[k]);
+            }
+            before += w[k];
         }
         __syncthreads();
-        for_row(row, [&](const float (&x)[8], int i, int) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int b = bins(x[j]);
-                if (b < kBins - 1) {
-                    atomicAdd(&s.count[b], 1u);
-                    if (by_p) atomicAdd(&s.sum[b], weight(x[j], m, inv_t));
-                }
-            }
-        });
-        __syncthreads();
-        uint32_t c[kBins / kThreads];
-        u64 w[kBins / kThreads], cs = 0, ws = 0, call, wall;
-#pragma unroll
-        for (int k = 0; k < kBins / kThreads; ++k) {
-            c[k] = s.count[tid * (kBins / kThreads) + k];
-            w[k] = s.sum[tid * (kBins / kThreads) + k];
-            cs += c[k];
-            ws += w[k];
-        }
-        const u64 cb = sum_before(s, cs, &call), wb = sum_before(s, ws, &wall);
-        // the bin where a leading part ends that has `need` elements, or weights
-        auto bin_of = [&](u64 need, bool by_weight) {
-            u64 cn = cb, wn = wb;
-#pragma unroll
-            for (int k = 0; k < kBins / kThreads; ++k) {
-                if (by_weight ? wn < need && wn + w[k] >= need : cn < need && cn + c[k] >= need) {
-                    s.bin = tid * (kBins / kThreads) + k;
-                    s.rest = (uint32_t)cn;
-                    s.before = wn;
-                }
-                cn += c[k];
-                wn += w[k];
-            }
-            __syncthreads();
-        };
-        u64 whole = wall;  // weights of the first top_k
-        if (by_k && (u64)top_k <= call) {
-            bin_of((u64)top_k, false);
-            find_cut(s, row, bins, inv_t, (int)s.bin, s.rest, s.before, (u64)top_k, false);
+        cut = s.cut;
+    } else if (mode == kMany) {
+        u64 whole = scan.all_w;
+        if (k_cuts) {
+            find_cut(s, row, l, (u64)l.top_k, false);
             cut = s.cut;
             whole = s.through;
             __syncthreads();
         }
-        if (by_p) {
-            const u64 need = max((u64)1, (u64)ceil((double)fmaxf(top_p, 0.f) * (double)whole));
-            bin_of(need, true);
-            find_cut(s, row, bins, inv_t, (int)s.bin, s.rest, s.before, need, true);
+        if (l.by_p) {
+            const u64 need = l.need(whole);
+            scan.find(s, need, true);
+            find_cut(s, row, l, need, true);
             cut = max(cut, s.cut);
-            __syncthreads();
         }
+        for (int r = wave; r < ranges; r += kWaves) {
+            const u64 sum = sum_of(row, l, r, cut, kBins);
+            if (lane == 0) s.range[r] = sum;
+        }
+        __syncthreads();
     }
+    draw_ranges(s, a, row, l, t, cut);
+}
 
-    // kept weights, segment by segment
-    const double least_w = (double)fminf(fmaxf(min_p, 0.f), 1.f) * kUnit;
-    auto kept = [&](float x, int i) -> u64 {
-        if (i < 0 || i >= row.V || x == -INFINITY || place_of(x, i) < cut) return 0;
-        const u64 w = weight(x, m, inv_t);
-        return (double)w >= least_w ? w : 0;
-    };
-    for_row(row, [&](const float (&x)[8], int i, int seg) {
-        u64 sum = 0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) sum += kept(x[j], i + j);
-        sum = wave_sum(sum);
-        if (lane == 0) s.segment[seg] = sum;
-    });
-    __syncthreads();
-    const int segments = (row.end() + kTile - 1) / kTile * kWaves, per = (segments + kThreads - 1) / kThreads;
-    u64 mine = 0, whole;
-    for (int k = 0; k < per; ++k)
-        if (tid * per + k < segments) mine += s.segment[tid * per + k];
-    u64 at = sum_before(s, mine, &whole);
-    const float u = fmaxf(a.uniform[t], 0.f);
-    const u64 goal = u < 1.f ? min((u64)((double)u * (double)whole), whole - 1) : whole - 1;  // the first running sum above it
-    for (int k = 0; k < per; ++k)
-        if (tid * per + k < segments) {
-            const u64 x = s.segment[tid * per + k];
-            if (at <= goal && at + x > goal) {
-                s.bin = tid * per + k;
-                s.before = at;
-            }
-            at += x;
+// A workgroup a row.
+template <typename E> __global__ __launch_bounds__(kThreads) void sample_kernel(Sample a)
+{
+    __shared__ Shared s;
+    const int64_t t = blockIdx.x;
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    const Row<E> row(a, t);
+    const float2 ends = ends_of(s, row, 0);
+    const Limits l(a, t, ends.x, ends.y);
+    if (l.none || l.greedy) {
+        const int first = l.none ? -1 : first_of(s, row, l.m, 0);
+        if (tid == 0) {
+            a.token[t] = first;
+            if (a.logprob) a.logprob[t] = l.none ? -INFINITY : 0.f;
         }
-    __syncthreads();
-    if (wave == 0) {
-        const int v = (int)s.bin * 512 + 8 * lane, i = v - row.pad;
-        float x[8];
-        row.load(v, x);
-        u64 sum = 0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) sum += kept(x[j], i + j);
-        u64 up = sum;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const u64 y = shfl_up64(up, d);
-            if (lane >= d) up += y;
-        }
-        u64 running = s.before + up - sum;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const u64 w = kept(x[j], i + j);
-            if (running <= goal && running + w > goal) {
-                a.token[t] = i + j;
-                if (a.logprob)
-                    a.logprob[t] = (float)(((double)x[j] - (double)m) * inv_t * 0.6931471805599453 - log((double)whole / kUnit));
-            }
-            running += w;
-        }
+        return;
     }
+    if (!l.cuts()) {
+        const u64 sum = sum_of(row, l, wave, 0, kBins);
+        if (lane == 0) s.range[wave] = sum;
+        __syncthreads();
+        draw_ranges(s, a, row, l, t, 0);
+        return;
+    }
+    fill_bins(s, row, l, 0);
+    const Scan scan(s);
+    const bool k_cuts = decide(s, l, scan);
+    if (tid == 0) s.cursor = 0;
+    __syncthreads();
+    if (s.mode == kFew || s.mode == kInBin) collect(row, l, 0, s.mode == kFew ? 0 : s.bin, s.bin, &s.cursor, s.list);
+    if (s.mode == kInBin || s.mode == kWhole) {
+        const u64 sum = sum_of(row, l, wave, 0, s.bin);
+        if (lane == 0) s.range[wave] = sum;
+    }
+    __syncthreads();
+    finish(s, a, row, l, t, scan, k_cuts);
 }
 
 }  // namespace
 
-hipError_t launch_sample(const Sample &a, hipStream_t s)
+hipError_t launch_sample(Sample a, hipStream_t s)
 {
+    const int groups = (a.V + 7 + 7) / 8;
+    a.parts = 1;
+    a.per = (groups + kWaves * 64 - 1) / (kWaves * 64) * 64;
     const dim3 grid((unsigned)a.T), block(kThreads);
     if (a.dt == IVF_F32) hipLaunchKernelGGL((sample_kernel<float>), grid, block, 0, s, a);
     else if (a.dt == IVF_F16) hipLaunchKernelGGL((sample_kernel<_Float16>), grid, block, 0, s, a);
