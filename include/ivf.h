@@ -738,11 +738,15 @@ size_t ivf_kv_attend_bytes(const ivf_kv_cache *cache, int32_t q_heads, int64_t T
  *   out_logprob [T] fp32 logarithm of the token's share of what remains (0 for a
  *               row that takes the largest, -infinity with a token of -1); may be NULL
  * The conventions are those of the cache's calls; rows need only be aligned to their
- * elements. No workspace. Errors: IVF_EINVAL, IVF_EUNSUPPORTED (type, V, T above
- * 4194303), IVF_EDEVICE. */
+ * elements. Workspace: ivf_sample_bytes(). Errors: IVF_EINVAL, IVF_EUNSUPPORTED
+ * (type, V, T above 4194303), IVF_ENOMEM, IVF_EDEVICE. */
 ivf_status ivf_sample(ivf_ctx *ctx, const void *logits, int dt, int64_t row_stride, int64_t T, int64_t V,
                       const float *uniform, const float *temperature, const int32_t *top_k,
                       const float *top_p, const float *min_p, int32_t *out_token, float *out_logprob);
+
+/* Workspace of ivf_sample for T rows of V logits, cuts: with top_k or top_p (0 where
+ * none is used, or for sizes that it refuses). */
+size_t ivf_sample_bytes(int64_t T, int64_t V, int32_t cuts);
 
 /* Measures the fp32 MFMA pipe for reporting: enqueues a probe kernel that
  * runs only v_mfma_f32_32x32x2_f32 (register operands, two waves per SIMD on

@@ -62,6 +62,7 @@ SIGNATURES = [
     ("ivf_kv_attend", _INT, [_P, _P, _P, _I64, _I64, _I32, _I64, _P, _P, _P, _P, _I64, _I32, _P, _I32,
                              ctypes.c_float, _I64, _P, _P]),
     ("ivf_sample", _INT, [_P, _P, _INT, _I64, _I64, _I64, _P, _P, _P, _P, _P, _P, _P]),
+    ("ivf_sample_bytes", _SZ, [_I64, _I64, _I32]),
     ("ivf_kv_attend_terms", _INT, [_P, _P, _P, _I64, _I64, _I32, _I64, _P, _P, _P, _P, _I64, _I32, _P, _I32,
                                    ctypes.c_float, _I64, _P, _P, _P]),
 ]
@@ -852,6 +853,7 @@ def ivf_kv_attend(ctx: Context, cache: KVCache, q, start, request, position, tab
 # ---- the token that follows ---------------------------------------------------
 
 _logit_types = None
+_sample_bytes = {}  # workspace of calls of given sizes
 
 
 def ivf_sample(ctx: Context, logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None):
@@ -887,6 +889,14 @@ def ivf_sample(ctx: Context, logits, uniform, temperature=None, top_k=None, top_
             None if min_p is None else _ints(ctx, min_p, "min_p", shape, f32))
     token, logprob = torch.unsafe_split_with_sizes(torch.empty(2 * T, dtype=torch.int32, device=logits.device), (T, T))
     logprob = logprob.view(f32)
+    sizes = T, V, int(top_k is not None or top_p is not None)
+    need = _sample_bytes.get(sizes)
+    if need is None:
+        if len(_sample_bytes) >= 1024:
+            _sample_bytes.clear()
+        need = _sample_bytes[sizes] = ctx.lib.ivf_sample_bytes(*sizes)
+    if need:
+        ctx.ensure_workspace(need)
     lib, handle = ctx.bind()
     st = lib.ivf_sample(handle, logits.data_ptr(), dt, stride if T > 1 else 0, T, V, *args, token.data_ptr(),
                         logprob.data_ptr())

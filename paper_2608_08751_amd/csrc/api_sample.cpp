@@ -10,6 +10,17 @@ using namespace ivf;
 
 extern "C" {
 
+size_t ivf_sample_bytes(int64_t T, int64_t V, int32_t cuts)
+{
+    if (T < 1 || T > INT32_MAX || check_threads(nullptr, T * 1024) != IVF_OK || V < 1 || V > kSampleMaxVocab) return 0;
+    int num_cus = 256, dev = 0;
+    if (hipGetDevice(&dev) == hipSuccess) {
+        int n = 0;
+        if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && n > 0) num_cus = n;
+    }
+    return sample_workspace(T, sample_parts(T, V, num_cus), cuts != 0, nullptr, nullptr);
+}
+
 ivf_status ivf_sample(ivf_ctx *ctx, const void *logits, int dt, int64_t row_stride, int64_t T, int64_t V,
                       const float *uniform, const float *temperature, const int32_t *top_k, const float *top_p,
                       const float *min_p, int32_t *out_token, float *out_logprob)
@@ -33,10 +44,16 @@ ivf_status ivf_sample(ivf_ctx *ctx, const void *logits, int dt, int64_t row_stri
                             {temperature, (size_t)T * 4}, {top_k, (size_t)T * 4}, {top_p, (size_t)T * 4}, {min_p, (size_t)T * 4}};
         const Span outs[] = {{out_token, (size_t)T * 4}, {out_logprob, (size_t)T * 4}};
         if ((st = no_overlap(ctx, outs, 2, ins, 6)) != IVF_OK) return st;
-        Sample a = {logits, dt, row_stride, T, (int)V, uniform, temperature, top_k, top_p, min_p, out_token, out_logprob};
+        Sample a = {logits, dt, row_stride, T, (int)V, uniform, temperature, top_k, top_p, min_p, out_token, out_logprob, 0, 0};
+        const int parts = sample_parts(T, V, ctx->num_cus);
+        const bool cuts = top_k || top_p;
+        const size_t need = sample_workspace(T, parts, cuts, nullptr, nullptr);
+        if (need && (st = check_ws(ctx, need)) != IVF_OK) return st;
+        SampleShare share;
+        sample_workspace(T, parts, cuts, need ? (char *)ctx->ws : nullptr, &share);
         DeviceGuard g(ctx->device);
         if (!g.ok) return fail(ctx, IVF_EDEVICE, "no usable device (context device %d)", ctx->device);
-        TIMED("sample", launch_sample(a, ctx->stream));
+        TIMED("sample", launch_sample(a, parts, share, ctx->stream));
         ctx->last_stats = nullptr;
         return IVF_OK;
     });

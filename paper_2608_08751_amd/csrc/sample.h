@@ -25,6 +25,25 @@ struct Sample {
     int parts, per;  // workgroups a row; groups of eight logits a wave
 };
 
-hipError_t launch_sample(Sample a, hipStream_t s);
+// What the launches of a call that shares rows out hand on (workspace), for T rows of `parts` parts.
+struct SampleShare {
+    float2 *ends;                // [T][parts] largest and least logit
+    int *first;                  // [T][parts] where the largest stands
+    unsigned long long *range;   // [T][parts * 16] sums of weights
+    uint32_t *cursor;            // [T][2]
+    // with top_k or top_p
+    void *decision;              // [T]
+    unsigned long long *list;    // [T][kSampleList]
+    uint32_t *count;             // [T][parts][bins]
+    unsigned long long *sum;
+};
+
+// Rows of fewer logits are taken by one workgroup in one launch.
+constexpr int64_t kSampleOne = 16384;
+
+// Workgroups that share a row; 0: one launch. Bytes of the workspace (0 with it), and with a base what lies where.
+int sample_parts(int64_t T, int64_t V, int num_cus);
+size_t sample_workspace(int64_t T, int parts, bool cuts, char *base, SampleShare *x);
+hipError_t launch_sample(Sample a, int parts, const SampleShare &x, hipStream_t s);
 
 }  // namespace ivf

@@ -75,37 +75,52 @@ template <typename E> struct Row {
     __device__ __forceinline__ int groups() const { return (V + pad + 7) >> 3; }
     __device__ __forceinline__ int first_of(int g) const { return 8 * g - pad; }
     __device__ __forceinline__ int range_of(int i) const { return ((i + pad) >> 3) / per; }
-    // the elements of group g, -infinity outside the row
-    __device__ __forceinline__ void load(int g, float (&x)[8]) const
+    // Eight elements as they lie in memory.
+    struct Group {
+        uint4 w[sizeof(E) / 2];
+        __device__ __forceinline__ void to(float (&x)[8]) const
+        {
+            typedef E E8 __attribute__((ext_vector_type(8)));
+            const E8 y = __builtin_bit_cast(E8, *this);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = clean(widen((E)y[j]));
+        }
+    };
+    // group g, -infinity outside the row and from group `end` on
+    __device__ __forceinline__ Group load(int g, int end) const
     {
+        Group y;
         const int i = first_of(g);
-        if (i >= 0 && i + 8 <= V) {
-            union {
-                uint4 w[sizeof(E) / 2];
-                E e[8];
-            } y;
+        if (g < end && i >= 0 && i + 8 <= V) {
 #pragma unroll
             for (int k = 0; k < (int)sizeof(E) / 2; ++k) y.w[k] = ((const uint4 *)(p + i))[k];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = clean(widen(y.e[j]));
         } else {
+            typedef E E8 __attribute__((ext_vector_type(8)));
+            E8 z;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = i + j >= 0 && i + j < V ? clean(widen(p[i + j])) : -INFINITY;
+            for (int j = 0; j < 8; ++j) z[j] = g < end && i + j >= 0 && i + j < V ? p[i + j] : (E)-INFINITY;
+            y = __builtin_bit_cast(Group, z);
         }
+        return y;
     }
-    // Calls f(x[8], index of x[0]) for the groups of range r, all lanes each time (-infinity past its end).
+    // Calls f(x[8], index of x[0]) for the groups of range r, all lanes each time (-infinity past its end). Four
+    // groups a lane are loaded at a time: a wave alone waits for each otherwise.
     template <typename F> __device__ __forceinline__ void for_range(int r, F f) const
     {
+        constexpr int U = 4;
         const int lane = threadIdx.x & 63, end = min((r + 1) * per, groups());
-        for (int g = r * per; g < end; g += 64) {
-            float x[8];
-            if (g + lane < end) {
-                load(g + lane, x);
-            } else {
+        for (int g = r * per; g < end; g += 64 * U) {
+            Group y[U];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) x[j] = -INFINITY;
+            for (int k = 0; k < U; ++k) y[k] = load(g + 64 * k + lane, end);
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                if (g + 64 * k < end) {
+                    float x[8];
+                    y[k].to(x);
+                    f(x, first_of(g + 64 * k + lane));
+                }
             }
-            f(x, first_of(g + lane));
         }
     }
 };
@@ -140,8 +155,8 @@ __device__ __forceinline__ u64 wave_sum(u64 x)
     return x;
 }
 
-// How the kept part of a row ends: nowhere; in the last of few elements, all listed; in a listed bin; or in one that
-// has more elements than a list.
+// How the kept part of a row ends: nowhere; in a bin that is listed with all bins before it; in one that is listed
+// alone; or in one of more elements than a list holds.
 enum Mode { kWhole, kFew, kInBin, kMany };
 
 struct Shared {
@@ -156,9 +171,17 @@ struct Shared {
     int bin;
     uint32_t rest;
     u64 before;
-    uint32_t cursor;
+    uint32_t cursor[2];  // of the list: elements of the bins before (from its front on) and of the bin (from its end back)
     u64 cut, through;
-    int mode, token;
+    int mode, found;
+};
+
+// What `decide` finds, for the launch that draws.
+struct Decision {
+    int mode, bin;
+    uint32_t rest;
+    int k_cuts;
+    u64 before, all_w;
 };
 
 // The sum of x over the threads before this one; *all: over all of them.
@@ -191,7 +214,7 @@ struct Limits {
     bool none, greedy, by_k, by_p;
     int top_k;
     float top_p;
-    double least_w;
+    u64 least_w;  // of what min_p keeps
     __device__ __forceinline__ Limits(const Sample &a, int64_t t, float high, float low)
     {
         // (beyond 2^60 the range of the bins would not hold in fp32; no number stays none)
@@ -207,7 +230,7 @@ struct Limits {
         top_p = a.top_p ? a.top_p[t] : 1.f;
         by_k = top_k > 0 && top_k < a.V;
         by_p = top_p < 1.f;
-        least_w = (a.min_p ? (double)fminf(fmaxf(a.min_p[t], 0.f), 1.f) : 0.0) * kUnit;
+        least_w = a.min_p ? (u64)ceil((double)fminf(fmaxf(a.min_p[t], 0.f), 1.f) * kUnit) : 0;
     }
     __device__ __forceinline__ bool cuts() const { return !none && !greedy && (by_k || by_p); }
     __device__ __forceinline__ int bin(float x) const { return (int)fminf((m - x) * per, (float)(kBins - 1)); }
@@ -217,7 +240,7 @@ struct Limits {
     {
         if (cut && place_of(x, i) < cut) return 0;
         const u64 w = weigh(x);
-        return (double)w >= least_w ? w : 0;
+        return w >= least_w ? w : 0;
     }
     // the weights that top_p of `whole` asks for
     __device__ __forceinline__ u64 need(u64 whole) const
@@ -227,7 +250,7 @@ struct Limits {
 };
 
 // The largest and the least logit of a part (16 ranges), the least of those above -infinity; all threads get them.
-template <typename E> __device__ float2 ends_of(Shared &s, const Row<E> &row, int part)
+template <typename E> __device__ __forceinline__ float2 ends_of(Shared &s, const Row<E> &row, int part)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     float high = -INFINITY, low = INFINITY;
@@ -256,7 +279,7 @@ template <typename E> __device__ float2 ends_of(Shared &s, const Row<E> &row, in
 }
 
 // The lowest index of the part at which the largest logit stands; thread 0 gets it.
-template <typename E> __device__ int first_of(Shared &s, const Row<E> &row, float m, int part)
+template <typename E> __device__ __forceinline__ int first_of(Shared &s, const Row<E> &row, float m, int part)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int first = INT32_MAX;
@@ -273,28 +296,29 @@ template <typename E> __device__ int first_of(Shared &s, const Row<E> &row, floa
     return first;
 }
 
-// Kept weights of range r (a wave); those of bins from `bin` on apart.
-template <typename E> __device__ u64 sum_of(const Row<E> &row, const Limits &l, int r, u64 cut, int bin)
+// Kept weights of range r (a wave): of all of it, of bins before `bin`, or from the cut on.
+enum Part { kAll, kBefore, kFromCut };
+template <Part PART, typename E> __device__ __forceinline__ u64 sum_of(const Row<E> &row, const Limits &l, int r, u64 cut, int bin)
 {
     u64 sum = 0;
     row.for_range(r, [&](const float (&x)[8], int i) {
-        if (bin < kBins - 1 || cut) {
+        if (PART != kAll) {
             float most = x[0];
 #pragma unroll
             for (int j = 1; j < 8; ++j) most = fmaxf(most, x[j]);
-            if (!__any(l.bin(most) < bin && order_of(most) >= (uint32_t)(cut >> 32))) return;
+            if (!__any(PART == kBefore ? l.bin(most) < bin : order_of(most) >= (uint32_t)(cut >> 32))) return;
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const u64 w = l.kept(x[j], i + j, cut);
-            if (l.bin(x[j]) < bin) sum += w;
+            const u64 w = l.kept(x[j], i + j, PART == kFromCut ? cut : 0);
+            if (PART != kBefore || l.bin(x[j]) < bin) sum += w;
         }
     });
     return wave_sum(sum);
 }
 
 // Numbers and weights of the part's bins, in LDS.
-template <typename E> __device__ void fill_bins(Shared &s, const Row<E> &row, const Limits &l, int part)
+template <typename E> __device__ __forceinline__ void fill_bins(Shared &s, const Row<E> &row, const Limits &l, int part)
 {
     const int tid = threadIdx.x;
     for (int b = tid; b < kBins; b += kThreads) {
@@ -350,68 +374,76 @@ struct Scan {
     }
 };
 
-// Where the kept part ends (without min_p), from the row's bins: s.mode, s.bin, s.rest, s.before. Returns whether top_k
-// cuts (else there are no more elements that weigh something).
-__device__ bool decide(Shared &s, const Limits &l, const Scan &scan)
+// Where the kept part ends (without min_p), from the row's bins in LDS. All threads get it; s.bin, s.rest and s.before
+// hold what it says too.
+__device__ __forceinline__ Decision decide(Shared &s, const Limits &l, const Scan &scan)
 {
-    const bool k_cuts = l.by_k && (u64)l.top_k <= scan.all_c;
-    if (k_cuts) scan.find(s, (u64)l.top_k, false);
-    else if (l.by_p) scan.find(s, l.need(scan.all_w), true);
-    if (threadIdx.x == 0) {
-        if (!k_cuts && !l.by_p) {
-            s.mode = kWhole;
-            s.bin = kBins - 1;
-        } else if (s.rest + s.count[s.bin] <= kList) {
-            s.mode = kFew;
-        } else {
-            // (with both, top_p goes by what top_k leaves)
-            s.mode = !(k_cuts && l.by_p) && s.count[s.bin] <= kList ? kInBin : kMany;
-        }
+    Decision d;
+    // (where top_k leaves out only what weighs nothing it cuts nothing)
+    d.k_cuts = l.by_k && (u64)l.top_k <= scan.all_c;
+    d.all_w = scan.all_w;
+    if (!d.k_cuts && !l.by_p) {
+        d.mode = kWhole;
+        d.bin = kBins - 1;
+        d.rest = 0;
+        d.before = 0;
+        return d;
     }
-    __syncthreads();
-    return k_cuts;
+    if (d.k_cuts) scan.find(s, (u64)l.top_k, false);
+    else scan.find(s, l.need(scan.all_w), true);
+    d.bin = s.bin;
+    d.rest = s.rest;
+    d.before = s.before;
+    const uint32_t here = s.count[d.bin];
+    // (with both, top_p goes by what top_k leaves)
+    d.mode = d.rest + here <= kList ? kFew : !(d.k_cuts && l.by_p) && here <= kList ? kInBin : kMany;
+    return d;
 }
 
-// The part's elements of bins lo ... hi, in no order. `cursor` and `list` are in LDS or device memory.
+// The part's elements of bin `last`, and with `before` of the bins before it, in no order. cursor and list are in LDS or
+// device memory; what would not find room is left out.
 template <typename E>
-__device__ void collect(const Row<E> &row, const Limits &l, int part, int lo, int hi, uint32_t *cursor, u64 *list)
+__device__ __forceinline__ void collect(const Row<E> &row, const Limits &l, int part, bool before, int last, uint32_t *cursor, u64 *list)
 {
     const int lane = threadIdx.x & 63;
     row.for_range(part * kWaves + (threadIdx.x >> 6), [&](const float (&x)[8], int i) {
         float most = x[0];
 #pragma unroll
         for (int j = 1; j < 8; ++j) most = fmaxf(most, x[j]);
-        if (!__any(l.bin(most) <= hi)) return;
-        uint32_t hits = 0;
+        if (!__any(l.bin(most) <= last)) return;
+        uint32_t hits[2] = {0, 0};
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const int b = l.bin(x[j]);
-            hits |= (uint32_t)(b >= lo && b <= hi) << j;
+            hits[0] |= (uint32_t)(before && b < last) << j;
+            hits[1] |= (uint32_t)(b == last) << j;
         }
-        const uint32_t n = __popc(hits);
-        uint32_t up = n;
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const uint32_t y = __shfl_up(up, d);
-            if (lane >= d) up += y;
-        }
-        const uint32_t all = __builtin_amdgcn_readlane(up, 63);
-        if (!all) return;
-        uint32_t at = 0;
-        if (lane == 0) at = atomicAdd(cursor, all);
-        at = __builtin_amdgcn_readfirstlane(at) + up - n;
+        for (int h = 0; h < 2; ++h) {
+            if (!__any(hits[h] != 0)) continue;
+            const uint32_t n = __popc(hits[h]);
+            uint32_t up = n;
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (hits >> j & 1) {
-                if (at < kList) list[at] = place_of(x[j], i + j);
-                ++at;
+            for (int d = 1; d < 64; d <<= 1) {
+                const uint32_t y = __shfl_up(up, d);
+                if (lane >= d) up += y;
             }
+            uint32_t at = 0;
+            if (lane == 63) at = atomicAdd(&cursor[h], up);
+            at = __builtin_amdgcn_readlane(at, 63) + up - n;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (hits[h] >> j & 1) {
+                    if (at < kList) list[h ? kList - 1 - at : at] = place_of(x[j], i + j);
+                    ++at;
+                }
+        }
     });
 }
 
 // Sorts list[0, n), descending, in LDS; up to the next power of two it is filled with zeros. Strides of up to 64
 // stay inside what a wave holds.
-__device__ void sort_list(u64 *list, int n)
+__device__ __forceinline__ void sort_list(u64 *list, int n)
 {
     const int tid = threadIdx.x;
     int m = 2;
@@ -438,8 +470,8 @@ __device__ void sort_list(u64 *list, int n)
     __syncthreads();
 }
 
-// Finds the token whose running sum passes `goal` among a wave's or workgroup's elements, in the order of threads
-// and of w[8]: called with the sum before this thread's.
+// Finds the token whose running sum passes `goal` among w[N], in the order of threads and of N: called
+// with the sum before this thread's.
 template <int N>
 __device__ __forceinline__ void pick(Shared &s, const Sample &a, const Limits &l, int64_t t, u64 running, u64 goal, u64 whole,
                                      const u64 (&w)[N], const float (&x)[N], const int (&index)[N])
@@ -450,7 +482,6 @@ __device__ __forceinline__ void pick(Shared &s, const Sample &a, const Limits &l
             a.token[t] = index[j];
             if (a.logprob)
                 a.logprob[t] = (float)(((double)x[j] - l.md) * l.inv_t * 0.6931471805599453 - log((double)whole / kUnit));
-            s.token = index[j];
         }
         running += w[j];
     }
@@ -463,69 +494,128 @@ __device__ __forceinline__ u64 goal_of(const Sample &a, int64_t t, u64 whole)
     return u < 1.f ? min((u64)((double)u * (double)whole), whole - 1) : whole - 1;
 }
 
-// kFew: all that can be kept is listed, n elements.
-__device__ void draw_listed(Shared &s, const Sample &a, const Limits &l, int64_t t, int n, bool k_cuts, u64 all_w)
+// The element of s.segment[0, n) (places, any order; put in order here) at which a leading part ends: the
+// rank-th (from 1), or with rank 0 the first whose weights, on top of `before`, reach `need`. Writes s.cut (its place) and
+// s.through (the weights up to it).
+__device__ __forceinline__ void cut_listed(Shared &s, const Limits &l, int n, uint32_t rank, u64 before, u64 need)
 {
     const int tid = threadIdx.x;
-    sort_list(s.list, n);
+    sort_list(s.segment, n);
     u64 place[2], w[2], all;
-    int i2[2];
-    float x2[2];
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-        place[k] = 2 * tid + k < n ? s.list[2 * tid + k] : 0;
+        place[k] = 2 * tid + k < n ? s.segment[2 * tid + k] : 0;
         w[k] = place[k] ? l.weigh(number_of((uint32_t)(place[k] >> 32))) : 0;
     }
-    if (tid == 0) s.rest = n;
-    const u64 before = sum_before(s, w[0] + w[1], &all);
-    const int most = k_cuts ? l.top_k : n;  // elements that top_k leaves
-    if (l.by_p) {
-        u64 whole = all_w;
-        if (k_cuts) {
-            if ((most - 1) / 2 == tid) s.through = before + w[0] + (most % 2 ? 0 : w[1]);
-            __syncthreads();
-            whole = s.through;
-        }
-        const u64 need = l.need(whole);
-        if (before < need && before + w[0] >= need) s.rest = 2 * tid + 1;
-        else if (before + w[0] < need && before + w[0] + w[1] >= need) s.rest = 2 * tid + 2;
-    }
-    __syncthreads();
-    // what is kept, in the order of the indexes: a weight takes 44 bits, an index 20
-    const int keep = min(most, (int)s.rest);
-    if (tid == 0) s.cursor = 0;
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < 2; ++k)
-        if (2 * tid + k < keep && (double)w[k] >= l.least_w)
-            s.segment[atomicAdd(&s.cursor, 1u)] = (u64)(uint32_t)(kSampleMaxVocab - 1 - index_of(place[k])) << 44 | w[k];
-    __syncthreads();
-    const int kept = (int)s.cursor;
-    sort_list(s.segment, kept);
+    before += sum_before(s, w[0] + w[1], &all);
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-        const u64 e = 2 * tid + k < kept ? s.segment[2 * tid + k] : 0;
-        w[k] = e & 0xfffffffffffull;
-        i2[k] = e ? min((int)(kSampleMaxVocab - 1) - (int)(e >> 44), a.V - 1) : 0;  // (no entry: weighs nothing)
-    }
-    u64 whole;
-    const u64 running = sum_before(s, w[0] + w[1], &whole);
-    const u64 goal = goal_of(a, t, whole);
-    if (running <= goal && running + w[0] + w[1] > goal) {
-        // the logit from its weight would lose what small ones have: from the row
-        const int64_t at = t * a.stride;
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            x2[k] = clean(a.dt == IVF_F32   ? ((const float *)a.logits)[at + i2[k]]
-                          : a.dt == IVF_F16 ? widen(((const _Float16 *)a.logits)[at + i2[k]])
-                                            : widen(((const __bf16 *)a.logits)[at + i2[k]]));
+        if (place[k] && (rank ? 2 * tid + k + 1 == (int)rank : before < need && before + w[k] >= need)) {
+            s.cut = place[k];
+            s.through = before + w[k];
         }
-        pick(s, a, l, t, running, goal, whole, w, x2, i2);
+        before += w[k];
+    }
+    __syncthreads();
+}
+
+// The place of the last element that is kept (min_p apart), with what `decide` asks for in the list; n: the
+// list's elements of the bins before the last one, m: of that one. bins() puts the row's bins into LDS.
+template <typename Bins> __device__ __forceinline__ u64 last_kept(Shared &s, const Limits &l, const Decision &d, int n, int m, Bins bins)
+{
+    const int tid = threadIdx.x;
+    for (int i = tid; i < m; i += kThreads) s.segment[i] = s.list[kList - 1 - i];
+    __syncthreads();
+    if (!d.k_cuts) {
+        cut_listed(s, l, m, 0, d.before, l.need(d.all_w));
+        return s.cut;
+    }
+    cut_listed(s, l, m, (uint32_t)l.top_k - d.rest, d.before, 0);
+    u64 cut = s.cut;
+    if (!l.by_p) return cut;
+    // top_p of what top_k leaves: in the same bin or in one before it
+    const u64 need = l.need(s.through);
+    __syncthreads();
+    if (need > d.before) {
+        cut_listed(s, l, m, 0, d.before, need);
+    } else {
+        bins();
+        Scan(s).find(s, need, true);
+        const int bin = s.bin;
+        const u64 before = s.before;
+        if (tid == 0) s.found = 0;
+        __syncthreads();
+        for (int i = tid; i < n; i += kThreads) {
+            const u64 p = s.list[i];
+            if (l.bin(number_of((uint32_t)(p >> 32))) == bin) s.segment[atomicAdd(&s.found, 1)] = p;
+        }
+        __syncthreads();
+        cut_listed(s, l, s.found, 0, before, need);
+    }
+    return max(cut, s.cut);
+}
+
+// kFew: the token from the list alone. Weights are summed in up to 2,048 buckets of neighbouring indexes; the
+// elements of the one where the running sum passes the goal are put in order.
+template <typename E>
+__device__ __forceinline__ void draw_listed(Shared &s, const Sample &a, const Row<E> &row, const Limits &l, int64_t t, int n, int m, u64 cut)
+{
+    const int tid = threadIdx.x;
+    int shift = 0;
+    while (a.V - 1 >> shift >= kBins) ++shift;
+    for (int b = tid; b < kBins; b += kThreads) s.sum[b] = 0;
+    __syncthreads();
+    u64 w[2];
+    int bucket[2];
+    uint32_t index[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int e = tid + k * kThreads;
+        const bool there = e < n || e >= kList - m;
+        const u64 place = there ? s.list[e] : 0;
+        index[k] = (uint32_t)index_of(place);
+        w[k] = there ? l.kept(number_of((uint32_t)(place >> 32)), (int)index[k], cut) : 0;
+        bucket[k] = w[k] ? (int)(index[k] >> shift) : -1;
+        if (w[k]) atomicAdd(&s.sum[bucket[k]], w[k]);
+    }
+    __syncthreads();
+    u64 whole;
+    const u64 x0 = s.sum[2 * tid], x1 = s.sum[2 * tid + 1];
+    const u64 at = sum_before(s, x0 + x1, &whole);
+    const u64 goal = goal_of(a, t, whole);
+    if (at <= goal && at + x0 + x1 > goal) {
+        const bool second = at + x0 <= goal;
+        s.bin = 2 * tid + second;
+        s.before = second ? at + x0 : at;
+    }
+    if (tid == 0) s.found = 0;
+    __syncthreads();
+    // a weight takes 44 bits, an index 20; the lowest index first
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+        if (bucket[k] == s.bin) s.segment[atomicAdd(&s.found, 1)] = (u64)(uint32_t)(kSampleMaxVocab - 1 - index[k]) << 44 | w[k];
+    __syncthreads();
+    const int found = s.found;
+    sort_list(s.segment, found);
+    float x[2];
+    int i[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const u64 e = 2 * tid + k < found ? s.segment[2 * tid + k] : 0;
+        w[k] = e & 0xfffffffffffull;
+        i[k] = w[k] ? (int)(kSampleMaxVocab - 1) - (int)(e >> 44) : 0;  // (no entry: weighs nothing)
+    }
+    u64 all;
+    const u64 running = s.before + sum_before(s, w[0] + w[1], &all);
+    if (running <= goal && running + w[0] + w[1] > goal) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) x[k] = clean(widen(row.p[i[k]]));
+        pick(s, a, l, t, running, goal, whole, w, x, i);
     }
 }
 
 // The token from the ranges' kept weights (s.range): the range where the running sum passes the goal, once more.
-template <typename E> __device__ void draw_ranges(Shared &s, const Sample &a, const Row<E> &row, const Limits &l, int64_t t, u64 cut)
+template <typename E> __device__ __forceinline__ void draw_ranges(Shared &s, const Sample &a, const Row<E> &row, const Limits &l, int64_t t, u64 cut)
 {
     const int tid = threadIdx.x, ranges = row.parts * kWaves;
     u64 whole, x = tid < ranges ? s.range[tid] : 0;
@@ -535,7 +625,6 @@ template <typename E> __device__ void draw_ranges(Shared &s, const Sample &a, co
         s.bin = tid;
         s.before = at;
     }
-    if (tid == 0) s.token = -1;
     __syncthreads();
     u64 base = s.before;
     const int end = min((s.bin + 1) * row.per, row.groups());
@@ -543,12 +632,7 @@ template <typename E> __device__ void draw_ranges(Shared &s, const Sample &a, co
         float y[8];
         int index[8];
         u64 w[8], sum = 0, all;
-        if (g0 + tid < end) {
-            row.load(g0 + tid, y);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] = -INFINITY;
-        }
+        row.load(g0 + tid, end).to(y);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             index[j] = row.first_of(g0 + tid) + j;
@@ -565,7 +649,7 @@ template <typename E> __device__ void draw_ranges(Shared &s, const Sample &a, co
 // kMany: the cut of one limit by going over the row, in one workgroup. It is the first element whose elements number
 // `need`, or whose weights reach `need` (by_weight), and lies in s.bin (s.rest and s.before come before it).
 // Writes s.cut (its place) and s.through (the weights up to it). All threads call it.
-template <typename E> __device__ void find_cut(Shared &s, const Row<E> &row, const Limits &l, u64 need, bool by_weight)
+template <typename E> __device__ __forceinline__ void find_cut(Shared &s, const Row<E> &row, const Limits &l, u64 need, bool by_weight)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, ranges = row.parts * kWaves;
     const int bin = s.bin;
@@ -594,12 +678,12 @@ template <typename E> __device__ void find_cut(Shared &s, const Row<E> &row, con
         u64 all;
         const u64 cb = count + sum_before(s, c, &all), wb = sum + sum_before(s, w, &all);
         if (c && (by_weight ? wb < need && wb + w >= need : cb < need && cb + c >= need)) {
-            s.cursor = 255 - tid;
+            s.cursor[0] = 255 - tid;
             s.rest = (uint32_t)cb;
             s.before = wb;
         }
         __syncthreads();
-        prefix |= s.cursor << shift;
+        prefix |= s.cursor[0] << shift;
         count = s.rest;
         sum = s.before;
     }
@@ -610,7 +694,7 @@ template <typename E> __device__ void find_cut(Shared &s, const Row<E> &row, con
     auto equal_of = [&](int seg, float (&x)[8]) {
         u64 equal = 0;
         if (64 * seg + lane < row.groups()) {
-            row.load(64 * seg + lane, x);
+            row.load(64 * seg + lane, row.groups()).to(x);
 #pragma unroll
             for (int j = 0; j < 8; ++j) equal += order_of(x[j]) == prefix;
         }
@@ -656,54 +740,40 @@ template <typename E> __device__ void find_cut(Shared &s, const Row<E> &row, con
     __syncthreads();
 }
 
-// The row's token once its bins are in LDS and what `decide` asks for is collected: s.list and s.cursor, and s.range.
-template <typename E>
-__device__ void finish(Shared &s, const Sample &a, const Row<E> &row, const Limits &l, int64_t t, const Scan &scan, bool k_cuts)
+// The row's token, with what `decide` asks for in the list and in s.range.
+template <typename E, typename Bins>
+__device__ __forceinline__ void finish(Shared &s, const Sample &a, const Row<E> &row, const Limits &l, int64_t t, const Decision &d, Bins bins)
 {
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, ranges = row.parts * kWaves;
-    const int mode = s.mode;
-    if (mode == kFew) {
-        draw_listed(s, a, l, t, (int)min(s.cursor, (uint32_t)kList), k_cuts, scan.all_w);
-        return;
-    }
+    const int n = (int)min(s.cursor[0], (uint32_t)kList), m = (int)min(s.cursor[1], (uint32_t)(kList - n));
     u64 cut = 0;
-    if (mode == kInBin) {
-        const int n = (int)min(s.cursor, (uint32_t)kList);
-        const u64 need = k_cuts ? (u64)l.top_k - s.rest : l.need(scan.all_w) - s.before;  // of the list
-        sort_list(s.list, n);
-        u64 place[2], w[2], all;
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            place[k] = 2 * tid + k < n ? s.list[2 * tid + k] : 0;
-            w[k] = place[k] ? l.weigh(number_of((uint32_t)(place[k] >> 32))) : 0;
+    if (d.mode == kFew || d.mode == kInBin) {
+        cut = last_kept(s, l, d, n, m, bins);
+        __syncthreads();
+        if (d.mode == kFew) {
+            draw_listed(s, a, row, l, t, n, m, cut);
+            return;
         }
-        u64 before = sum_before(s, w[0] + w[1], &all);
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            if (place[k] && (k_cuts ? (u64)(2 * tid + k + 1) <= need : before < need)) {
-                if (k_cuts ? (u64)(2 * tid + k + 1) == need : before + w[k] >= need) s.cut = place[k];
-                if ((double)w[k] >= l.least_w) atomicAdd(&s.range[row.range_of(index_of(place[k]))], w[k]);
-            }
-            before += w[k];
+        for (int e = kList - m + tid; e < kList; e += kThreads) {
+            const u64 place = s.list[e];
+            const u64 w = l.kept(number_of((uint32_t)(place >> 32)), index_of(place), cut);
+            if (w) atomicAdd(&s.range[row.range_of(index_of(place))], w);
         }
         __syncthreads();
-        cut = s.cut;
-    } else if (mode == kMany) {
-        u64 whole = scan.all_w;
-        if (k_cuts) {
-            find_cut(s, row, l, (u64)l.top_k, false);
-            cut = s.cut;
+    } else if (d.mode == kMany) {
+        bins();
+        u64 whole = d.all_w;
+#pragma unroll 1
+        for (int by_p = !d.k_cuts; by_p <= (int)l.by_p; ++by_p) {
+            const u64 need = by_p ? l.need(whole) : (u64)l.top_k;
+            Scan(s).find(s, need, by_p);
+            find_cut(s, row, l, need, by_p);
+            cut = max(cut, s.cut);
             whole = s.through;
             __syncthreads();
         }
-        if (l.by_p) {
-            const u64 need = l.need(whole);
-            scan.find(s, need, true);
-            find_cut(s, row, l, need, true);
-            cut = max(cut, s.cut);
-        }
         for (int r = wave; r < ranges; r += kWaves) {
-            const u64 sum = sum_of(row, l, r, cut, kBins);
+            const u64 sum = sum_of<kFromCut>(row, l, r, cut, 0);
             if (lane == 0) s.range[r] = sum;
         }
         __syncthreads();
@@ -729,38 +799,197 @@ template <typename E> __global__ __launch_bounds__(kThreads) void sample_kernel(
         return;
     }
     if (!l.cuts()) {
-        const u64 sum = sum_of(row, l, wave, 0, kBins);
+        const u64 sum = sum_of<kAll>(row, l, wave, 0, 0);
         if (lane == 0) s.range[wave] = sum;
         __syncthreads();
         draw_ranges(s, a, row, l, t, 0);
         return;
     }
     fill_bins(s, row, l, 0);
-    const Scan scan(s);
-    const bool k_cuts = decide(s, l, scan);
-    if (tid == 0) s.cursor = 0;
+    const Decision d = decide(s, l, Scan(s));
+    if (tid < 2) s.cursor[tid] = 0;
     __syncthreads();
-    if (s.mode == kFew || s.mode == kInBin) collect(row, l, 0, s.mode == kFew ? 0 : s.bin, s.bin, &s.cursor, s.list);
-    if (s.mode == kInBin || s.mode == kWhole) {
-        const u64 sum = sum_of(row, l, wave, 0, s.bin);
+    if (d.mode == kFew || d.mode == kInBin) collect(row, l, 0, d.mode == kFew, d.bin, s.cursor, s.list);
+    if (d.mode == kInBin || d.mode == kWhole) {
+        const u64 sum = sum_of<kBefore>(row, l, wave, 0, d.bin);
         if (lane == 0) s.range[wave] = sum;
     }
     __syncthreads();
-    finish(s, a, row, l, t, scan, k_cuts);
+    finish(s, a, row, l, t, d, [] {});
 }
+
+// The same in four launches, parts of a row by workgroups of their own (blockIdx.x = row * parts + part); what
+// one finds is in device memory (SampleShare) for the next.
+template <typename E> __global__ __launch_bounds__(kThreads) void sample_ends_kernel(Sample a, SampleShare x)
+{
+    __shared__ Shared s;
+    const int64_t t = blockIdx.x / a.parts;
+    const int part = blockIdx.x % a.parts;
+    const float2 ends = ends_of(s, Row<E>(a, t), part);
+    if (threadIdx.x == 0) x.ends[blockIdx.x] = ends;
+    if (part == 0 && threadIdx.x < 2) x.cursor[2 * t + threadIdx.x] = 0;
+}
+
+__device__ __forceinline__ Limits shared_limits(const Sample &a, const SampleShare &x, int64_t t)
+{
+    float2 ends = x.ends[t * a.parts];
+    for (int p = 1; p < a.parts; ++p) {
+        const float2 y = x.ends[t * a.parts + p];
+        ends = make_float2(fmaxf(ends.x, y.x), fminf(ends.y, y.y));
+    }
+    return Limits(a, t, ends.x, ends.y);
+}
+
+template <typename E> __global__ __launch_bounds__(kThreads) void sample_bins_kernel(Sample a, SampleShare x)
+{
+    __shared__ Shared s;
+    const int64_t t = blockIdx.x / a.parts;
+    const int part = blockIdx.x % a.parts, tid = threadIdx.x;
+    const Row<E> row(a, t);
+    const Limits l = shared_limits(a, x, t);
+    if (l.none) return;
+    if (l.greedy) {
+        const int first = first_of(s, row, l.m, part);
+        if (tid == 0) x.first[blockIdx.x] = first;
+        return;
+    }
+    if (!l.cuts()) {
+        const u64 sum = sum_of<kAll>(row, l, part * kWaves + (tid >> 6), 0, 0);
+        if ((tid & 63) == 0) x.range[(int64_t)blockIdx.x * kWaves + (tid >> 6)] = sum;
+        return;
+    }
+    fill_bins(s, row, l, part);
+    for (int b = tid; b < kBins; b += kThreads) {
+        x.count[(int64_t)blockIdx.x * kBins + b] = s.count[b];
+        if (l.by_p) x.sum[(int64_t)blockIdx.x * kBins + b] = s.sum[b];
+    }
+}
+
+// The row's bins from its parts', in LDS.
+__device__ __forceinline__ void load_bins(Shared &s, const Sample &a, const SampleShare &x, const Limits &l, int64_t t)
+{
+    for (int b = threadIdx.x; b < kBins; b += kThreads) {
+        uint32_t count = 0;
+        u64 sum = 0;
+        for (int p = 0; p < a.parts; ++p) {
+            count += x.count[(t * a.parts + p) * kBins + b];
+            if (l.by_p) sum += x.sum[(t * a.parts + p) * kBins + b];
+        }
+        s.count[b] = count;
+        s.sum[b] = sum;
+    }
+    __syncthreads();
+}
+
+template <typename E> __global__ __launch_bounds__(kThreads) void sample_collect_kernel(Sample a, SampleShare x)
+{
+    __shared__ Shared s;
+    const int64_t t = blockIdx.x / a.parts;
+    const int part = blockIdx.x % a.parts, tid = threadIdx.x;
+    const Row<E> row(a, t);
+    const Limits l = shared_limits(a, x, t);
+    if (!l.cuts()) return;
+    load_bins(s, a, x, l, t);
+    const Decision d = decide(s, l, Scan(s));
+    if (part == 0 && tid == 0) ((Decision *)x.decision)[t] = d;
+    if (d.mode == kFew || d.mode == kInBin) collect(row, l, part, d.mode == kFew, d.bin, x.cursor + 2 * t, (u64 *)x.list + t * kList);
+    if (d.mode == kInBin || d.mode == kWhole) {
+        const u64 sum = sum_of<kBefore>(row, l, part * kWaves + (tid >> 6), 0, d.bin);
+        if ((tid & 63) == 0) x.range[(int64_t)blockIdx.x * kWaves + (tid >> 6)] = sum;
+    }
+}
+
+template <typename E> __global__ __launch_bounds__(kThreads) void sample_draw_kernel(Sample a, SampleShare x)
+{
+    __shared__ Shared s;
+    const int64_t t = blockIdx.x;
+    const int tid = threadIdx.x, ranges = a.parts * kWaves;
+    const Row<E> row(a, t);
+    const Limits l = shared_limits(a, x, t);
+    if (l.none || l.greedy) {
+        if (tid == 0) {
+            int first = INT32_MAX;
+            for (int p = 0; p < a.parts; ++p) first = min(first, l.none ? -1 : x.first[t * a.parts + p]);
+            a.token[t] = first;
+            if (a.logprob) a.logprob[t] = l.none ? -INFINITY : 0.f;
+        }
+        return;
+    }
+    if (tid < ranges) s.range[tid] = x.range[t * ranges + tid];
+    if (!l.cuts()) {
+        __syncthreads();
+        draw_ranges(s, a, row, l, t, 0);
+        return;
+    }
+    const Decision d = ((const Decision *)x.decision)[t];
+    if (tid < 2) s.cursor[tid] = x.cursor[2 * t + tid];
+    __syncthreads();
+    const int n = (int)min(s.cursor[0], (uint32_t)kList), m = (int)min(s.cursor[1], (uint32_t)(kList - n));
+    for (int e = tid; e < kList; e += kThreads)
+        if (e < n || e >= kList - m) s.list[e] = ((const u64 *)x.list)[t * kList + e];
+    __syncthreads();
+    finish(s, a, row, l, t, d, [&] { load_bins(s, a, x, l, t); });
+}
+
+template <typename E> hipError_t launch(const Sample &a, const SampleShare &x, hipStream_t s)
+{
+    const dim3 rows((unsigned)a.T), parts((unsigned)(a.T * a.parts)), block(kThreads);
+    if (!x.ends) {
+        hipLaunchKernelGGL((sample_kernel<E>), rows, block, 0, s, a);
+        return hipGetLastError();
+    }
+    hipLaunchKernelGGL((sample_ends_kernel<E>), parts, block, 0, s, a, x);
+    hipLaunchKernelGGL((sample_bins_kernel<E>), parts, block, 0, s, a, x);
+    if (a.top_k || a.top_p) hipLaunchKernelGGL((sample_collect_kernel<E>), parts, block, 0, s, a, x);
+    hipLaunchKernelGGL((sample_draw_kernel<E>), rows, block, 0, s, a, x);
+    return hipGetLastError();
+}
+
+size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 
 }  // namespace
 
-hipError_t launch_sample(Sample a, hipStream_t s)
+int sample_parts(int64_t T, int64_t V, int num_cus)
+{
+    if (V < kSampleOne) return 0;
+    return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(num_cus / T, kSampleMaxParts), V / 4096));
+}
+
+size_t sample_workspace(int64_t T, int parts, bool cuts, char *base, SampleShare *x)
+{
+    size_t at = 0;
+    auto take = [&](size_t n) {
+        char *p = base ? base + at : nullptr;
+        at += align256(n);
+        return (void *)p;
+    };
+    SampleShare y = {};
+    if (parts) {
+        const size_t P = (size_t)T * parts;
+        y.ends = (float2 *)take(P * 8);
+        y.first = (int *)take(P * 4);
+        y.range = (unsigned long long *)take(P * kWaves * 8);
+        y.cursor = (uint32_t *)take((size_t)T * 8);
+        if (cuts) {
+            y.decision = take((size_t)T * sizeof(Decision));
+            y.list = (unsigned long long *)take((size_t)T * kList * 8);
+            y.count = (uint32_t *)take(P * kBins * 4);
+            y.sum = (unsigned long long *)take(P * kBins * 8);
+        }
+    }
+    if (x) *x = y;
+    return at;
+}
+
+hipError_t launch_sample(Sample a, int parts, const SampleShare &x, hipStream_t s)
 {
     const int groups = (a.V + 7 + 7) / 8;
-    a.parts = 1;
-    a.per = (groups + kWaves * 64 - 1) / (kWaves * 64) * 64;
-    const dim3 grid((unsigned)a.T), block(kThreads);
-    if (a.dt == IVF_F32) hipLaunchKernelGGL((sample_kernel<float>), grid, block, 0, s, a);
-    else if (a.dt == IVF_F16) hipLaunchKernelGGL((sample_kernel<_Float16>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((sample_kernel<__bf16>), grid, block, 0, s, a);
-    return hipGetLastError();
+    a.parts = std::max(parts, 1);
+    const int waves = kWaves * a.parts;
+    a.per = (groups + waves * 64 - 1) / (waves * 64) * 64;
+    return a.dt == IVF_F32   ? launch<float>(a, x, s)
+           : a.dt == IVF_F16 ? launch<_Float16>(a, x, s)
+                             : launch<__bf16>(a, x, s);
 }
 
 }  // namespace ivf

@@ -10,6 +10,7 @@ def sample(ctx, logits=P(0), dt=B.IVF_BF16, stride=1024, T=10, V=1000, uniform=P
 
 
 def test_sample_refusals(vctx):  # noqa: F811
+    vctx.lib.ivf_set_workspace(vctx.handle, (1 << 46) + (1 << 40), 1 << 36)
     assert sample(vctx) == B.IVF_EDEVICE  # every check passed
     assert sample(vctx, temperature=None, top_k=None, top_p=None, min_p=None, logprob=None) == B.IVF_EDEVICE
     assert sample(vctx, T=0, logits=None, uniform=None, token=None) == B.IVF_OK
@@ -24,3 +25,18 @@ def test_sample_refusals(vctx):  # noqa: F811
         assert sample(vctx, **bad) == B.IVF_EINVAL, bad
         assert vctx.error()
     assert vctx.lib.ivf_sample(None, None, 2, 0, 0, 1, None, None, None, None, None, None, None) == B.IVF_EINVAL
+
+
+def test_sample_bytes_are_what_the_call_asks_for(vctx):  # noqa: F811
+    off = dict(temperature=None, top_k=None, top_p=None, min_p=None)
+    for T, V in ((1, 1), (1, 32_000), (3, 1 << 20), (64, 128_000), (250, 100_003), (300, 1000), (5000, 20_000)):
+        for cuts in (0, 1):
+            need = vctx.lib.ivf_sample_bytes(T, V, cuts)
+            vctx.lib.ivf_set_workspace(vctx.handle, None, 0)
+            got = sample(vctx, T=T, V=V, stride=V, **({} if cuts else off))
+            assert got == (B.IVF_ENOMEM if need else B.IVF_EDEVICE), (T, V, cuts)
+            assert not need or str(need) in vctx.error()
+            vctx.lib.ivf_set_workspace(vctx.handle, (1 << 46) + (1 << 40), need)
+            assert sample(vctx, T=T, V=V, stride=V, **({} if cuts else off)) == B.IVF_EDEVICE
+    for T, V in ((0, 100), (-1, 100), (1, 0), (1, (1 << 20) + 1), (1 << 22, 100_000), (1 << 60, 100_000)):
+        assert vctx.lib.ivf_sample_bytes(T, V, 1) == 0

@@ -158,6 +158,21 @@ def test_values_that_are_not_finite(ctx, kind):
     run(ctx, x, rng.random(T), top_k=np.full(T, V - 1))
 
 
+@pytest.mark.parametrize("bits", [0x7FC0, 0xFFC0, 0x7F81, 0xFFBF])
+def test_numbers_of_no_kind(ctx, bits):
+    """Quiet and signaling ones of both signs count as -infinity."""
+    import torch
+
+    rng = np.random.default_rng(bits)
+    x = tensor(logits(rng, 4, 20_000), "bf16")
+    where = torch.from_numpy(rng.random((4, 20_000)) < 0.3).cuda()
+    x = torch.where(where, torch.full_like(x, bits - 65536 if bits > 32767 else bits, dtype=torch.int16), x.view(torch.int16))
+    x = x.view(torch.bfloat16)
+    assert bool(torch.isnan(x)[where].all())
+    for which in LIMITS:
+        run(ctx, x, rng.random(4), **some(rng, 4, 20_000, which))
+
+
 def test_arguments_beyond_their_ranges(ctx):
     rng = np.random.default_rng(4)
     inf, nan = np.inf, np.nan
