@@ -147,13 +147,34 @@ __device__ __forceinline__ u64 weight(float x, double m, double inv_t)
     return (u64)__double_as_longlong(__longlong_as_double((long long)b) + 4503599627370496.0) & 0xfffffffffffffull;
 }
 
-__device__ __forceinline__ u64 shfl_up64(u64 x, int d) { return (u64)__shfl_up((long long)x, d); }
-__device__ __forceinline__ u64 wave_sum(u64 x)
+// Lane exchanges without LDS: x of the lane that CTRL names in the rows of MASK, 0 where there is none.
+template <int CTRL, int MASK> __device__ __forceinline__ u64 moved(u64 x)
 {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) x += (u64)__shfl_xor((long long)x, d);
-    return x;
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)x, CTRL, MASK, 0xf, false);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(x >> 32), CTRL, MASK, 0xf, false);
+    return (u64)hi << 32 | lo;
 }
+// The sum of x over this lane and those before it in its row of 16.
+__device__ __forceinline__ u64 row_scan(u64 x)
+{
+    x += moved<0x111, 0xf>(x);  // one lane up, two, four, eight
+    x += moved<0x112, 0xf>(x);
+    x += moved<0x114, 0xf>(x);
+    return x + moved<0x118, 0xf>(x);
+}
+// ... in the wave.
+__device__ __forceinline__ u64 wave_scan(u64 x)
+{
+    x = row_scan(x);
+    x += moved<0x142, 0xa>(x);         // the last lane of rows 0 and 2 to rows 1 and 3
+    return x + moved<0x143, 0xc>(x);   // lane 31 to rows 2 and 3
+}
+__device__ __forceinline__ u64 of_lane(u64 x, int lane)
+{
+    return (u64)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(x >> 32), lane) << 32 |
+           (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, lane);
+}
+__device__ __forceinline__ u64 wave_sum(u64 x) { return of_lane(wave_scan(x), 63); }
 
 // How the kept part of a row ends: nowhere; in a bin that is listed with all bins before it; in one that is listed
 // alone; or in one of more elements than a list holds.
@@ -172,8 +193,9 @@ struct Shared {
     uint32_t rest;
     u64 before;
     uint32_t cursor[2];  // of the list: elements of the bins before (from its front on) and of the bin (from its end back)
+    uint32_t at[2];
     u64 cut, through;
-    int mode, found;
+    int found;
 };
 
 // What `decide` finds, for the launch that draws.
@@ -187,23 +209,14 @@ struct Decision {
 // The sum of x over the threads before this one; *all: over all of them.
 __device__ __forceinline__ u64 sum_before(Shared &s, u64 x, u64 *all)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    u64 up = x;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const u64 y = shfl_up64(up, d);
-        if (lane >= d) up += y;
-    }
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const u64 up = wave_scan(x);
     __syncthreads();
     if (lane == 63) s.waves[wave] = up;
     __syncthreads();
-    u64 before = up - x, total = 0;
-    for (int w = 0; w < kWaves; ++w) {
-        if (w < wave) before += s.waves[w];
-        total += s.waves[w];
-    }
-    *all = total;
-    return before;
+    const u64 waves = row_scan(s.waves[lane % kWaves]);
+    *all = of_lane(waves, kWaves - 1);
+    return up - x + (wave ? of_lane(waves, wave - 1) : 0);
 }
 
 // What a row asks for, with its largest and least logit.
@@ -400,12 +413,13 @@ __device__ __forceinline__ Decision decide(Shared &s, const Limits &l, const Sca
     return d;
 }
 
-// The part's elements of bin `last`, and with `before` of the bins before it, in no order. cursor and list are in LDS or
-// device memory; what would not find room is left out.
+// The part's elements of bin `last`, and with `before` of the bins before it, in no order, in s.list; what would not
+// find room is left out. All threads call it.
 template <typename E>
-__device__ __forceinline__ void collect(const Row<E> &row, const Limits &l, int part, bool before, int last, uint32_t *cursor, u64 *list)
+__device__ __forceinline__ void collect(Shared &s, const Row<E> &row, const Limits &l, int part, bool before, int last)
 {
-    const int lane = threadIdx.x & 63;
+    if (threadIdx.x < 2) s.cursor[threadIdx.x] = 0;
+    __syncthreads();
     row.for_range(part * kWaves + (threadIdx.x >> 6), [&](const float (&x)[8], int i) {
         float most = x[0];
 #pragma unroll
@@ -420,21 +434,12 @@ __device__ __forceinline__ void collect(const Row<E> &row, const Limits &l, int 
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            if (!__any(hits[h] != 0)) continue;
-            const uint32_t n = __popc(hits[h]);
-            uint32_t up = n;
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const uint32_t y = __shfl_up(up, d);
-                if (lane >= d) up += y;
-            }
-            uint32_t at = 0;
-            if (lane == 63) at = atomicAdd(&cursor[h], up);
-            at = __builtin_amdgcn_readlane(at, 63) + up - n;
+            if (!hits[h]) continue;
+            uint32_t at = atomicAdd(&s.cursor[h], (uint32_t)__popc(hits[h]));
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 if (hits[h] >> j & 1) {
-                    if (at < kList) list[h ? kList - 1 - at : at] = place_of(x[j], i + j);
+                    if (at < kList) s.list[h ? kList - 1 - at : at] = place_of(x[j], i + j);
                     ++at;
                 }
         }
@@ -446,7 +451,22 @@ __device__ __forceinline__ void collect(const Row<E> &row, const Limits &l, int 
 __device__ __forceinline__ void sort_list(u64 *list, int n)
 {
     const int tid = threadIdx.x;
-    int m = 2;
+    __syncthreads();
+    if (n <= 128) {
+        // each by the number of larger ones (equal ones by their position)
+        const u64 mine = tid < n ? list[tid] : 0;
+        int larger = 0;
+        if (tid < n)
+            for (int e = 0; e < n; ++e) {
+                const u64 other = list[e];
+                larger += other > mine || (other == mine && e < tid);
+            }
+        __syncthreads();
+        if (tid < n) list[larger] = mine;
+        __syncthreads();
+        return;
+    }
+    int m = 256;
     while (m < n) m <<= 1;
     for (int i = n + tid; i < m; i += kThreads) list[i] = 0;
     __syncthreads();
@@ -460,7 +480,7 @@ __device__ __forceinline__ void sort_list(u64 *list, int n)
                     list[i + j] = a;
                 }
             }
-            if (j > 64 || (j == 1 && k >= 128)) {
+            if (j > 64 || (j == 1 && k >= 128)) {  // else a wave's own
                 __syncthreads();
             } else {
                 __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -722,13 +742,7 @@ template <typename E> __device__ __forceinline__ void find_cut(Shared &s, const 
     __syncthreads();
     if (wave == 0) {
         const u64 equal = equal_of(s.bin, x);
-        u64 up = equal;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const u64 y = shfl_up64(up, d);
-            if (lane >= d) up += y;
-        }
-        u64 n = s.before + up - equal;
+        u64 n = s.before + wave_scan(equal) - equal;
         if (equal)
 #pragma unroll
             for (int j = 0; j < 8; ++j)
@@ -807,9 +821,7 @@ template <typename E> __global__ __launch_bounds__(kThreads) void sample_kernel(
     }
     fill_bins(s, row, l, 0);
     const Decision d = decide(s, l, Scan(s));
-    if (tid < 2) s.cursor[tid] = 0;
-    __syncthreads();
-    if (d.mode == kFew || d.mode == kInBin) collect(row, l, 0, d.mode == kFew, d.bin, s.cursor, s.list);
+    if (d.mode == kFew || d.mode == kInBin) collect(s, row, l, 0, d.mode == kFew, d.bin);
     if (d.mode == kInBin || d.mode == kWhole) {
         const u64 sum = sum_of<kBefore>(row, l, wave, 0, d.bin);
         if (lane == 0) s.range[wave] = sum;
@@ -871,10 +883,12 @@ __device__ __forceinline__ void load_bins(Shared &s, const Sample &a, const Samp
     for (int b = threadIdx.x; b < kBins; b += kThreads) {
         uint32_t count = 0;
         u64 sum = 0;
-        for (int p = 0; p < a.parts; ++p) {
-            count += x.count[(t * a.parts + p) * kBins + b];
-            if (l.by_p) sum += x.sum[(t * a.parts + p) * kBins + b];
-        }
+#pragma unroll
+        for (int p = 0; p < kSampleMaxParts; ++p)
+            if (p < a.parts) {
+                count += x.count[(t * a.parts + p) * kBins + b];
+                if (l.by_p) sum += x.sum[(t * a.parts + p) * kBins + b];
+            }
         s.count[b] = count;
         s.sum[b] = sum;
     }
@@ -892,7 +906,19 @@ template <typename E> __global__ __launch_bounds__(kThreads) void sample_collect
     load_bins(s, a, x, l, t);
     const Decision d = decide(s, l, Scan(s));
     if (part == 0 && tid == 0) ((Decision *)x.decision)[t] = d;
-    if (d.mode == kFew || d.mode == kInBin) collect(row, l, part, d.mode == kFew, d.bin, x.cursor + 2 * t, (u64 *)x.list + t * kList);
+    if (d.mode == kFew || d.mode == kInBin) {
+        // in LDS first: an addition to the row's cursors returns after microseconds
+        collect(s, row, l, part, d.mode == kFew, d.bin);
+        __syncthreads();
+        if (tid < 2) s.at[tid] = atomicAdd(&x.cursor[2 * t + tid], s.cursor[tid]);
+        __syncthreads();
+        u64 *list = (u64 *)x.list + t * kList;
+        const uint32_t n = min(s.cursor[0], (uint32_t)kList), m = min(s.cursor[1], (uint32_t)kList - n);
+        for (uint32_t e = tid; e < n; e += kThreads)
+            if (s.at[0] + e < kList) list[s.at[0] + e] = s.list[e];
+        for (uint32_t e = tid; e < m; e += kThreads)
+            if (s.at[1] + e < kList) list[kList - 1 - s.at[1] - e] = s.list[kList - 1 - e];
+    }
     if (d.mode == kInBin || d.mode == kWhole) {
         const u64 sum = sum_of<kBefore>(row, l, part * kWaves + (tid >> 6), 0, d.bin);
         if ((tid & 63) == 0) x.range[(int64_t)blockIdx.x * kWaves + (tid >> 6)] = sum;
