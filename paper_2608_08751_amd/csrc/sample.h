@@ -38,10 +38,7 @@ struct SampleShare {
     unsigned long long *sum;
 };
 
-// Rows of fewer logits are taken by one workgroup in one launch.
-constexpr int64_t kSampleOne = 16384;
-
-// Workgroups that share a row; 0: one launch. Bytes of the workspace (0 with it), and with a base what lies where.
+// Workgroups that share a row; 0: one a row, in one launch. Bytes of the workspace (0 with it), and with a base what lies where.
 int sample_parts(int64_t T, int64_t V, int num_cus);
 size_t sample_workspace(int64_t T, int parts, bool cuts, char *base, SampleShare *x);
 hipError_t launch_sample(Sample a, int parts, const SampleShare &x, hipStream_t s);

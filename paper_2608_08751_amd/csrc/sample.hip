@@ -126,21 +126,30 @@ template <typename E> struct Row {
 };
 
 // w = 2^43 exp((x - m) / t) to the nearest whole number; 2^f by a polynomial of degree 9 in f (fitted on
-// [-1/2, 1/2] with 2^0 = 1, relative error 2^-44.6). -infinity weighs nothing.
-__device__ __forceinline__ u64 weight(float x, double m, double inv_t)
+// [-1/2, 1/2] with 2^0 = 1, relative error 2^-44.6). -infinity weighs nothing. Bound by its instructions: 22 and some
+// ten around it, 16 of them in fp64, for each logit. The coefficients are kept in scalar registers: in vector
+// registers each addition would first copy its own (16 instructions; 250 rows of 100,003 without limits 47 us, so 42).
+struct Coefficients {
+    double c[8];
+    __device__ __forceinline__ Coefficients()
+    {
+        const double k[8] = {1.325522487405178e-06,  1.5252686845751567e-05, 0.00015403455852473414, 0.0013333558179043862,
+                             0.009618129159402536,   0.055504108664760424,   0.2402265069581299,     0.6931471805599453};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            c[i] = k[i];
+            asm("" : "+s"(c[i]));
+        }
+    }
+};
+__device__ __forceinline__ u64 weight(float x, double m, double inv_t, const Coefficients &k)
 {
     constexpr double kRound = 6755399441055744.0;  // 1.5 2^52: the sum's low bits are the nearest whole number
     const double d = fmax(((double)x - m) * inv_t, -60.0);
     const double n = d + kRound, f = d - (n - kRound);
     double r = 1.020312117214188e-07;
-    r = fma(r, f, 1.325522487405178e-06);
-    r = fma(r, f, 1.5252686845751567e-05);
-    r = fma(r, f, 0.00015403455852473414);
-    r = fma(r, f, 0.0013333558179043862);
-    r = fma(r, f, 0.009618129159402536);
-    r = fma(r, f, 0.055504108664760424);
-    r = fma(r, f, 0.2402265069581299);
-    r = fma(r, f, 0.6931471805599453);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r = fma(r, f, k.c[i]);
     r = fma(r, f, 1.0);
     // times 2^(n + 43) in the exponent; + 2^52 rounds
     const u64 b = (u64)__double_as_longlong(r) + ((u64)(uint32_t)((int)__double_as_longlong(n) + 43) << 52);
@@ -228,15 +237,18 @@ struct Limits {
     int top_k;
     float top_p;
     u64 least_w;  // of what min_p keeps
-    __device__ __forceinline__ Limits(const Sample &a, int64_t t, float high, float low)
+    // (beyond 2^60 the range of the bins would not hold in fp32; no number stays none)
+    static __device__ __forceinline__ float temperature_of(const Sample &a, int64_t t)
     {
-        // (beyond 2^60 the range of the bins would not hold in fp32; no number stays none)
-        const float given = a.temperature ? a.temperature[t] : 1.f, temp = given > 0x1p60f ? 0x1p60f : given;
-        m = high;
-        md = (double)high;
+        const float given = a.temperature ? a.temperature[t] : 1.f;
+        return given > 0x1p60f ? 0x1p60f : given;
+    }
+    __device__ __forceinline__ Limits(const Sample &a, int64_t t, float high, float low)
+        : m(high), md((double)high), inv_t(1.4426950408889634 / (double)temperature_of(a, t))
+    {
+        const float temp = temperature_of(a, t);
         none = high == -INFINITY;
         greedy = !(temp > 0.f);
-        inv_t = 1.4426950408889634 / (double)temp;
         // beyond 31 temperatures a weight is below 2^-44
         per = ((float)(kBins - 1) - 0.5f) / fmaxf(fminf(high - low, 31.f * temp), 1e-30f);
         top_k = a.top_k ? a.top_k[t] : 0;
@@ -247,12 +259,12 @@ struct Limits {
     }
     __device__ __forceinline__ bool cuts() const { return !none && !greedy && (by_k || by_p); }
     __device__ __forceinline__ int bin(float x) const { return (int)fminf((m - x) * per, (float)(kBins - 1)); }
-    __device__ __forceinline__ u64 weigh(float x) const { return weight(x, md, inv_t); }
+    __device__ __forceinline__ u64 weigh(float x, const Coefficients &k = Coefficients()) const { return weight(x, md, inv_t, k); }
     // the weight of an element that is kept, else 0
-    __device__ __forceinline__ u64 kept(float x, int i, u64 cut) const
+    __device__ __forceinline__ u64 kept(float x, int i, u64 cut, const Coefficients &k = Coefficients()) const
     {
         if (cut && place_of(x, i) < cut) return 0;
-        const u64 w = weigh(x);
+        const u64 w = weigh(x, k);
         return w >= least_w ? w : 0;
     }
     // the weights that top_p of `whole` asks for
@@ -313,6 +325,7 @@ template <typename E> __device__ __forceinline__ int first_of(Shared &s, const R
 enum Part { kAll, kBefore, kFromCut };
 template <Part PART, typename E> __device__ __forceinline__ u64 sum_of(const Row<E> &row, const Limits &l, int r, u64 cut, int bin)
 {
+    const Coefficients k;
     u64 sum = 0;
     row.for_range(r, [&](const float (&x)[8], int i) {
         if (PART != kAll) {
@@ -323,7 +336,7 @@ template <Part PART, typename E> __device__ __forceinline__ u64 sum_of(const Row
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const u64 w = l.kept(x[j], i + j, PART == kFromCut ? cut : 0);
+            const u64 w = l.kept(x[j], i + j, PART == kFromCut ? cut : 0, k);
             if (PART != kBefore || l.bin(x[j]) < bin) sum += w;
         }
     });
@@ -339,13 +352,14 @@ template <typename E> __device__ __forceinline__ void fill_bins(Shared &s, const
         s.sum[b] = 0;
     }
     __syncthreads();
+    const Coefficients k;
     row.for_range(part * kWaves + (tid >> 6), [&](const float (&x)[8], int) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const int b = l.bin(x[j]);
             if (b < kBins - 1) {
                 atomicAdd(&s.count[b], 1u);
-                if (l.by_p) atomicAdd(&s.sum[b], l.weigh(x[j]));
+                if (l.by_p) atomicAdd(&s.sum[b], l.weigh(x[j], k));
             }
         }
     });
@@ -975,10 +989,15 @@ size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 
 }  // namespace
 
+// One launch takes 8-17 us where four take 12-25 (up to 16,000 logits), but a workgroup goes over 128,000 in 120 us with
+// top_p (four of them 58, eight 55; 32 rows), 43 without limits (21, 18). Rows are shared out while that
+// leaves every part 8,000 logits and a CU: top_p of 32,000 logits, one row 32.3 us in one launch, 29.6 in four
+// parts, 64 rows 38.9 and 40.3; 128 rows of 32,000 and 64,000 39.4 and 68.7, in two parts 42.9 and 58.2; 250 rows
+// of 128,000 130, in two parts 143.
 int sample_parts(int64_t T, int64_t V, int num_cus)
 {
-    if (V < kSampleOne) return 0;
-    return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(num_cus / T, kSampleMaxParts), V / 4096));
+    const int64_t parts = std::min<int64_t>(std::min<int64_t>(num_cus / T, kSampleMaxParts), V / 8000);
+    return parts < 2 || (parts == 2 && V < 48000) ? 0 : (int)parts;
 }
 
 size_t sample_workspace(int64_t T, int parts, bool cuts, char *base, SampleShare *x)
