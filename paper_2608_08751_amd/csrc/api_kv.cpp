@@ -119,7 +119,7 @@ ivf_status attend(ivf_ctx *ctx, const ivf_kv_cache *cache, const void *q, int64_
         const float scale2 = fabsf(scale) * 1.44269504089f;  // of exponents to the base 2
         if (!isfinite(scale2)) return fail(ctx, IVF_EINVAL, "scale must be finite, and of magnitude below 2.3e38");
         const ivf_kv_terms none = {}, &given = terms ? *terms : none;
-        KvTerms x = {given.cap, given.slopes, given.first, given.prefix};
+        KvTerms x = {given.cap, {}, given.slopes, given.first, given.prefix};
         if (x.cap != 0.f) {
             if (!(x.cap >= 0x1p-40f && x.cap <= 0x1p40f)) return fail(ctx, IVF_EINVAL, "cap must be 0, or from 2^-40 to 2^40");
             const float by_cap = fabsf(scale) / x.cap;
@@ -161,6 +161,8 @@ ivf_status attend(ivf_ctx *ctx, const ivf_kv_cache *cache, const void *q, int64_
         const bool has_terms = x.cap != 0.f || x.slopes || x.first || x.prefix;
         if (x.cap != 0.f) a.scale = std::max(fabsf(scale) / x.cap, 0x1p-149f);
         x.cap *= 1.44269504089f;
+        const float near[5] = {0.99999994f, -0.333323091f, 0.133101732f, -0.0521014817f, 0.0154754277f};
+        for (int i = 0; i < 5; ++i) x.near[i] = near[i] * x.cap;
         a.out = out;
         a.lse = out_lse;
         a.small_rows = p.small_rows;

@@ -132,10 +132,13 @@ struct KvAttend {
 // these as members of KvAttend the kernels without terms spilled 17 registers.)
 struct KvTerms {
     float cap;
+    float near[5];                  // of tanh's polynomial for small scores, times the cap
     const float *slopes;            // [query heads], or null
     const int32_t *first, *prefix;  // [T], or null
 };
-struct KvNoTerms {};
+struct KvNoTerms {
+    static constexpr bool kCap = false, kBias = false;
+};
 
 // Which kernels take a call, in how many parts, and what those need.
 struct KvAttendPlan {

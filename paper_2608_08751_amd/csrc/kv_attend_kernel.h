@@ -229,18 +229,20 @@ void kv_attend_kernel(KvAttend a, Terms terms)
         }
 
         // the steps of 32 keys of this part, wave by wave
-        int strips, s_end, step;
+        int strips, s_end, step, all_steps;
         bool whole;  // all of the unit's steps
         int slot = 0;
         if (SPARSE) {
             strips = lim_max < 0 ? 0 : a.count << strip_shift;
             const int steps = (strips + 1) >> 1, per = (steps + a.splits - 1) / a.splits;
+            all_steps = steps;
             step = min((int64_t)steps, (int64_t)split * per);
             s_end = min((int64_t)steps, (int64_t)step + per);
             whole = a.splits == 1;
         } else {
             strips = (lim_max + 16) >> 4;
             const int steps = TERMS ? ranges.count : (strips + 1) >> 1;
+            all_steps = steps;
             step = 0;
             s_end = steps;
             whole = true;
@@ -266,7 +268,14 @@ void kv_attend_kernel(KvAttend a, Terms terms)
         int keys = -1, ahead = 0;
         auto look = [&](int first_step) {
             const int64_t st = (int64_t)first_step + (lane >> 1) * TEAM;
-            const int64_t v = 2 * (TERMS && !SPARSE && st < s_end ? ranges.at((int)st) : st) + (lane & 1);
+            int64_t at = st;
+            if constexpr (TERMS) {
+                // with a bias the nearest keys come first: scores that grow from step to step would raise the
+                // reference, and rescale all sums, again and again
+                if (terms.slopes) at = all_steps - 1 - st;
+                if (!SPARSE && st < s_end) at = ranges.at((int)at);
+            }
+            const int64_t v = 2 * at + (lane & 1);
             rec_lo = rec_hi = 0;
             keys = -1;
             if (st < s_end && v < strips) {
@@ -346,7 +355,7 @@ void kv_attend_kernel(KvAttend a, Terms terms)
 #pragma unroll
             for (int i = 0; i < kOwn; ++i) t[i] = PACK ? (second ? st[1][i] : st[0][i]) : st[i / 4][i % 4];
             if constexpr (TERMS) {
-                scale_scores(t, a.scale, terms.cap);
+                scale_scores(t, a.scale, terms);
                 if (terms.slopes) {
 #pragma unroll
                     for (int e = 0; e < kOwn / 4; ++e) {

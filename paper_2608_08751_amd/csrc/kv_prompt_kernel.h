@@ -79,7 +79,7 @@ __global__ __launch_bounds__(PromptShape<D>::threads, 2) void kv_prompt_kernel(K
         slope[ct] = 0.f;
         if constexpr (TERMS) {
             pos[ct] = have ? a.position[tok[ct]] : -1;  // for the bias, beyond the table too
-            if (terms.slopes) slope[ct] = terms.slopes[qhead[ct]] * 1.44269504089f;
+            if (Terms::kBias) slope[ct] = terms.slopes[qhead[ct]] * 1.44269504089f;
         }
         mine[ct] = false;
         const elem *q = (const elem *)a.q.p + (have ? tok[ct] * a.q.ts + (int64_t)qhead[ct] * a.q.hs : 0);
@@ -188,6 +188,11 @@ __global__ __launch_bounds__(PromptShape<D>::threads, 2) void kv_prompt_kernel(K
 
         const int ntiles = TERMS ? ranges.count : (int)(((int64_t)gmax + kTileKeys) / kTileKeys);  // 0 where gmax is -1
         static_assert(kTileKeys == 128 || kTileKeys == 64, "steps of the ranges");
+        // The k-th tile. With a bias the nearest keys come first: scores that grow from tile to tile would raise the
+        // reference, and rescale all sums, again and again (2,048 tokens after 8,192: 543 us, so 344).
+        auto tile_at = [&](int k) __attribute__((always_inline)) {
+            return !TERMS ? k : ranges.at(Terms::kBias ? ntiles - 1 - k : k);
+        };
         const int per = (ntiles + a.splits - 1) / a.splits;
         const int k0 = min((int64_t)ntiles, (int64_t)split * per), k1 = min(ntiles, k0 + per);
         if (k0 >= k1) continue;
@@ -196,7 +201,7 @@ __global__ __launch_bounds__(PromptShape<D>::threads, 2) void kv_prompt_kernel(K
         // lane i keeps the block of this wave's strip of the i-th next tile
         int pages = -1, ahead = 0;
         auto look = [&](int k) __attribute__((always_inline)) {
-            const int64_t key = (TERMS ? (int64_t)ranges.at(min(k + lane, ntiles)) : (int64_t)(k + lane)) * kTileKeys + 16 * wave;
+            const int64_t key = (TERMS ? (int64_t)tile_at(min(k + lane, ntiles - 1)) : (int64_t)(k + lane)) * kTileKeys + 16 * wave;
             pages = -1;
             if (key <= gmax) {
                 const int id = table[key >> a.c.shift];
@@ -215,7 +220,7 @@ __global__ __launch_bounds__(PromptShape<D>::threads, 2) void kv_prompt_kernel(K
             ++ahead;
             if (page >= 0) {
                 const uint8_t *rec = a.c.rec + ((int64_t)page * a.c.heads + head) * rec_bytes;
-                const StripBase base = StripBase::at<D>(rec, (kWaves * (TERMS ? ranges.at(k) : k) + wave) & strip_mask);
+                const StripBase base = StripBase::at<D>(rec, (kWaves * tile_at(k) + wave) & strip_mask);
                 keys.load(base, k_offs);
                 vals.load(base, v_offs);
             }
@@ -231,7 +236,7 @@ __global__ __launch_bounds__(PromptShape<D>::threads, 2) void kv_prompt_kernel(K
                 for (int j = 0; j < kOut; ++j) vdst[128 * j] = (u32x2){0, 0};
                 return;
             }
-            const int key = (TERMS ? ranges.at(k) : k) * kTileKeys + 16 * wave;
+            const int key = tile_at(k) * kTileKeys + 16 * wave;
             auto piece = [&](auto piece_c) {
                 constexpr int c = decltype(piece_c)::value, S = P::size(c);
                 const float ks = kv_scale(keys.ks[c]);
@@ -255,7 +260,7 @@ __global__ __launch_bounds__(PromptShape<D>::threads, 2) void kv_prompt_kernel(K
         };
         // 64 keys of a tile
         auto compute = [&](int k, int part) __attribute__((always_inline)) {
-            const int buf = k & 1, first = (TERMS ? ranges.at(k) : k) * kTileKeys + 64 * part;
+            const int buf = k & 1, first = tile_at(k) * kTileKeys + 64 * part;
             if (TERMS ? !seen.any(first, 64) : first > wmax) return;  // uniform over the wave
             f32x4 st[4][CT];
 #pragma unroll
@@ -269,33 +274,61 @@ __global__ __launch_bounds__(PromptShape<D>::threads, 2) void kv_prompt_kernel(K
                     for (int ct = 0; ct < CT; ++ct) st[e][ct] = TT::mfma(x, qf[ct][w], st[e][ct]);
                 }
             }
+            // a score is factor * st, with a bias + tilt * key + lift, to the base 2
+            float factor = Terms::kCap ? 1.f : a.scale, tilt[CT], lift[CT];
             const int *none = &absent[buf][4 * part];
             const int gone = none[0] | none[1] << 1 | none[2] << 2 | none[3] << 3;
             if constexpr (TERMS) {
-                const bool part_of = !seen.all(first, 64) || __builtin_amdgcn_readfirstlane(gone);
+                if constexpr (Terms::kCap) {
 #pragma unroll
-                for (int ct = 0; ct < CT; ++ct) {
+                    for (int ct = 0; ct < CT; ++ct) {
+                        float t[16];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        float t[4] = {st[e][ct][0], st[e][ct][1], st[e][ct][2], st[e][ct][3]};
-                        scale_scores(t, a.scale, terms.cap);
-                        if (terms.slopes) {
-                            const float apart = (float)(pos[ct] - first - 4 * h);  // above 2^24 rounded, as the bias is
+                        for (int i = 0; i < 16; ++i) t[i] = st[i / 4][ct][i % 4];
+                        cap_scores(t, a.scale, terms);
 #pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                t[i] = __builtin_fmaf(-slope[ct], fabsf(apart - (float)(16 * e + i)), t[i]);
-                        }
-                        st[e][ct] = (f32x4){t[0], t[1], t[2], t[3]};
-                        asm volatile("" : "+v"(st[e][ct]));  // four at a time
+                        for (int i = 0; i < 16; ++i) st[i / 4][ct][i % 4] = t[i];
                     }
-                    if (part_of) {
+                }
+                if constexpr (Terms::kBias) {
+                    // keys past the position that a prefix shows: their distance grows the other way
+                    const bool turns = first < seen.prefix_max && first + 63 > seen.pos_min;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
+                    for (int ct = 0; ct < CT; ++ct) {
+                        const float apart = (float)(pos[ct] - first - 4 * h);  // above 2^24 rounded, as the bias is
+                        tilt[ct] = slope[ct];
+                        lift[ct] = -slope[ct] * apart;
+                        if (turns) {
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                if ((gone >> e & 1) || !sight[ct].sees(first + 4 * h + 16 * e + i)) st[e][ct][i] = -INFINITY;
-                                asm volatile("" : "+v"(st[e][ct][i]));  // one comparison at a time: no stack of masks
+                            for (int i = 0; i < 16; ++i)
+                                st[i / 4][ct][i % 4] = __builtin_fmaf(-slope[ct], fabsf(apart - (float)(16 * (i / 4) + i % 4)),
+                                                                      st[i / 4][ct][i % 4] * factor);
+                            tilt[ct] = lift[ct] = 0.f;
+                        }
+                    }
+                    if (turns) factor = 1.f;
+                }
+                if (!seen.all(first, 64) || __builtin_amdgcn_readfirstlane(gone)) {
+                    // which ends of the rows' ranges lie in these keys: uniform over the wave
+                    const bool low = first < seen.first_max, prefix = first < seen.prefix_max;
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct) {
+                        const int at = first + 4 * h;
+                        const int to = sight[ct].pos - at, from = sight[ct].first - at, end = sight[ct].prefix - at;
+                        auto mask = [&](auto sees) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const int last = (gone >> e & 1) ? -1 : to, before = (gone >> e & 1) ? -1 : end;
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) {
+                                    if (!sees(16 * e + i, last, before)) st[e][ct][i] = -INFINITY;
+                                    asm volatile("" : "+v"(st[e][ct][i]));  // one comparison at a time: no stack of masks
+                                }
                             }
+                        };
+                        if (prefix) mask([&](int c, int last, int before) { return (c <= last && c >= from) || c < before; });
+                        else if (low) mask([&](int c, int last, int) { return c <= last && c >= from; });
+                        else mask([&](int c, int last, int) { return c <= last; });
                     }
                 }
             } else if (first + 63 > wmin || __builtin_amdgcn_readfirstlane(gone)) {
@@ -319,19 +352,25 @@ __global__ __launch_bounds__(PromptShape<D>::threads, 2) void kv_prompt_kernel(K
                 float p[4][4], part_sum;
                 auto probabilities = [&]() {
                     part_sum = 0.f;
+                    const float base = Terms::kBias ? lift[ct] - sub[ct] : -sub[ct];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) p[e][i] = exp2_fast(TERMS ? st[e][ct][i] - sub[ct] : __builtin_fmaf(st[e][ct][i], a.scale, -sub[ct]));
+                        for (int i = 0; i < 4; ++i)
+                            p[e][i] = exp2_fast(__builtin_fmaf(st[e][ct][i], factor,
+                                                               Terms::kBias ? __builtin_fmaf(tilt[ct], (float)(16 * e + i), base) : base));
                         part_sum += (p[e][0] + p[e][1]) + (p[e][2] + p[e][3]);
                     }
                 };
                 probabilities();
                 if (__ballot(part_sum > kMost || ref[ct] == -INFINITY)) {
-                    float mx = st[0][ct][0];
+                    float mx = -INFINITY;
 #pragma unroll
-                    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, st[i / 4][ct][i % 4]);
-                    const float top = fmaxf(ref[ct], max_over_h(TERMS ? mx : mx * a.scale));
+                    for (int i = 0; i < 16; ++i) {
+                        const float x = st[i / 4][ct][i % 4];
+                        mx = fmaxf(mx, Terms::kBias ? __builtin_fmaf(x, factor, tilt[ct] * (float)(16 * (i / 4) + i % 4)) : x);
+                    }
+                    const float top = fmaxf(ref[ct], max_over_h(Terms::kBias ? mx + lift[ct] : mx * factor));
                     const float f = ref[ct] == top ? 1.f : exp2_fast(ref[ct] - top);
                     ref[ct] = top;
                     sub[ct] = top == -INFINITY ? 0.f : top - kCarry;

@@ -14,7 +14,12 @@
 
 namespace ivf {
 
-template <typename Terms> constexpr bool has_terms = std::is_same<Terms, KvTerms>::value;
+template <typename Terms> constexpr bool has_terms = !std::is_same<Terms, KvNoTerms>::value;
+
+// Terms of a kernel of their own: with a cap or not, with a bias or not (always with sights).
+template <bool CAP, bool BIAS> struct KvTermsOf : KvTerms {
+    static constexpr bool kCap = CAP, kBias = BIAS;
+};
 
 // The keys that a row sees; last_key: the last that its table has room for. A row that does not count or stands
 // at no position sees nothing.
@@ -99,7 +104,8 @@ struct KvSteps {
 
 // tanh x. Up to 1 by a polynomial in x^2 (fitted to the relative error over [0, 1]: 1.6e-7 with its roundings), beyond
 // that by 1 - 2 / (1 + exp 2x), whose last subtraction costs at most a bit there (at 0 it would leave an absolute
-// error of the whole cap's rounding).
+// error of the whole cap's rounding). Up to 0.6 five terms do (1.8e-7): they come with the cap multiplied in
+// (KvTerms::near), two instructions a score less.
 __device__ __forceinline__ float tanh_near(float x)
 {
     const float z = x * x;
@@ -117,31 +123,47 @@ __device__ __forceinline__ float tanh_far(float x)
     return 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * 2.88539008f));
 }
 
-// The N scores of a lane, to the base 2, from its products with the query: capped or scaled. The polynomial
-// alone serves where no lane has a score beyond the cap.
-template <int N> __device__ __forceinline__ void scale_scores(float (&t)[N], float scale, float cap)
+// The N capped scores of a lane, to the base 2, from its products with the query (scale: by the cap). Which form is
+// taken goes by the largest score of the wave's lanes.
+template <int N> __device__ __forceinline__ void cap_scores(float (&t)[N], float scale, const KvTerms &x)
 {
-    if (cap == 0.f) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) t[i] *= scale;
-        return;
-    }
     float most = 0.f;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        t[i] *= scale;
-        most = fmaxf(most, fabsf(t[i]));
-    }
-    if (!__ballot(most > 1.f)) {
+    for (int i = 0; i < N; ++i) most = fmaxf(most, fabsf(t[i]));
+    if (!__ballot(most * scale > 0.6f)) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) t[i] = tanh_near(t[i]) * cap;
+        for (int i = 0; i < N; ++i) {
+            const float y = t[i] * scale, z = y * y;
+            float p = __builtin_fmaf(x.near[4], z, x.near[3]);
+            p = __builtin_fmaf(p, z, x.near[2]);
+            p = __builtin_fmaf(p, z, x.near[1]);
+            t[i] = y * __builtin_fmaf(p, z, x.near[0]);
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) t[i] *= scale;
+    if (!__ballot(most * scale > 1.f)) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) t[i] = tanh_near(t[i]) * x.cap;
         return;
     }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const float near = tanh_near(t[i]), far = tanh_far(t[i]);
-        t[i] = (fabsf(t[i]) <= 1.f ? near : far) * cap;
+        t[i] = (fabsf(t[i]) <= 1.f ? near : far) * x.cap;
     }
+}
+
+// Scores to the base 2, capped or scaled.
+template <int N> __device__ __forceinline__ void scale_scores(float (&t)[N], float scale, const KvTerms &x)
+{
+    if (x.cap != 0.f) {
+        cap_scores(t, scale, x);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) t[i] *= scale;
 }
 
 }  // namespace ivf
