@@ -703,6 +703,9 @@ def ivf_kv_copy(ctx: Context, cache: KVCache, to, source, source_cache: KVCache 
         ctx.check(st, "ivf_kv_copy")
 
 
+_reclaim_bytes = {}  # workspace of calls of given sizes
+
+
 def ivf_kv_reclaim(ctx: Context, cached, block_size: int, table, blocks: int, moves: int = 0):
     """The blocks (of `blocks`) that no request holds: request b holds those of the
     first ceil(cached[b] / block_size) columns of its row of `table` (int32 [B, columns]).
@@ -722,7 +725,12 @@ def ivf_kv_reclaim(ctx: Context, cached, block_size: int, table, blocks: int, mo
     ins = (_ints(ctx, cached, "cached", (B,), i32), B, block_size, _ints(ctx, table, "table", shape, i32), cols, blocks, moves)
     whole = torch.empty(6 + blocks + 2 * moves, dtype=i32, device=table.device)  # info (two words each) comes first
     info, free, source, to = torch.unsafe_split_with_sizes(whole, (6, blocks, moves, moves))
-    need = ctx.lib.ivf_kv_reclaim_bytes(B, block_size, cols, blocks, moves)
+    sizes = B, block_size, cols, blocks, moves
+    need = _reclaim_bytes.get(sizes)
+    if need is None:
+        if len(_reclaim_bytes) >= 1024:
+            _reclaim_bytes.clear()
+        need = _reclaim_bytes[sizes] = ctx.lib.ivf_kv_reclaim_bytes(*sizes)
     if need:
         ctx.ensure_workspace(need)
     at = whole.data_ptr()

@@ -12,7 +12,7 @@ namespace ivf {
 constexpr int kKvMaxRequests = 16384;  // of one plan: their prefix sums lie in LDS
 constexpr int kKvMaxSelectCols = 32768;  // block scores of a row lie in LDS
 constexpr int kKvMaxCount = 4096;
-constexpr int kKvFewBlocks = 1 << 18;    // whose bits lie in one workgroup's LDS
+constexpr int kKvFewBlocks = 1 << 15;    // and table entries that one workgroup reclaims
 constexpr int kKvMaxUnits = 1024;  // whose key ranges are shared out evenly (prefix sums in LDS)
 
 struct KvCache {

@@ -128,7 +128,7 @@ __global__ __launch_bounds__(THREADS) void kv_fork_kernel(const int32_t *__restr
 }
 
 // Copies pairs of blocks, kPiece bytes of records a workgroup at a time (the last
-// of a pair with the summaries). Bound by memory, read + written.
+// of a pair with the summaries). Bound by memory, read + written: 139 MB 22 us, 276 MB 51 us, 6.3 and 5.4 TB/s.
 constexpr int kPiece = 16384;
 __global__ __launch_bounds__(256) void kv_copy_kernel(KvCache dst, KvCache src, const int32_t *__restrict__ to,
                                                       const int32_t *__restrict__ source, int64_t units, uint32_t pieces)
@@ -176,6 +176,27 @@ template <int THREADS, typename F> __device__ __forceinline__ void for_entries(c
     }
 }
 
+// The same in one workgroup for up to 2^31 entries: a thread an entry, four loads each at a time, none of which waits
+// for another.
+template <int THREADS, typename F> __device__ __forceinline__ void for_few_entries(const KvReclaim &a, F f)
+{
+    const uint32_t all = (uint32_t)(a.B * a.cols), cols = (uint32_t)a.cols;
+    for (uint32_t e0 = threadIdx.x; e0 < all; e0 += 4 * THREADS) {
+        int32_t id[4], n[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t e = min(e0 + k * THREADS, all - 1);
+            id[k] = a.table[e];
+            n[k] = a.cached[e / cols];
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t e = e0 + k * THREADS;
+            if (e < all && (int)(e % cols) < held(n[k], a.shift, a.cols)) f(e, id[k]);
+        }
+    }
+}
+
 // With U blocks in use, the used ones at U and beyond (as many as there are holes below U)
 // move into the holes, both in ascending order, the first `made` of them.
 struct Moves {
@@ -210,30 +231,22 @@ struct Bits {
 constexpr int kOne = 1024;
 __global__ __launch_bounds__(kOne) void kv_reclaim_one_kernel(KvReclaim a)
 {
-    constexpr int kWords = kKvFewBlocks / 32, kPer = kWords / kOne;
+    constexpr int kWords = kKvFewBlocks / 32;
     __shared__ uint32_t word[kWords + 1], before[kWords + 1];
     const int tid = threadIdx.x;
     const int words = (int)(a.blocks + 31) / 32;
     for (int w = tid; w <= words; w += kOne) word[w] = 0;
     __syncthreads();
-    for_entries<kOne>(a, [&](int64_t e) {
-        const int id = a.table[e];
+    for_few_entries<kOne>(a, [&](uint32_t, int id) {
         if (id >= 0 && id < a.blocks) atomicOr(&word[id >> 5], 1u << (id & 31));
     });
     __syncthreads();
-    const int per = (words + kOne - 1) / kOne;
-    uint32_t mine = 0, all;
-    for (int k = 0; k < per; ++k)
-        if (tid * per + k < words) mine += __popc(word[tid * per + k]);
-    uint32_t at = sum_before<kOne>(mine, &all);
-    for (int k = 0; k < per; ++k)
-        if (tid * per + k < words) {
-            before[tid * per + k] = at;
-            at += __popc(word[tid * per + k]);
-        }
+    static_assert(kWords <= kOne, "a thread's word");
+    uint32_t all;
+    const uint32_t below = sum_before<kOne>(tid < words ? __popc(word[tid]) : 0, &all);
+    if (tid < words) before[tid] = below;
     if (tid == 0) before[words] = all;
     __syncthreads();
-    static_assert(kPer * kOne == kWords, "a thread's words");
     const Bits bits = {word, before};
     Moves m;
     m.used = all;
@@ -253,8 +266,7 @@ __global__ __launch_bounds__(kOne) void kv_reclaim_one_kernel(KvReclaim a)
     }
     if (m.made == 0) return;
     __syncthreads();  // to[] is read
-    for_entries<kOne>(a, [&](int64_t e) {
-        const int id = a.table[e];
+    for_few_entries<kOne>(a, [&](uint32_t e, int id) {
         if (id < m.used || id >= a.blocks) return;
         const int64_t r = bits.below(id) - m.below;
         if (r < m.made) a.table[e] = a.to[r];
@@ -357,9 +369,10 @@ unsigned entry_groups(const KvReclaim &a, int num_cus)
     return (unsigned)std::max<int64_t>(1, std::min<int64_t>((units + 3) / 4, (int64_t)num_cus * 8));
 }
 
-// One workgroup reads a table at some hundred entries per microsecond.
-constexpr int64_t kOneEntries = 16384;
-bool in_one(int64_t blocks, int64_t entries) { return blocks <= kKvFewBlocks && entries <= kOneEntries; }
+// One workgroup takes tables of few entries and blocks in one launch, without moves and with: 16,000 entries, 4,000
+// blocks 9.8 and 15.2 us, in several launches 22.1 and 25.4; 16,000 blocks 15.3 and 20.8, 25.3 and 30.4; 65,000
+// blocks 37.5 and 43.9, 28.9 and 34.2; 64,000 entries, 16,000 blocks 29.9 and 51.8, 33.2 and 36.0.
+bool in_one(int64_t blocks, int64_t entries) { return blocks <= kKvFewBlocks && entries <= kKvFewBlocks; }
 
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 

@@ -199,7 +199,7 @@ def run_reclaim(ctx, cached, bs, table, blocks, moves):
 
 
 RECLAIMS = [  # requests, columns, blocks, block size, moves: in one workgroup, and in several launches
-    (1, 1, 1, 16, 0), (1, 3, 31, 64, 5), (4, 9, 64, 16, 40), (16, 70, 1100, 64, 2000), (7, 300, 2101, 16, 3),
+    (1, 1, 1, 16, 0), (1, 3, 31, 64, 5), (4, 9, 64, 16, 40), (3, 10_000, 32_768, 16, 32_768), (3, 10_000, 32_767, 16, 99), (3, 10_000, 32_769, 16, 99), (16, 70, 1100, 64, 2000), (7, 300, 2101, 16, 3),
     (60, 260, 10_000, 32, 100), (1, 16_384, 20_000, 16, 9999),
     (70, 300, 15_001, 32, 0), (70, 300, 15_001, 32, 10_000), (70, 300, 200_000, 32, 17), (3, 9, 300_001, 16, 50),
     (2000, 40, 70_000, 16, 70_000), (1, 20_000, 66_000, 16, 66_000),
@@ -320,14 +320,15 @@ def test_samples_of_one_prompt(ctx, kind, dim, bs, length):
     check()
 
 
-def test_captured_on_another_stream(ctx):
+@pytest.mark.parametrize("blocks", [25_000, 60_000])
+def test_captured_on_another_stream(ctx, blocks):
     """Fork, copy and reclaim as a graph, replayed on other lengths and tables in the same buffers."""
     import torch
 
     import paper_2608_08751_amd as ivf
 
     rng = np.random.default_rng(3)
-    B, cols, bs, blocks, moves = 40, 500, 16, 25_000, 3000
+    B, cols, bs, moves = 40, 500, 16, 3000
     cache = ivf.KVCache.empty(blocks, 1, 64, bs)
     table, cached, free = ints(np.zeros((B, cols))), ints(np.zeros(B)), ints(np.zeros(30))
     parent, child = ints(np.zeros(12)), ints(np.zeros(12))
