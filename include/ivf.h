@@ -584,7 +584,9 @@ ivf_status ivf_kv_copy(ivf_ctx *ctx, const ivf_kv_cache *cache, const ivf_kv_cac
  * held ones are 0 ... U - 1 afterwards.
  *   cached      [B] int32        table [B][table_cols] int32, updated
  *   out_free    [blocks] int32: the blocks that are free after the moves,
- *               ascending, -1 behind them; may be NULL
+ *               ascending, -1 behind them (out_info[2] says how many: to
+ *               ivf_kv_plan and ivf_kv_fork an entry of -1 is a block that is
+ *               none); may be NULL
  *   out_source, out_to [moves] int32, -1 behind the pairs; NULL when moves is 0
  *   out_info    [3] int64: U, moves made, blocks - U; may be NULL
  * B = 0: all are free, cached and table may be NULL.

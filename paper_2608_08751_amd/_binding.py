@@ -726,7 +726,7 @@ def ivf_kv_reclaim(ctx: Context, cached, block_size: int, table, blocks: int, mo
     whole = torch.empty(6 + blocks + 2 * moves, dtype=i32, device=table.device)  # info (two words each) comes first
     info, free, source, to = torch.unsafe_split_with_sizes(whole, (6, blocks, moves, moves))
     sizes = B, block_size, cols, blocks, moves
-    need = _reclaim_bytes.get(sizes)
+    need = _reclaim_bytes.get(sizes)  # (goes by sizes alone)
     if need is None:
         if len(_reclaim_bytes) >= 1024:
             _reclaim_bytes.clear()
@@ -861,7 +861,7 @@ def ivf_kv_attend(ctx: Context, cache: KVCache, q, start, request, position, tab
 # ---- the token that follows ---------------------------------------------------
 
 _logit_types = None
-_sample_bytes = {}  # workspace of calls of given sizes
+_sample_bytes = {}  # workspace of calls of given sizes on a device
 
 
 def ivf_sample(ctx: Context, logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None):
@@ -898,11 +898,12 @@ def ivf_sample(ctx: Context, logits, uniform, temperature=None, top_k=None, top_
     token, logprob = torch.unsafe_split_with_sizes(torch.empty(2 * T, dtype=torch.int32, device=logits.device), (T, T))
     logprob = logprob.view(f32)
     sizes = T, V, int(top_k is not None or top_p is not None)
-    need = _sample_bytes.get(sizes)
+    need = _sample_bytes.get((ctx.device, sizes))
     if need is None:
         if len(_sample_bytes) >= 1024:
             _sample_bytes.clear()
-        need = _sample_bytes[sizes] = ctx.lib.ivf_sample_bytes(*sizes)
+        with torch.cuda.device(ctx.device):  # it goes by the device's compute units
+            need = _sample_bytes[ctx.device, sizes] = ctx.lib.ivf_sample_bytes(*sizes)
     if need:
         ctx.ensure_workspace(need)
     lib, handle = ctx.bind()

@@ -179,6 +179,24 @@ def test_masks(ctx, c, mask):
     run(ctx, "bf16" if c["dim"] % 128 else "f16", seed=len(mask), mask=mask, **c)
 
 
+@pytest.mark.parametrize("terms", [dict(), dict(cap=5.0, slopes=[0.2, 0.003])], ids=["sights", "all"])
+@pytest.mark.parametrize("c", [
+    dict(lens=[1200], new=[1100], heads=4, group=8, dim=64, bs=16), dict(lens=[1100, 700, 650], new=[600, 1, 500], heads=8, group=4, dim=128, bs=64),
+    dict(lens=[480, 90, 3, 600], new=[400, 9, 1, 300], heads=3, group=4, dim=192, bs=32)], ids=name)
+def test_a_few_rows_that_see_much_more(ctx, c, terms):
+    """The last rows of every request see all,
+    some in the middle nothing, the others a short window and a few first keys."""
+    rng = np.random.default_rng(1)
+
+    def sight(p):
+        start, request, position = batch(c["lens"], c["new"])
+        last = np.asarray(c["lens"])[request] - position <= 7
+        kind = rng.random(len(p)) < 0.1
+        return np.where(last, 0, np.where(kind, p + 1, p - 20)), np.where(last | kind, 0, np.minimum(p + 1, 3))
+
+    run(ctx, "bf16" if c["dim"] == 128 else "f16", seed=8, sight=sight, **terms, **c)
+
+
 @pytest.mark.parametrize("kind,cap,scale", [("bf16", 0.02, None), ("f16", 1.0, None), ("bf16", 5.0, -0.2), ("f16", 30.0, 0.9),
                                             ("bf16", 2.0**-40, None), ("f16", 2.0**40, None)])
 @pytest.mark.parametrize("c", LAYOUTS, ids=name)
