@@ -176,21 +176,22 @@ template <int THREADS, typename F> __device__ __forceinline__ void for_entries(c
     }
 }
 
-// The same in one workgroup for up to 2^31 entries: a thread an entry, four loads each at a time, none of which waits
+// The same in one workgroup for up to 2^31 entries: a thread an entry, eight loads each at a time, none of which waits
 // for another.
 template <int THREADS, typename F> __device__ __forceinline__ void for_few_entries(const KvReclaim &a, F f)
 {
+    constexpr int U = 8;
     const uint32_t all = (uint32_t)(a.B * a.cols), cols = (uint32_t)a.cols;
-    for (uint32_t e0 = threadIdx.x; e0 < all; e0 += 4 * THREADS) {
-        int32_t id[4], n[4];
+    for (uint32_t e0 = threadIdx.x; e0 < all; e0 += U * THREADS) {
+        int32_t id[U], n[U];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < U; ++k) {
             const uint32_t e = min(e0 + k * THREADS, all - 1);
             id[k] = a.table[e];
             n[k] = a.cached[e / cols];
         }
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < U; ++k) {
             const uint32_t e = e0 + k * THREADS;
             if (e < all && (int)(e % cols) < held(n[k], a.shift, a.cols)) f(e, id[k]);
         }

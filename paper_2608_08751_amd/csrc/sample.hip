@@ -51,19 +51,27 @@ __device__ __forceinline__ float number_of(uint32_t o)
 __device__ __forceinline__ u64 place_of(float x, int i) { return (u64)order_of(x) << 32 | (uint32_t)~i; }
 __device__ __forceinline__ int index_of(u64 place) { return (int)~(uint32_t)place; }
 
-// A logit as it counts: no number as -infinity, +infinity as the largest number.
-__device__ __forceinline__ float clean(float x) { return fminf(x == x ? x : -INFINITY, 3.40282347e38f); }
+constexpr float kLargest = 3.40282347e38f;  // what +infinity counts as
 
 __device__ __forceinline__ float widen(float x) { return x; }
 __device__ __forceinline__ float widen(_Float16 x) { return (float)x; }
 __device__ __forceinline__ float widen(__bf16 x) { return (float)x; }
 
+// The larger of a number and a logit; a logit that is no number is passed over (by a comparison: the maximum
+// instruction passes on a signaling NaN).
+__device__ __forceinline__ float larger(float most, float x) { return x > most ? x : most; }
+
+// A logit that is no number has no weight and no bin but the last as it is: d and the bin's number below, which
+// differences have quieted, are kept in range by maximum and minimum. +infinity, which would make differences of no kind, is
+// replaced, in rows whose largest logit it is.
+//
 // A row of V logits, taken in groups of eight that begin at multiples of 16 bytes. A range is the groups that one
 // wave goes over, `per` of them; a row has parts * kWaves ranges.
 template <typename E> struct Row {
     const E *p;
     int V, pad;  // elements of the first group that lie before the row
     int per, parts;
+    bool infinite = false;  // whether there is +infinity
     __device__ __forceinline__ Row(const Sample &a, int64_t t)
     {
         p = (const E *)a.logits + t * a.stride;
@@ -78,12 +86,16 @@ template <typename E> struct Row {
     // Eight elements as they lie in memory.
     struct Group {
         uint4 w[sizeof(E) / 2];
-        __device__ __forceinline__ void to(float (&x)[8]) const
+        __device__ __forceinline__ void to(float (&x)[8], bool infinite) const
         {
             typedef E E8 __attribute__((ext_vector_type(8)));
             const E8 y = __builtin_bit_cast(E8, *this);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = clean(widen((E)y[j]));
+            for (int j = 0; j < 8; ++j) x[j] = widen((E)y[j]);
+            if (infinite) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] = x[j] == INFINITY ? kLargest : x[j];
+            }
         }
     };
     // group g, -infinity outside the row and from group `end` on
@@ -117,7 +129,7 @@ template <typename E> struct Row {
             for (int k = 0; k < U; ++k) {
                 if (g + 64 * k < end) {
                     float x[8];
-                    y[k].to(x);
+                    y[k].to(x, infinite);
                     f(x, first_of(g + 64 * k + lane));
                 }
             }
@@ -244,13 +256,13 @@ struct Limits {
         return given > 0x1p60f ? 0x1p60f : given;
     }
     __device__ __forceinline__ Limits(const Sample &a, int64_t t, float high, float low)
-        : m(high), md((double)high), inv_t(1.4426950408889634 / (double)temperature_of(a, t))
+        : m(fminf(high, kLargest)), md((double)fminf(high, kLargest)), inv_t(1.4426950408889634 / (double)temperature_of(a, t))
     {
         const float temp = temperature_of(a, t);
         none = high == -INFINITY;
         greedy = !(temp > 0.f);
         // beyond 31 temperatures a weight is below 2^-44
-        per = ((float)(kBins - 1) - 0.5f) / fmaxf(fminf(high - low, 31.f * temp), 1e-30f);
+        per = ((float)(kBins - 1) - 0.5f) / fmaxf(fminf(m - low, 31.f * temp), 1e-30f);
         top_k = a.top_k ? a.top_k[t] : 0;
         top_p = a.top_p ? a.top_p[t] : 1.f;
         by_k = top_k > 0 && top_k < a.V;
@@ -265,6 +277,7 @@ struct Limits {
     {
         if (cut && place_of(x, i) < cut) return 0;
         const u64 w = weigh(x, k);
+        if (!least_w) return w;  // uniform over the workgroup
         return w >= least_w ? w : 0;
     }
     // the weights that top_p of `whole` asks for
@@ -282,7 +295,7 @@ template <typename E> __device__ __forceinline__ float2 ends_of(Shared &s, const
     row.for_range(part * kWaves + wave, [&](const float (&x)[8], int) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            high = fmaxf(high, x[j]);
+            high = larger(high, x[j]);
             low = fminf(low, x[j] > -INFINITY ? x[j] : INFINITY);
         }
     });
@@ -329,9 +342,9 @@ template <Part PART, typename E> __device__ __forceinline__ u64 sum_of(const Row
     u64 sum = 0;
     row.for_range(r, [&](const float (&x)[8], int i) {
         if (PART != kAll) {
-            float most = x[0];
+            float most = -INFINITY;
 #pragma unroll
-            for (int j = 1; j < 8; ++j) most = fmaxf(most, x[j]);
+            for (int j = 0; j < 8; ++j) most = larger(most, x[j]);
             if (!__any(PART == kBefore ? l.bin(most) < bin : order_of(most) >= (uint32_t)(cut >> 32))) return;
         }
 #pragma unroll
@@ -435,9 +448,9 @@ __device__ __forceinline__ void collect(Shared &s, const Row<E> &row, const Limi
     if (threadIdx.x < 2) s.cursor[threadIdx.x] = 0;
     __syncthreads();
     row.for_range(part * kWaves + (threadIdx.x >> 6), [&](const float (&x)[8], int i) {
-        float most = x[0];
+        float most = -INFINITY;
 #pragma unroll
-        for (int j = 1; j < 8; ++j) most = fmaxf(most, x[j]);
+        for (int j = 0; j < 8; ++j) most = larger(most, x[j]);
         if (!__any(l.bin(most) <= last)) return;
         uint32_t hits[2] = {0, 0};
 #pragma unroll
@@ -597,9 +610,12 @@ __device__ __forceinline__ void draw_listed(Shared &s, const Sample &a, const Ro
     const int tid = threadIdx.x;
     int shift = 0;
     while (a.V - 1 >> shift >= kBins) ++shift;
-    for (int b = tid; b < kBins; b += kThreads) s.sum[b] = 0;
+    const bool few = n + m <= 128;  // all in order at once: no buckets
+    if (!few)
+        for (int b = tid; b < kBins; b += kThreads) s.sum[b] = 0;
+    if (tid == 0) s.found = 0;
     __syncthreads();
-    u64 w[2];
+    u64 w[2], whole, goal;
     int bucket[2];
     uint32_t index[2];
 #pragma unroll
@@ -609,20 +625,25 @@ __device__ __forceinline__ void draw_listed(Shared &s, const Sample &a, const Ro
         const u64 place = there ? s.list[e] : 0;
         index[k] = (uint32_t)index_of(place);
         w[k] = there ? l.kept(number_of((uint32_t)(place >> 32)), (int)index[k], cut) : 0;
-        bucket[k] = w[k] ? (int)(index[k] >> shift) : -1;
-        if (w[k]) atomicAdd(&s.sum[bucket[k]], w[k]);
+        bucket[k] = w[k] ? few ? 0 : (int)(index[k] >> shift) : -1;
+        if (!few && w[k]) atomicAdd(&s.sum[bucket[k]], w[k]);
     }
-    __syncthreads();
-    u64 whole;
-    const u64 x0 = s.sum[2 * tid], x1 = s.sum[2 * tid + 1];
-    const u64 at = sum_before(s, x0 + x1, &whole);
-    const u64 goal = goal_of(a, t, whole);
-    if (at <= goal && at + x0 + x1 > goal) {
-        const bool second = at + x0 <= goal;
-        s.bin = 2 * tid + second;
-        s.before = second ? at + x0 : at;
+    if (few) {
+        if (tid == 0) {
+            s.bin = 0;
+            s.before = 0;
+        }
+    } else {
+        __syncthreads();
+        const u64 x0 = s.sum[2 * tid], x1 = s.sum[2 * tid + 1];
+        const u64 at = sum_before(s, x0 + x1, &whole);
+        goal = goal_of(a, t, whole);
+        if (at <= goal && at + x0 + x1 > goal) {
+            const bool second = at + x0 <= goal;
+            s.bin = 2 * tid + second;
+            s.before = second ? at + x0 : at;
+        }
     }
-    if (tid == 0) s.found = 0;
     __syncthreads();
     // a weight takes 44 bits, an index 20; the lowest index first
 #pragma unroll
@@ -641,9 +662,13 @@ __device__ __forceinline__ void draw_listed(Shared &s, const Sample &a, const Ro
     }
     u64 all;
     const u64 running = s.before + sum_before(s, w[0] + w[1], &all);
+    if (few) {
+        whole = all;
+        goal = goal_of(a, t, whole);
+    }
     if (running <= goal && running + w[0] + w[1] > goal) {
 #pragma unroll
-        for (int k = 0; k < 2; ++k) x[k] = clean(widen(row.p[i[k]]));
+        for (int k = 0; k < 2; ++k) x[k] = fminf(widen(row.p[i[k]]), kLargest);
         pick(s, a, l, t, running, goal, whole, w, x, i);
     }
 }
@@ -666,7 +691,7 @@ template <typename E> __device__ __forceinline__ void draw_ranges(Shared &s, con
         float y[8];
         int index[8];
         u64 w[8], sum = 0, all;
-        row.load(g0 + tid, end).to(y);
+        row.load(g0 + tid, end).to(y, row.infinite);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             index[j] = row.first_of(g0 + tid) + j;
@@ -728,7 +753,7 @@ template <typename E> __device__ __forceinline__ void find_cut(Shared &s, const 
     auto equal_of = [&](int seg, float (&x)[8]) {
         u64 equal = 0;
         if (64 * seg + lane < row.groups()) {
-            row.load(64 * seg + lane, row.groups()).to(x);
+            row.load(64 * seg + lane, row.groups()).to(x, row.infinite);
 #pragma unroll
             for (int j = 0; j < 8; ++j) equal += order_of(x[j]) == prefix;
         }
@@ -815,9 +840,10 @@ template <typename E> __global__ __launch_bounds__(kThreads) void sample_kernel(
     __shared__ Shared s;
     const int64_t t = blockIdx.x;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-    const Row<E> row(a, t);
+    Row<E> row(a, t);
     const float2 ends = ends_of(s, row, 0);
     const Limits l(a, t, ends.x, ends.y);
+    row.infinite = l.m == kLargest;
     if (l.none || l.greedy) {
         const int first = l.none ? -1 : first_of(s, row, l.m, 0);
         if (tid == 0) {
@@ -871,8 +897,9 @@ template <typename E> __global__ __launch_bounds__(kThreads) void sample_bins_ke
     __shared__ Shared s;
     const int64_t t = blockIdx.x / a.parts;
     const int part = blockIdx.x % a.parts, tid = threadIdx.x;
-    const Row<E> row(a, t);
+    Row<E> row(a, t);
     const Limits l = shared_limits(a, x, t);
+    row.infinite = l.m == kLargest;
     if (l.none) return;
     if (l.greedy) {
         const int first = first_of(s, row, l.m, part);
@@ -914,8 +941,9 @@ template <typename E> __global__ __launch_bounds__(kThreads) void sample_collect
     __shared__ Shared s;
     const int64_t t = blockIdx.x / a.parts;
     const int part = blockIdx.x % a.parts, tid = threadIdx.x;
-    const Row<E> row(a, t);
+    Row<E> row(a, t);
     const Limits l = shared_limits(a, x, t);
+    row.infinite = l.m == kLargest;
     if (!l.cuts()) return;
     load_bins(s, a, x, l, t);
     const Decision d = decide(s, l, Scan(s));
@@ -944,8 +972,9 @@ template <typename E> __global__ __launch_bounds__(kThreads) void sample_draw_ke
     __shared__ Shared s;
     const int64_t t = blockIdx.x;
     const int tid = threadIdx.x, ranges = a.parts * kWaves;
-    const Row<E> row(a, t);
+    Row<E> row(a, t);
     const Limits l = shared_limits(a, x, t);
+    row.infinite = l.m == kLargest;
     if (l.none || l.greedy) {
         if (tid == 0) {
             int first = INT32_MAX;
