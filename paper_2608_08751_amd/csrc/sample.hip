@@ -440,13 +440,15 @@ __device__ __forceinline__ Decision decide(Shared &s, const Limits &l, const Sca
     return d;
 }
 
-// The part's elements of bin `last`, and with `before` of the bins before it, in no order, in s.list; what would not
-// find room is left out. All threads call it.
-template <typename E>
-__device__ __forceinline__ void collect(Shared &s, const Row<E> &row, const Limits &l, int part, bool before, int last)
+// The part's elements of bin `last` in no order, in s.list (what would not find room is left out); and of the bins before
+// it the elements too (FEW), or the wave's sum of kept weights. All threads call it.
+template <bool FEW, typename E>
+__device__ __forceinline__ u64 collect(Shared &s, const Row<E> &row, const Limits &l, int part, int last)
 {
     if (threadIdx.x < 2) s.cursor[threadIdx.x] = 0;
     __syncthreads();
+    const Coefficients c;
+    u64 sum = 0;
     row.for_range(part * kWaves + (threadIdx.x >> 6), [&](const float (&x)[8], int i) {
         float most = -INFINITY;
 #pragma unroll
@@ -456,11 +458,15 @@ __device__ __forceinline__ void collect(Shared &s, const Row<E> &row, const Limi
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const int b = l.bin(x[j]);
-            hits[0] |= (uint32_t)(before && b < last) << j;
+            if (FEW) hits[0] |= (uint32_t)(b < last) << j;
             hits[1] |= (uint32_t)(b == last) << j;
+            if (!FEW) {
+                const u64 w = l.kept(x[j], i + j, 0, c);
+                if (b < last) sum += w;
+            }
         }
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = FEW ? 0 : 1; h < 2; ++h) {
             if (!hits[h]) continue;
             uint32_t at = atomicAdd(&s.cursor[h], (uint32_t)__popc(hits[h]));
 #pragma unroll
@@ -471,6 +477,7 @@ __device__ __forceinline__ void collect(Shared &s, const Row<E> &row, const Limi
                 }
         }
     });
+    return FEW ? 0 : wave_sum(sum);
 }
 
 // Sorts list[0, n), descending, in LDS; up to the next power of two it is filled with zeros. Strides of up to 64
@@ -567,8 +574,8 @@ __device__ __forceinline__ void cut_listed(Shared &s, const Limits &l, int n, ui
 }
 
 // The place of the last element that is kept (min_p apart), with what `decide` asks for in the list; n: the
-// list's elements of the bins before the last one, m: of that one. bins() puts the row's bins into LDS.
-template <typename Bins> __device__ __forceinline__ u64 last_kept(Shared &s, const Limits &l, const Decision &d, int n, int m, Bins bins)
+// list's elements of the bins before the last one, m: of that one.
+__device__ __forceinline__ u64 last_kept(Shared &s, const Limits &l, const Decision &d, int n, int m)
 {
     const int tid = threadIdx.x;
     for (int i = tid; i < m; i += kThreads) s.segment[i] = s.list[kList - 1 - i];
@@ -586,7 +593,18 @@ template <typename Bins> __device__ __forceinline__ u64 last_kept(Shared &s, con
     if (need > d.before) {
         cut_listed(s, l, m, 0, d.before, need);
     } else {
-        bins();
+        // (all their elements are listed)
+        for (int b = tid; b < kBins; b += kThreads) {
+            s.count[b] = 0;
+            s.sum[b] = 0;
+        }
+        __syncthreads();
+        for (int i = tid; i < n; i += kThreads) {
+            const float x = number_of((uint32_t)(s.list[i] >> 32));
+            atomicAdd(&s.count[l.bin(x)], 1u);
+            atomicAdd(&s.sum[l.bin(x)], l.weigh(x));
+        }
+        __syncthreads();
         Scan(s).find(s, need, true);
         const int bin = s.bin;
         const u64 before = s.before;
@@ -801,7 +819,7 @@ __device__ __forceinline__ void finish(Shared &s, const Sample &a, const Row<E> 
     const int n = (int)min(s.cursor[0], (uint32_t)kList), m = (int)min(s.cursor[1], (uint32_t)(kList - n));
     u64 cut = 0;
     if (d.mode == kFew || d.mode == kInBin) {
-        cut = last_kept(s, l, d, n, m, bins);
+        cut = last_kept(s, l, d, n, m);
         __syncthreads();
         if (d.mode == kFew) {
             draw_listed(s, a, row, l, t, n, m, cut);
@@ -861,11 +879,11 @@ template <typename E> __global__ __launch_bounds__(kThreads) void sample_kernel(
     }
     fill_bins(s, row, l, 0);
     const Decision d = decide(s, l, Scan(s));
-    if (d.mode == kFew || d.mode == kInBin) collect(s, row, l, 0, d.mode == kFew, d.bin);
-    if (d.mode == kInBin || d.mode == kWhole) {
-        const u64 sum = sum_of<kBefore>(row, l, wave, 0, d.bin);
-        if (lane == 0) s.range[wave] = sum;
-    }
+    u64 sum = 0;
+    if (d.mode == kFew) collect<true>(s, row, l, 0, d.bin);
+    else if (d.mode == kInBin) sum = collect<false>(s, row, l, 0, d.bin);
+    else if (d.mode == kWhole) sum = sum_of<kBefore>(row, l, wave, 0, d.bin);
+    if (lane == 0) s.range[wave] = sum;
     __syncthreads();
     finish(s, a, row, l, t, d, [] {});
 }
@@ -948,9 +966,13 @@ template <typename E> __global__ __launch_bounds__(kThreads) void sample_collect
     load_bins(s, a, x, l, t);
     const Decision d = decide(s, l, Scan(s));
     if (part == 0 && tid == 0) ((Decision *)x.decision)[t] = d;
+    u64 sum = 0;
+    if (d.mode == kFew) collect<true>(s, row, l, part, d.bin);
+    else if (d.mode == kInBin) sum = collect<false>(s, row, l, part, d.bin);
+    else if (d.mode == kWhole) sum = sum_of<kBefore>(row, l, part * kWaves + (tid >> 6), 0, d.bin);
+    if ((tid & 63) == 0) x.range[(int64_t)blockIdx.x * kWaves + (tid >> 6)] = sum;
     if (d.mode == kFew || d.mode == kInBin) {
         // in LDS first: an addition to the row's cursors returns after microseconds
-        collect(s, row, l, part, d.mode == kFew, d.bin);
         __syncthreads();
         if (tid < 2) s.at[tid] = atomicAdd(&x.cursor[2 * t + tid], s.cursor[tid]);
         __syncthreads();
@@ -960,10 +982,6 @@ template <typename E> __global__ __launch_bounds__(kThreads) void sample_collect
             if (s.at[0] + e < kList) list[s.at[0] + e] = s.list[e];
         for (uint32_t e = tid; e < m; e += kThreads)
             if (s.at[1] + e < kList) list[kList - 1 - s.at[1] - e] = s.list[kList - 1 - e];
-    }
-    if (d.mode == kInBin || d.mode == kWhole) {
-        const u64 sum = sum_of<kBefore>(row, l, part * kWaves + (tid >> 6), 0, d.bin);
-        if ((tid & 63) == 0) x.range[(int64_t)blockIdx.x * kWaves + (tid >> 6)] = sum;
     }
 }
 
