@@ -44,6 +44,11 @@
 // tokens x 8 heads over 24 blocks of 64 keys 286 us (calls one after the other 343), vector units 77 % and matrix
 // units 29 % busy, 11 TB/s from L2. Its launch bound of three waves a SIMD costs one or two spilled registers at
 // 128 channels.
+//
+// With terms in the scores (kv_terms.h) steps that no row of the unit sees are left out, and a step whose keys all rows
+// see takes no masks. 64 single tokens of up to 32,000, variants in turn: 173 us without terms, 184 with a bias or a
+// prefix, 196 with a cap, 200 with cap and bias: the cache's read does not hide the terms wholly. 32 windows of 4,096
+// keys in contexts of up to 50,000, capped, 143 MB: 40 us (3.6 TB/s) and 5 to join.
 #pragma once
 
 #include "kv.h"

@@ -128,7 +128,7 @@ __global__ __launch_bounds__(THREADS) void kv_fork_kernel(const int32_t *__restr
 }
 
 // Copies pairs of blocks, kPiece bytes of records a workgroup at a time (the last
-// of a pair with the summaries). Bound by memory, read + written: 139 MB 22 us, 276 MB 51 us, 6.3 and 5.4 TB/s.
+// of a pair with the summaries). Bound by memory, read + written: 139 MB 26 us, 276 MB 56 us, 5.3 and 4.9 TB/s.
 constexpr int kPiece = 16384;
 __global__ __launch_bounds__(256) void kv_copy_kernel(KvCache dst, KvCache src, const int32_t *__restrict__ to,
                                                       const int32_t *__restrict__ source, int64_t units, uint32_t pieces)

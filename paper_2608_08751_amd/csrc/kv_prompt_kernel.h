@@ -18,6 +18,12 @@
 // (1,340 TFLOP/s). 256 channels: 1,370 us, 450 TFLOP/s: an operand from LDS serves one product of 16 rows, and
 // one wave a SIMD has nothing to do meanwhile (matrix units 19 %, vector units 21 % busy).
 // Probabilities are rounded to the cache's type, as in the single-token kernel.
+//
+// With terms in the scores (kv_terms.h; kernels of their own for a cap and for a bias): 2,048 tokens after 8,192 in f16,
+// variants in turn: 294 us without terms, with a prefix that sees itself 322, with a bias 344 (the bias of a tile's
+// first key goes into what is subtracted anyway), with a cap 419, with all three 462, vector units 67 % and matrix
+// units 30 % busy. 4,000 tokens of documents of 450 behind 611 shared ones, the last 32 of which see all: 127 us, vector units 41 %,
+// matrix units 28 % busy, waits 45 %: the rows that see all 36 tiles of keys are the longest way through.
 #pragma once
 
 #include "kv.h"
