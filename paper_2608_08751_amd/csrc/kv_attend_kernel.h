@@ -221,7 +221,7 @@ void kv_attend_kernel(KvAttend a, Terms terms)
             lim_max = seen.last();
             if (terms.slopes) {
                 pos = a.position[t0 + row_tok];
-                slope = terms.slopes[head * a.group + (int)(row - row_tok * (uint32_t)a.group)] * 1.44269504089f;
+                slope = slope_of(terms, head * a.group + (int)(row - row_tok * (uint32_t)a.group));
             }
         } else {
 #pragma unroll

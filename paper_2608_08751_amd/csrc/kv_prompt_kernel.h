@@ -85,7 +85,7 @@ __global__ __launch_bounds__(PromptShape<D>::threads, 2) void kv_prompt_kernel(K
         slope[ct] = 0.f;
         if constexpr (TERMS) {
             pos[ct] = have ? a.position[tok[ct]] : -1;  // for the bias, beyond the table too
-            if (Terms::kBias) slope[ct] = terms.slopes[qhead[ct]] * 1.44269504089f;
+            if (Terms::kBias) slope[ct] = slope_of(terms, qhead[ct]);
         }
         mine[ct] = false;
         const elem *q = (const elem *)a.q.p + (have ? tok[ct] * a.q.ts + (int64_t)qhead[ct] * a.q.hs : 0);

@@ -21,6 +21,14 @@ template <bool CAP, bool BIAS> struct KvTermsOf : KvTerms {
     static constexpr bool kCap = CAP, kBias = BIAS;
 };
 
+// A head's slope, to the base 2. One of 2^14 leaves a key that is one further away no weight, and the biases of a step's
+// 64 keys stay within 2^20: the prompt kernel subtracts them in another order for the reference than for the
+// probabilities, which then differ by less than a unit of the exponent (beyond 2^30 they would be infinite).
+__device__ __forceinline__ float slope_of(const KvTerms &x, int head)
+{
+    return fminf(fmaxf(x.slopes[head], -0x1p14f), 0x1p14f) * 1.44269504089f;
+}
+
 // The keys that a row sees; last_key: the last that its table has room for. A row that does not count or stands
 // at no position sees nothing.
 struct KvSight {

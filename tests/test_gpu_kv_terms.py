@@ -210,6 +210,30 @@ def test_slopes(ctx, c, slopes):
     run(ctx, "f16" if c["dim"] % 128 else "bf16", seed=len(slopes), slopes=slopes, **c)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("slope", [2.0**14, 1e6, 1e19, 3.4e38])
+@pytest.mark.parametrize("c", LAYOUTS, ids=name)
+def test_slopes_beyond_any_score(ctx, c, slope, kind):
+    # A key one further away weighs exp(-2^14) = 0, so that a row is its own token's value. Its probability is rounded
+    # once, over a sum that is not, and the result once: 2 u.
+    import paper_2608_08751_amd as ivf
+
+    lens, new, heads, group, dim, bs = (c[k] for k in ("lens", "new", "heads", "group", "dim", "bs"))
+    cache, table, keys, values = make(ctx, kind, lens, heads, dim, bs, 5)
+    start, request, position = batch(lens, new)
+    T, Hq = len(request), heads * group
+    out, lse = ivf.ivf_kv_attend(ctx, cache, queries(T, Hq, dim, kind, 5), ints(start), ints(request), ints(position), ints(table),
+                                 dim**-0.5, int(max(new)), slopes=dev(np.full(Hq, slope, np.float32)))
+    out, lse = as_np(out).reshape(T, Hq, dim), as_np(lse)
+    assert np.isfinite(out).all() and np.isfinite(lse).all()
+    u = {"bf16": 2.0**-8, "f16": 2.0**-11}[kind]
+    for t in range(T):
+        block, at = table[request[t], position[t] // bs], position[t] % bs
+        for g in range(Hq):
+            v = values[block, g // group, at]
+            assert (np.abs(out[t, g] - v) <= 2.01 * u * np.abs(v)).all(), (t, g)
+
+
 @pytest.mark.parametrize("mask", ["window", "prefix", "mixed"])
 @pytest.mark.parametrize("c", LAYOUTS, ids=name)
 def test_all_terms(ctx, c, mask):
