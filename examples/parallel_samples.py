@@ -44,6 +44,11 @@ def sampled(logits, u, temperature, top_k, top_p):
     return (total <= u.cpu().double()[:, None] * total[:, -1:]).sum(1)
 
 
+def follow(last, token, request):
+    """Writes a batch's tokens to its requests' entries of `last`, which has one entry more: the padding's (request -1)."""
+    last.scatter_(0, torch.where(request >= 0, request, last.shape[0] - 1).long(), token)
+
+
 def run(prompts=2, samples=4, prompt=300, steps=12, heads=2, group=4, dim=64, block_size=32, vocab=5000, window=128, sink=4,
         cap=30.0, dtype=torch.bfloat16, seed=0):
     """Returns a dict: microseconds a step, the last step's largest error relative to its largest output, whether
@@ -91,8 +96,8 @@ def run(prompts=2, samples=4, prompt=300, steps=12, heads=2, group=4, dim=64, bl
 
     # a decoding step of one token for every request that goes on; the others bring none
     live = (cached > 0).int()
-    last = torch.zeros(rows, dtype=torch.int32, device="cuda")
-    last[prompts:] = tokens[plan.start[1:prompts + 1].long() - 1].int().repeat_interleave(samples)
+    last = torch.zeros(rows + 1, dtype=torch.int32, device="cuda")
+    last[prompts:rows] = tokens[plan.start[1:prompts + 1].long() - 1].int().repeat_interleave(samples)
     uniform = torch.zeros(rows, device="cuda")
     full = lambda v, kind: torch.full((rows,), v, dtype=kind, device="cuda")  # noqa: E731
     limits = dict(temperature=full(0.8, torch.float32), top_k=full(50, torch.int32), top_p=full(0.95, torch.float32))
@@ -104,8 +109,7 @@ def run(prompts=2, samples=4, prompt=300, steps=12, heads=2, group=4, dim=64, bl
         q, out = layer(last[at], plan, 1)
         logits.copy_((out.flatten(1) @ w_out) @ embed.T)
         token, _ = ivf.ivf_sample(ctx, logits, uniform, **limits)
-        there = plan.request >= 0
-        last.scatter_(0, torch.where(there, at, rows - 1), torch.where(there, token, last[rows - 1]))
+        follow(last, token, plan.request)
         used.add_(plan.info[2])
         cached.add_(live)
         return q, out, token, plan.request
@@ -128,7 +132,7 @@ def run(prompts=2, samples=4, prompt=300, steps=12, heads=2, group=4, dim=64, bl
         for _ in range(n):
             uniform.uniform_()
             graph.replay()
-            drawn.append(last[prompts:].clone())
+            drawn.append(last[prompts:rows].clone())
 
     begin.record()
     decode(steps)
