@@ -687,8 +687,8 @@ ivf_status ivf_kv_attend(ivf_ctx *ctx, const ivf_kv_cache *cache, const void *q,
  * head alone, a prefix that sees itself in both directions. Keys that no row of
  * a group sees are not read.
  *   cap      0, or from 2^-40 to 2^40, with scale / cap 0 or a normal number
- *   slopes   [q_heads] fp32, or NULL; beyond 2^14 in magnitude as 2^14. Scores are
- *            fp32, their bias with them: that of a row's largest score has to stay within
+ *   slopes   [q_heads] fp32, or NULL; beyond 2^14 in magnitude as 2^14. One that is no
+ *            number makes its head's rows NaN that see a key. Scores are fp32, their bias with them: that of a row's largest score has to stay within
  *            2^20 (slopes below 0, rows that see far keys alone)
  *   first    [T] int32 or NULL; above p: only the prefix is seen
  *   prefix   [T] int32 or NULL; at most the request's tokens in the cache (slots

@@ -87,6 +87,10 @@ __global__ __launch_bounds__(PromptShape<D>::threads, 2) void kv_prompt_kernel(K
             pos[ct] = have ? a.position[tok[ct]] : -1;  // for the bias, beyond the table too
             if (Terms::kBias) slope[ct] = slope_of(terms, qhead[ct]);
         }
+        // a slope that is no number makes scores so by way of the query: masks are set before the bias is added, and
+        // rows that see nothing stay zero
+        const bool no_slope = Terms::kBias && slope[ct] != slope[ct];
+        if (no_slope) slope[ct] = 0.f;
         mine[ct] = false;
         const elem *q = (const elem *)a.q.p + (have ? tok[ct] * a.q.ts + (int64_t)qhead[ct] * a.q.hs : 0);
 #pragma unroll
@@ -97,7 +101,7 @@ __global__ __launch_bounds__(PromptShape<D>::threads, 2) void kv_prompt_kernel(K
                 if (have) x = *(const u32x4 *)(q + P::off(c) + P::size(c) / 4 * h + 8 * d);
                 // a channel that is not finite makes every score NaN, as in the single-token kernel: an
                 // infinity alone may score -infinity with all keys, which is how masked ones look
-                if (!TT::finite(x)) x = (u32x4){0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu};
+                if (!TT::finite(x) || no_slope) x = (u32x4){0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu};
                 qf[ct][P::off(c) / 32 + d] = x ^ a.q_flip;
             }
     }

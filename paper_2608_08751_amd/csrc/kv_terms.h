@@ -22,11 +22,14 @@ template <bool CAP, bool BIAS> struct KvTermsOf : KvTerms {
 };
 
 // A head's slope, to the base 2. One of 2^14 leaves a key that is one further away no weight, and the biases of a step's
-// 64 keys stay within 2^20: the prompt kernel subtracts them in another order for the reference than for the
-// probabilities, which then differ by less than a unit of the exponent (beyond 2^30 they would be infinite).
+// 64 keys stay within 63 x 2^14 x 1.443 < 2^21, where fp32 numbers lie 2^-3 apart: the prompt kernel subtracts them in
+// another order for the reference than for the probabilities, a rounding of the bias, of its sum with the score and of
+// the sum with the reference, 2^-4 each (scores are small beside such biases), so that the two differ by less than a
+// unit of the exponent (beyond 2^30 they would be infinite). Comparisons leave a slope that is no number as it is.
 __device__ __forceinline__ float slope_of(const KvTerms &x, int head)
 {
-    return fminf(fmaxf(x.slopes[head], -0x1p14f), 0x1p14f) * 1.44269504089f;
+    const float s = x.slopes[head];
+    return (s > 0x1p14f ? 0x1p14f : s < -0x1p14f ? -0x1p14f : s) * 1.44269504089f;
 }
 
 // The keys that a row sees; last_key: the last that its table has room for. A row that does not count or stands

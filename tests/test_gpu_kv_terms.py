@@ -234,6 +234,24 @@ def test_slopes_beyond_any_score(ctx, c, slope, kind):
             assert (np.abs(out[t, g] - v) <= 2.01 * u * np.abs(v)).all(), (t, g)
 
 
+@pytest.mark.parametrize("mask,cap", [(None, 0.0), ("mixed", 0.0), ("prefix", 0.0), ("mixed", 5.0), ("one window", 5.0)], ids=str)
+@pytest.mark.parametrize("c", LAYOUTS, ids=name)
+def test_slopes_that_are_no_number(ctx, c, mask, cap):
+    """Their heads' rows are no number where they see a key; rows that see none, and the other heads, are as ever."""
+    for kind, slopes in (("bf16", [math.nan, 0.05]), ("f16", [0.3, -math.nan, 0.0])):
+        out, lse = run(ctx, kind, seed=len(slopes), mask=mask, cap=cap, slopes=slopes, **c)
+        bad = np.isnan(np.resize(slopes, lse.shape[1]))
+        assert not np.isnan(lse[:, ~bad]).any() and (np.isnan(lse[:, bad]) == ~np.isinf(lse[:, bad])).all()
+        assert bad.all() or np.isfinite(out[:, ~bad]).all()
+
+
+@pytest.mark.parametrize("kind,T,heads,group,dim,bs,count", [("bf16", 5, 2, 12, 128, 64, 4), ("f16", 300, 8, 2, 96, 16, 3), ("f16", 30, 2, 4, 192, 32, 6)])
+def test_slopes_that_are_no_number_and_selected_blocks(ctx, kind, T, heads, group, dim, bs, count):
+    lens = [max(T // 2, 1) + 150, T - max(T // 2, 1) + 333]
+    run(ctx, kind, lens, [max(T // 2, 1), T - max(T // 2, 1)], heads, group, dim, bs, T, mask="mixed", slopes=[0.1, math.nan, 0.002],
+        count=count)
+
+
 @pytest.mark.parametrize("mask", ["window", "prefix", "mixed"])
 @pytest.mark.parametrize("c", LAYOUTS, ids=name)
 def test_all_terms(ctx, c, mask):
