@@ -95,13 +95,21 @@ __global__ __launch_bounds__(THREADS) void kv_fork_kernel(const int32_t *__restr
         if (i < n && rank[i] >= 0) rank[i] += (int)before;
     }
     __syncthreads();
-    if (info && blockIdx.x == 0 && tid == 0) {
-        info[0] = all;
-        info[1] = min((int64_t)all, n_free);
+    // the last workgroup counts the blocks that were taken, entries of -1 are none; the others take the rows
+    const unsigned groups = gridDim.x - (info != nullptr);
+    if (blockIdx.x == groups) {
+        uint32_t got = 0, taken;
+        for (int i = tid; i < min((int64_t)all, n_free); i += THREADS) got += free_blocks[i] >= 0;
+        sum_before<THREADS>(got, &taken);
+        if (tid == 0) {
+            info[0] = all;
+            info[1] = taken;
+        }
+        return;
     }
     const uint32_t chunks = (uint32_t)(cols + kChunk - 1) / kChunk;
     const int64_t units = (int64_t)n * chunks;
-    for (int64_t u = (int64_t)blockIdx.x * (THREADS / 64) + wave; u < units; u += (int64_t)gridDim.x * (THREADS / 64)) {
+    for (int64_t u = (int64_t)blockIdx.x * (THREADS / 64) + wave; u < units; u += (int64_t)groups * (THREADS / 64)) {
         const int i = (int)((uint64_t)u / chunks), r = rank[i];
         const int j0 = (int)((uint64_t)u % chunks) * kChunk;
         if (r == -2) {
@@ -386,7 +394,8 @@ hipError_t launch_kv_fork(const int32_t *parent, const int32_t *child, int n, in
     const bool few = n <= 2048 && B <= 2048;
     const int waves = (few ? 256 : 1024) / 64;
     const int64_t units = (int64_t)n * ((cols + kChunk - 1) / kChunk);
-    const unsigned grid = (unsigned)std::max<int64_t>(1, std::min<int64_t>((units + waves - 1) / waves, (int64_t)num_cus * (few ? 4 : 1)));
+    const unsigned groups = (unsigned)std::max<int64_t>(1, std::min<int64_t>((units + waves - 1) / waves, (int64_t)num_cus * (few ? 4 : 1)));
+    const unsigned grid = groups + (info != nullptr);
     if (few)
         hipLaunchKernelGGL((kv_fork_kernel<256, 8>), dim3(grid), dim3(256), 0, s, parent, child, n, cached, B, shift,
                            table, cols, free_blocks, n_free, source, to, info);

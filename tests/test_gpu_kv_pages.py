@@ -320,6 +320,30 @@ def test_samples_of_one_prompt(ctx, kind, dim, bs, length):
     check()
 
 
+FREE_WITHOUT_BLOCKS = [  # lists that end early, as ivf_kv_reclaim writes them, and others with entries that are no block
+    [], [-1], [-1] * 40, [7], [7, 9, -1, -1], [7, 9, 11, -1, -1, -1, -1, -1], [-1, 7, -1, 9, 11], list(range(100, 130)) + [-1] * 9,
+    [5, -7, 6, -(2**31)]]
+
+
+@pytest.mark.parametrize("free", FREE_WITHOUT_BLOCKS, ids=lambda f: "%d-of-%d" % (sum(x >= 0 for x in f), len(f)))
+@pytest.mark.parametrize("n", [1, 3, 5, 30, 3000])
+def test_fork_says_how_many_blocks_it_took(ctx, n, free):
+    """Entries of free_blocks that are no block are not counted; the forks that they fall to have no last block."""
+    import paper_2608_08751_amd as ivf
+
+    bs, cols = 16, 3
+    cached = [20] + [0] * n
+    table = np.full((n + 1, cols), -1, np.int32)
+    table[0, :2] = 40, 41
+    got_cached, got_table = ints(cached), ints(table)
+    fork = ivf.ivf_kv_fork(ctx, ints([0] * n), ints(range(1, n + 1)), got_cached, bs, got_table, ints(free), want_info=True)
+    taken = (free + [-1] * n)[:n]
+    want = [x if x >= 0 else -1 for x in taken]
+    assert fork.info.tolist() == [n, sum(x >= 0 for x in taken)]
+    assert fork.to.tolist() == want and fork.source.tolist() == [41 if x >= 0 else -1 for x in want]
+    assert (got_table[1:, 1] >= 0).sum() == int(fork.info[1]) and got_cached.tolist() == [20] * (n + 1)
+
+
 @pytest.mark.parametrize("blocks", [25_000, 60_000])
 def test_captured_on_another_stream(ctx, blocks):
     """Fork, copy and reclaim as a graph, replayed on other lengths and tables in the same buffers."""
