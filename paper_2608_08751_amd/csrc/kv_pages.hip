@@ -61,6 +61,16 @@ __global__ __launch_bounds__(THREADS) void kv_fork_kernel(const int32_t *__restr
     __shared__ uint32_t read[THREADS * PER / 32];  // rows that are parents
     __shared__ int32_t rank[THREADS * PER];  // of the block that a fork takes; -1: none, -2: the fork does not count
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    // with info the last workgroup counts the blocks that are taken, entries of -1 are none; the others take the rows
+    const unsigned groups = gridDim.x - (info != nullptr);
+    int32_t id[PER];
+    if (blockIdx.x == groups) {
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            const int i = tid + k * THREADS;
+            id[k] = i < n && i < n_free ? free_blocks[i] : -1;
+        }
+    }
     for (int b = tid; b < B; b += THREADS) last[b] = -1;
     for (int b = tid; b * 32 < B; b += THREADS) read[b] = 0;
     __syncthreads();
@@ -95,11 +105,10 @@ __global__ __launch_bounds__(THREADS) void kv_fork_kernel(const int32_t *__restr
         if (i < n && rank[i] >= 0) rank[i] += (int)before;
     }
     __syncthreads();
-    // the last workgroup counts the blocks that were taken, entries of -1 are none; the others take the rows
-    const unsigned groups = gridDim.x - (info != nullptr);
     if (blockIdx.x == groups) {
         uint32_t got = 0, taken;
-        for (int i = tid; i < min((int64_t)all, n_free); i += THREADS) got += free_blocks[i] >= 0;
+#pragma unroll
+        for (int k = 0; k < PER; ++k) got += tid + k * THREADS < (int)all && id[k] >= 0;
         sum_before<THREADS>(got, &taken);
         if (tid == 0) {
             info[0] = all;
@@ -394,8 +403,9 @@ hipError_t launch_kv_fork(const int32_t *parent, const int32_t *child, int n, in
     const bool few = n <= 2048 && B <= 2048;
     const int waves = (few ? 256 : 1024) / 64;
     const int64_t units = (int64_t)n * ((cols + kChunk - 1) / kChunk);
-    const unsigned groups = (unsigned)std::max<int64_t>(1, std::min<int64_t>((units + waves - 1) / waves, (int64_t)num_cus * (few ? 4 : 1)));
-    const unsigned grid = groups + (info != nullptr);
+    // (with info a workgroup more, which the CUs still hold at once)
+    const int64_t most = std::max<int64_t>((int64_t)num_cus * (few ? 4 : 1) - (info != nullptr), 1);
+    const unsigned grid = (unsigned)std::max<int64_t>(1, std::min<int64_t>((units + waves - 1) / waves, most)) + (info != nullptr);
     if (few)
         hipLaunchKernelGGL((kv_fork_kernel<256, 8>), dim3(grid), dim3(256), 0, s, parent, child, n, cached, B, shift,
                            table, cols, free_blocks, n_free, source, to, info);
