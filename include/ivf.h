@@ -531,7 +531,10 @@ typedef struct {
  *               beyond the table)
  *   out_request, out_position [T] int32; past the last token -1
  *   out_info    [4] int64: tokens, blocks asked for, blocks taken, requests
- *               that the table's columns do not hold; may be NULL
+ *               that the table's columns do not hold; may be NULL. Taken: of as
+ *               many entries of free_blocks as were asked for those that are a
+ *               block (one below 0 is none; the list's next entry is that
+ *               behind all that were asked for)
  * B = 0 writes the outputs too, those that are not NULL; its inputs and table
  * may be NULL.
  * Errors: IVF_EINVAL, IVF_EUNSUPPORTED (B, sizes), IVF_EDEVICE. */
@@ -555,10 +558,8 @@ ivf_status ivf_kv_plan(ivf_ctx *ctx, const int32_t *cached, const int32_t *added
  *   cached      [B] int32 tokens that requests have, updated; B <= 16384
  *   table       [B][table_cols] int32, updated
  *   out_source, out_to [n] int32
- *   out_info    [2] int64: blocks asked for, blocks taken: of as many entries of
- *               free_blocks those that are a block (one below 0 is none; the
- *               list's next entry is that behind all that were asked for);
- *               may be NULL
+ *   out_info    [2] int64: blocks asked for, blocks taken (as ivf_kv_plan
+ *               counts them); may be NULL
  * A parent's last block without a table entry stays without one.
  * Errors: as ivf_kv_plan. */
 ivf_status ivf_kv_fork(ivf_ctx *ctx, const int32_t *parent, const int32_t *child, int64_t n, int32_t *cached,

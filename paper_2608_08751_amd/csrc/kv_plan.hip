@@ -74,19 +74,39 @@ __global__ __launch_bounds__(THREADS) void kv_plan_kernel(
     const int64_t total = min(tall, T);
     if (blockIdx.x == 0) {
         for (int b = tid; b < B; b += THREADS) start[b] = first[b];
-        if (tid == 0) {
-            if (start) start[B] = (int32_t)total;
-            if (info) {
-                info[0] = tall;
-                info[1] = ball;
-                info[2] = min(ball, n_free);
-                info[3] = beyond;
-            }
+        if (tid == 0 && start) start[B] = (int32_t)total;
+    }
+
+    // the last workgroup counts the blocks that were taken, entries of -1 are none; the others take the rest
+    const unsigned groups = gridDim.x - (info != nullptr);
+    if (blockIdx.x == groups) {
+        constexpr int U = 16;  // loads of a thread that do not wait for each other
+        const int64_t asked = min(ball, n_free);
+        int64_t taken = 0;
+        for (int64_t r0 = tid; r0 < asked; r0 += U * THREADS) {
+            int32_t id[U];
+#pragma unroll
+            for (int k = 0; k < U; ++k) id[k] = free_blocks[min(r0 + k * THREADS, asked - 1)];
+#pragma unroll
+            for (int k = 0; k < U; ++k) taken += r0 + k * THREADS < asked && id[k] >= 0;
         }
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) taken += __shfl_xor(taken, d);
+        if (lane == 0) wave_sum[0][wave] = taken;  // (read by all before the last barrier)
+        __syncthreads();
+        if (tid == 0) {
+            taken = 0;
+            for (int w = 0; w < THREADS / 64; ++w) taken += wave_sum[0][w];
+            info[0] = tall;
+            info[1] = ball;
+            info[2] = taken;
+            info[3] = beyond;
+        }
+        return;
     }
 
     // tokens
-    for (int64_t t = (int64_t)blockIdx.x * THREADS + tid; t < T; t += (int64_t)gridDim.x * THREADS) {
+    for (int64_t t = (int64_t)blockIdx.x * THREADS + tid; t < T; t += (int64_t)groups * THREADS) {
         int b = -1;
         int64_t slot = -1, pos = -1;
         if (t < total) {
@@ -118,7 +138,7 @@ __global__ __launch_bounds__(THREADS) void kv_plan_kernel(
     }
 
     // table rows, a wave each: columns from the first new block on
-    for (int b = blockIdx.x * (THREADS / 64) + wave; b < B; b += gridDim.x * (THREADS / 64)) {
+    for (int b = blockIdx.x * (THREADS / 64) + wave; b < B; b += groups * (THREADS / 64)) {
         const int64_t c = max(cached[b], 0), a = max(added[b], 0);
         const int64_t o = blocks_of(c, shift), n = blocks_of(c + a, shift);
         for (int64_t j = o + lane; j < cols; j += 64) {
@@ -137,7 +157,9 @@ hipError_t launch_kv_plan(const int32_t *cached, const int32_t *added, int B, in
     const int threads = B <= 2048 ? 256 : 1024;
     int64_t grid = (T + threads - 1) / threads;
     grid = std::max<int64_t>(grid, (B + threads / 64 - 1) / (threads / 64));
-    grid = std::max<int64_t>(1, std::min<int64_t>(grid, (int64_t)num_cus * (B <= 2048 ? 2 : 1)));
+    // (with info a workgroup more, which the CUs still hold at once)
+    const int64_t most = std::max<int64_t>((int64_t)num_cus * (B <= 2048 ? 2 : 1) - (info != nullptr), 1);
+    grid = std::max<int64_t>(1, std::min<int64_t>(grid, most)) + (info != nullptr);
     if (B <= 2048)
         hipLaunchKernelGGL((kv_plan_kernel<256, 8>), dim3((unsigned)grid), dim3(256), 0, s, cached, added, B, shift,
                            table, cols, free_blocks, n_free, T, start, slots, request, position, info);

@@ -344,6 +344,56 @@ def test_fork_says_how_many_blocks_it_took(ctx, n, free):
     assert (got_table[1:, 1] >= 0).sum() == int(fork.info[1]) and got_cached.tolist() == [20] * (n + 1)
 
 
+@pytest.mark.parametrize("free", FREE_WITHOUT_BLOCKS, ids=lambda f: "%d-of-%d" % (sum(x >= 0 for x in f), len(f)))
+@pytest.mark.parametrize("B,added", [(1, 1), (1, 100), (5, 40), (40, 1), (3000, 20)])
+def test_plan_says_how_many_blocks_it_took(ctx, B, added, free):
+    import paper_2608_08751_amd as ivf
+
+    bs, cols = 16, -(-added // 16) + 1
+    table = ints(np.full((B, cols), -1))
+    plan = ivf.ivf_kv_plan(ctx, ints([0] * B), ints([added] * B), bs, table, ints(free), B * added, want_info=True)
+    asked = B * -(-added // bs)
+    taken = sum(x >= 0 for x in free[:asked])
+    assert plan.info.tolist() == [B * added, asked, taken, 0]
+    assert int((table >= 0).sum()) == taken
+    assert int((plan.slots >= 0).sum()) == sum(min(bs, added - j * bs) for r, x in enumerate(free[:asked]) if x >= 0
+                                               for j in [r % -(-added // bs)])
+
+
+def test_what_reclaim_lists_runs_dry(ctx):
+    """Its list as it is, padding and all, until no block is left: every call says what was missing."""
+    import paper_2608_08751_amd as ivf
+
+    bs, blocks = 16, 12
+    table = np.full((9, 4), -1, np.int32)
+    table[0, :3] = 2, 5, 11
+    table, cached = ints(table), ints([40] + [0] * 8)
+    free = ivf.ivf_kv_reclaim(ctx, cached, bs, table, blocks).free
+    assert free.tolist() == [0, 1, 3, 4, 6, 7, 8, 9, 10, -1, -1, -1]
+    fork = ivf.ivf_kv_fork(ctx, ints([0] * 5), ints(range(1, 6)), cached, bs, table, free, want_info=True)
+    assert fork.info.tolist() == [5, 5]
+    free = ivf.ivf_kv_reclaim(ctx, cached, bs, table, blocks).free
+    plan = ivf.ivf_kv_plan(ctx, cached, ints([0] * 6 + [64, 1, 1]), bs, table, free, 66, want_info=True)
+    assert plan.info.tolist() == [66, 6, 4, 0]  # four blocks were free
+    assert (plan.slots < 0).tolist() == [False] * 64 + [True] * 2
+    cached += ints([0] * 6 + [64, 0, 0])
+    free = ivf.ivf_kv_reclaim(ctx, cached, bs, table, blocks).free
+    assert free.tolist() == [-1] * blocks
+    fork = ivf.ivf_kv_fork(ctx, ints([0]), ints([7]), cached, bs, table, free, want_info=True)
+    assert fork.info.tolist() == [1, 0] and fork.to.tolist() == [-1]
+
+
+@pytest.mark.parametrize("T", [300_000, 1_000_000])
+def test_plan_of_many_blocks_says_how_many_it_took(ctx, T):
+    import paper_2608_08751_amd as ivf
+
+    rng = np.random.default_rng(T)
+    asked = -(-T // 16)
+    free = np.where(rng.random(asked + 50) < 0.1, -1, np.arange(asked + 50))
+    plan = ivf.ivf_kv_plan(ctx, ints([0]), ints([T]), 16, ints(np.full((1, asked), -1)), ints(free), T, want_info=True)
+    assert plan.info.tolist() == [T, asked, int((free[:asked] >= 0).sum()), 0]
+
+
 @pytest.mark.parametrize("blocks", [25_000, 60_000])
 def test_captured_on_another_stream(ctx, blocks):
     """Fork, copy and reclaim as a graph, replayed on other lengths and tables in the same buffers."""
