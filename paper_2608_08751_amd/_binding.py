@@ -880,9 +880,9 @@ def ivf_sample(ctx: Context, logits, uniform, temperature=None, top_k=None, top_
     if dt is None or logits.get_device() != ctx.device:
         raise TypeError("logits must be float32, float16 or bfloat16 on device %d, got %s on %s" % (
             ctx.device, logits.dtype, logits.device))
-    if logits.requires_grad and _grad_enabled():
-        raise RuntimeError("logits require a gradient, and sampling has no backward pass: detach them, or call under "
-                           "torch.no_grad()")
+    if (logits.requires_grad or (temperature is not None and temperature.requires_grad)) and _grad_enabled():
+        raise RuntimeError("logits or temperature require a gradient, and sampling has no backward pass: detach them, or call "
+                           "under torch.no_grad()")
     if logits.dim() != 2 or logits.shape[1] < 1:
         raise ValueError("logits must be [T, V] with V >= 1, got %s" % (tuple(logits.shape),))
     T, V = logits.shape

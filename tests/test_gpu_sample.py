@@ -271,3 +271,19 @@ def test_no_rows_and_refused_arguments(ctx):
                               ((x.clone().requires_grad_(), u), {}, RuntimeError)):
         with pytest.raises(error):
             ivf.ivf_sample(ctx, *args, **more)
+
+
+def test_a_temperature_that_requires_a_gradient_is_refused(ctx):
+    """The log-probabilities go by it, and there is no backward pass; without gradients it is taken as it is."""
+    import torch
+
+    import paper_2608_08751_amd as ivf
+
+    x, u = torch.randn(3, 10, device="cuda"), torch.rand(3, device="cuda")
+    t = torch.ones(3, device="cuda", requires_grad=True)
+    with pytest.raises(RuntimeError):
+        ivf.ivf_sample(ctx, x, u, temperature=t)
+    want = ivf.ivf_sample(ctx, x, u, temperature=t.detach())
+    with torch.no_grad():
+        got = ivf.ivf_sample(ctx, x, u, temperature=t)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
