@@ -544,17 +544,18 @@ ivf_status ivf_kv_plan(ivf_ctx *ctx, const int32_t *cached, const int32_t *added
                        int64_t *out_slots, int32_t *out_request, int32_t *out_position,
                        int64_t *out_info);
 
-/* Requests that go on from another's tokens (several samples of one prompt,
- * beams): fork i makes row child[i] of the table a copy of row parent[i],
- * with cached[child[i]] = cached[parent[i]]. The blocks are shared but for the
- * last one, where that is partly filled: in its place the child gets the next
- * of free_blocks (forks in order; -1 where they do not suffice), and the pair
- * (out_source[i], out_to[i]) says what ivf_kv_copy has to copy in every cache that
- * the table serves (-1, -1: nothing). Columns past the tokens become -1.
+/* Requests that go on from another's tokens (several samples of one prompt):
+ * fork i makes row child[i] of the table a copy of row parent[i], with
+ * cached[child[i]] = cached[parent[i]]. The blocks are shared but for the last
+ * one, where that is partly filled: in its place the child gets the next of
+ * free_blocks (forks in order; -1 where they do not suffice), and the pair
+ * (out_source[i], out_to[i]) says what ivf_kv_copy has to copy in every cache
+ * that the table serves (-1, -1: nothing). Columns past the tokens become -1.
  *   parent, child [n] int32, n <= 16384: rows. A fork whose rows are the same
  *               or outside [0, B), whose child a later such fork names too, or
  *               is the parent of one, is left out: it changes nothing and its
- *               pair is (-1, -1).
+ *               pair is (-1, -1). So rows that go on in each other's place
+ *               (beams) need a second set of rows to go to.
  *   cached      [B] int32 tokens that requests have, updated; B <= 16384
  *   table       [B][table_cols] int32, updated
  *   out_source, out_to [n] int32
@@ -590,7 +591,7 @@ ivf_status ivf_kv_copy(ivf_ctx *ctx, const ivf_kv_cache *cache, const ivf_kv_cac
  *   out_free    [blocks] int32: the blocks that are free after the moves,
  *               ascending, -1 behind them (out_info[2] says how many: to
  *               ivf_kv_plan and ivf_kv_fork an entry of -1 is a block that is
- *               none); may be NULL
+ *               none, and not counted as taken); may be NULL
  *   out_source, out_to [moves] int32, -1 behind the pairs; NULL when moves is 0
  *   out_info    [3] int64: U, moves made, blocks - U; may be NULL
  * B = 0: all are free, cached and table may be NULL.
@@ -690,10 +691,16 @@ ivf_status ivf_kv_attend(ivf_ctx *ctx, const ivf_kv_cache *cache, const void *q,
  * context's first tokens (prefix), documents that see themselves and a shared
  * head alone, a prefix that sees itself in both directions. Keys that no row of
  * a group sees are not read.
- *   cap      0, or from 2^-40 to 2^40, with scale / cap 0 or a normal number
- *   slopes   [q_heads] fp32, or NULL; beyond 2^14 in magnitude as 2^14. One that is no
- *            number makes its head's rows NaN that see a key. Scores are fp32, their bias with them: that of a row's largest score has to stay within
- *            2^20 (slopes below 0, rows that see far keys alone)
+ *   cap      0, or from 2^-40 to 2^40, with scale / cap 0 or a normal number.
+ *            The tanh is a polynomial or an exponential, each within 5e-7 of
+ *            it, by the largest of the scores that are computed together
+ *            (masked ones and other rows' among them): a row's results may
+ *            differ in their last bits with what is beside it in the batch
+ *            or the cache
+ *   slopes   [q_heads] fp32, or NULL; beyond 2^14 in magnitude as 2^14. One that
+ *            is no number makes its head's rows NaN that see a key. Scores are
+ *            fp32, their bias with them: that of a row's largest score has to
+ *            stay within 2^20 (slopes below 0, rows that see far keys alone)
  *   first    [T] int32 or NULL; above p: only the prefix is seen
  *   prefix   [T] int32 or NULL; at most the request's tokens in the cache (slots
  *            behind them hold whatever they hold), and not of a token whose

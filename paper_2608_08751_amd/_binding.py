@@ -634,7 +634,8 @@ def ivf_kv_plan(ctx: Context, cached, added, block_size: int, table, free_blocks
     bring added[b] more, `tokens` in all. Fills `table` (int32 [B, columns]) in
     place with blocks of free_blocks (int32, taken in order) and returns
     KVPlan(start [B + 1], slots int64 [tokens], request [tokens], position
-    [tokens], info int64 [4] or None)."""
+    [tokens], info int64 [4] or None: tokens, blocks asked for, blocks taken, requests
+    beyond the table)."""
     import torch
 
     i32 = torch.int32
@@ -666,7 +667,8 @@ def ivf_kv_fork(ctx: Context, parent, child, cached, block_size: int, table, fre
     (int32 [B, columns]) and `cached` (int32 [B]) become those of `parent`, in place, a
     partly filled last block replaced by one of free_blocks (int32, taken in order).
     Returns KVFork(source [n], to [n], info int64 [2] or None): the pairs that
-    ivf_kv_copy has to copy, -1 where there is nothing to copy."""
+    ivf_kv_copy has to copy, -1 where there is nothing to copy; blocks asked for and
+    taken. A row that is a parent is no child in the same call: such forks are left out."""
     import torch
 
     i32 = torch.int32

@@ -193,8 +193,8 @@ template <int THREADS, typename F> __device__ __forceinline__ void for_entries(c
     }
 }
 
-// The same in one workgroup for up to 2^31 entries: a thread an entry, eight loads each at a time, none of which waits
-// for another.
+// The same in one workgroup for few entries (kKvFewBlocks at most): a thread an entry, eight loads each at a time, none
+// of which waits for another.
 template <int THREADS, typename F> __device__ __forceinline__ void for_few_entries(const KvReclaim &a, F f)
 {
     constexpr int U = 8;

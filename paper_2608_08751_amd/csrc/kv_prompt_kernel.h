@@ -23,7 +23,10 @@
 // variants in turn: 294 us without terms, with a prefix that sees itself 322, with a bias 344 (the bias of a tile's
 // first key goes into what is subtracted anyway), with a cap 419, with all three 462, vector units 67 % and matrix
 // units 30 % busy. 4,000 tokens of documents of 450 behind 611 shared ones, the last 32 of which see all: 127 us, vector units 41 %,
-// matrix units 28 % busy, waits 45 %: the rows that see all 36 tiles of keys are the longest way through.
+// matrix units 28 % busy, waits 45 %: the rows that see all 36 tiles of keys are the longest way through (8 of 504 workgroups, 3.5 us
+// a tile; the others take some 8). Windows of 1,024 keys 59 us (580 TFLOP/s), with a cap 68; of 4,096 151 (910). 192 and 256
+// channels, all keys: 976 and 1,391 us, with a cap 1,303 and 1,804 (360 and 340 TFLOP/s); windows of 1,024 159 and 245, with a cap 197
+// and 264.
 #pragma once
 
 #include "kv.h"

@@ -23,8 +23,10 @@
 // One workgroup takes a row in one launch, or up to eight share it in four. Bound, where weights are needed, by the
 // fp64 exponential's instructions: 250 whole rows of 100,003 in f16 (50 MB) 39 us, vector units 73 % busy, a pass over
 // them by itself 11; 64 rows of 128,000 in bf16, limits mixed, 53 us (ends 4.9, bins 14.6, collect 18.9, draw 16.3): a
-// workgroup of 32,000 elements a CU, in rounds that wait for LDS, barriers and the caches. One row of 32,000: 28 us, four
-// launches; of 1,000: 14, in one.
+// workgroup of 32,000 elements a CU, in rounds that wait for LDS, barriers and the caches. One row of 32,000: 29 us, four
+// launches; of 1,000: 14, in one. Rows that take the largest logit: 64 of 128,000 16 us, 250 of 100,003 20. With top_k of
+// 40,000 and top_p, which end in a bin of more elements than a list holds, one row of 128,000 takes 234 us and 64 take 219: draw's
+// one workgroup a row goes over it some ten times (top_p alone 40 and 57).
 #include "sample.h"
 
 #include "ivf.h"
